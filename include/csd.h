@@ -57,7 +57,7 @@ typedef enum {
     CSD_ERR_IO = 6
 } csd_status_t;
 
-typedef enum { CSD_F32 = 0, CSD_BF16 = 1 } csd_dtype_t;
+typedef enum { CSD_F32 = 0, CSD_BF16 = 1, CSD_F16 = 2 } csd_dtype_t;   /* CSD_F16: the decode-pass operators only */
 
 /* Largest K (draft tokens per row) a step accepts: one warp lane per position. */
 #define CSD_MAX_K 32
@@ -485,6 +485,159 @@ csd_status_t csd_ocm_load(csd_ocm_t **out, const char *path, uint64_t n_slots, i
 
 /* Copy the statistics block to the HOST struct.  Synchronises `stream`. */
 csd_status_t csd_ocm_stats(const csd_ocm_t *ocm, csd_stats_t *host_out, void *stream);
+
+/* ---- the target pass around a step: positions, cache, attention -------------------------------------
+ *
+ * Algorithm 1 verifies gamma drafted tokens with ONE parallel target pass: per layer, the gamma + 1 new tokens' queries
+ * and keys are turned by their positions, keys and values join the row's cache, and the queries read the whole cache.
+ * The entry points below are that part of the pass and the cache's bookkeeping between steps:
+ *     csd_cache_extend (cache, T = K + 1)                 room for the last token and the K drafted ones
+ *     per layer:  csd_rope_append(q, k, v, ...)           turn, store
+ *                 csd_attention(q', ...)                  read
+ *     csd_step / csd_step_lmhead                          accept_len
+ *     csd_cache_commit(cache, accept_len)                 keep the last token and the accepted ones, free the rest
+ * with csd_cache_fork where rows continue other rows (beams, shared prompts) and csd_cache_compact where a pool has to
+ * shrink.  Nothing here synchronises unless it says so; lengths, page tables and counts stay on the device.
+ */
+
+/* ---- rotary positions ---- */
+typedef enum { CSD_ROPE_HALF = 0, CSD_ROPE_INTERLEAVED = 1 } csd_rope_layout_t;
+typedef enum {
+    CSD_ROPE_PLAIN = 0,   /* theta_i = base^(-2i/rot)                                                                   */
+    CSD_ROPE_LINEAR = 1,  /* theta_i / factor                                                                          */
+    CSD_ROPE_BASE = 2,    /* base grows to base * factor^(rot/(rot-2)): the slowest pair is stretched by `factor`         */
+    CSD_ROPE_PARTS = 3,   /* n_i = original_len theta_i / 2 pi turns within the trained length: pairs with n_i <= low are
+                             divided by factor, pairs with n_i >= high kept, a blend linear in n_i between               */
+    CSD_ROPE_YARN = 4     /* the blend linear in i, between the pairs that make `high` and `low` turns (rounded outwards);
+                             turned values grow by 0.1 ln(factor) + 1                                                  */
+} csd_rope_scaling_t;
+
+/* The rotation as the kernels take it.  Device array; magnitude multiplies the turned elements. */
+typedef struct {
+    const uint64_t *steps;      /* DEVICE [rot/2]: theta_i / 2 pi as a fraction of 2^64, so that position * step mod 2^64
+                                   is the angle, exactly reduced at any position                                      */
+    int rot;                    /* rotated elements of a head, even, 2 .. dim; the rest pass through                    */
+    csd_rope_layout_t layout;   /* pairs (i, i + rot/2), or (2i, 2i + 1)                                                */
+    float magnitude;
+} csd_rope_t;
+
+/* Fills the HOST array steps[rot/2] and *magnitude for base > 1, factor >= 1 and the scaling above (original_len, low
+ * and high only count for PARTS and YARN; 0 < low < high).  The caller copies steps to the device once.  Host function.
+ * Errors: INVALID_ARG. */
+csd_status_t csd_rope_steps(int rot, double base, csd_rope_scaling_t scaling, double factor, double original_len, double low,
+                            double high, uint64_t *steps, float *magnitude);
+
+/* y[b,s,h,:] = x[b,s,h,:] turned by positions[b,s] (inverse != 0: by minus that angle -- the gradient of the operation
+ * for the gradient of its result).  x, y: [B, S, H, D], strides in elements, D contiguous, F32, BF16 or F16; y may be x
+ * (same strides) and must not overlap it otherwise.  positions: int32, element (b,s) at b*pos_stride_b + s*pos_stride_s (0: shared).  Sums and
+ * products in float32, rounded once.  16-byte accesses where base, strides, rot/2 and D allow, element-wise otherwise.
+ * One launch; asynchronous.  B, S or H of 0 does nothing.
+ * Errors: INVALID_ARG (null, negative size, rot odd or outside 2 .. D, unknown type or layout), UNSUPPORTED (more than
+ * 2^31 blocks), CUDA. */
+csd_status_t csd_rope(const void *x, void *y, csd_dtype_t dtype, int B, int S, int H, int D,
+                      int64_t x_stride_b, int64_t x_stride_s, int64_t x_stride_h,
+                      int64_t y_stride_b, int64_t y_stride_s, int64_t y_stride_h,
+                      const int32_t *positions, int64_t pos_stride_b, int64_t pos_stride_s,
+                      const csd_rope_t *rope, int inverse, void *stream);
+
+/* ---- the paged cache ---- */
+#define CSD_CACHE_MAX_ROWS 4096
+/* sticky flags of a cache */
+#define CSD_CACHE_FULL      0x1u  /* an extension found too few free pages: nothing was granted              */
+#define CSD_CACHE_ROW_FULL  0x2u  /* a row would have passed max_pages: nothing was granted                  */
+#define CSD_CACHE_BAD_PAGE  0x4u  /* a table in use holds an id outside the pool: that access was skipped     */
+#define CSD_CACHE_BAD_ROW   0x8u  /* a fork named a parent row that does not exist: the row was left as it is */
+#define CSD_CACHE_INTERNAL  0x10u /* a wait inside a kernel ran out: a bug of the library, results unreliable  */
+
+/* A cache: pages of keys and values, and which page holds what.  HOST struct of caller-owned DEVICE memory.
+ * Element (layer, page, head, token, d) of k and of v lies at layer*stride_layer + page*stride_page + head*stride_head +
+ * token*stride_token + d (elements; multiples of 8; bases 16-byte aligned).  Within a page the heads * page_size * dim
+ * elements are dense in either order: heads outside tokens (stride_token = dim, stride_head = page_size*dim) or tokens
+ * outside heads (stride_head = dim, stride_token = heads*dim).
+ * meta: csd_cache_meta_bytes bytes, 256-byte aligned; what it holds and where is csd_cache_meta_layout's answer, and
+ * copying it saves or restores the bookkeeping.  scratch: csd_cache_scratch_bytes bytes, 256-byte aligned; no
+ * initialisation; one call at a time. */
+typedef struct {
+    void *k, *v;
+    csd_dtype_t dtype;                    /* CSD_BF16 or CSD_F16                                        */
+    int layers, n_pages, page_size;       /* page_size: a power of two, 8 .. 256                         */
+    int heads, dim;                       /* key/value heads; dim a multiple of 8, 8 .. 256              */
+    int64_t stride_layer, stride_page, stride_head, stride_token;
+    int rows, max_pages;                  /* rows <= CSD_CACHE_MAX_ROWS; most pages of a row              */
+    void *meta;
+    void *scratch;
+} csd_cache_t;
+
+/* Byte offsets within meta (all arrays int32 unless said). */
+typedef struct {
+    size_t flags;       /* uint32: CSD_CACHE_* flags, sticky until csd_cache_rebuild            */
+    size_t lens;        /* [rows] tokens in each row, those of the last extension included      */
+    size_t granted;     /* [rows] tokens that the last extension gave the row (0 after any other change) */
+    size_t table;       /* [rows, max_pages] page of each page_size tokens; -1 where there is none */
+    size_t refs;        /* [n_pages] rows that use the page                                       */
+    size_t free_bits;   /* uint32 [ceil(n_pages/32)] bit p: page p is free                        */
+    size_t total;
+} csd_cache_layout_t;
+size_t csd_cache_meta_bytes(int rows, int max_pages, int n_pages);          /* 0 on an invalid shape */
+csd_status_t csd_cache_meta_layout(int rows, int max_pages, int n_pages, csd_cache_layout_t *out);
+size_t csd_cache_scratch_bytes(int rows, int max_pages, int n_pages);
+
+/* Counts and free pages from the tables and lengths in meta, flags cleared: after the caller has written those (zeroed
+ * meta and rebuild: an empty cache).  Table entries beyond a row's length become -1.  Three launches; asynchronous. */
+csd_status_t csd_cache_rebuild(const csd_cache_t *cache, void *stream);
+
+/* Room for T more tokens in every row, or n_new[row] (DEVICE [rows]; negative counts as 0).  All rows or none: where the
+ * free pages do not suffice, or a row would pass max_pages, lengths and tables stay and granted is 0 (flags say why).
+ * Pages are handed out lowest id first, rows in order.  A row whose last page is partly filled and also used by other
+ * rows first gets a copy of it, in every layer, as a page of its own (rows taken in order: the last row that still has the page keeps
+ * it).  lens then count the new tokens; granted says how many.  Two launches (bookkeeping, copies); asynchronous.
+ * Errors: INVALID_ARG (null, T < 0), UNSUPPORTED, CUDA. */
+csd_status_t csd_cache_extend(const csd_cache_t *cache, int T, const int32_t *n_new, void *stream);
+
+/* Rows become shorter: to min(lens, max(new_lens, 0)) tokens (DEVICE [rows]); pages past that are given up, and are free
+ * once no row uses them.  One launch. */
+csd_status_t csd_cache_truncate(const csd_cache_t *cache, const int32_t *new_lens, void *stream);
+/* After a verification step: of the tokens granted by the last extension, row b keeps the first min(granted[b],
+ * accept_len[b] + 1) -- the token that was emitted before the step and the accepted drafts.  One launch. */
+csd_status_t csd_cache_commit(const csd_cache_t *cache, const int32_t *accept_len, void *stream);
+/* Row b continues the tokens of row parent[b] as it was when the call started (DEVICE [rows]; b itself: unchanged;
+ * negative: the row becomes empty), sharing its pages.  The permutation and the one-to-many forms of a search over beams,
+ * and freeing rows, are this call.  Two launches. */
+csd_status_t csd_cache_fork(const csd_cache_t *cache, const int32_t *parent, void *stream);
+/* With n pages in use, they become pages 0 .. n-1: the i-th lowest page in use at or above n moves to the i-th lowest free
+ * one below, in every layer; tables and counts follow.  Three launches. */
+csd_status_t csd_cache_compact(const csd_cache_t *cache, void *stream);
+
+/* One launch for the new tokens of a layer, turned at their places and stored: token t of row b lies at place
+ * lens[b] - n_new[b] + t (n_new NULL: T for every row).  q' to q_out [rows, T, q_heads, dim] (dense; may be q itself), k'
+ * and v to their page slots.  A token that does not exist (t >= n_new[b], or a negative place) gets a zero query and
+ * stores nothing.  q, k, v: [rows, T, heads, dim] of the cache's type, strides in elements, dim contiguous (slices of one projection's
+ * output qualify).  rope NULL: no rotation.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+csd_status_t csd_rope_append(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int q_heads,
+                             const void *k, int64_t k_stride_b, int64_t k_stride_t, int64_t k_stride_h,
+                             const void *v, int64_t v_stride_b, int64_t v_stride_t, int64_t v_stride_h,
+                             void *q_out, int T, const csd_cache_t *cache, int layer, const csd_rope_t *rope,
+                             const int32_t *n_new, void *stream);
+
+/* Attention of the T newest tokens of every row over its cache: with g = q_heads / heads,
+ *     out[b,t,h] = sum_j w_j v_j,  w = softmax_j(scale q[b,t,h].k_j),  lse[b,t,h] = ln sum_j exp(scale q[b,t,h].k_j)
+ * over the places j <= lens[b] - n_new[b] + t of key head h / g.  A token that sees nothing (an empty row, t >= n_new[b], a
+ * negative place) gives zeros and lse = -inf; what lies in places that a token does not see, infinities and NaN included,
+ * does not reach its result.
+ * q: [rows, T, q_heads, dim] of the cache's type, strides in elements, dim contiguous, 16-byte aligned (base and
+ * strides); T <= CSD_MAX_K + 1; out: dense, the cache's type, 16-byte aligned; lse: float [rows, T, q_heads] or NULL.
+ * scale: finite.  Scores, maxima and sums are float32; the weights are rounded to the cache's type for the second product
+ * and counted in the sum before that rounding.
+ * The places of all rows and heads are split evenly over the GPU; a (row, head) that several blocks read is joined by the
+ * last of them to finish, in a fixed order, so results are bit-reproducible for given lengths.
+ * workspace: csd_attention_workspace_bytes bytes, 256-byte aligned, initialised once with csd_workspace_init; one call at a
+ * time; any shape that it is large enough for.
+ * One launch; asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (q_heads not a multiple of heads, T), WORKSPACE, CUDA. */
+size_t csd_attention_workspace_bytes(int rows, int T, int q_heads, int heads, int dim);
+csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads,
+                           const csd_cache_t *cache, int layer, float scale, const int32_t *n_new,
+                           void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- helpers ---- */
 

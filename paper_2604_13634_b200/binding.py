@@ -18,7 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # CSD_DEBUG=1 in the environment selects the bounds-checked build of the same sources
 LIB_PATH = os.path.join(_HERE, "libcsd_debug.so" if os.environ.get("CSD_DEBUG", "0") not in ("", "0") else "libcsd.so")
 
-CSD_F32, CSD_BF16 = 0, 1
+CSD_F32, CSD_BF16, CSD_F16 = 0, 1, 2
 CSD_MAX_K = 32
 FLAG_NAN_LOGIT, FLAG_BAD_DRAFT, FLAG_PROBE_EXHAUSTED, FLAG_COUNT_SATURATED, FLAG_INTERNAL = 1, 2, 4, 8, 16
 
@@ -32,6 +32,9 @@ EXPORTS = [
     "csd_lmhead_workspace_bytes", "csd_verify_lmhead", "csd_step_lmhead", "csd_lmhead_shape",
     "csd_early_exit_workspace_bytes", "csd_step_early_exit", "csd_lmhead_set_tuning", "csd_lmhead_set_pairing", "csd_lmhead_uses_pairs",
     "csd_sampled_set_rounds", "csd_sampled_launches",
+    "csd_rope_steps", "csd_rope", "csd_rope_append", "csd_attention_workspace_bytes", "csd_attention",
+    "csd_cache_meta_bytes", "csd_cache_meta_layout", "csd_cache_scratch_bytes", "csd_cache_rebuild", "csd_cache_extend",
+    "csd_cache_truncate", "csd_cache_commit", "csd_cache_fork", "csd_cache_compact",
 ]
 
 

@@ -9,6 +9,7 @@
 #include <new>
 
 #include "../../include/csd.h"
+#include "csd_host.h"
 #include "csd_common.cuh"
 #include "csd_ocm.cuh"
 #include "csd_step.cuh"
@@ -1055,9 +1056,7 @@ size_t lmhead_workspace_most(int B, int K, int H, int V)
     return a > b ? a : b;
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+using host::EncodeTiledFn;
 
 EncodeTiledFn encode_tiled_fn()
 {
@@ -1628,3 +1627,13 @@ const char *csd_status_string(csd_status_t status)
 }
 
 }  // extern "C"
+
+namespace csd {
+namespace host {
+
+EncodeTiledFn encode_tiled() { return encode_tiled_fn(); }
+int multiprocessors() { return sm_count(); }
+void other_work_enqueued() { chain_break(); }
+
+}  // namespace host
+}  // namespace csd

@@ -1,0 +1,454 @@
+// C ABI of the decode-pass operators: rotary positions, the paged cache, attention over it (declared in include/csd.h).
+#include <climits>
+#include <cmath>
+#include <cstring>
+
+#include "../../include/csd.h"
+#include "csd_host.h"
+#include "csd_attention.cuh"
+#include "csd_pages.cuh"
+#include "csd_rope.cuh"
+
+using namespace csd;
+
+namespace {
+
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+csd_status_t launched() { return cudaGetLastError() == cudaSuccess ? CSD_OK : CSD_ERR_CUDA; }
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// ---- rotary positions ---------------------------------------------------------------------------
+
+bool rope_ok(const csd_rope_t *r, int D)
+{
+    return r->steps && r->rot >= 2 && r->rot % 2 == 0 && r->rot <= D &&
+           (r->layout == CSD_ROPE_HALF || r->layout == CSD_ROPE_INTERLEAVED) && std::isfinite(r->magnitude);
+}
+
+// 16-byte accesses need every unit of every head to begin on a 16-byte boundary.
+template <int P>
+bool units_fit(int rot, int D)
+{
+    return D % P == 0 && rot % (2 * P) == 0;
+}
+
+template <int P>
+int units_of(int rot, int D)
+{
+    return rot / (2 * P) + (D - rot + 2 * P - 1) / (2 * P);
+}
+
+template <typename T, int P>
+csd_status_t launch_rope(rope::RopeParams p, csd_rope_layout_t layout, cudaStream_t st)
+{
+    p.units = units_of<P>(p.turn.rot, p.D);
+    p.groups = (p.H + rope::kHeads - 1) / rope::kHeads;
+    p.threads = static_cast<long long>(p.B) * p.S * p.groups * p.units;
+    const long long blocks = (p.threads + rope::kThreads - 1) / rope::kThreads;
+    if (blocks > INT_MAX) return CSD_ERR_UNSUPPORTED;
+    if (layout == CSD_ROPE_HALF)
+        rope::rope_kernel<T, P, true><<<static_cast<unsigned int>(blocks), rope::kThreads, 0, st>>>(p);
+    else
+        rope::rope_kernel<T, P, false><<<static_cast<unsigned int>(blocks), rope::kThreads, 0, st>>>(p);
+    return launched();
+}
+
+template <typename T>
+csd_status_t run_rope(const rope::RopeParams &p, csd_rope_layout_t layout, cudaStream_t st)
+{
+    constexpr int P = 16 / static_cast<int>(sizeof(T));
+    const long long all = p.xb | p.xs | p.xh | p.yb | p.ys | p.yh;
+    if (units_fit<P>(p.turn.rot, p.D) && all % P == 0 && aligned16(p.x) && aligned16(p.y)) return launch_rope<T, P>(p, layout, st);
+    return launch_rope<T, 1>(p, layout, st);
+}
+
+template <typename T, int P>
+csd_status_t launch_append(rope::AppendParams p, csd_rope_layout_t layout, cudaStream_t st)
+{
+    p.units = units_of<P>(p.turn.rot, p.D);
+    p.q_groups = (p.Hq + rope::kHeads - 1) / rope::kHeads;
+    p.kv_groups = (p.Hkv + rope::kHeads - 1) / rope::kHeads;
+    p.threads = static_cast<long long>(p.B) * p.T * (p.q_groups + 2 * p.kv_groups) * p.units;
+    const long long blocks = (p.threads + rope::kThreads - 1) / rope::kThreads;
+    if (blocks > INT_MAX) return CSD_ERR_UNSUPPORTED;
+    if (layout == CSD_ROPE_HALF)
+        rope::rope_append_kernel<T, P, true><<<static_cast<unsigned int>(blocks), rope::kThreads, 0, st>>>(p);
+    else
+        rope::rope_append_kernel<T, P, false><<<static_cast<unsigned int>(blocks), rope::kThreads, 0, st>>>(p);
+    return launched();
+}
+
+template <typename T>
+csd_status_t run_append(const rope::AppendParams &p, csd_rope_layout_t layout, cudaStream_t st)
+{
+    constexpr int P = 8;
+    const long long all = p.qb | p.qt | p.qh | p.kb | p.kt | p.kh | p.vb | p.vt | p.vh;
+    if (units_fit<P>(p.turn.rot, p.D) && all % P == 0 && aligned16(p.q) && aligned16(p.k) && aligned16(p.v) && aligned16(p.q_out))
+        return launch_append<T, P>(p, layout, st);
+    return launch_append<T, 1>(p, layout, st);
+}
+
+// ---- the cache ----------------------------------------------------------------------------------
+
+constexpr int kStatusWords = 64;                     // flags, page copies wanted, reserved
+
+bool cache_shape_ok(int rows, int max_pages, int n_pages)
+{
+    return rows > 0 && rows <= CSD_CACHE_MAX_ROWS && max_pages > 0 && n_pages > 0 && n_pages <= (1 << 28) &&
+           static_cast<long long>(rows) * (max_pages + 1ll) <= (1ll << 31) - 1;
+}
+
+csd_cache_layout_t meta_layout(int rows, int max_pages, int n_pages)
+{
+    csd_cache_layout_t l;
+    size_t at = 0;
+    auto take = [&](size_t words) {
+        const size_t o = at;
+        at = align_up(at + words * 4, 256);
+        return o;
+    };
+    l.flags = take(kStatusWords);
+    l.lens = take(static_cast<size_t>(rows));
+    l.granted = take(static_cast<size_t>(rows));
+    l.table = take(static_cast<size_t>(rows) * max_pages);
+    l.refs = take(static_cast<size_t>(n_pages));
+    l.free_bits = take((static_cast<size_t>(n_pages) + 31) / 32);
+    l.total = at;
+    return l;
+}
+
+struct ScratchLayout {
+    size_t moves, list, staged, total;
+};
+
+ScratchLayout scratch_layout(int rows, int max_pages, int n_pages)
+{
+    ScratchLayout s;
+    // a copy per row (extend) or per second page (compact), and one word more
+    const size_t pairs = static_cast<size_t>(rows > n_pages / 2 ? rows : n_pages / 2) + 1;
+    s.moves = 0;
+    s.list = align_up(pairs * 8, 256);
+    s.staged = s.list + align_up(static_cast<size_t>(n_pages) * 4, 256);
+    s.total = s.staged + align_up(static_cast<size_t>(rows) * (max_pages + 1) * 4, 256);
+    return s;
+}
+
+csd_status_t check_cache(const csd_cache_t *c)
+{
+    if (!c || !c->k || !c->v || !c->meta || !c->scratch) return CSD_ERR_INVALID_ARG;
+    if (c->dtype != CSD_BF16 && c->dtype != CSD_F16) return c->dtype == CSD_F32 ? CSD_ERR_UNSUPPORTED : CSD_ERR_INVALID_ARG;
+    if (c->layers <= 0 || c->n_pages <= 0 || c->heads <= 0 || c->dim <= 0 || c->rows <= 0 || c->max_pages <= 0) return CSD_ERR_INVALID_ARG;
+    if (c->page_size < 8 || c->page_size > 256 || (c->page_size & (c->page_size - 1)) != 0) return CSD_ERR_UNSUPPORTED;
+    if (c->dim % 8 != 0 || c->dim > 256 || c->heads > 4096) return CSD_ERR_UNSUPPORTED;
+    if (!cache_shape_ok(c->rows, c->max_pages, c->n_pages) || static_cast<long long>(c->max_pages) * c->page_size > (1ll << 30)) return CSD_ERR_UNSUPPORTED;
+    if (!aligned16(c->k) || !aligned16(c->v)) return CSD_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(c->meta) & 255u) || (reinterpret_cast<uintptr_t>(c->scratch) & 255u)) return CSD_ERR_INVALID_ARG;
+    const int64_t page = static_cast<int64_t>(c->heads) * c->page_size * c->dim;
+    const bool heads_outside = c->stride_token == c->dim && c->stride_head == static_cast<int64_t>(c->page_size) * c->dim;
+    const bool tokens_outside = c->stride_head == c->dim && c->stride_token == static_cast<int64_t>(c->heads) * c->dim;
+    // (with one head or eight-token pages the two orders can coincide; either reading is then the same memory)
+    const bool one_head = c->heads == 1 && c->stride_token == c->dim;
+    if (!heads_outside && !tokens_outside && !one_head) return CSD_ERR_INVALID_ARG;
+    if (c->stride_page < page || c->stride_page % 8 != 0 || c->stride_page > (1ll << 36)) return CSD_ERR_INVALID_ARG;
+    if (c->layers > 1) {
+        if (c->stride_layer % 8 != 0 || c->stride_layer > (1ll << 40)) return CSD_ERR_INVALID_ARG;
+        const bool layers_outside = c->stride_layer >= (c->n_pages - 1ll) * c->stride_page + page;
+        const bool pages_outside = c->stride_layer >= page && c->stride_page >= (c->layers - 1ll) * c->stride_layer + page;
+        if (!layers_outside && !pages_outside) return CSD_ERR_INVALID_ARG;
+    }
+    return CSD_OK;
+}
+
+pages::View view_of(const csd_cache_t *c)
+{
+    const csd_cache_layout_t l = meta_layout(c->rows, c->max_pages, c->n_pages);
+    const ScratchLayout s = scratch_layout(c->rows, c->max_pages, c->n_pages);
+    char *m = static_cast<char *>(c->meta), *x = static_cast<char *>(c->scratch);
+    pages::View v;
+    v.rows = c->rows;
+    v.max_pages = c->max_pages;
+    v.n_pages = c->n_pages;
+    v.page_size = c->page_size;
+    v.page_shift = 0;
+    while ((1 << v.page_shift) < c->page_size) ++v.page_shift;
+    v.words = (c->n_pages + 31) / 32;
+    v.flags = reinterpret_cast<unsigned int *>(m + l.flags);
+    v.n_moves = reinterpret_cast<int *>(m + l.flags) + 1;
+    v.lens = reinterpret_cast<int *>(m + l.lens);
+    v.granted = reinterpret_cast<int *>(m + l.granted);
+    v.table = reinterpret_cast<int *>(m + l.table);
+    v.refs = reinterpret_cast<int *>(m + l.refs);
+    v.free_bits = reinterpret_cast<unsigned int *>(m + l.free_bits);
+    v.moves = reinterpret_cast<int *>(x + s.moves);
+    v.list = reinterpret_cast<int *>(x + s.list);
+    v.staged = reinterpret_cast<int *>(x + s.staged);
+    return v;
+}
+
+// The copies that the bookkeeping launch before has listed; at most `most` pages.
+csd_status_t copy_pages(const csd_cache_t *c, const pages::View &v, long long most, cudaStream_t st)
+{
+    pages::CopyParams p;
+    p.k = static_cast<char *>(c->k);
+    p.v = static_cast<char *>(c->v);
+    p.layer_bytes = c->stride_layer * 2;
+    p.page_stride_bytes = c->stride_page * 2;
+    p.page_bytes = c->heads * c->page_size * c->dim * 2;
+    p.layers = c->layers;
+    p.pieces = (p.page_bytes + pages::kCopyBytes - 1) / pages::kCopyBytes;
+    p.n_moves = v.n_moves;
+    p.moves = v.moves;
+    const long long items = most * p.layers * 2 * p.pieces, per_block = pages::kCopyThreads / 32;
+    long long blocks = (items + per_block - 1) / per_block;
+    const long long cap = static_cast<long long>(host::multiprocessors()) * 8;
+    if (blocks > cap) blocks = cap;
+    if (blocks < 1) return CSD_OK;
+    pages::pages_copy_kernel<<<static_cast<unsigned int>(blocks), pages::kCopyThreads, 0, st>>>(p);
+    return launched();
+}
+
+// ---- attention ----------------------------------------------------------------------------------
+
+template <typename T>
+void launch_attention_simple(const attention::Params &p, cudaStream_t st)
+{
+    attention::attention_simple_kernel<T><<<static_cast<unsigned int>(p.B * p.T * p.Hq), 128, 0, st>>>(p);
+}
+
+}  // namespace
+
+extern "C" {
+
+csd_status_t csd_rope_steps(int rot, double base, csd_rope_scaling_t scaling, double factor, double original_len, double low,
+                            double high, uint64_t *steps, float *magnitude)
+{
+    if (!steps || !magnitude || rot < 2 || rot % 2 != 0 || rot > 65536) return CSD_ERR_INVALID_ARG;
+    if (!(base > 1.0) || !std::isfinite(base) || !(factor >= 1.0) || !std::isfinite(factor)) return CSD_ERR_INVALID_ARG;
+    if (scaling < CSD_ROPE_PLAIN || scaling > CSD_ROPE_YARN) return CSD_ERR_INVALID_ARG;
+    if (scaling >= CSD_ROPE_PARTS &&
+        (!(original_len > 0.0) || !std::isfinite(original_len) || !(low > 0.0) || !(high > low) || !std::isfinite(high)))
+        return CSD_ERR_INVALID_ARG;
+    const double two_pi = 2.0 * 3.14159265358979323846;
+    const double b = scaling == CSD_ROPE_BASE && rot > 2 ? base * std::pow(factor, rot / (rot - 2.0)) : base;
+    double from = 0.0, to = 0.0;                     // pairs between which the blend of YARN goes
+    if (scaling == CSD_ROPE_YARN) {
+        from = std::floor(rot * std::log(original_len / (high * two_pi)) / (2.0 * std::log(base)));
+        to = std::ceil(rot * std::log(original_len / (low * two_pi)) / (2.0 * std::log(base)));
+        if (from < 0.0) from = 0.0;
+        if (to > rot - 1.0) to = rot - 1.0;
+        if (to - from < 0.001) to = from + 0.001;
+    }
+    for (int i = 0; i < rot / 2; ++i) {
+        double th = std::pow(b, -2.0 * i / rot), keep = 1.0;
+        if (scaling == CSD_ROPE_LINEAR) keep = 0.0;
+        if (scaling == CSD_ROPE_PARTS) keep = (original_len * th / two_pi - low) / (high - low);
+        if (scaling == CSD_ROPE_YARN) keep = 1.0 - (i - from) / (to - from);
+        keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+        if (scaling != CSD_ROPE_PLAIN && scaling != CSD_ROPE_BASE) th = th * keep + th / factor * (1.0 - keep);
+        steps[i] = static_cast<uint64_t>(std::nearbyint(th / two_pi * 18446744073709551616.0));    // below 2^62
+    }
+    *magnitude = scaling == CSD_ROPE_YARN ? static_cast<float>(0.1 * std::log(factor) + 1.0) : 1.0f;
+    return CSD_OK;
+}
+
+csd_status_t csd_rope(const void *x, void *y, csd_dtype_t dtype, int B, int S, int H, int D, int64_t x_stride_b, int64_t x_stride_s,
+                      int64_t x_stride_h, int64_t y_stride_b, int64_t y_stride_s, int64_t y_stride_h, const int32_t *positions,
+                      int64_t pos_stride_b, int64_t pos_stride_s, const csd_rope_t *rope, int inverse, void *stream)
+{
+    if (!rope || B < 0 || S < 0 || H < 0 || D <= 0 || !rope_ok(rope, D)) return CSD_ERR_INVALID_ARG;
+    if (dtype != CSD_F32 && dtype != CSD_BF16 && dtype != CSD_F16) return CSD_ERR_INVALID_ARG;
+    if (B == 0 || S == 0 || H == 0) return CSD_OK;
+    if (!x || !y || !positions) return CSD_ERR_INVALID_ARG;
+    host::other_work_enqueued();
+    rope::RopeParams p;
+    std::memset(&p, 0, sizeof p);
+    p.x = x;
+    p.y = y;
+    p.B = B; p.S = S; p.H = H; p.D = D;
+    p.xb = x_stride_b; p.xs = x_stride_s; p.xh = x_stride_h;
+    p.yb = y_stride_b; p.ys = y_stride_s; p.yh = y_stride_h;
+    p.positions = positions;
+    p.pb = pos_stride_b; p.ps = pos_stride_s;
+    p.turn.steps = reinterpret_cast<const unsigned long long *>(rope->steps);
+    p.turn.rot = rope->rot;
+    p.turn.magnitude = rope->magnitude;
+    p.inverse = inverse;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == CSD_F32) return run_rope<float>(p, rope->layout, st);
+    if (dtype == CSD_BF16) return run_rope<__nv_bfloat16>(p, rope->layout, st);
+    return run_rope<__half>(p, rope->layout, st);
+}
+
+csd_status_t csd_rope_append(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int q_heads, const void *k,
+                             int64_t k_stride_b, int64_t k_stride_t, int64_t k_stride_h, const void *v, int64_t v_stride_b,
+                             int64_t v_stride_t, int64_t v_stride_h, void *q_out, int T, const csd_cache_t *cache, int layer,
+                             const csd_rope_t *rope, const int32_t *n_new, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    if (!q || !k || !v || !q_out || T <= 0 || q_heads <= 0 || layer < 0 || layer >= cache->layers) return CSD_ERR_INVALID_ARG;
+    if (rope && !rope_ok(rope, cache->dim)) return CSD_ERR_INVALID_ARG;
+    host::other_work_enqueued();
+    const pages::View pv = view_of(cache);
+    rope::AppendParams p;
+    std::memset(&p, 0, sizeof p);
+    p.q = q; p.k = k; p.v = v;
+    p.q_out = q_out;
+    p.k_pool = static_cast<char *>(cache->k) + layer * cache->stride_layer * 2;
+    p.v_pool = static_cast<char *>(cache->v) + layer * cache->stride_layer * 2;
+    p.B = cache->rows; p.T = T; p.Hq = q_heads; p.Hkv = cache->heads; p.D = cache->dim;
+    p.qb = q_stride_b; p.qt = q_stride_t; p.qh = q_stride_h;
+    p.kb = k_stride_b; p.kt = k_stride_t; p.kh = k_stride_h;
+    p.vb = v_stride_b; p.vt = v_stride_t; p.vh = v_stride_h;
+    p.pool_page = cache->stride_page; p.pool_head = cache->stride_head; p.pool_token = cache->stride_token;
+    p.page_shift = pv.page_shift;
+    p.n_pages = cache->n_pages;
+    p.max_pages = cache->max_pages;
+    p.table = pv.table; p.lens = pv.lens; p.n_new = n_new;
+    p.flags = pv.flags;
+    if (rope) {
+        p.turn.steps = reinterpret_cast<const unsigned long long *>(rope->steps);
+        p.turn.rot = rope->rot;
+        p.turn.magnitude = rope->magnitude;
+    }
+    const csd_rope_layout_t layout = rope ? rope->layout : CSD_ROPE_HALF;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return cache->dtype == CSD_BF16 ? run_append<__nv_bfloat16>(p, layout, st) : run_append<__half>(p, layout, st);
+}
+
+size_t csd_cache_meta_bytes(int rows, int max_pages, int n_pages)
+{
+    return cache_shape_ok(rows, max_pages, n_pages) ? meta_layout(rows, max_pages, n_pages).total : 0;
+}
+
+csd_status_t csd_cache_meta_layout(int rows, int max_pages, int n_pages, csd_cache_layout_t *out)
+{
+    if (!out || !cache_shape_ok(rows, max_pages, n_pages)) return CSD_ERR_INVALID_ARG;
+    *out = meta_layout(rows, max_pages, n_pages);
+    return CSD_OK;
+}
+
+size_t csd_cache_scratch_bytes(int rows, int max_pages, int n_pages)
+{
+    return cache_shape_ok(rows, max_pages, n_pages) ? scratch_layout(rows, max_pages, n_pages).total : 0;
+}
+
+csd_status_t csd_cache_rebuild(const csd_cache_t *cache, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    host::other_work_enqueued();
+    const pages::View v = view_of(cache);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (cudaMemsetAsync(v.flags, 0, kStatusWords * 4, st) != cudaSuccess ||
+        cudaMemsetAsync(v.refs, 0, static_cast<size_t>(cache->n_pages) * 4, st) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CSD_ERR_CUDA;
+    }
+    pages::rebuild_count_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, st>>>(v);
+    pages::rebuild_bits_kernel<<<static_cast<unsigned int>((v.n_pages + pages::kRowThreads - 1) / pages::kRowThreads), pages::kRowThreads, 0, st>>>(v);
+    return launched();
+}
+
+csd_status_t csd_cache_extend(const csd_cache_t *cache, int T, const int32_t *n_new, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    if (T < 0) return CSD_ERR_INVALID_ARG;
+    host::other_work_enqueued();
+    const pages::View v = view_of(cache);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    pages::extend_kernel<<<1, pages::kBlock, 0, st>>>(v, n_new, T);
+    if (launched() != CSD_OK) return CSD_ERR_CUDA;
+    return copy_pages(cache, v, cache->rows, st);
+}
+
+static csd_status_t shorten(const csd_cache_t *cache, const int32_t *new_lens, const int32_t *accept_len, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    if (!new_lens && !accept_len) return CSD_ERR_INVALID_ARG;
+    host::other_work_enqueued();
+    const pages::View v = view_of(cache);
+    pages::truncate_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, static_cast<cudaStream_t>(stream)>>>(v, new_lens, accept_len);
+    return launched();
+}
+
+csd_status_t csd_cache_truncate(const csd_cache_t *cache, const int32_t *new_lens, void *stream) { return shorten(cache, new_lens, nullptr, stream); }
+
+csd_status_t csd_cache_commit(const csd_cache_t *cache, const int32_t *accept_len, void *stream) { return shorten(cache, nullptr, accept_len, stream); }
+
+csd_status_t csd_cache_fork(const csd_cache_t *cache, const int32_t *parent, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    if (!parent) return CSD_ERR_INVALID_ARG;
+    host::other_work_enqueued();
+    const pages::View v = view_of(cache);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    pages::fork_stage_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, st>>>(v, parent);
+    pages::fork_commit_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, st>>>(v, parent);
+    return launched();
+}
+
+csd_status_t csd_cache_compact(const csd_cache_t *cache, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    host::other_work_enqueued();
+    const pages::View v = view_of(cache);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    pages::compact_kernel<<<1, pages::kBlock, 0, st>>>(v);
+    pages::rename_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, st>>>(v);
+    if (launched() != CSD_OK) return CSD_ERR_CUDA;
+    return copy_pages(cache, v, cache->n_pages / 2, st);
+}
+
+size_t csd_attention_workspace_bytes(int rows, int T, int q_heads, int heads, int dim)
+{
+    if (rows <= 0 || rows > CSD_CACHE_MAX_ROWS || T <= 0 || T > CSD_MAX_K + 1 || heads <= 0 || heads > 4096 || q_heads <= 0 || q_heads % heads != 0 ||
+        dim <= 0 || dim > 256 || dim % 8 != 0)
+        return 0;
+    return 4096;
+}
+
+csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads,
+                           const csd_cache_t *cache, int layer, float scale, const int32_t *n_new, void *out, float *lse,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    if (!q || !out || !workspace || T <= 0 || q_heads <= 0 || layer < 0 || layer >= cache->layers || !std::isfinite(scale)) return CSD_ERR_INVALID_ARG;
+    const size_t need = csd_attention_workspace_bytes(cache->rows, T, q_heads, cache->heads, cache->dim);
+    if (need == 0) return CSD_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(out) || (q_stride_b | q_stride_t | q_stride_h) % 8 != 0) return CSD_ERR_INVALID_ARG;
+    if (workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return CSD_ERR_WORKSPACE;
+    host::other_work_enqueued();
+    const pages::View pv = view_of(cache);
+    attention::Params p;
+    std::memset(&p, 0, sizeof p);
+    p.q = q;
+    p.k_pool = static_cast<char *>(cache->k) + layer * cache->stride_layer * 2;
+    p.v_pool = static_cast<char *>(cache->v) + layer * cache->stride_layer * 2;
+    p.out = out;
+    p.lse = lse;
+    p.B = cache->rows; p.T = T; p.Hq = q_heads; p.Hkv = cache->heads; p.D = cache->dim; p.group = q_heads / cache->heads;
+    p.qb = q_stride_b; p.qt = q_stride_t; p.qh = q_stride_h;
+    p.pool_page = cache->stride_page; p.pool_head = cache->stride_head; p.pool_token = cache->stride_token;
+    p.page_shift = pv.page_shift;
+    p.n_pages = cache->n_pages;
+    p.max_pages = cache->max_pages;
+    p.table = pv.table; p.lens = pv.lens; p.n_new = n_new;
+    p.flags = pv.flags;
+    p.scale = scale;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (cache->dtype == CSD_BF16)
+        launch_attention_simple<__nv_bfloat16>(p, st);
+    else
+        launch_attention_simple<__half>(p, st);
+    return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,264 @@
+"""ctypes binding of the decode-pass operators: rotary positions, the paged cache, attention over it.
+
+Like binding.py: argument marshalling only, one function per entry point of include/csd.h, every failure raises.
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+from ctypes import POINTER, Structure, byref, c_double, c_float, c_int, c_int64, c_size_t, c_uint64, c_void_p
+
+import torch
+
+from .binding import CSD_BF16, CSD_F16, CSD_F32, CSD_MAX_K, CsdError, _check, _ptr, _stream_ptr, lib
+
+CACHE_FULL, CACHE_ROW_FULL, CACHE_BAD_PAGE, CACHE_BAD_ROW, CACHE_INTERNAL = 1, 2, 4, 8, 16
+
+_DTYPES = {torch.float32: CSD_F32, torch.bfloat16: CSD_BF16, torch.float16: CSD_F16}
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3, "yarn": 4}
+_RANGES = {"parts": (1.0, 4.0), "yarn": (1.0, 32.0)}          # turns: pairs that make fewer are stretched, more are kept
+
+
+class RopeStruct(Structure):
+    _fields_ = [("steps", c_void_p), ("rot", c_int), ("layout", c_int), ("magnitude", c_float)]
+
+
+class CacheStruct(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("dtype", c_int), ("layers", c_int), ("n_pages", c_int), ("page_size", c_int),
+                ("heads", c_int), ("dim", c_int), ("stride_layer", c_int64), ("stride_page", c_int64), ("stride_head", c_int64),
+                ("stride_token", c_int64), ("rows", c_int), ("max_pages", c_int), ("meta", c_void_p), ("scratch", c_void_p)]
+
+
+class CacheLayout(Structure):
+    _fields_ = [(n, c_size_t) for n in ("flags", "lens", "granted", "table", "refs", "free_bits", "total")]
+
+
+_strides3 = [c_int64] * 3
+SIGNATURES = {
+    "csd_rope_steps": (c_int, [c_int, c_double, c_int, c_double, c_double, c_double, c_double, POINTER(c_uint64), POINTER(c_float)]),
+    "csd_rope": (c_int, [c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, *_strides3, *_strides3, c_void_p, c_int64, c_int64,
+                         POINTER(RopeStruct), c_int, c_void_p]),
+    "csd_rope_append": (c_int, [c_void_p, *_strides3, c_int, c_void_p, *_strides3, c_void_p, *_strides3, c_void_p, c_int,
+                                POINTER(CacheStruct), c_int, POINTER(RopeStruct), c_void_p, c_void_p]),
+    "csd_cache_meta_bytes": (c_size_t, [c_int, c_int, c_int]),
+    "csd_cache_meta_layout": (c_int, [c_int, c_int, c_int, POINTER(CacheLayout)]),
+    "csd_cache_scratch_bytes": (c_size_t, [c_int, c_int, c_int]),
+    "csd_cache_rebuild": (c_int, [POINTER(CacheStruct), c_void_p]),
+    "csd_cache_extend": (c_int, [POINTER(CacheStruct), c_int, c_void_p, c_void_p]),
+    "csd_cache_truncate": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
+    "csd_cache_commit": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
+    "csd_cache_fork": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
+    "csd_cache_compact": (c_int, [POINTER(CacheStruct), c_void_p]),
+    "csd_attention_workspace_bytes": (c_size_t, [c_int] * 5),
+    "csd_attention": (c_int, [c_void_p, *_strides3, c_int, c_int, POINTER(CacheStruct), c_int, c_float, c_void_p, c_void_p, c_void_p,
+                              c_void_p, c_size_t, c_void_p]),
+}
+
+_typed = None
+
+
+def _lib():
+    global _typed
+    if _typed is None:
+        L = lib()
+        for name, (res, args) in SIGNATURES.items():
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = res, args
+        _typed = L
+    return _typed
+
+
+def csd_rope_steps(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_len: float = 8192,
+                   low: float | None = None, high: float | None = None):
+    """(steps, magnitude): the rotation per position of each pair as a 64-bit fraction of a turn (an int64 CPU tensor
+    with the same bits), and the factor on turned elements."""
+    if scaling not in _SCALINGS:
+        raise CsdError(f"unknown scaling {scaling!r}: one of {sorted(_SCALINGS)}")
+    lo, hi = _RANGES.get(scaling, (1.0, 2.0))
+    steps = (c_uint64 * max(1, rot // 2))()
+    magnitude = c_float()
+    _check(_lib().csd_rope_steps(rot, base, _SCALINGS[scaling], factor, original_len, lo if low is None else low, hi if high is None else high,
+                                 steps, byref(magnitude)), "csd_rope_steps")
+    return torch.frombuffer(steps, dtype=torch.int64).clone(), float(magnitude.value)
+
+
+class RopePlan:
+    """A rotation in device memory: `rot` elements of every head, frequencies base^(-2i/rot), scaled for long contexts."""
+
+    def __init__(self, rot: int, base: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+                 original_len: float = 8192, low: float | None = None, high: float | None = None, device="cuda"):
+        if layout not in _LAYOUTS:
+            raise CsdError(f"unknown layout {layout!r}: one of {sorted(_LAYOUTS)}")
+        steps, self.magnitude = csd_rope_steps(rot, base, scaling, factor, original_len, low, high)
+        self.rot, self.layout = rot, layout
+        self.steps = steps.to(device)
+        self._struct = RopeStruct(self.steps.data_ptr(), rot, _LAYOUTS[layout], self.magnitude)
+
+
+def csd_rope(x, positions, plan: RopePlan, out=None, inverse: bool = False, stream=None):
+    """x [B, S, H, D] turned by positions [B, S] int32 (or [S], shared by the batch); `inverse` turns back, which is the
+    gradient.  `out` may be x itself.  Returns out."""
+    assert x.is_cuda and x.dim() == 4 and x.stride(3) == 1 and positions.is_cuda and positions.dtype == torch.int32
+    if x.dtype not in _DTYPES:
+        raise CsdError(f"x must be float32, bfloat16 or float16, got {x.dtype}")
+    out = torch.empty_like(x) if out is None else out
+    B, S, H, D = x.shape
+    assert out.shape == x.shape and out.dtype == x.dtype and out.stride(3) == 1 and out.is_cuda
+    assert tuple(positions.shape) in ((B, S), (S,))
+    pb, ps = positions.stride() if positions.dim() == 2 else (0, positions.stride(0))
+    rc = _lib().csd_rope(x.data_ptr(), out.data_ptr(), _DTYPES[x.dtype], B, S, H, D, *x.stride()[:3], *out.stride()[:3],
+                         positions.data_ptr(), pb, ps, byref(plan._struct), 1 if inverse else 0, _stream_ptr(stream))
+    _check(rc, "csd_rope")
+    return out
+
+
+class PagedCache:
+    """Keys and values of `rows` sequences in pages, with the bookkeeping on the device.
+
+    k, v: [layers, n_pages, kv_heads, page_size, head_dim] views (whatever lies outside within a page); pass your own to
+    adopt them.  table, lens, granted, refs are views of `meta`: copying meta saves or restores the bookkeeping.
+    """
+
+    def __init__(self, rows: int, n_pages: int, page_size: int, layers: int, kv_heads: int, head_dim: int, dtype: torch.dtype,
+                 max_len: int, k=None, v=None, token_major: bool = False, device="cuda"):
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise CsdError(f"a cache holds bfloat16 or float16, got {dtype}")
+        if page_size <= 0 or max_len <= 0:
+            raise CsdError(f"unsupported page_size={page_size} max_len={max_len}")
+        shape = (layers, n_pages, kv_heads, page_size, head_dim)
+        dev = k.device if k is not None else torch.device(device)
+        if k is None:
+            made = (layers, n_pages, page_size, kv_heads, head_dim) if token_major else shape
+            k, v = (torch.zeros(made, dtype=dtype, device=dev) for _ in range(2))
+            if token_major:
+                k, v = k.transpose(2, 3), v.transpose(2, 3)
+        assert tuple(k.shape) == shape == tuple(v.shape) and k.dtype == v.dtype == dtype and k.is_cuda and v.device == k.device
+        assert k.stride() == v.stride() and k.stride(4) == 1
+        self.rows, self.n_pages, self.page_size, self.layers = rows, n_pages, page_size, layers
+        self.kv_heads, self.head_dim, self.dtype = kv_heads, head_dim, dtype
+        self.max_pages = -(-max_len // page_size)
+        self.k, self.v = k, v
+        L = _lib()
+        shape3 = (rows, self.max_pages, n_pages)
+        bytes_ = int(L.csd_cache_meta_bytes(*shape3))
+        if bytes_ == 0:
+            raise CsdError(f"unsupported cache: rows={rows} max_pages={self.max_pages} n_pages={n_pages}")
+        lay = CacheLayout()
+        _check(L.csd_cache_meta_layout(*shape3, byref(lay)), "csd_cache_meta_layout")
+        self.meta = torch.zeros(bytes_ // 4, dtype=torch.int32, device=dev)
+        self.scratch = torch.empty(int(L.csd_cache_scratch_bytes(*shape3)), dtype=torch.uint8, device=dev)
+        part = lambda off, n: self.meta[off // 4:off // 4 + n]  # noqa: E731
+        self.lens, self.granted = part(lay.lens, rows), part(lay.granted, rows)
+        self.table = part(lay.table, rows * self.max_pages).view(rows, self.max_pages)
+        self.refs = part(lay.refs, n_pages)
+        self._flags = part(lay.flags, 1)
+        # strides of dimensions of size 1 mean nothing to torch; the library reads them
+        st = list(k.stride())
+        if kv_heads == 1:
+            st[2], st[3] = page_size * head_dim, head_dim
+        if n_pages == 1:
+            st[1] = kv_heads * page_size * head_dim
+        self._struct = CacheStruct(k.data_ptr(), v.data_ptr(), _DTYPES[dtype], layers, n_pages, page_size, kv_heads, head_dim, st[0],
+                                   st[1], st[2], st[3], rows, self.max_pages, self.meta.data_ptr(), self.scratch.data_ptr())
+        csd_cache_rebuild(self)
+
+    def load(self, table: torch.Tensor, lens: torch.Tensor, stream=None):
+        """Take over page tables [rows, <= max_pages] and lengths [rows] (a checkpoint, or pages filled elsewhere)."""
+        assert table.dtype == lens.dtype == torch.int32 and table.shape[0] == self.rows == lens.shape[0]
+        assert table.shape[1] <= self.max_pages
+        with torch.cuda.stream(torch.cuda.current_stream() if stream is None else stream):
+            self.table[:, :table.shape[1]].copy_(table)
+            self.lens.copy_(lens)
+        csd_cache_rebuild(self, stream)
+
+    def reset(self, stream=None):
+        """Empty every row, free every page, clear the flags."""
+        with torch.cuda.stream(torch.cuda.current_stream() if stream is None else stream):
+            self.lens.zero_()
+        csd_cache_rebuild(self, stream)
+
+    def stats(self) -> dict:
+        """flags, pages in use, pages shared, tokens.  Synchronises."""
+        return dict(flags=int(self._flags.item()), pages=int((self.refs > 0).sum()), shared=int((self.refs > 1).sum()),
+                    tokens=int(self.lens.sum()))
+
+
+def _rows_arg(t, cache: PagedCache, what: str):
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == (cache.rows,), what
+    return t.data_ptr()
+
+
+def csd_cache_rebuild(cache: PagedCache, stream=None):
+    """Counts and free pages from cache.table and cache.lens; clears the flags."""
+    _check(_lib().csd_cache_rebuild(byref(cache._struct), _stream_ptr(stream)), "csd_cache_rebuild")
+
+
+def csd_cache_extend(cache: PagedCache, T: int, n_new=None, stream=None):
+    """Room for T (or n_new[row]) more tokens in every row; cache.granted says how many each row got (all rows or none)."""
+    _check(_lib().csd_cache_extend(byref(cache._struct), T, _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream)), "csd_cache_extend")
+
+
+def csd_cache_truncate(cache: PagedCache, new_lens, stream=None):
+    """Rows keep their first new_lens[row] tokens."""
+    _check(_lib().csd_cache_truncate(byref(cache._struct), _rows_arg(new_lens, cache, "new_lens"), _stream_ptr(stream)), "csd_cache_truncate")
+
+
+def csd_cache_commit(cache: PagedCache, accept_len, stream=None):
+    """After a verification step: of the last extension's tokens, the first accept_len[row] + 1 stay."""
+    _check(_lib().csd_cache_commit(byref(cache._struct), _rows_arg(accept_len, cache, "accept_len"), _stream_ptr(stream)), "csd_cache_commit")
+
+
+def csd_cache_fork(cache: PagedCache, parent, stream=None):
+    """Row b continues row parent[b]'s tokens (itself: unchanged; negative: empty), sharing its pages."""
+    _check(_lib().csd_cache_fork(byref(cache._struct), _rows_arg(parent, cache, "parent"), _stream_ptr(stream)), "csd_cache_fork")
+
+
+def csd_cache_compact(cache: PagedCache, stream=None):
+    """The pages in use become the lowest ones."""
+    _check(_lib().csd_cache_compact(byref(cache._struct), _stream_ptr(stream)), "csd_cache_compact")
+
+
+def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | None, q_out=None, n_new=None, stream=None):
+    """The new tokens of a layer: q [rows, T, q_heads, D] turned into q_out (dense; returned), k turned and v as it is into
+    their page slots.  plan None: no rotation."""
+    B, T, Hq, D = q.shape
+    q_out = torch.empty((B, T, Hq, D), dtype=q.dtype, device=q.device) if q_out is None else q_out
+    assert q.is_cuda and k.is_cuda and v.is_cuda and q.dtype == k.dtype == v.dtype == q_out.dtype == cache.dtype
+    assert B == cache.rows and D == cache.head_dim and tuple(k.shape) == tuple(v.shape) == (B, T, cache.kv_heads, D)
+    assert q.stride(3) == k.stride(3) == v.stride(3) == 1 and tuple(q_out.shape) == (B, T, Hq, D) and q_out.is_contiguous()
+    rc = _lib().csd_rope_append(q.data_ptr(), *q.stride()[:3], Hq, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3],
+                                q_out.data_ptr(), T, byref(cache._struct), layer, byref(plan._struct) if plan is not None else None,
+                                _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream))
+    _check(rc, "csd_rope_append")
+    return q_out
+
+
+class AttentionBuffers:
+    """Caller-owned outputs and workspace of csd_attention for one cache, T new tokens per row and q_heads query heads."""
+
+    def __init__(self, cache: PagedCache, T: int, q_heads: int):
+        self.T, self.q_heads = T, q_heads
+        dev = cache.k.device
+        self.ws_bytes = int(_lib().csd_attention_workspace_bytes(cache.rows, T, q_heads, cache.kv_heads, cache.head_dim))
+        if self.ws_bytes == 0:
+            raise CsdError(f"unsupported attention: rows={cache.rows} T={T} q_heads={q_heads} kv_heads={cache.kv_heads} dim={cache.head_dim}")
+        self.out = torch.empty(cache.rows, T, q_heads, cache.head_dim, dtype=cache.dtype, device=dev)
+        self.lse = torch.empty(cache.rows, T, q_heads, dtype=torch.float32, device=dev)
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+        _check(lib().csd_workspace_init(_ptr(self.workspace), self.ws_bytes, _stream_ptr()), "csd_workspace_init")
+
+
+def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale: float | None = None, n_new=None, stream=None):
+    """buf.out, buf.lse: attention of the T newest tokens of every row, q [rows, T, q_heads, D], over its cache."""
+    assert q.is_cuda and q.dtype == cache.dtype and q.stride(3) == 1
+    assert tuple(q.shape) == (cache.rows, buf.T, buf.q_heads, cache.head_dim)
+    scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else scale
+    rc = _lib().csd_attention(q.data_ptr(), *q.stride()[:3], buf.T, buf.q_heads, byref(cache._struct), layer, c_float(scale),
+                              _rows_arg(n_new, cache, "n_new"), buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(),
+                              buf.ws_bytes, _stream_ptr(stream))
+    _check(rc, "csd_attention")
+    return buf.out
