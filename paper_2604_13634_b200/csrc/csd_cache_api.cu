@@ -1,4 +1,5 @@
 // C ABI of the decode-pass operators: rotary positions, the paged cache, attention over it (declared in include/csd.h).
+#include <atomic>
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -211,10 +212,145 @@ csd_status_t copy_pages(const csd_cache_t *c, const pages::View &v, long long mo
 
 // ---- attention ----------------------------------------------------------------------------------
 
-template <typename T>
-void launch_attention_simple(const attention::Params &p, cudaStream_t st)
+constexpr int kMaxDevices = 64;
+constexpr int kSmemPerSm = 228 * 1024, kSmemReserved = 1024, kSmemStatic = 1024;     // per block: the system's, and the kernel's own
+
+struct AttentionPlan {
+    int rows, row_tiles, tile_rows, dp, grid, stages, smem;
+    size_t splits_off, parts_off, total;
+};
+
+template <typename C>
+AttentionPlan attention_plan(int rows, int B)
 {
-    attention::attention_simple_kernel<T><<<static_cast<unsigned int>(p.B * p.T * p.Hq), 128, 0, st>>>(p);
+    AttentionPlan a;
+    a.rows = rows;
+    a.tile_rows = C::kRows;
+    a.dp = C::DP;
+    a.row_tiles = (rows + C::kRows - 1) / C::kRows;
+    a.grid = host::multiprocessors() * C::kBlocksPerSm;
+    const int limit = kSmemPerSm / C::kBlocksPerSm - kSmemReserved - kSmemStatic;
+    const int fixed = 1024 + C::kQBytes + C::kMlBytes + (B + 1) * 4;
+    a.stages = (limit - fixed) / C::kStageBytes;
+    if (a.stages > attention::kMaxStages) a.stages = attention::kMaxStages;
+    a.smem = fixed + a.stages * C::kStageBytes;
+    a.splits_off = 0;
+    a.parts_off = align_up(static_cast<size_t>(a.grid) * sizeof(attention::Split), 256);
+    a.total = a.parts_off + static_cast<size_t>(2) * a.grid * C::kSlotFloats * 4;
+    return a;
+}
+
+// The variant for `rows` query rows per (row, key head) and dim elements: the smallest row tile that holds them, at most
+// 128 rows (64 beyond dim 128); more rows are further row tiles, which read the keys again.
+template <typename T, typename F>
+auto with_config(int rows, int dim, F f)
+{
+    using attention::Config;
+    if (dim <= 64) {
+        if (rows <= 16) return f(Config<T, 64, 1, 1, 4, 1, 2>());
+        if (rows <= 32) return f(Config<T, 64, 2, 1, 4, 1, 2>());
+        if (rows <= 64) return f(Config<T, 64, 2, 2, 4, 2, 1>());
+        return f(Config<T, 64, 2, 2, 2, 4, 1>());
+    }
+    if (dim <= 128) {
+        if (rows <= 16) return f(Config<T, 128, 1, 1, 4, 1, 2>());
+        if (rows <= 32) return f(Config<T, 128, 2, 1, 4, 1, 2>());
+        if (rows <= 64) return f(Config<T, 128, 2, 2, 4, 2, 1>());
+        return f(Config<T, 128, 2, 2, 2, 4, 1>());
+    }
+    if (rows <= 16) return f(Config<T, 256, 1, 1, 4, 1, 1>());
+    if (rows <= 32) return f(Config<T, 256, 1, 1, 4, 2, 1>());
+    return f(Config<T, 256, 1, 1, 2, 4, 1>());
+}
+
+AttentionPlan attention_plan_of(int T, int group, int dim, int B)
+{
+    return with_config<__nv_bfloat16>(T * group, dim, [&](auto cfg) { return attention_plan<decltype(cfg)>(T * group, B); });
+}
+
+bool attention_shape_ok(int rows, int T, int q_heads, int heads, int dim)
+{
+    if (rows <= 0 || rows > CSD_CACHE_MAX_ROWS || T <= 0 || T > CSD_MAX_K + 1 || heads <= 0 || heads > 4096 || q_heads <= 0 || q_heads > (1 << 16) ||
+        q_heads % heads != 0 || dim <= 0 || dim > 256 || dim % 8 != 0)
+        return false;
+    return static_cast<long long>(rows) * T * q_heads <= (1ll << 27);
+}
+
+// A layer's keys or values as [n_pages, heads, page_size, dim] with boxes of 64 elements x box_rows places, 128-byte swizzle.
+bool make_pool_map(CUtensorMap *map, const csd_cache_t *c, const void *pool, int layer, int box_rows)
+{
+    const host::EncodeTiledFn fn = host::encode_tiled();
+    if (!fn) return false;
+    char *base = static_cast<char *>(const_cast<void *>(pool)) + layer * c->stride_layer * 2;
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c->dim), static_cast<cuuint64_t>(c->page_size), static_cast<cuuint64_t>(c->heads),
+                                static_cast<cuuint64_t>(c->n_pages)};
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(c->stride_token) * 2, static_cast<cuuint64_t>(c->stride_head) * 2,
+                                   static_cast<cuuint64_t>(c->stride_page) * 2};
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_rows), 1, 1};
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    return fn(map, c->dtype == CSD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, box, ones,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Lets the kernel use the shared memory it wants; once per device.
+template <typename C>
+bool attention_ready()
+{
+    static std::atomic<bool> done[kMaxDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) {
+        (void)cudaGetLastError();
+        return false;
+    }
+    if (done[dev].load()) return true;
+    // what the warpgroups take from one another has to be there at launch, or the larger share would be waited for
+    cudaFuncAttributes attr;
+    if (cudaFuncGetAttributes(&attr, attention::attention_kernel<C>) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return false;
+    }
+    if (C::kMoveRegs && attr.numRegs * C::kGroups < C::kConsumerRegs * (C::kGroups - 1) + C::kProducerRegs) return false;
+    if (cudaFuncSetAttribute(attention::attention_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             kSmemPerSm / C::kBlocksPerSm - kSmemReserved - kSmemStatic) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return false;
+    }
+    done[dev].store(true);
+    return true;
+}
+
+template <typename C>
+csd_status_t run_attention(attention::Params p, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
+{
+    if (!attention_ready<C>()) return CSD_ERR_CUDA;
+    const AttentionPlan a = attention_plan<C>(p.T * p.group, p.B);
+    p.rows = a.rows;
+    p.row_tiles = a.row_tiles;
+    p.n_stages = a.stages;
+    p.min_tiles = 1;
+    p.box_rows = cache->page_size < C::kTile ? cache->page_size : C::kTile;
+    p.splits = reinterpret_cast<attention::Split *>(ws + a.splits_off);
+    p.parts = reinterpret_cast<float *>(ws + a.parts_off);
+    CUtensorMap map_k, map_v;
+    if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
+    attention::attention_kernel<C><<<static_cast<unsigned int>(a.grid), C::kThreads, static_cast<size_t>(a.smem), st>>>(map_k, map_v, p);
+    if (launched() != CSD_OK) return CSD_ERR_CUDA;
+    const int most = a.rows < C::kRows ? a.rows : C::kRows;
+    cudaLaunchConfig_t cfg;
+    std::memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(static_cast<unsigned int>(a.grid), static_cast<unsigned int>((most + 7) / 8));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, attention::attention_join_kernel<typename C::T, C::DP>, p, static_cast<int>(C::kRows)) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CSD_ERR_CUDA;
+    }
+    return CSD_OK;
 }
 
 }  // namespace
@@ -408,10 +544,8 @@ csd_status_t csd_cache_compact(const csd_cache_t *cache, void *stream)
 
 size_t csd_attention_workspace_bytes(int rows, int T, int q_heads, int heads, int dim)
 {
-    if (rows <= 0 || rows > CSD_CACHE_MAX_ROWS || T <= 0 || T > CSD_MAX_K + 1 || heads <= 0 || heads > 4096 || q_heads <= 0 || q_heads % heads != 0 ||
-        dim <= 0 || dim > 256 || dim % 8 != 0)
-        return 0;
-    return 4096;
+    if (!attention_shape_ok(rows, T, q_heads, heads, dim)) return 0;
+    return attention_plan_of(T, q_heads / heads, dim, rows).total;
 }
 
 csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads,
@@ -421,6 +555,7 @@ csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t
     const csd_status_t ok = check_cache(cache);
     if (ok != CSD_OK) return ok;
     if (!q || !out || !workspace || T <= 0 || q_heads <= 0 || layer < 0 || layer >= cache->layers || !std::isfinite(scale)) return CSD_ERR_INVALID_ARG;
+    if (static_cast<long long>(cache->rows) * cache->max_pages * cache->page_size > (1ll << 35)) return CSD_ERR_UNSUPPORTED;   // tiles are counted in 32 bits
     const size_t need = csd_attention_workspace_bytes(cache->rows, T, q_heads, cache->heads, cache->dim);
     if (need == 0) return CSD_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(out) || (q_stride_b | q_stride_t | q_stride_h) % 8 != 0) return CSD_ERR_INVALID_ARG;
@@ -430,25 +565,21 @@ csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t
     attention::Params p;
     std::memset(&p, 0, sizeof p);
     p.q = q;
-    p.k_pool = static_cast<char *>(cache->k) + layer * cache->stride_layer * 2;
-    p.v_pool = static_cast<char *>(cache->v) + layer * cache->stride_layer * 2;
     p.out = out;
     p.lse = lse;
     p.B = cache->rows; p.T = T; p.Hq = q_heads; p.Hkv = cache->heads; p.D = cache->dim; p.group = q_heads / cache->heads;
     p.qb = q_stride_b; p.qt = q_stride_t; p.qh = q_stride_h;
-    p.pool_page = cache->stride_page; p.pool_head = cache->stride_head; p.pool_token = cache->stride_token;
     p.page_shift = pv.page_shift;
     p.n_pages = cache->n_pages;
     p.max_pages = cache->max_pages;
     p.table = pv.table; p.lens = pv.lens; p.n_new = n_new;
     p.flags = pv.flags;
-    p.scale = scale;
+    p.scale_log2 = scale * kLog2e;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (cache->dtype == CSD_BF16)
-        launch_attention_simple<__nv_bfloat16>(p, st);
-    else
-        launch_attention_simple<__half>(p, st);
-    return launched();
+    char *ws = static_cast<char *>(workspace);
+    auto go = [&](auto cfg) { return run_attention<decltype(cfg)>(p, cache, layer, ws, st); };
+    if (cache->dtype == CSD_BF16) return with_config<__nv_bfloat16>(T * p.group, p.D, go);
+    return with_config<__half>(T * p.group, p.D, go);
 }
 
 }  // extern "C"
