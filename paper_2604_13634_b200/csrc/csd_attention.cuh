@@ -69,6 +69,13 @@ struct Params {
     int n_stages, min_tiles;
     Split *splits;                         // [gridDim.x]
     float *parts;                          // [2 gridDim.x] slots of kRows * (DP + 2) floats
+    // the tensor-memory kernel alone
+    int tile_rows;                         // query rows of a row tile: a multiple of 8, at most 128
+    int halves, d16;                       // 64-element columns of a tile; dim rounded up to 16
+    int part_stride;                       // floats between rows of a part
+    unsigned int tmem_cols;
+    const void *k_pool, *v_pool;           // of this layer
+    long long pool_page, pool_head, pool_token;
 };
 
 template <typename T_, int DP_, int MT_, int NK_, int KG_, int RG_, int kBlocksPerSm_>
@@ -208,6 +215,74 @@ __device__ __forceinline__ void walk_next(Walk &w, const int *base, int B, int H
 __device__ __forceinline__ int row_len(const Params &p, int b) { return min(max(__ldg(p.lens + b), 0), p.max_pages << p.page_shift); }
 __device__ __forceinline__ int row_news(const Params &p, int b) { return p.n_new ? min(max(__ldg(p.n_new + b), 0), p.T) : p.T; }
 
+// base[b + 1] holds the tiles of row b; becomes base[b] = tiles of the rows before b.  One warp.
+__device__ __forceinline__ void scan_tiles(int *base, int B)
+{
+    const int lane = threadIdx.x & 31;
+    int sum = 0;
+    for (int b0 = 0; b0 < B; b0 += 32) {
+        int v = b0 + lane < B ? base[b0 + lane + 1] : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(kFull, v, d);
+            if (lane >= d) v += o;
+        }
+        if (b0 + lane < B) base[b0 + lane + 1] = sum + v;
+        sum += __shfl_sync(kFull, v, 31);
+    }
+    if (lane == 0) base[0] = 0;
+}
+
+// The page that lane f < per_tile looks after in a tile; -1: nothing to load.
+template <int kTile>
+__device__ __forceinline__ int tile_page(const Params &p, const Walk &x, int len, int lane, int per_tile)
+{
+    const int place = x.j * kTile + lane * p.box_rows;
+    if (lane >= per_tile || place >= len) return -1;
+    const int id = __ldg(p.table + static_cast<long long>(x.b) * p.max_pages + (place >> p.page_shift));
+    if (id >= 0 && id < p.n_pages) return id;
+    atomicOr(p.flags, CSD_CACHE_BAD_PAGE);
+    return p.n_pages;                                    // outside the tensor map: reads as zeros
+}
+
+// Zeros for rows that have nothing to read.
+template <typename T>
+__device__ __forceinline__ void zero_empty_rows(const Params &p, const int *base, int tid, int threads)
+{
+    for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
+        if (base[b + 1] != base[b]) continue;
+        const long long row0 = static_cast<long long>(b) * p.T * p.Hq;
+        uint4 *o = reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + row0 * p.D);
+        const int vecs = p.T * p.Hq * p.D / 8;
+        for (int i = tid; i < vecs; i += threads) o[i] = make_uint4(0, 0, 0, 0);
+        if (p.lse)
+            for (int i = tid; i < p.T * p.Hq; i += threads) p.lse[row0 + i] = -INFINITY;
+    }
+}
+
+// Adds w v for the infinities and NaN among 32 elements (from c0) of the values in places [from, to], which the product left
+// out, to one row's accumulators; w is computed again.  Rare: straight from global memory.
+template <typename T>
+__device__ __noinline__ void add_left_out(const Params &p, int b, int h, int tok, int head, int c0, int from, int to, float m, float (&o)[32])
+{
+    const T *q = static_cast<const T *>(p.q) + b * p.qb + tok * p.qt + head * p.qh;
+    for (int key = from; key <= to; ++key) {
+        const int page = __ldg(p.table + static_cast<long long>(b) * p.max_pages + (key >> p.page_shift));
+        if (page < 0 || page >= p.n_pages) continue;
+        const long long at = page * p.pool_page + h * p.pool_head + (key & ((1 << p.page_shift) - 1)) * p.pool_token;
+        const T *k = static_cast<const T *>(p.k_pool) + at, *v = static_cast<const T *>(p.v_pool) + at;
+        float x = 0.f;
+        for (int d = 0; d < p.D; ++d) x += rope::to_f32(q[d]) * rope::to_f32(k[d]);
+        const float w = ex2_approx(x * p.scale_log2 - m);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            if (c0 + e >= p.D) break;
+            const float y = rope::to_f32(v[c0 + e]);
+            if (!isfinite(y)) o[e] += w * y;
+        }
+    }
+}
+
 template <typename C>
 __global__ void __launch_bounds__(C::kThreads, C::kBlocksPerSm)
 attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p)
@@ -247,20 +322,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         base[b + 1] = news > 0 ? (len + kTile - 1) / kTile : 0;
     }
     __syncthreads();
-    if (warp == 0) {
-        int sum = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 32) {
-            int v = b0 + lane < p.B ? base[b0 + lane + 1] : 0;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up_sync(kFull, v, d);
-                if (lane >= d) v += o;
-            }
-            if (b0 + lane < p.B) base[b0 + lane + 1] = sum + v;
-            sum += __shfl_sync(kFull, v, 31);
-        }
-        if (lane == 0) base[0] = 0;
-    }
+    if (warp == 0) scan_tiles(base, p.B);
     __syncthreads();
     const int units_per_row = p.Hkv * p.row_tiles;
     const long long total = static_cast<long long>(base[p.B]) * units_per_row;
@@ -277,19 +339,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             const int per_tile = kTile / p.box_rows;               // pages of a tile (1 where a page is larger)
             const unsigned int box_bytes = static_cast<unsigned int>(p.box_rows) * 128u;
             int len = row_len(p, w.b), len_of = w.b;
-            // lane f < per_tile looks after page f of the tile; its id is fetched a tile ahead
-            auto fetch = [&](const Walk &x, int x_len) {
-                const int place = x.j * kTile + lane * p.box_rows;
-                int id = -1;                                        // nothing to load
-                if (lane < per_tile && place < x_len) {
-                    id = __ldg(p.table + static_cast<long long>(x.b) * p.max_pages + (place >> p.page_shift));
-                    if (id < 0 || id >= p.n_pages) {                // reads as zeros: outside the tensor map
-                        atomicOr(p.flags, CSD_CACHE_BAD_PAGE);
-                        id = p.n_pages;
-                    }
-                }
-                return id;
-            };
+            // ids are fetched a tile ahead
+            auto fetch = [&](const Walk &x, int x_len) { return tile_page<kTile>(p, x, x_len, lane, per_tile); };
             int id = fetch(w, len);
             int it = 0;
             for (long long t = t0; t < t1; ++t, ++it) {
@@ -348,16 +399,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const int rg = warp / KG, kg = warp % KG;
         const int g = lane >> 2, qd = lane & 3;
         const int cthreads = C::kWarps * 32;
-        // zeros for rows that have nothing to read
-        for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
-            if (base[b + 1] != base[b]) continue;
-            const long long row0 = static_cast<long long>(b) * p.T * p.Hq;
-            uint4 *o = reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + row0 * p.D);
-            const int vecs = p.T * p.Hq * p.D / 8;
-            for (int i = tid; i < vecs; i += cthreads) o[i] = make_uint4(0, 0, 0, 0);
-            if (p.lse)
-                for (int i = tid; i < p.T * p.Hq; i += cthreads) p.lse[row0 + i] = -INFINITY;
-        }
+        zero_empty_rows<T>(p, base, tid, cthreads);
         Walk w;
         if (t0 < t1) w = walk_to(t0, base, p.B, p.Hkv, p.row_tiles);
         int it = 0;
@@ -716,6 +758,413 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (*give_up && tid % 32 == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);
 }
 
+// ---- more than 16 query rows per key head: products on the tensor-memory path -------------------------------------------
+//
+// The same split over the blocks, parts and join; inside a block
+//   warps 0..3  softmax: thread r owns query row r of the row tile.  It reads the row's 64 scores of a tile from tensor
+//               memory, writes the weights back there in the cache's type, and keeps (m, l) in registers
+//   warp 4      one thread issues the products: S = Q K^T (tcgen05.mma, M = 128 query rows, N = 64 places, both operands from
+//               shared memory) into one of two score buffers, O += P V (P from tensor memory, V read with places as its K)
+//   warp 5      the page loads
+// A row tile is always computed as 128 rows: rows that do not exist read whatever follows in shared memory and feed accumulator
+// rows that nobody reads.
+// The reference m of a row only moves when a tile's maximum exceeds it by 2^8 (weights up to 2^8 are harmless in float32 sums
+// and in either cache type), so the accumulators in tensor memory are rescaled a few times per unit, not per tile.
+constexpr int kTcTile = 64;
+constexpr int kTcThreads = 192;
+constexpr int kTcMaxSlots = 16;
+constexpr unsigned int kTcScoreCols = 64, kTcOutCol = 128;     // tensor memory: scores at 0 and 64 (weights over them), output from 128
+
+template <typename T>
+__device__ __forceinline__ unsigned int tc_instr(int n, bool b_mn_major)
+{
+    constexpr unsigned int type = sizeof(T) == 2 && ExponentBits<T>::value == 0x7f80u ? 1u : 0u;     // 1: bf16, 0: f16
+    return (1u << 4) | (type << 7) | (type << 10) | (b_mn_major ? 1u << 16 : 0u) | (static_cast<unsigned int>(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+// Values as the second operand: rows of 64 elements (128 bytes, swizzled) are K, the elements within them N.
+__device__ __forceinline__ unsigned long long value_desc(unsigned int smem_addr, unsigned int column_bytes)
+{
+    unsigned long long d = 0;
+    d |= static_cast<unsigned long long>((smem_addr & 0x3FFFFu) >> 4);
+    d |= static_cast<unsigned long long>(column_bytes >> 4) << 16;           // to the next 64 elements of N
+    d |= static_cast<unsigned long long>(1024 >> 4) << 32;                   // to the next 8 places of K
+    d |= 1ull << 46;
+    d |= 2ull << 61;
+    return d;
+}
+__device__ __forceinline__ void tc_mma_ss(unsigned int d, unsigned long long a, unsigned long long b, unsigned int idesc, unsigned int accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(unsigned int d, unsigned int a, unsigned long long b, unsigned int idesc, unsigned int accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b),
+                 "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+// Order of the loads of a run of n tiles of one unit: K0, K1, V0, K2, V1, ..., K(n-1), V(n-2), V(n-1).
+__device__ __forceinline__ int k_item(int i) { return i == 0 ? 0 : 2 * i - 1; }
+__device__ __forceinline__ int v_item(int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; }
+
+template <typename T, int kBlocksPerSm>
+__global__ void __launch_bounds__(kTcThreads, kBlocksPerSm)
+attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p)
+{
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) unsigned long long bar_words[2 * kTcMaxSlots + 6];
+    __shared__ unsigned int tmem_base_slot;
+    __shared__ int give_up_flag, odd_run;
+    volatile int *give_up = &give_up_flag;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const unsigned int q_smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const unsigned int ring = q_smem + p.halves * p.tile_rows * 128;
+    const unsigned int slot_bytes = static_cast<unsigned int>(p.halves) * (kTcTile * 128);
+    int *base = reinterpret_cast<int *>(smem_raw + (ring - smem_u32(smem_raw)) + p.n_stages * slot_bytes);      // [B + 1]
+    const unsigned int bars = smem_u32(bar_words);
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (kTcMaxSlots + s); };
+    auto s_full = [&](int i) { return bars + 8u * (2 * kTcMaxSlots + i); };
+    auto p_ready = [&](int i) { return bars + 8u * (2 * kTcMaxSlots + 2 + i); };
+    const unsigned int pv_done = bars + 8u * (2 * kTcMaxSlots + 4), q_ready = bars + 8u * (2 * kTcMaxSlots + 5);
+
+    if (tid == 0) {
+        give_up_flag = 0;
+        odd_run = 0;
+        for (int s = 0; s < p.n_stages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(s_full(i), 1);
+            mbar_init(p_ready(i), 4);
+        }
+        mbar_init(pv_done, 1);
+        mbar_init(q_ready, 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        p.splits[blockIdx.x].parts = 0;
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    for (int b = tid; b < p.B; b += kTcThreads) {
+        const int len = row_len(p, b), news = row_news(p, b);
+        base[b + 1] = news > 0 ? (len + kTcTile - 1) / kTcTile : 0;
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(smem_u32(&tmem_base_slot), p.tmem_cols);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    if (warp == 0) scan_tiles(base, p.B);
+    __syncthreads();
+    const unsigned int tmem = tmem_base_slot;
+    const long long total = static_cast<long long>(base[p.B]) * p.Hkv * p.row_tiles;
+    long long G = gridDim.x;
+    if (total < G * p.min_tiles) G = max(1ll, total / p.min_tiles);
+    const long long c = blockIdx.x;
+    const long long t0 = c < G ? c * total / G : total, t1 = c < G ? (c + 1) * total / G : total;
+    auto slot_of = [&](int item) { return item % p.n_stages; };
+    auto phase_of = [&](int item) { return static_cast<unsigned int>(item / p.n_stages) & 1u; };
+
+    if (warp == 5) {
+        // ---- page loads ----
+        if (t0 < t1) {
+            Walk w = walk_to(t0, base, p.B, p.Hkv, p.row_tiles);
+            const int per_tile = kTcTile / p.box_rows;
+            const unsigned int box_bytes = static_cast<unsigned int>(p.box_rows) * 128u;
+            int len = row_len(p, w.b), len_of = w.b;
+            auto fetch = [&](const Walk &x, int x_len) { return tile_page<kTcTile>(p, x, x_len, lane, per_tile); };
+            auto load = [&](const CUtensorMap *map, const Walk &x, int page, int item) {
+                const int s = slot_of(item);
+                const unsigned int there = __ballot_sync(kFull, page >= 0);
+                int ok = 1;
+                if (lane == 0) {
+                    ok = mbar_wait(empty(s), phase_of(item) ^ 1u, give_up) ? 1 : 0;
+                    if (ok) mbar_expect_tx(full(s), static_cast<unsigned int>(__popc(there)) * box_bytes * p.halves);
+                }
+                ok = __shfl_sync(kFull, ok, 0);
+                if (ok && page >= 0) {
+                    const int in_page = p.box_rows == kTcTile ? (x.j * kTcTile) & ((1 << p.page_shift) - 1) : 0;
+                    const unsigned int at = ring + s * slot_bytes + lane * box_bytes;
+                    for (int hf = 0; hf < p.halves; ++hf) tma_load_page(at + hf * (kTcTile * 128), map, full(s), hf * 64, in_page, x.h, page);
+                }
+                return ok != 0;
+            };
+            int id = fetch(w, len), item = 0, before = -1;
+            Walk w_before = w;
+            bool first = true, ok = true;
+            for (long long t = t0; t < t1 && ok; ++t) {
+                const Walk now = w;
+                const int page = id;
+                const bool last = now.j + 1 == now.n || t + 1 == t1;
+                if (t + 1 < t1) {
+                    walk_next(w, base, p.B, p.Hkv, p.row_tiles);
+                    if (w.b != len_of) {
+                        len = row_len(p, w.b);
+                        len_of = w.b;
+                    }
+                    id = fetch(w, len);
+                }
+                ok = load(&map_k, now, page, item++);
+                if (!first && ok) ok = load(&map_v, w_before, before, item++);
+                if (last && ok) ok = load(&map_v, now, page, item++);
+                first = last;
+                before = page;
+                w_before = now;
+            }
+            // every commit aimed at the slots' barriers has landed before the block ends
+            if (lane == 0)
+                for (int k = 0; k < p.n_stages && ok; ++k, ++item) ok = mbar_wait(empty(slot_of(item)), phase_of(item) ^ 1u, give_up);
+        }
+    } else if (warp == 4) {
+        // ---- products ----
+        if (lane == 0 && t0 < t1) {
+            Walk w = walk_to(t0, base, p.B, p.Hkv, p.row_tiles);
+            const unsigned int idesc_qk = tc_instr<T>(kTcTile, false), idesc_pv = tc_instr<T>(p.d16, true);
+            int n0 = 0, items = 0, run = 0;                    // tiles and loads of the runs before; runs
+            bool ok = true;
+            for (long long t = t0; t < t1 && ok; ++run) {
+                const int ns = static_cast<int>(min(static_cast<long long>(w.n - w.j), t1 - t));
+                ok = mbar_wait(q_ready, run & 1, give_up);
+                for (int i = 0; i <= ns && ok; ++i) {
+                    if (i < ns) {
+                        const int item = items + k_item(i), s = slot_of(item), x = n0 + i;
+                        if (!(ok = mbar_wait(full(s), phase_of(item), give_up))) break;
+                        ptx::tc_fence_after();
+                        const unsigned int k_at = ring + s * slot_bytes;
+                        for (int ks = 0; ks < p.d16 / 16; ++ks)
+                            tc_mma_ss(tmem + (x & 1) * kTcScoreCols, ptx::operand_desc(q_smem + (ks >> 2) * (p.tile_rows * 128)) + 2ull * (ks & 3),
+                                      ptx::operand_desc(k_at + (ks >> 2) * (kTcTile * 128)) + 2ull * (ks & 3), idesc_qk, ks != 0);
+                        ptx::tc_commit(empty(s));
+                        ptx::tc_commit(s_full(x & 1));
+                    }
+                    if (i > 0) {
+                        const int u = i - 1, x = n0 + u, item = items + v_item(u, ns), s = slot_of(item);
+                        if (!(ok = mbar_wait(p_ready(x & 1), (x >> 1) & 1, give_up))) break;
+                        if (!(ok = mbar_wait(full(s), phase_of(item), give_up))) break;
+                        ptx::tc_fence_after();
+                        const unsigned int v_at = ring + s * slot_bytes;
+#pragma unroll
+                        for (int kk = 0; kk < kTcTile / 16; ++kk)
+                            tc_mma_ts(tmem + kTcOutCol, tmem + (x & 1) * kTcScoreCols + 8 * kk, value_desc(v_at + kk * (16 * 128), kTcTile * 128), idesc_pv,
+                                      (u | kk) != 0);
+                        ptx::tc_commit(empty(s));
+                        ptx::tc_commit(pv_done);
+                    }
+                }
+                n0 += ns;
+                items += 2 * ns;
+                t += ns;
+                w.j += ns - 1;
+                if (t < t1) walk_next(w, base, p.B, p.Hkv, p.row_tiles);
+            }
+        }
+    } else {
+        // ---- softmax, rows in and out ----
+        zero_empty_rows<T>(p, base, tid, 128);
+        Walk w;
+        if (t0 < t1) w = walk_to(t0, base, p.B, p.Hkv, p.row_tiles);
+        const unsigned int my_lanes = static_cast<unsigned int>(32 * warp) << 16;
+        int n = 0, items = 0, run = 0;
+        for (long long t = t0; t < t1; ++run) {
+            const int b = w.b, h = w.h, rt = w.rt, j0 = w.j;
+            const int ns = static_cast<int>(min(static_cast<long long>(w.n - j0), t1 - t));
+            const int len = row_len(p, b), news = row_news(p, b);
+            const int rows_here = min(p.tile_rows, p.rows - rt * p.tile_rows);
+            const int chunks = p.halves * 8;
+            for (int i = tid; i < rows_here * chunks; i += 128) {
+                const int r = i / chunks, ch = i - r * chunks;
+                const int rr = rt * p.tile_rows + r, tok = rr / p.group, hh = h * p.group + rr - tok * p.group;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (ch * 8 < p.D) x = __ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + b * p.qb + tok * p.qt + hh * p.qh + ch * 8));
+                const unsigned int at = q_smem + (ch >> 3) * (p.tile_rows * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            ptx::tc_fence_before();                              // the output of the run before has been read
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_ready);
+            const int r = tid, rr = rt * p.tile_rows + r, tok = rr / p.group;
+            const int limit = r < rows_here && tok < news ? len - news + tok : -1;
+            const bool warp_has = 32 * warp < rows_here;
+            float m = 0.f, l = 0.f;                              // l == 0: nothing seen yet, m is arbitrary
+
+            for (int i = 0; i < ns; ++i, ++n) {
+                const int key0 = (j0 + i) * kTcTile;
+                const bool edge = key0 + kTcTile - 1 > len - news;
+                const unsigned int s_at = tmem + my_lanes + (n & 1) * kTcScoreCols;
+                mbar_wait(s_full(n & 1), (n >> 1) & 1, give_up);
+                ptx::tc_fence_after();
+                if (warp_has) {
+                    float x[32], y[32];
+                    ptx::tmem_ld64(s_at, x, y);
+                    const unsigned long long sc2 = pack2(p.scale_log2, p.scale_log2), m2 = pack2(-m, -m);
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        unpack2(fma2(pack2(x[j], x[j + 1]), sc2, m2), x[j], x[j + 1]);
+                        unpack2(fma2(pack2(y[j], y[j + 1]), sc2, m2), y[j], y[j + 1]);
+                    }
+                    if (edge) {
+                        const int left = limit - key0;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            if (j > left) x[j] = -INFINITY;
+                            if (32 + j > left) y[j] = -INFINITY;
+                        }
+                    }
+                    float mx = fmaxf(x[0], y[0]), my = fmaxf(x[1], y[1]);
+#pragma unroll
+                    for (int j = 2; j < 32; j += 2) {
+                        mx = fmaxf(mx, fmaxf(x[j], y[j]));
+                        my = fmaxf(my, fmaxf(x[j + 1], y[j + 1]));
+                    }
+                    mx = fmaxf(mx, my);
+                    float up = 0.f, f = 1.f;
+                    if (limit >= 0) {
+                        if (l == 0.f) {
+                            up = mx == -INFINITY ? 0.f : mx;
+                        } else if (mx > 8.f) {
+                            up = mx;
+                            f = ex2_approx(-mx);
+                        }
+                    }
+                    if (__any_sync(kFull, up != 0.f)) {
+                        m += up;
+                        l *= f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            x[j] -= up;
+                            y[j] -= up;
+                        }
+                    }
+                    // the weights go into the second product in the cache's type: relative error 2^-9 (2^-12) of each, of random
+                    // sign, where the result itself is rounded to that type; the sum l is taken before the rounding
+                    unsigned int w2[32];
+                    unsigned long long sum0 = pack2(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        const float a0 = ex2_approx(x[j]), a1 = ex2_approx(x[j + 1]), b0 = ex2_approx(y[j]), b1 = ex2_approx(y[j + 1]);
+                        sum0 = add2(sum0, pack2(a0, a1));
+                        sum1 = add2(sum1, pack2(b0, b1));
+                        w2[j / 2] = pack_pair<T>(a0, a1);
+                        w2[16 + j / 2] = pack_pair<T>(b0, b1);
+                    }
+                    float s0, s1;
+                    unpack2(add2(sum0, sum1), s0, s1);
+                    l += s0 + s1;
+                    ptx::tmem_st32(s_at, w2);
+                    if (__any_sync(kFull, f != 1.f)) {
+                        // the products before have to be complete; the next one waits for these weights
+                        mbar_wait(pv_done, (n - 1) & 1, give_up);
+                        ptx::tc_fence_after();
+                        for (int c0 = 0; c0 < p.d16; c0 += 32) {
+                            float o[32];
+                            ptx::tmem_ld32(tmem + my_lanes + kTcOutCol + c0, o);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) w2[j] = __float_as_uint(o[j] * f);
+                            ptx::tmem_st32(tmem + my_lanes + kTcOutCol + c0, w2);
+                        }
+                    }
+                    ptx::tmem_wait_st();
+                }
+                if (edge) {
+                    // A weight of zero does not silence an infinity or NaN in the values.  Places beyond the row hold anything:
+                    // zeroed.  Such a value in a place of a later new token is left out here and handed to the rows that see it at the end.
+                    const int item = items + v_item(i, ns), s = slot_of(item);
+                    mbar_wait(full(s), phase_of(item), give_up);
+                    const unsigned int v_at = ring + s * slot_bytes;
+                    const int from = max(len - news + 1 - key0, 0);
+                    for (int k = tid; k < (kTcTile - from) * chunks; k += 128) {
+                        const int kr = from + k / chunks, ch = k % chunks;
+                        const unsigned int at = v_at + (ch >> 3) * (kTcTile * 128) + kr * 128 + (((ch & 7) ^ (kr & 7)) << 4);
+                        unsigned int v[4] = {0u, 0u, 0u, 0u}, z[4] = {0u, 0u, 0u, 0u};
+                        bool store = key0 + kr >= len;
+                        if (!store) {
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                z[e] = finite_only<T>(v[e]);
+                                store |= z[e] != v[e];
+                            }
+                            if (store) odd_run = run + 1;
+                        }
+                        if (store) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(z[0]), "r"(z[1]), "r"(z[2]), "r"(z[3]) : "memory");
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_ready(n & 1));
+            }
+
+            // ---- the run's rows ----
+            mbar_wait(pv_done, (n - 1) & 1, give_up);
+            ptx::tc_fence_after();
+            consumer_barrier(128);                              // odd_run of all four warps
+            const bool odd = *static_cast<volatile int *>(&odd_run) == run + 1;
+            const bool whole = j0 == 0 && ns == w.n;
+            const bool seen = limit >= 0 && l != 0.f;            // (NaN counts as seen)
+            const int head = h * p.group + rr - tok * p.group;
+            const long long row = (static_cast<long long>(b) * p.T + tok) * p.Hq + head;
+            float *part = p.parts + static_cast<long long>(2 * static_cast<int>(c) + (j0 == 0 ? 1 : 0)) * p.tile_rows * (p.part_stride + 2);
+            if (warp_has) {
+                const float inv = 1.f / l;
+                for (int c0 = 0; c0 < p.D; c0 += 32) {
+                    float o[32];
+                    ptx::tmem_ld32(tmem + my_lanes + kTcOutCol + c0, o);
+                    if (odd && seen) {
+                        float z[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) z[e] = o[e];
+                        add_left_out<T>(p, b, h, tok, head, c0, max(len - news + 1, j0 * kTcTile), min(limit, (j0 + ns) * kTcTile - 1), m, z);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = z[e];
+                    }
+                    if (r < rows_here) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) {
+                            if (c0 + e >= p.D) break;
+                            if (whole) {
+                                uint4 v = make_uint4(0, 0, 0, 0);
+                                if (seen)
+                                    v = make_uint4(pack_pair<T>(o[e] * inv, o[e + 1] * inv), pack_pair<T>(o[e + 2] * inv, o[e + 3] * inv),
+                                                   pack_pair<T>(o[e + 4] * inv, o[e + 5] * inv), pack_pair<T>(o[e + 6] * inv, o[e + 7] * inv));
+                                *reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + row * p.D + c0 + e) = v;
+                            } else {
+                                float4 *to = reinterpret_cast<float4 *>(part + static_cast<long long>(r) * p.part_stride + c0 + e);
+                                __stcg(to, seen ? make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f));
+                                __stcg(to + 1, seen ? make_float4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]) : make_float4(0.f, 0.f, 0.f, 0.f));
+                            }
+                        }
+                    }
+                }
+                if (r < rows_here) {
+                    if (!whole)
+                        __stcg(reinterpret_cast<float2 *>(part + static_cast<long long>(p.tile_rows) * p.part_stride + 2 * r), make_float2(seen ? m : -INFINITY, seen ? l : 0.f));
+                    else if (p.lse)
+                        p.lse[row] = seen ? (m + log2f(l)) * kLn2 : -INFINITY;
+                }
+            }
+            if (!whole && j0 == 0 && tid == 0) {
+                const long long last = t + w.n - 1;
+                p.splits[blockIdx.x].unit = (b * p.Hkv + h) * p.row_tiles + rt;
+                p.splits[blockIdx.x].parts = static_cast<int>(((last + 1) * G - 1) / total) - static_cast<int>(c) + 1;
+            }
+            t += ns;
+            items += 2 * ns;
+            w.j = j0 + ns - 1;
+            if (t < t1) walk_next(w, base, p.B, p.Hkv, p.row_tiles);
+        }
+        ptx::tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 1) ptx::tmem_dealloc(tmem, p.tmem_cols);
+    if (*give_up && lane == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);
+}
+
 // Joins the parts of split units.  Block (c, y): the unit that begins in block c of the kernel before, query rows 8 y ..; a warp per row.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) attention_join_kernel(const Params p, int rows_per_tile)
@@ -752,12 +1201,22 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Params p, int
         for (int i = 0; i < here; ++i) {
             const float f = __shfl_sync(kFull, wt, i);
             const float *from = slot(i0 + i) + r * DP + lane * E;
+            if constexpr (E == 2) {
+                if (lane * E < p.D) {
+                    const float2 y = __ldcg(reinterpret_cast<const float2 *>(from));
+                    o[0] += f * y.x;
+                    o[1] += f * y.y;
+                }
+            } else {
 #pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                if (lane * E + e < p.D) {
-                    const float2 y = __ldcg(reinterpret_cast<const float2 *>(from + e));
-                    o[e] += f * y.x;
-                    o[e + 1] += f * y.y;
+                for (int e = 0; e < E; e += 4) {
+                    if (lane * E + e < p.D) {
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(from + e));
+                        o[e] += f * y.x;
+                        o[e + 1] += f * y.y;
+                        o[e + 2] += f * y.z;
+                        o[e + 3] += f * y.w;
+                    }
                 }
             }
         }

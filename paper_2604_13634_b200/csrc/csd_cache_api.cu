@@ -240,32 +240,48 @@ AttentionPlan attention_plan(int rows, int B)
     return a;
 }
 
-// The variant for `rows` query rows per (row, key head) and dim elements: the smallest row tile that holds them, at most
-// 128 rows (64 beyond dim 128); more rows are further row tiles, which read the keys again.
 template <typename T, typename F>
-auto with_config(int rows, int dim, F f)
+auto with_config(int dim, F f)
 {
     using attention::Config;
-    if (dim <= 64) {
-        if (rows <= 16) return f(Config<T, 64, 1, 1, 4, 1, 2>());
-        if (rows <= 32) return f(Config<T, 64, 2, 1, 4, 1, 2>());
-        if (rows <= 64) return f(Config<T, 64, 2, 2, 4, 2, 1>());
-        return f(Config<T, 64, 2, 2, 2, 4, 1>());
-    }
-    if (dim <= 128) {
-        if (rows <= 16) return f(Config<T, 128, 1, 1, 4, 1, 2>());
-        if (rows <= 32) return f(Config<T, 128, 2, 1, 4, 1, 2>());
-        if (rows <= 64) return f(Config<T, 128, 2, 2, 4, 2, 1>());
-        return f(Config<T, 128, 2, 2, 2, 4, 1>());
-    }
-    if (rows <= 16) return f(Config<T, 256, 1, 1, 4, 1, 1>());
-    if (rows <= 32) return f(Config<T, 256, 1, 1, 4, 2, 1>());
-    return f(Config<T, 256, 1, 1, 2, 4, 1>());
+    if (dim <= 64) return f(Config<T, 64, 1, 1, 4, 1, 2>());
+    if (dim <= 128) return f(Config<T, 128, 1, 1, 4, 1, 2>());
+    return f(Config<T, 256, 1, 1, 4, 1, 1>());
+}
+
+// Which kernel: up to 16 query rows per (row, key head) fit the register tiles of the mma.sync kernel; beyond, the tensor-memory
+// kernel, with row tiles of at most 128.
+bool attention_uses_tc(int rows) { return rows > 16; }
+
+// Two blocks per SM while their accumulators fit in half of the tensor memory each (128 + dim columns of 512).
+int tc_blocks(int dim) { return dim <= 128 ? 2 : 1; }
+
+AttentionPlan attention_tc_plan(int rows, int dim, int B)
+{
+    AttentionPlan a;
+    a.rows = rows;
+    a.row_tiles = (rows + 127) / 128;
+    a.tile_rows = ((rows + a.row_tiles - 1) / a.row_tiles + 7) / 8 * 8;
+    a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
+    a.dp = dim <= 64 ? 64 : (dim <= 128 ? 128 : 256);
+    a.grid = host::multiprocessors() * tc_blocks(dim);
+    const int halves = (dim + 63) / 64, slot = halves * attention::kTcTile * 128;
+    const int limit = kSmemPerSm / tc_blocks(dim) - kSmemReserved - kSmemStatic;
+    // the first product reads 128 query rows whatever the row tile: what follows the rows has to be there
+    const int fixed = 1024 + halves * a.tile_rows * 128 + (B + 1) * 4;
+    a.stages = (limit - fixed) / slot;
+    if (a.stages > attention::kTcMaxSlots) a.stages = attention::kTcMaxSlots;
+    a.smem = fixed + a.stages * slot;
+    a.splits_off = 0;
+    a.parts_off = align_up(static_cast<size_t>(a.grid) * sizeof(attention::Split), 256);
+    a.total = a.parts_off + static_cast<size_t>(2) * a.grid * a.tile_rows * (a.dp + 2) * 4;
+    return a;
 }
 
 AttentionPlan attention_plan_of(int T, int group, int dim, int B)
 {
-    return with_config<__nv_bfloat16>(T * group, dim, [&](auto cfg) { return attention_plan<decltype(cfg)>(T * group, B); });
+    if (attention_uses_tc(T * group)) return attention_tc_plan(T * group, dim, B);
+    return with_config<__nv_bfloat16>(dim, [&](auto cfg) { return attention_plan<decltype(cfg)>(T * group, B); });
 }
 
 bool attention_shape_ok(int rows, int T, int q_heads, int heads, int dim)
@@ -292,26 +308,20 @@ bool make_pool_map(CUtensorMap *map, const csd_cache_t *c, const void *pool, int
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Lets the kernel use the shared memory it wants; once per device.
-template <typename C>
-bool attention_ready()
+// Lets a kernel use the shared memory it wants, once per device; `split_regs` is what its warpgroups must find at launch, in
+// registers per thread summed over `groups` of them (a larger share than there is would be waited for).
+template <typename K>
+bool kernel_ready(K kernel, std::atomic<bool> (&done)[kMaxDevices], int smem, int groups, int split_regs)
 {
-    static std::atomic<bool> done[kMaxDevices];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) {
         (void)cudaGetLastError();
         return false;
     }
     if (done[dev].load()) return true;
-    // what the warpgroups take from one another has to be there at launch, or the larger share would be waited for
     cudaFuncAttributes attr;
-    if (cudaFuncGetAttributes(&attr, attention::attention_kernel<C>) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return false;
-    }
-    if (C::kMoveRegs && attr.numRegs * C::kGroups < C::kConsumerRegs * (C::kGroups - 1) + C::kProducerRegs) return false;
-    if (cudaFuncSetAttribute(attention::attention_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             kSmemPerSm / C::kBlocksPerSm - kSmemReserved - kSmemStatic) != cudaSuccess) {
+    if (cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs * groups < split_regs ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
         (void)cudaGetLastError();
         return false;
     }
@@ -319,10 +329,34 @@ bool attention_ready()
     return true;
 }
 
+template <typename T, int DP>
+csd_status_t launch_join(const attention::Params &p, int grid, int tile_rows, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg;
+    std::memset(&cfg, 0, sizeof cfg);
+    const int most = p.rows < tile_rows ? p.rows : tile_rows;
+    cfg.gridDim = dim3(static_cast<unsigned int>(grid), static_cast<unsigned int>((most + 7) / 8));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, attention::attention_join_kernel<T, DP>, p, tile_rows) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CSD_ERR_CUDA;
+    }
+    return CSD_OK;
+}
+
 template <typename C>
 csd_status_t run_attention(attention::Params p, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
 {
-    if (!attention_ready<C>()) return CSD_ERR_CUDA;
+    static std::atomic<bool> ready[kMaxDevices];
+    if (!kernel_ready(attention::attention_kernel<C>, ready, kSmemPerSm / C::kBlocksPerSm - kSmemReserved - kSmemStatic, C::kGroups,
+                      C::kMoveRegs ? C::kConsumerRegs * (C::kGroups - 1) + C::kProducerRegs : 0))
+        return CSD_ERR_CUDA;
     const AttentionPlan a = attention_plan<C>(p.T * p.group, p.B);
     p.rows = a.rows;
     p.row_tiles = a.row_tiles;
@@ -335,22 +369,47 @@ csd_status_t run_attention(attention::Params p, const csd_cache_t *cache, int la
     if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
     attention::attention_kernel<C><<<static_cast<unsigned int>(a.grid), C::kThreads, static_cast<size_t>(a.smem), st>>>(map_k, map_v, p);
     if (launched() != CSD_OK) return CSD_ERR_CUDA;
-    const int most = a.rows < C::kRows ? a.rows : C::kRows;
-    cudaLaunchConfig_t cfg;
-    std::memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = dim3(static_cast<unsigned int>(a.grid), static_cast<unsigned int>((most + 7) / 8));
-    cfg.blockDim = dim3(256);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, attention::attention_join_kernel<typename C::T, C::DP>, p, static_cast<int>(C::kRows)) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return CSD_ERR_CUDA;
-    }
-    return CSD_OK;
+    return launch_join<typename C::T, C::DP>(p, a.grid, C::kRows, st);
+}
+
+template <typename T, int kBlocks>
+csd_status_t run_attention_tc(attention::Params p, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
+{
+    static std::atomic<bool> ready[kMaxDevices];
+    if (!kernel_ready(attention::attention_tc_kernel<T, kBlocks>, ready, kSmemPerSm / kBlocks - kSmemReserved - kSmemStatic, 1, 0)) return CSD_ERR_CUDA;
+    const AttentionPlan a = attention_tc_plan(p.T * p.group, p.D, p.B);
+    p.rows = a.rows;
+    p.row_tiles = a.row_tiles;
+    p.tile_rows = a.tile_rows;
+    p.part_stride = a.dp;
+    p.halves = (p.D + 63) / 64;
+    p.d16 = (p.D + 15) / 16 * 16;
+    p.tmem_cols = kBlocks == 2 ? 256u : 512u;
+    p.n_stages = a.stages;
+    p.min_tiles = 1;
+    p.box_rows = cache->page_size < attention::kTcTile ? cache->page_size : attention::kTcTile;
+    p.splits = reinterpret_cast<attention::Split *>(ws + a.splits_off);
+    p.parts = reinterpret_cast<float *>(ws + a.parts_off);
+    p.k_pool = static_cast<char *>(cache->k) + layer * cache->stride_layer * 2;
+    p.v_pool = static_cast<char *>(cache->v) + layer * cache->stride_layer * 2;
+    p.pool_page = cache->stride_page;
+    p.pool_head = cache->stride_head;
+    p.pool_token = cache->stride_token;
+    CUtensorMap map_k, map_v;
+    if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
+    attention::attention_tc_kernel<T, kBlocks><<<static_cast<unsigned int>(a.grid), attention::kTcThreads, static_cast<size_t>(a.smem), st>>>(map_k, map_v, p);
+    if (launched() != CSD_OK) return CSD_ERR_CUDA;
+    if (a.dp == 64) return launch_join<T, 64>(p, a.grid, a.tile_rows, st);
+    if (a.dp == 128) return launch_join<T, 128>(p, a.grid, a.tile_rows, st);
+    return launch_join<T, 256>(p, a.grid, a.tile_rows, st);
+}
+
+template <typename T>
+csd_status_t run_attention_any(const attention::Params &p, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
+{
+    if (attention_uses_tc(p.T * p.group))
+        return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2>(p, cache, layer, ws, st) : run_attention_tc<T, 1>(p, cache, layer, ws, st);
+    return with_config<T>(p.D, [&](auto cfg) { return run_attention<decltype(cfg)>(p, cache, layer, ws, st); });
 }
 
 }  // namespace
@@ -577,9 +636,7 @@ csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t
     p.scale_log2 = scale * kLog2e;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
-    auto go = [&](auto cfg) { return run_attention<decltype(cfg)>(p, cache, layer, ws, st); };
-    if (cache->dtype == CSD_BF16) return with_config<__nv_bfloat16>(T * p.group, p.D, go);
-    return with_config<__half>(T * p.group, p.D, go);
+    return cache->dtype == CSD_BF16 ? run_attention_any<__nv_bfloat16>(p, cache, layer, ws, st) : run_attention_any<__half>(p, cache, layer, ws, st);
 }
 
 }  // extern "C"

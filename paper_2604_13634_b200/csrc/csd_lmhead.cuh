@@ -76,6 +76,15 @@ using ptx::mbar_init;
 using ptx::mbar_try_wait;
 using ptx::mbar_wait;
 using ptx::smem_u32;
+using ptx::operand_desc;
+using ptx::tc_commit;
+using ptx::tc_fence_after;
+using ptx::tc_fence_before;
+using ptx::tmem_alloc;
+using ptx::tmem_dealloc;
+using ptx::tmem_ld32;
+using ptx::tmem_ld64;
+using ptx::tmem_relinquish;
 
 __device__ __forceinline__ void tma_load_2d(unsigned int dst, const CUtensorMap *map, unsigned int bar, int x, int y)
 {
@@ -84,21 +93,6 @@ __device__ __forceinline__ void tma_load_2d(unsigned int dst, const CUtensorMap 
                  : "memory");
 }
 
-__device__ __forceinline__ void tmem_alloc(unsigned int smem_dst, unsigned int cols)
-{
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(cols) : "memory");
-}
-__device__ __forceinline__ void tmem_relinquish() { asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_dealloc(unsigned int taddr, unsigned int cols)
-{
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(unsigned int bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
 // D[tmem] (+)= A[smem] * B[smem]^T, bf16 operands, fp32 accumulators.
 __device__ __forceinline__ void tc_mma_bf16(unsigned int d_tmem, unsigned long long a_desc, unsigned long long b_desc, unsigned int idesc,
                                             unsigned int accumulate)
@@ -107,51 +101,6 @@ __device__ __forceinline__ void tc_mma_bf16(unsigned int d_tmem, unsigned long l
                  "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
                  : "memory");
 }
-// 32 consecutive accumulator columns of this thread's TMEM lane.  The load is asynchronous; load and wait are one
-// statement so that nothing can read the registers in between.
-__device__ __forceinline__ void tmem_ld32(unsigned int taddr, float (&x)[32])
-{
-    unsigned int r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr)
-        : "memory");
-#pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
-}
-// 64 consecutive columns: two loads in flight, one wait.
-__device__ __forceinline__ void tmem_ld64(unsigned int taddr, float (&x)[32], float (&y)[32])
-{
-    unsigned int r[64];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%64];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%65];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
-        : "r"(taddr), "r"(taddr + 32u)
-        : "memory");
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        x[j] = __uint_as_float(r[j]);
-        y[j] = __uint_as_float(r[32 + j]);
-    }
-}
-
-// Shared-memory operand descriptor of a K-major bf16 tile stored as rows of 128 bytes with the 128-byte swizzle
-// (what the TMA loads above produce): groups of 8 rows lie 1024 bytes apart, the tile starts on a 1 KiB boundary.
-__device__ __forceinline__ unsigned long long operand_desc(unsigned int smem_addr)
-{
-    unsigned long long d = 0;
-    d |= static_cast<unsigned long long>((smem_addr & 0x3FFFFu) >> 4);     // start address
-    d |= 1ull << 16;                                                       // leading-dimension offset: unused for this layout
-    d |= static_cast<unsigned long long>(1024 >> 4) << 32;                 // stride between 8-row groups
-    d |= 1ull << 46;                                                       // descriptor version of this architecture
-    d |= 2ull << 61;                                                       // 128-byte swizzle
-    return d;
-}
-
 __device__ __forceinline__ unsigned int instr_desc(int n)
 {
     // fp32 accumulators, bf16 A and B, both K-major, N = n, M = 128
