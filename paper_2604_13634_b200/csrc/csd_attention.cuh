@@ -48,10 +48,11 @@ using rope::from_f32;
 constexpr int kMaxStages = 12;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// What the first block of a split unit leaves for the join: parts lie in slot 2 c + 1 of that block and slots 2 (c + i) of the next ones.
+// What the first block of a split unit leaves for the join: its parts lie in slot 2 first + 1 and slots 2 (first + i), i = 1 .. parts - 1.
 struct Split {
     int unit;                 // (row * heads + head) * row tiles + row tile
-    int parts;                // 0: no split unit begins in this block
+    int first;                // that block
+    int parts;                // 0: not split
 };
 
 struct Params {
@@ -66,8 +67,10 @@ struct Params {
     const int *table, *lens, *n_new;
     unsigned int *flags;
     float scale_log2;
-    int n_stages, min_tiles;
-    Split *splits;                         // [gridDim.x]
+    int n_stages;
+    int run_cost;                          // what beginning and ending a unit costs a block, in tiles
+    int by_unit;                           // splits are indexed by unit (no more units than blocks), else by first block
+    Split *splits;                         // [min(units, gridDim.x)]
     float *parts;                          // [2 gridDim.x] slots of kRows * (DP + 2) floats
     // the tensor-memory kernel alone
     int tile_rows;                         // query rows of a row tile: a multiple of 8, at most 128
@@ -173,49 +176,78 @@ __device__ __forceinline__ unsigned int finite_only(unsigned int two)
 
 __device__ __forceinline__ void consumer_barrier(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
 
-// Walks a block's run of tiles: row b, key head h, row tile rt, tile j of n.
-struct Walk {
-    int b, h, rt, j, n;
+// The split.  A unit of n tiles counts n + run_cost positions, the first run_cost of them empty: what its beginning and its end
+// cost a block.  The positions of all units are split evenly over the blocks; a block's share [x, x1) is a few runs of tiles.
+struct Run {
+    int b, h, rt;             // row, key head, row tile
+    int j0, ns, n;            // first tile, tiles here, tiles of the unit
+    long long at;             // position of the unit's first tile
 };
 
-// base[b]: tiles of the rows before b (one head, one row tile).  Tile t of all lies in row b with base[b] hr <= t < base[b+1] hr.
-__device__ __forceinline__ Walk walk_to(long long t, const int *base, int B, int Hkv, int row_tiles)
-{
-    const long long hr = static_cast<long long>(Hkv) * row_tiles;
-    int lo = 0, hi = B - 1;                              // the last b with base[b] * hr <= t has tiles
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (base[mid] * hr <= t) lo = mid; else hi = mid - 1;
-    }
-    Walk w;
-    w.b = lo;
-    w.n = base[lo + 1] - base[lo];
-    const long long rest = t - base[lo] * hr;
-    const int hrt = static_cast<int>(rest / w.n);
-    w.j = static_cast<int>(rest - static_cast<long long>(hrt) * w.n);
-    w.h = hrt / row_tiles;
-    w.rt = hrt - w.h * row_tiles;
-    return w;
-}
+struct Runs {
+    const int *base;          // base[b]: positions of the rows before b (one head, one row tile)
+    int B, Hkv, row_tiles, cost;
+    int b, h, rt;
+    long long x, x1, unit;    // next position, end of the share, first position of the unit
 
-__device__ __forceinline__ void walk_next(Walk &w, const int *base, int B, int Hkv, int row_tiles)
-{
-    if (++w.j < w.n) return;
-    w.j = 0;
-    if (++w.rt < row_tiles) return;
-    w.rt = 0;
-    if (++w.h < Hkv) return;
-    w.h = 0;
-    do {
-        ++w.b;
-    } while (w.b < B && base[w.b + 1] == base[w.b]);
-    w.n = w.b < B ? base[w.b + 1] - base[w.b] : 1;
-}
+    __device__ __forceinline__ void begin(const Params &p, const int *base_, long long x0, long long end)
+    {
+        base = base_;
+        B = p.B;
+        Hkv = p.Hkv;
+        row_tiles = p.row_tiles;
+        cost = p.run_cost;
+        x = x0;
+        x1 = end;
+        b = h = rt = 0;
+        unit = 0;
+        if (x >= x1) return;
+        const long long hr = static_cast<long long>(Hkv) * row_tiles;
+        int lo = 0, hi = B - 1;                              // the last row whose positions begin at or before x has some
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (base[mid] * hr <= x) lo = mid; else hi = mid - 1;
+        }
+        b = lo;
+        const int each = base[b + 1] - base[b];
+        const int hrt = static_cast<int>((x - base[b] * hr) / each);
+        unit = base[b] * hr + static_cast<long long>(hrt) * each;
+        h = hrt / row_tiles;
+        rt = hrt - h * row_tiles;
+    }
+
+    __device__ __forceinline__ bool next(Run &r)
+    {
+        while (x < x1) {
+            const int each = base[b + 1] - base[b];
+            r.b = b;
+            r.h = h;
+            r.rt = rt;
+            r.n = each - cost;
+            r.at = unit + cost;
+            r.j0 = max(static_cast<int>(x - r.at), 0);
+            r.ns = static_cast<int>(min(static_cast<long long>(r.n), x1 - r.at)) - r.j0;
+            unit += each;
+            x = unit;
+            if (++rt == row_tiles) {
+                rt = 0;
+                if (++h == Hkv) {
+                    h = 0;
+                    do {
+                        ++b;
+                    } while (b < B && base[b + 1] == base[b]);
+                }
+            }
+            if (r.ns > 0) return true;
+        }
+        return false;
+    }
+};
 
 __device__ __forceinline__ int row_len(const Params &p, int b) { return min(max(__ldg(p.lens + b), 0), p.max_pages << p.page_shift); }
 __device__ __forceinline__ int row_news(const Params &p, int b) { return p.n_new ? min(max(__ldg(p.n_new + b), 0), p.T) : p.T; }
 
-// base[b + 1] holds the tiles of row b; becomes base[b] = tiles of the rows before b.  One warp.
+// base[b + 1] holds the positions of row b; becomes base[b] = positions of the rows before b.  One warp.
 __device__ __forceinline__ void scan_tiles(int *base, int B)
 {
     const int lane = threadIdx.x & 31;
@@ -235,14 +267,41 @@ __device__ __forceinline__ void scan_tiles(int *base, int B)
 
 // The page that lane f < per_tile looks after in a tile; -1: nothing to load.
 template <int kTile>
-__device__ __forceinline__ int tile_page(const Params &p, const Walk &x, int len, int lane, int per_tile)
+__device__ __forceinline__ int tile_page(const Params &p, int b, int j, int len, int lane, int per_tile)
 {
-    const int place = x.j * kTile + lane * p.box_rows;
+    const int place = j * kTile + lane * p.box_rows;
     if (lane >= per_tile || place >= len) return -1;
-    const int id = __ldg(p.table + static_cast<long long>(x.b) * p.max_pages + (place >> p.page_shift));
+    const int id = __ldg(p.table + static_cast<long long>(b) * p.max_pages + (place >> p.page_shift));
     if (id >= 0 && id < p.n_pages) return id;
     atomicOr(p.flags, CSD_CACHE_BAD_PAGE);
     return p.n_pages;                                    // outside the tensor map: reads as zeros
+}
+
+// This block's share of the positions, and the block that a position belongs to.
+struct Share {
+    long long total, G, x0, x1;
+    __device__ __forceinline__ Share(const Params &p, const int *base)
+    {
+        total = static_cast<long long>(base[p.B]) * p.Hkv * p.row_tiles;
+        G = max(1ll, min(static_cast<long long>(gridDim.x), total));
+        const long long c = blockIdx.x;
+        x0 = c < G ? c * total / G : total;
+        x1 = c < G ? (c + 1) * total / G : total;
+    }
+    __device__ __forceinline__ int owner(long long x) const { return static_cast<int>(((x + 1) * G - 1) / total); }
+};
+
+// The block with a unit's first tile says whether it was split.
+__device__ __forceinline__ void note_split(const Params &p, const Share &s, const Run &r)
+{
+    if (r.j0 != 0) return;
+    const int unit = (r.b * p.Hkv + r.h) * p.row_tiles + r.rt;
+    const int parts = r.ns == r.n ? 0 : s.owner(r.at + r.n - 1) - static_cast<int>(blockIdx.x) + 1;
+    if (!p.by_unit && parts == 0) return;
+    Split *to = p.splits + (p.by_unit ? unit : static_cast<int>(blockIdx.x));
+    to->unit = unit;
+    to->first = blockIdx.x;
+    to->parts = parts;
 }
 
 // Zeros for rows that have nothing to read.
@@ -251,6 +310,8 @@ __device__ __forceinline__ void zero_empty_rows(const Params &p, const int *base
 {
     for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
         if (base[b + 1] != base[b]) continue;
+        if (p.by_unit)
+            for (int i = tid; i < p.Hkv * p.row_tiles; i += threads) p.splits[b * p.Hkv * p.row_tiles + i].parts = 0;
         const long long row0 = static_cast<long long>(b) * p.T * p.Hq;
         uint4 *o = reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + row0 * p.D);
         const int vecs = p.T * p.Hq * p.D / 8;
@@ -313,73 +374,63 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             mbar_init(empty(s), C::kWarps);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        p.splits[blockIdx.x].parts = 0;
+        if (!p.by_unit) p.splits[blockIdx.x].parts = 0;
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // tiles of each row; rows without any give zeros
     for (int b = tid; b < p.B; b += C::kThreads) {
         const int len = row_len(p, b), news = row_news(p, b);
-        base[b + 1] = news > 0 ? (len + kTile - 1) / kTile : 0;
+        base[b + 1] = news > 0 && len > 0 ? (len + kTile - 1) / kTile + p.run_cost : 0;
     }
     __syncthreads();
     if (warp == 0) scan_tiles(base, p.B);
     __syncthreads();
-    const int units_per_row = p.Hkv * p.row_tiles;
-    const long long total = static_cast<long long>(base[p.B]) * units_per_row;
-    long long G = gridDim.x;
-    if (total < G * p.min_tiles) G = max(1ll, total / p.min_tiles);
-    const long long c = blockIdx.x;
-    const long long t0 = c < G ? c * total / G : total, t1 = c < G ? (c + 1) * total / G : total;
+    const Share share(p, base);
 
     if (warp >= C::kWarps) {
         // ---- producer: one warp of its group ----
         if constexpr (C::kMoveRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kProducerRegs));
-        if (warp == C::kWarps && t0 < t1) {
-            Walk w = walk_to(t0, base, p.B, p.Hkv, p.row_tiles);
+        if (warp == C::kWarps) {
+            Runs runs;
+            runs.begin(p, base, share.x0, share.x1);
+            Run r, rn;
+            bool more = runs.next(r);
             const int per_tile = kTile / p.box_rows;               // pages of a tile (1 where a page is larger)
             const unsigned int box_bytes = static_cast<unsigned int>(p.box_rows) * 128u;
-            int len = row_len(p, w.b), len_of = w.b;
-            // ids are fetched a tile ahead
-            auto fetch = [&](const Walk &x, int x_len) { return tile_page<kTile>(p, x, x_len, lane, per_tile); };
-            int id = fetch(w, len);
+            int len = more ? row_len(p, r.b) : 0;
+            // page ids are fetched a tile ahead
+            int id = more ? tile_page<kTile>(p, r.b, r.j0, len, lane, per_tile) : -1;
             int it = 0;
-            for (long long t = t0; t < t1; ++t, ++it) {
-                const Walk now = w;
-                const int my_page = id;
-                const bool unit_ends = now.j + 1 == now.n || t + 1 == t1;
-                if (t + 1 < t1) {
-                    walk_next(w, base, p.B, p.Hkv, p.row_tiles);
-                    if (w.b != len_of) {
-                        len = row_len(p, w.b);
-                        len_of = w.b;
+            bool ok = true;
+            while (more && ok) {
+                const bool follows = runs.next(rn);
+                const int len_next = follows ? row_len(p, rn.b) : 0;
+                for (int i = 0; i < r.ns && ok; ++i, ++it) {
+                    const int page = id, j = r.j0 + i;
+                    id = i + 1 < r.ns ? tile_page<kTile>(p, r.b, j + 1, len, lane, per_tile)
+                                      : (follows ? tile_page<kTile>(p, rn.b, rn.j0, len_next, lane, per_tile) : -1);
+                    const int s = it % p.n_stages;
+                    const unsigned int there = __ballot_sync(kFull, page >= 0);
+                    if (lane == 0) {
+                        ok = mbar_wait(empty(s), ((it / p.n_stages) & 1) ^ 1, give_up);
+                        if (ok) {
+                            const unsigned int bytes = static_cast<unsigned int>(__popc(there)) * box_bytes * C::kHalves;
+                            mbar_expect_tx(full_k(s), bytes);
+                            mbar_expect_tx(full_v(s), bytes);
+                        }
                     }
-                    id = fetch(w, len);
-                }
-                const int s = it % p.n_stages;
-                const unsigned int there = __ballot_sync(kFull, my_page >= 0);
-                bool ok = true;
-                if (lane == 0) {
-                    ok = mbar_wait(empty(s), ((it / p.n_stages) & 1) ^ 1, give_up);
-                    if (ok) {
-                        const unsigned int bytes = static_cast<unsigned int>(__popc(there)) * box_bytes * C::kHalves;
-                        mbar_expect_tx(full_k(s), bytes);
-                        mbar_expect_tx(full_v(s), bytes);
+                    ok = __shfl_sync(kFull, ok ? 1 : 0, 0) != 0;
+                    if (ok && page >= 0) {
+                        const int in_page = p.box_rows == kTile ? (j * kTile) & ((1 << p.page_shift) - 1) : 0;
+                        const unsigned int at = ring + s * C::kStageBytes + lane * box_bytes;
+#pragma unroll
+                        for (int hf = 0; hf < C::kHalves; ++hf) tma_load_page(at + hf * (kTile * 128), &map_k, full_k(s), hf * 64, in_page, r.h, page);
+#pragma unroll
+                        for (int hf = 0; hf < C::kHalves; ++hf)
+                            tma_load_page(at + C::kTileBytes + hf * (kTile * 128), &map_v, full_v(s), hf * 64, in_page, r.h, page);
                     }
                 }
-                ok = __shfl_sync(kFull, ok ? 1 : 0, 0) != 0;
-                if (!ok) break;
-                if (my_page >= 0) {
-                    const int in_page = p.box_rows == kTile ? (now.j * kTile) & ((1 << p.page_shift) - 1) : 0;
-                    const unsigned int at = ring + s * C::kStageBytes + lane * box_bytes;
-#pragma unroll
-                    for (int hf = 0; hf < C::kHalves; ++hf)
-                        tma_load_page(at + hf * (kTile * 128), &map_k, full_k(s), hf * 64, in_page, now.h, my_page);
-#pragma unroll
-                    for (int hf = 0; hf < C::kHalves; ++hf)
-                        tma_load_page(at + C::kTileBytes + hf * (kTile * 128), &map_v, full_v(s), hf * 64, in_page, now.h, my_page);
-                }
-                if (unit_ends && KG > 1) {                           // the consumers join through the next stage
-                    ++it;
+                if (ok) {                                            // the consumers join through the next stage
                     const int sj = it % p.n_stages;
                     if (lane == 0) {
                         ok = mbar_wait(empty(sj), ((it / p.n_stages) & 1) ^ 1, give_up);
@@ -388,9 +439,12 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                             mbar_arrive(full_v(sj));
                         }
                     }
+                    ++it;
                     ok = __shfl_sync(kFull, ok ? 1 : 0, 0) != 0;
-                    if (!ok) break;
                 }
+                r = rn;
+                len = len_next;
+                more = follows;
             }
         }
     } else {
@@ -400,18 +454,18 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const int g = lane >> 2, qd = lane & 3;
         const int cthreads = C::kWarps * 32;
         zero_empty_rows<T>(p, base, tid, cthreads);
-        Walk w;
-        if (t0 < t1) w = walk_to(t0, base, p.B, p.Hkv, p.row_tiles);
+        Runs runs;
+        runs.begin(p, base, share.x0, share.x1);
+        Run run;
         int it = 0;
         const int swz = lane & 7;
         const unsigned int k_lane = (16 * NK * kg + ((lane >> 4) << 3) + swz) * 128u, k_chunk = (lane >> 3) & 1;
         const unsigned int v_lane = (16 * NK * kg + (((lane >> 3) & 1) << 3) + swz) * 128u, v_chunk = lane >> 4;
         const unsigned int q_lane = (16 * MT * rg + (((lane >> 3) & 1) << 3) + swz) * 128u, q_chunk = lane >> 4;
 
-        for (long long t = t0; t < t1;) {
+        while (runs.next(run)) {
             // ---- a unit, or the part of one that lies in this block ----
-            const int b = w.b, h = w.h, rt = w.rt, j0 = w.j;
-            const int j1 = static_cast<int>(min(static_cast<long long>(w.n), j0 + (t1 - t)));
+            const int b = run.b, h = run.h, rt = run.rt, j0 = run.j0, j1 = run.j0 + run.ns;
             const int len = row_len(p, b), news = row_news(p, b);
             const int rows_here = min(C::kRows, p.rows - rt * C::kRows);
             // its query rows: row r is token r / group, query head h * group + r % group
@@ -712,10 +766,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 if (lane == 0) mbar_arrive(empty(it % p.n_stages));
                 ++it;
             }
-            const bool whole = j0 == 0 && j1 == w.n;
-            const int unit = (b * p.Hkv + h) * p.row_tiles + rt;
+            const bool whole = run.ns == run.n;
             if (kg == 0) {
-                const int slot = 2 * static_cast<int>(c) + (j0 == 0 ? 1 : 0);
+                const int slot = 2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0);
                 float *part = p.parts + static_cast<long long>(slot) * C::kSlotFloats;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
@@ -741,17 +794,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                             if (qd == 0) __stcg(reinterpret_cast<float2 *>(part + C::kRows * DP + 2 * r), make_float2(m[mt][hh], L));
                         }
                     }
-                if (!whole && j0 == 0 && warp == 0 && lane == 0) {
-                    // the unit's last tile is (unit's first tile of all) + n - 1; the block that owns it ends the parts
-                    const long long last = t - j0 + w.n - 1;
-                    const int end = static_cast<int>(((last + 1) * G - 1) / total);
-                    p.splits[blockIdx.x].unit = unit;
-                    p.splits[blockIdx.x].parts = end - static_cast<int>(c) + 1;
-                }
+                if (tid == 0) note_split(p, share, run);
             }
-            t += j1 - j0;
-            w.j = j1 - 1;
-            if (t < t1) walk_next(w, base, p.B, p.Hkv, p.row_tiles);
             if constexpr (KG == 1) consumer_barrier(cthreads);          // the query rows in shared memory are done with
         }
     }
@@ -844,12 +888,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         mbar_init(pv_done, 1);
         mbar_init(q_ready, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        p.splits[blockIdx.x].parts = 0;
+        if (!p.by_unit) p.splits[blockIdx.x].parts = 0;
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     for (int b = tid; b < p.B; b += kTcThreads) {
         const int len = row_len(p, b), news = row_news(p, b);
-        base[b + 1] = news > 0 ? (len + kTcTile - 1) / kTcTile : 0;
+        base[b + 1] = news > 0 && len > 0 ? (len + kTcTile - 1) / kTcTile + p.run_cost : 0;
     }
     if (warp == 1) {
         ptx::tmem_alloc(smem_u32(&tmem_base_slot), p.tmem_cols);
@@ -861,73 +905,69 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     if (warp == 0) scan_tiles(base, p.B);
     __syncthreads();
     const unsigned int tmem = tmem_base_slot;
-    const long long total = static_cast<long long>(base[p.B]) * p.Hkv * p.row_tiles;
-    long long G = gridDim.x;
-    if (total < G * p.min_tiles) G = max(1ll, total / p.min_tiles);
-    const long long c = blockIdx.x;
-    const long long t0 = c < G ? c * total / G : total, t1 = c < G ? (c + 1) * total / G : total;
+    const Share share(p, base);
     auto slot_of = [&](int item) { return item % p.n_stages; };
     auto phase_of = [&](int item) { return static_cast<unsigned int>(item / p.n_stages) & 1u; };
 
     if (warp == 5) {
         // ---- page loads ----
-        if (t0 < t1) {
-            Walk w = walk_to(t0, base, p.B, p.Hkv, p.row_tiles);
-            const int per_tile = kTcTile / p.box_rows;
-            const unsigned int box_bytes = static_cast<unsigned int>(p.box_rows) * 128u;
-            int len = row_len(p, w.b), len_of = w.b;
-            auto fetch = [&](const Walk &x, int x_len) { return tile_page<kTcTile>(p, x, x_len, lane, per_tile); };
-            auto load = [&](const CUtensorMap *map, const Walk &x, int page, int item) {
-                const int s = slot_of(item);
-                const unsigned int there = __ballot_sync(kFull, page >= 0);
-                int ok = 1;
-                if (lane == 0) {
-                    ok = mbar_wait(empty(s), phase_of(item) ^ 1u, give_up) ? 1 : 0;
-                    if (ok) mbar_expect_tx(full(s), static_cast<unsigned int>(__popc(there)) * box_bytes * p.halves);
-                }
-                ok = __shfl_sync(kFull, ok, 0);
-                if (ok && page >= 0) {
-                    const int in_page = p.box_rows == kTcTile ? (x.j * kTcTile) & ((1 << p.page_shift) - 1) : 0;
-                    const unsigned int at = ring + s * slot_bytes + lane * box_bytes;
-                    for (int hf = 0; hf < p.halves; ++hf) tma_load_page(at + hf * (kTcTile * 128), map, full(s), hf * 64, in_page, x.h, page);
-                }
-                return ok != 0;
-            };
-            int id = fetch(w, len), item = 0, before = -1;
-            Walk w_before = w;
-            bool first = true, ok = true;
-            for (long long t = t0; t < t1 && ok; ++t) {
-                const Walk now = w;
-                const int page = id;
-                const bool last = now.j + 1 == now.n || t + 1 == t1;
-                if (t + 1 < t1) {
-                    walk_next(w, base, p.B, p.Hkv, p.row_tiles);
-                    if (w.b != len_of) {
-                        len = row_len(p, w.b);
-                        len_of = w.b;
-                    }
-                    id = fetch(w, len);
-                }
-                ok = load(&map_k, now, page, item++);
-                if (!first && ok) ok = load(&map_v, w_before, before, item++);
-                if (last && ok) ok = load(&map_v, now, page, item++);
-                first = last;
-                before = page;
-                w_before = now;
+        Runs runs;
+        runs.begin(p, base, share.x0, share.x1);
+        Run r, rn;
+        bool more = runs.next(r), ok = true;
+        const int per_tile = kTcTile / p.box_rows;               // pages of a tile (1 where a page is larger)
+        const unsigned int box_bytes = static_cast<unsigned int>(p.box_rows) * 128u;
+        int item = 0;
+        auto load = [&](const CUtensorMap *map, int h, int j, int page) {
+            const int s = slot_of(item);
+            const unsigned int there = __ballot_sync(kFull, page >= 0);
+            int fine = 1;
+            if (lane == 0) {
+                fine = mbar_wait(empty(s), phase_of(item) ^ 1u, give_up) ? 1 : 0;
+                if (fine) mbar_expect_tx(full(s), static_cast<unsigned int>(__popc(there)) * box_bytes * p.halves);
             }
-            // every commit aimed at the slots' barriers has landed before the block ends
-            if (lane == 0)
-                for (int k = 0; k < p.n_stages && ok; ++k, ++item) ok = mbar_wait(empty(slot_of(item)), phase_of(item) ^ 1u, give_up);
+            fine = __shfl_sync(kFull, fine, 0);
+            if (fine && page >= 0) {
+                const int in_page = p.box_rows == kTcTile ? (j * kTcTile) & ((1 << p.page_shift) - 1) : 0;
+                const unsigned int at = ring + s * slot_bytes + lane * box_bytes;
+                for (int hf = 0; hf < p.halves; ++hf) tma_load_page(at + hf * (kTcTile * 128), map, full(s), hf * 64, in_page, h, page);
+            }
+            ++item;
+            return fine != 0;
+        };
+        int len = more ? row_len(p, r.b) : 0;
+        int id = more ? tile_page<kTcTile>(p, r.b, r.j0, len, lane, per_tile) : -1;      // fetched a tile ahead
+        while (more && ok) {
+            const bool follows = runs.next(rn);
+            const int len_next = follows ? row_len(p, rn.b) : 0;
+            int before = -1;
+            for (int i = 0; i < r.ns && ok; ++i) {
+                const int page = id, j = r.j0 + i;
+                id = i + 1 < r.ns ? tile_page<kTcTile>(p, r.b, j + 1, len, lane, per_tile)
+                                  : (follows ? tile_page<kTcTile>(p, rn.b, rn.j0, len_next, lane, per_tile) : -1);
+                ok = load(&map_k, r.h, j, page);
+                if (ok && i > 0) ok = load(&map_v, r.h, j - 1, before);
+                if (ok && i + 1 == r.ns) ok = load(&map_v, r.h, j, page);
+                before = page;
+            }
+            r = rn;
+            len = len_next;
+            more = follows;
         }
+        // every commit aimed at the slots' barriers has landed before the block ends
+        if (lane == 0)
+            for (int k = 0; k < p.n_stages && ok; ++k, ++item) ok = mbar_wait(empty(slot_of(item)), phase_of(item) ^ 1u, give_up);
     } else if (warp == 4) {
         // ---- products ----
-        if (lane == 0 && t0 < t1) {
-            Walk w = walk_to(t0, base, p.B, p.Hkv, p.row_tiles);
+        if (lane == 0) {
+            Runs runs;
+            runs.begin(p, base, share.x0, share.x1);
+            Run r;
             const unsigned int idesc_qk = tc_instr<T>(kTcTile, false), idesc_pv = tc_instr<T>(p.d16, true);
-            int n0 = 0, items = 0, run = 0;                    // tiles and loads of the runs before; runs
+            int n0 = 0, items = 0;                             // tiles and loads of the runs before
             bool ok = true;
-            for (long long t = t0; t < t1 && ok; ++run) {
-                const int ns = static_cast<int>(min(static_cast<long long>(w.n - w.j), t1 - t));
+            for (int run = 0; ok && runs.next(r); ++run) {
+                const int ns = r.ns;
                 ok = mbar_wait(q_ready, run & 1, give_up);
                 for (int i = 0; i <= ns && ok; ++i) {
                     if (i < ns) {
@@ -957,32 +997,32 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 }
                 n0 += ns;
                 items += 2 * ns;
-                t += ns;
-                w.j += ns - 1;
-                if (t < t1) walk_next(w, base, p.B, p.Hkv, p.row_tiles);
             }
         }
     } else {
         // ---- softmax, rows in and out ----
         zero_empty_rows<T>(p, base, tid, 128);
-        Walk w;
-        if (t0 < t1) w = walk_to(t0, base, p.B, p.Hkv, p.row_tiles);
+        Runs runs;
+        runs.begin(p, base, share.x0, share.x1);
+        Run ru;
         const unsigned int my_lanes = static_cast<unsigned int>(32 * warp) << 16;
-        int n = 0, items = 0, run = 0;
-        for (long long t = t0; t < t1; ++run) {
-            const int b = w.b, h = w.h, rt = w.rt, j0 = w.j;
-            const int ns = static_cast<int>(min(static_cast<long long>(w.n - j0), t1 - t));
+        int n = 0, items = 0;
+        const int chunks = p.halves * 8;                          // 16-byte pieces of a query row, or of a row of the result
+        const int rows_at_once = 32 / chunks, sub = lane / chunks, ch = lane - sub * chunks;
+        for (int run = 0; runs.next(ru); ++run) {
+            const int b = ru.b, h = ru.h, rt = ru.rt, j0 = ru.j0, ns = ru.ns;
             const int len = row_len(p, b), news = row_news(p, b);
             const int rows_here = min(p.tile_rows, p.rows - rt * p.tile_rows);
-            const int chunks = p.halves * 8;
-            for (int i = tid; i < rows_here * chunks; i += 128) {
-                const int r = i / chunks, ch = i - r * chunks;
+            consumer_barrier(128);                               // rows of the run before have left through the same memory
+            for (int r = warp * rows_at_once + sub; r < rows_here; r += 4 * rows_at_once) {
+                if (sub >= rows_at_once) break;                   // (24 pieces leave lanes over)
                 const int rr = rt * p.tile_rows + r, tok = rr / p.group, hh = h * p.group + rr - tok * p.group;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (ch * 8 < p.D) x = __ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + b * p.qb + tok * p.qt + hh * p.qh + ch * 8));
                 const unsigned int at = q_smem + (ch >> 3) * (p.tile_rows * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                const bool there = ch * 8 < p.D;                  // elements beyond dim: zeros
+                const T *from = static_cast<const T *>(p.q) + b * p.qb + tok * p.qt + hh * p.qh + (there ? ch * 8 : 0);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(there ? 16 : 0) : "memory");
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             ptx::tc_fence_before();                              // the output of the run before has been read
             __syncwarp();
@@ -1073,6 +1113,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 if (edge) {
                     // A weight of zero does not silence an infinity or NaN in the values.  Places beyond the row hold anything:
                     // zeroed.  Such a value in a place of a later new token is left out here and handed to the rows that see it at the end.
+                    // (the loads up to the tile's keys have been consumed: with four slots that includes this slot's load before)
                     const int item = items + v_item(i, ns), s = slot_of(item);
                     mbar_wait(full(s), phase_of(item), give_up);
                     const unsigned int v_at = ring + s * slot_bytes;
@@ -1101,45 +1142,73 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             }
 
             // ---- the run's rows ----
+            // (a wait by parity is only sound one phase ahead: the last scores are complete, hence the output products up to the
+            // last but two)
+            if (ns > 1) mbar_wait(pv_done, n & 1, give_up);
             mbar_wait(pv_done, (n - 1) & 1, give_up);
             ptx::tc_fence_after();
             consumer_barrier(128);                              // odd_run of all four warps
             const bool odd = *static_cast<volatile int *>(&odd_run) == run + 1;
-            const bool whole = j0 == 0 && ns == w.n;
+            const bool whole = ns == ru.n;
             const bool seen = limit >= 0 && l != 0.f;            // (NaN counts as seen)
             const int head = h * p.group + rr - tok * p.group;
             const long long row = (static_cast<long long>(b) * p.T + tok) * p.Hq + head;
-            float *part = p.parts + static_cast<long long>(2 * static_cast<int>(c) + (j0 == 0 ? 1 : 0)) * p.tile_rows * (p.part_stride + 2);
+            float *part = p.parts + static_cast<long long>(2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0)) * p.tile_rows * (p.part_stride + 2);
             if (warp_has) {
-                const float inv = 1.f / l;
-                for (int c0 = 0; c0 < p.D; c0 += 32) {
-                    float o[32];
-                    ptx::tmem_ld32(tmem + my_lanes + kTcOutCol + c0, o);
-                    if (odd && seen) {
-                        float z[32];
+                // A thread has a row, memory wants rows side by side: each warp turns its 32 rows round in the memory of its query
+                // rows, which every product has read.  A row of it holds dim elements of the result, or half a row of a part.
+                const float inv = seen ? (whole ? 1.f / l : 1.f) : 0.f;
+                const int pitch = p.halves * 128, warp_rows = min(32, rows_here - 32 * warp);
+                const unsigned int my_row = q_smem + r * pitch;
+                const int passes = whole ? 1 : 2, cols = whole ? p.halves * 64 : p.halves * 32;
+                for (int pass = 0; pass < passes && pass * cols < p.D; ++pass) {
+                    for (int c0 = pass * cols; c0 < min((pass + 1) * cols, p.D); c0 += 32) {
+                        float o[32];
+                        ptx::tmem_ld32(tmem + my_lanes + kTcOutCol + c0, o);
+                        if (odd && seen) {
+                            float z[32];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) z[e] = o[e];
-                        add_left_out<T>(p, b, h, tok, head, c0, max(len - news + 1, j0 * kTcTile), min(limit, (j0 + ns) * kTcTile - 1), m, z);
+                            for (int e = 0; e < 32; ++e) z[e] = o[e];
+                            add_left_out<T>(p, b, h, tok, head, c0, max(len - news + 1, j0 * kTcTile), min(limit, (j0 + ns) * kTcTile - 1), m, z);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = z[e];
-                    }
-                    if (r < rows_here) {
+                            for (int e = 0; e < 32; ++e) o[e] = z[e];
+                        }
+                        if (r < rows_here) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            if (c0 + e >= p.D) break;
+                            for (int e = 0; e < 32; ++e) o[e] = seen ? o[e] * inv : 0.f;
                             if (whole) {
-                                uint4 v = make_uint4(0, 0, 0, 0);
-                                if (seen)
-                                    v = make_uint4(pack_pair<T>(o[e] * inv, o[e + 1] * inv), pack_pair<T>(o[e + 2] * inv, o[e + 3] * inv),
-                                                   pack_pair<T>(o[e + 4] * inv, o[e + 5] * inv), pack_pair<T>(o[e + 6] * inv, o[e + 7] * inv));
-                                *reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + row * p.D + c0 + e) = v;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(my_row + (((c0 / 8 + e) ^ (r & 7)) << 4)),
+                                                 "r"(pack_pair<T>(o[8 * e], o[8 * e + 1])), "r"(pack_pair<T>(o[8 * e + 2], o[8 * e + 3])),
+                                                 "r"(pack_pair<T>(o[8 * e + 4], o[8 * e + 5])), "r"(pack_pair<T>(o[8 * e + 6], o[8 * e + 7]))
+                                                 : "memory");
                             } else {
-                                float4 *to = reinterpret_cast<float4 *>(part + static_cast<long long>(r) * p.part_stride + c0 + e);
-                                __stcg(to, seen ? make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f));
-                                __stcg(to + 1, seen ? make_float4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]) : make_float4(0.f, 0.f, 0.f, 0.f));
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(my_row + ((((c0 - pass * cols) / 4 + e) ^ (r & 7)) << 4)),
+                                                 "f"(o[4 * e]), "f"(o[4 * e + 1]), "f"(o[4 * e + 2]), "f"(o[4 * e + 3])
+                                                 : "memory");
                             }
                         }
                     }
+                    __syncwarp();
+                    // lanes_row lanes a row, 16 bytes each
+                    const int d = whole ? ch * 8 : pass * cols + ch * 4;
+#pragma unroll 4
+                    for (int w0 = 0; w0 < warp_rows; w0 += rows_at_once) {
+                        const int wr = w0 + sub;
+                        const long long to = __shfl_sync(kFull, whole ? row * p.D : static_cast<long long>(r) * p.part_stride, wr & 31);
+                        if (sub >= rows_at_once || wr >= warp_rows || d >= p.D) continue;
+                        const int r2 = 32 * warp + wr;
+                        uint4 v;
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(q_smem + r2 * pitch + ((ch ^ (r2 & 7)) << 4)) : "memory");
+                        if (whole)
+                            *reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + to + d) = v;
+                        else
+                            __stcg(reinterpret_cast<uint4 *>(part + to + d), v);
+                    }
+                    __syncwarp();
                 }
                 if (r < rows_here) {
                     if (!whole)
@@ -1148,15 +1217,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         p.lse[row] = seen ? (m + log2f(l)) * kLn2 : -INFINITY;
                 }
             }
-            if (!whole && j0 == 0 && tid == 0) {
-                const long long last = t + w.n - 1;
-                p.splits[blockIdx.x].unit = (b * p.Hkv + h) * p.row_tiles + rt;
-                p.splits[blockIdx.x].parts = static_cast<int>(((last + 1) * G - 1) / total) - static_cast<int>(c) + 1;
-            }
-            t += ns;
+            if (tid == 0) note_split(p, share, ru);
             items += 2 * ns;
-            w.j = j0 + ns - 1;
-            if (t < t1) walk_next(w, base, p.B, p.Hkv, p.row_tiles);
         }
         ptx::tc_fence_before();
     }
@@ -1165,70 +1227,105 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     if (*give_up && lane == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);
 }
 
-// Joins the parts of split units.  Block (c, y): the unit that begins in block c of the kernel before, query rows 8 y ..; a warp per row.
+// Joins the parts of split units: block (x, y) four query rows of one of them.  The weights of all parts and rows first (a
+// thread per part and row), then each warp sums every fourth part, four rows side by side, so that a row of 40 parts costs a
+// few memory latencies and not forty; the four sums are added in order.
+constexpr int kJoinThreads = 128, kJoinRows = 4, kMaxGrid = 512;
+
 template <typename T, int DP>
-__global__ void __launch_bounds__(256) attention_join_kernel(const Params p, int rows_per_tile)
+__global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Params p, int tile_rows)
 {
+    __shared__ float2 part_ml[kMaxGrid][kJoinRows];                     // (m, l), then (weight, l)
+    __shared__ float red[4][kJoinRows], sums[4][kJoinRows];
+    __shared__ __align__(16) float rows[4][kJoinRows][DP];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int c = blockIdx.x, lane = threadIdx.x & 31;
-    const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
-    const int unit = __ldcg(&p.splits[c].unit), n = __ldcg(&p.splits[c].parts);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const Split sp = {__ldcg(&p.splits[blockIdx.x].unit), __ldcg(&p.splits[blockIdx.x].first), __ldcg(&p.splits[blockIdx.x].parts)};
+    const int n = sp.parts;
     if (n == 0) return;
-    const int rt = unit % p.row_tiles, bh = unit / p.row_tiles, b = bh / p.Hkv, h = bh - b * p.Hkv;
-    if (r >= min(rows_per_tile, p.rows - rt * rows_per_tile)) return;
-    const long long slot_floats = static_cast<long long>(rows_per_tile) * (DP + 2);
-    auto slot = [&](int i) { return p.parts + slot_floats * (i == 0 ? 2 * c + 1 : 2 * (c + i)); };
-    float M = -INFINITY;
-    for (int i = lane; i < n; i += 32) M = fmaxf(M, __ldcg(slot(i) + rows_per_tile * DP + 2 * r));
+    const int rt = sp.unit % p.row_tiles, bh = sp.unit / p.row_tiles, b = bh / p.Hkv, h = bh - b * p.Hkv;
+    const int r0 = blockIdx.y * kJoinRows, here = min(kJoinRows, min(tile_rows, p.rows - rt * tile_rows) - r0);
+    if (here <= 0) return;
+    const long long slot_floats = static_cast<long long>(tile_rows) * (DP + 2);
+    auto slot = [&](int i) { return p.parts + slot_floats * (i == 0 ? 2 * sp.first + 1 : 2 * (sp.first + i)); };
+    const int row = tid & 3;
+    float M = -INFINITY, L = 0.f;
+    for (int i = tid >> 2; i < n; i += kJoinThreads / 4) {
+        const float2 ml = row < here ? __ldcg(reinterpret_cast<const float2 *>(slot(i) + tile_rows * DP + 2 * (r0 + row))) : make_float2(-INFINITY, 0.f);
+        part_ml[i][row] = ml;
+        M = fmaxf(M, ml.x);
+    }
 #pragma unroll
-    for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, d));
+    for (int d = 4; d < 32; d <<= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, d));
+    if (lane < 4) red[warp][row] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(red[0][row], red[1][row]), fmaxf(red[2][row], red[3][row]));
+    for (int i = tid >> 2; i < n; i += kJoinThreads / 4) {
+        const float2 ml = part_ml[i][row];
+        const float w = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
+        part_ml[i][row].x = w;
+        L += w * ml.y;
+    }
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) L += __shfl_xor_sync(kFull, L, d);
+    if (lane < 4) sums[warp][row] = L;
+    __syncthreads();
     constexpr int E = DP / 32;                                          // columns of a lane: 2, 4 or 8, side by side
-    float o[E], L = 0.f;
+    float o[kJoinRows][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        float wt = 0.f, wl = 0.f;
-        if (i0 + lane < n) {
-            const float2 y = __ldcg(reinterpret_cast<const float2 *>(slot(i0 + lane) + rows_per_tile * DP + 2 * r));
-            wt = y.x == -INFINITY ? 0.f : ex2_approx(y.x - M);
-            wl = y.y * wt;
-        }
+    for (int k = 0; k < kJoinRows; ++k)
 #pragma unroll
-        for (int d = 16; d; d >>= 1) wl += __shfl_xor_sync(kFull, wl, d);
-        L += wl;
-        const int here = min(32, n - i0);
-#pragma unroll 8
-        for (int i = 0; i < here; ++i) {
-            const float f = __shfl_sync(kFull, wt, i);
-            const float *from = slot(i0 + i) + r * DP + lane * E;
-            if constexpr (E == 2) {
-                if (lane * E < p.D) {
-                    const float2 y = __ldcg(reinterpret_cast<const float2 *>(from));
-                    o[0] += f * y.x;
-                    o[1] += f * y.y;
-                }
-            } else {
+        for (int e = 0; e < E; ++e) o[k][e] = 0.f;
+    const bool mine = lane * E < p.D;
+#pragma unroll 4
+    for (int i = warp; i < n; i += 4) {
+        const float *from = slot(i) + r0 * DP + lane * E;
 #pragma unroll
-                for (int e = 0; e < E; e += 4) {
-                    if (lane * E + e < p.D) {
-                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(from + e));
-                        o[e] += f * y.x;
-                        o[e + 1] += f * y.y;
-                        o[e + 2] += f * y.z;
-                        o[e + 3] += f * y.w;
+        for (int k = 0; k < kJoinRows; ++k) {
+            if (k < here && mine) {
+                const float w = part_ml[i][k].x;
+                if constexpr (E == 2) {
+                    const float2 y = __ldcg(reinterpret_cast<const float2 *>(from + k * DP));
+                    o[k][0] += w * y.x;
+                    o[k][1] += w * y.y;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; e += 4) {
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(from + k * DP + e));
+                        o[k][e] += w * y.x;
+                        o[k][e + 1] += w * y.y;
+                        o[k][e + 2] += w * y.z;
+                        o[k][e + 3] += w * y.w;
                     }
                 }
             }
         }
     }
-    const int rr = rt * rows_per_tile + r, tok = rr / p.group, head = h * p.group + rr - tok * p.group;
-    const long long row = (static_cast<long long>(b) * p.T + tok) * p.Hq + head;
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    unsigned int *out = reinterpret_cast<unsigned int *>(static_cast<T *>(p.out) + row * p.D);
 #pragma unroll
-    for (int e = 0; e < E; e += 2)
-        if (lane * E + e < p.D) out[(lane * E + e) / 2] = pack_pair<T>(o[e] * inv, o[e + 1] * inv);
-    if (p.lse && lane == 0) p.lse[row] = L == 0.f ? -INFINITY : (fmaxf(M, -3e38f) + log2f(L)) * kLn2;
+    for (int k = 0; k < kJoinRows; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) rows[warp][k][lane * E + e] = o[k][e];
+    __syncthreads();
+    if (warp >= here) return;
+    // warp k finishes row k
+    L = (sums[0][warp] + sums[1][warp]) + (sums[2][warp] + sums[3][warp]);
+    const int rr = rt * tile_rows + r0 + warp, tok = rr / p.group, head = h * p.group + rr - tok * p.group;
+    const long long to = (static_cast<long long>(b) * p.T + tok) * p.Hq + head;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    unsigned int *out = reinterpret_cast<unsigned int *>(static_cast<T *>(p.out) + to * p.D);
+    for (int d = 2 * lane; d < p.D; d += 64) {
+        float2 y = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            y.x += rows[w][warp][d];
+            y.y += rows[w][warp][d + 1];
+        }
+        out[d / 2] = pack_pair<T>(y.x * inv, y.y * inv);
+    }
+    if (p.lse && lane == 0) {
+        const float m = fmaxf(fmaxf(red[0][warp], red[1][warp]), fmaxf(red[2][warp], red[3][warp]));
+        p.lse[to] = L == 0.f ? -INFINITY : (fmaxf(m, -3e38f) + log2f(L)) * kLn2;
+    }
 }
 
 }  // namespace attention

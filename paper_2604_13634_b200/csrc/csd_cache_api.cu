@@ -216,9 +216,15 @@ constexpr int kMaxDevices = 64;
 constexpr int kSmemPerSm = 228 * 1024, kSmemReserved = 1024, kSmemStatic = 1024;     // per block: the system's, and the kernel's own
 
 struct AttentionPlan {
-    int rows, row_tiles, tile_rows, dp, grid, stages, smem;
+    int rows, row_tiles, tile_rows, dp, grid, stages, smem, run_cost;
     size_t splits_off, parts_off, total;
 };
+
+int attention_grid(int blocks_per_sm)
+{
+    const int g = host::multiprocessors() * blocks_per_sm;
+    return g < attention::kMaxGrid ? g : attention::kMaxGrid;
+}
 
 template <typename C>
 AttentionPlan attention_plan(int rows, int B)
@@ -228,7 +234,8 @@ AttentionPlan attention_plan(int rows, int B)
     a.tile_rows = C::kRows;
     a.dp = C::DP;
     a.row_tiles = (rows + C::kRows - 1) / C::kRows;
-    a.grid = host::multiprocessors() * C::kBlocksPerSm;
+    a.grid = attention_grid(C::kBlocksPerSm);
+    a.run_cost = 1;
     const int limit = kSmemPerSm / C::kBlocksPerSm - kSmemReserved - kSmemStatic;
     const int fixed = 1024 + C::kQBytes + C::kMlBytes + (B + 1) * 4;
     a.stages = (limit - fixed) / C::kStageBytes;
@@ -260,18 +267,22 @@ AttentionPlan attention_tc_plan(int rows, int dim, int B)
 {
     AttentionPlan a;
     a.rows = rows;
-    a.row_tiles = (rows + 127) / 128;
-    a.tile_rows = ((rows + a.row_tiles - 1) / a.row_tiles + 7) / 8 * 8;
-    a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
     a.dp = dim <= 64 ? 64 : (dim <= 128 ? 128 : 256);
-    a.grid = host::multiprocessors() * tc_blocks(dim);
+    a.grid = attention_grid(tc_blocks(dim));
+    a.run_cost = 2;
     const int halves = (dim + 63) / 64, slot = halves * attention::kTcTile * 128;
     const int limit = kSmemPerSm / tc_blocks(dim) - kSmemReserved - kSmemStatic;
-    // the first product reads 128 query rows whatever the row tile: what follows the rows has to be there
-    const int fixed = 1024 + halves * a.tile_rows * 128 + (B + 1) * 4;
-    a.stages = (limit - fixed) / slot;
-    if (a.stages > attention::kTcMaxSlots) a.stages = attention::kTcMaxSlots;
-    a.smem = fixed + a.stages * slot;
+    // The kernel's waits want four slots at least; tables of thousands of rows leave room for fewer query rows.
+    for (int most = 128;; most /= 2) {
+        a.row_tiles = (rows + most - 1) / most;
+        a.tile_rows = ((rows + a.row_tiles - 1) / a.row_tiles + 7) / 8 * 8;
+        a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
+        const int fixed = 1024 + halves * a.tile_rows * 128 + (B + 1) * 4;
+        a.stages = (limit - fixed) / slot;
+        if (a.stages > attention::kTcMaxSlots) a.stages = attention::kTcMaxSlots;
+        a.smem = fixed + a.stages * slot;
+        if (a.stages >= 4 || most == 16) break;
+    }
     a.splits_off = 0;
     a.parts_off = align_up(static_cast<size_t>(a.grid) * sizeof(attention::Split), 256);
     a.total = a.parts_off + static_cast<size_t>(2) * a.grid * a.tile_rows * (a.dp + 2) * 4;
@@ -329,21 +340,34 @@ bool kernel_ready(K kernel, std::atomic<bool> (&done)[kMaxDevices], int smem, in
     return true;
 }
 
+// Common to both kernels: the plan's numbers, and what is known of the units before the lengths are read.
+void fill_plan(attention::Params &p, const AttentionPlan &a, char *ws)
+{
+    p.rows = a.rows;
+    p.row_tiles = a.row_tiles;
+    p.n_stages = a.stages;
+    p.run_cost = a.run_cost;
+    p.by_unit = static_cast<long long>(p.B) * p.Hkv * a.row_tiles <= a.grid ? 1 : 0;
+    p.splits = reinterpret_cast<attention::Split *>(ws + a.splits_off);
+    p.parts = reinterpret_cast<float *>(ws + a.parts_off);
+}
+
 template <typename T, int DP>
-csd_status_t launch_join(const attention::Params &p, int grid, int tile_rows, cudaStream_t st)
+csd_status_t launch_join(const attention::Params &p, const AttentionPlan &a, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg;
     std::memset(&cfg, 0, sizeof cfg);
-    const int most = p.rows < tile_rows ? p.rows : tile_rows;
-    cfg.gridDim = dim3(static_cast<unsigned int>(grid), static_cast<unsigned int>((most + 7) / 8));
-    cfg.blockDim = dim3(256);
+    const int most = a.rows < a.tile_rows ? a.rows : a.tile_rows;
+    cfg.gridDim = dim3(static_cast<unsigned int>(p.by_unit ? p.B * p.Hkv * a.row_tiles : a.grid),
+                       static_cast<unsigned int>((most + attention::kJoinRows - 1) / attention::kJoinRows));
+    cfg.blockDim = dim3(attention::kJoinThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, attention::attention_join_kernel<T, DP>, p, tile_rows) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, attention::attention_join_kernel<T, DP>, p, a.tile_rows) != cudaSuccess) {
         (void)cudaGetLastError();
         return CSD_ERR_CUDA;
     }
@@ -358,18 +382,13 @@ csd_status_t run_attention(attention::Params p, const csd_cache_t *cache, int la
                       C::kMoveRegs ? C::kConsumerRegs * (C::kGroups - 1) + C::kProducerRegs : 0))
         return CSD_ERR_CUDA;
     const AttentionPlan a = attention_plan<C>(p.T * p.group, p.B);
-    p.rows = a.rows;
-    p.row_tiles = a.row_tiles;
-    p.n_stages = a.stages;
-    p.min_tiles = 1;
+    fill_plan(p, a, ws);
     p.box_rows = cache->page_size < C::kTile ? cache->page_size : C::kTile;
-    p.splits = reinterpret_cast<attention::Split *>(ws + a.splits_off);
-    p.parts = reinterpret_cast<float *>(ws + a.parts_off);
     CUtensorMap map_k, map_v;
     if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
     attention::attention_kernel<C><<<static_cast<unsigned int>(a.grid), C::kThreads, static_cast<size_t>(a.smem), st>>>(map_k, map_v, p);
     if (launched() != CSD_OK) return CSD_ERR_CUDA;
-    return launch_join<typename C::T, C::DP>(p, a.grid, C::kRows, st);
+    return launch_join<typename C::T, C::DP>(p, a, st);
 }
 
 template <typename T, int kBlocks>
@@ -378,18 +397,13 @@ csd_status_t run_attention_tc(attention::Params p, const csd_cache_t *cache, int
     static std::atomic<bool> ready[kMaxDevices];
     if (!kernel_ready(attention::attention_tc_kernel<T, kBlocks>, ready, kSmemPerSm / kBlocks - kSmemReserved - kSmemStatic, 1, 0)) return CSD_ERR_CUDA;
     const AttentionPlan a = attention_tc_plan(p.T * p.group, p.D, p.B);
-    p.rows = a.rows;
-    p.row_tiles = a.row_tiles;
+    fill_plan(p, a, ws);
     p.tile_rows = a.tile_rows;
     p.part_stride = a.dp;
     p.halves = (p.D + 63) / 64;
     p.d16 = (p.D + 15) / 16 * 16;
     p.tmem_cols = kBlocks == 2 ? 256u : 512u;
-    p.n_stages = a.stages;
-    p.min_tiles = 1;
     p.box_rows = cache->page_size < attention::kTcTile ? cache->page_size : attention::kTcTile;
-    p.splits = reinterpret_cast<attention::Split *>(ws + a.splits_off);
-    p.parts = reinterpret_cast<float *>(ws + a.parts_off);
     p.k_pool = static_cast<char *>(cache->k) + layer * cache->stride_layer * 2;
     p.v_pool = static_cast<char *>(cache->v) + layer * cache->stride_layer * 2;
     p.pool_page = cache->stride_page;
@@ -399,9 +413,9 @@ csd_status_t run_attention_tc(attention::Params p, const csd_cache_t *cache, int
     if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
     attention::attention_tc_kernel<T, kBlocks><<<static_cast<unsigned int>(a.grid), attention::kTcThreads, static_cast<size_t>(a.smem), st>>>(map_k, map_v, p);
     if (launched() != CSD_OK) return CSD_ERR_CUDA;
-    if (a.dp == 64) return launch_join<T, 64>(p, a.grid, a.tile_rows, st);
-    if (a.dp == 128) return launch_join<T, 128>(p, a.grid, a.tile_rows, st);
-    return launch_join<T, 256>(p, a.grid, a.tile_rows, st);
+    if (a.dp == 64) return launch_join<T, 64>(p, a, st);
+    if (a.dp == 128) return launch_join<T, 128>(p, a, st);
+    return launch_join<T, 256>(p, a, st);
 }
 
 template <typename T>
