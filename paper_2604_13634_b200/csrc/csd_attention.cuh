@@ -374,9 +374,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             mbar_init(empty(s), C::kWarps);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        if (!p.by_unit) p.splits[blockIdx.x].parts = 0;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     }
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    ptx::wait_for_stream();
+    if (tid == 0 && !p.by_unit) p.splits[blockIdx.x].parts = 0;
     // tiles of each row; rows without any give zeros
     for (int b = tid; b < p.B; b += C::kThreads) {
         const int len = row_len(p, b), news = row_news(p, b);
@@ -888,16 +890,18 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         mbar_init(pv_done, 1);
         mbar_init(q_ready, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        if (!p.by_unit) p.splits[blockIdx.x].parts = 0;
-    }
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    for (int b = tid; b < p.B; b += kTcThreads) {
-        const int len = row_len(p, b), news = row_news(p, b);
-        base[b + 1] = news > 0 && len > 0 ? (len + kTcTile - 1) / kTcTile + p.run_cost : 0;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     }
     if (warp == 1) {
         ptx::tmem_alloc(smem_u32(&tmem_base_slot), p.tmem_cols);
         ptx::tmem_relinquish();
+    }
+    ptx::wait_for_stream();
+    if (tid == 0 && !p.by_unit) p.splits[blockIdx.x].parts = 0;
+    for (int b = tid; b < p.B; b += kTcThreads) {
+        const int len = row_len(p, b), news = row_news(p, b);
+        base[b + 1] = news > 0 && len > 0 ? (len + kTcTile - 1) / kTcTile + p.run_cost : 0;
     }
     ptx::tc_fence_before();
     __syncthreads();
@@ -1238,7 +1242,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Para
     __shared__ float2 part_ml[kMaxGrid][kJoinRows];                     // (m, l), then (weight, l)
     __shared__ float red[4][kJoinRows], sums[4][kJoinRows];
     __shared__ __align__(16) float rows[4][kJoinRows][DP];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    ptx::wait_for_stream();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const Split sp = {__ldcg(&p.splits[blockIdx.x].unit), __ldcg(&p.splits[blockIdx.x].first), __ldcg(&p.splits[blockIdx.x].parts)};
     const int n = sp.parts;

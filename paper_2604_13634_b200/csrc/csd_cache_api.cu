@@ -16,7 +16,28 @@ namespace {
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-csd_status_t launched() { return cudaGetLastError() == cudaSuccess ? CSD_OK : CSD_ERR_CUDA; }
+// A launch that may begin beside the end of what is before it on the stream (the kernels wait themselves before they touch
+// global memory).
+template <typename... P, typename... A>
+csd_status_t launch(void (*kernel)(P...), dim3 grid, unsigned int threads, size_t smem, cudaStream_t st, const A &...args)
+{
+    cudaLaunchConfig_t cfg;
+    std::memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CSD_ERR_CUDA;
+    }
+    return CSD_OK;
+}
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -49,11 +70,8 @@ csd_status_t launch_rope(rope::RopeParams p, csd_rope_layout_t layout, cudaStrea
     p.threads = static_cast<long long>(p.B) * p.S * p.groups * p.units;
     const long long blocks = (p.threads + rope::kThreads - 1) / rope::kThreads;
     if (blocks > INT_MAX) return CSD_ERR_UNSUPPORTED;
-    if (layout == CSD_ROPE_HALF)
-        rope::rope_kernel<T, P, true><<<static_cast<unsigned int>(blocks), rope::kThreads, 0, st>>>(p);
-    else
-        rope::rope_kernel<T, P, false><<<static_cast<unsigned int>(blocks), rope::kThreads, 0, st>>>(p);
-    return launched();
+    return launch(layout == CSD_ROPE_HALF ? rope::rope_kernel<T, P, true> : rope::rope_kernel<T, P, false>, dim3(static_cast<unsigned int>(blocks)),
+                  rope::kThreads, 0, st, p);
 }
 
 template <typename T>
@@ -74,11 +92,8 @@ csd_status_t launch_append(rope::AppendParams p, csd_rope_layout_t layout, cudaS
     p.threads = static_cast<long long>(p.B) * p.T * (p.q_groups + 2 * p.kv_groups) * p.units;
     const long long blocks = (p.threads + rope::kThreads - 1) / rope::kThreads;
     if (blocks > INT_MAX) return CSD_ERR_UNSUPPORTED;
-    if (layout == CSD_ROPE_HALF)
-        rope::rope_append_kernel<T, P, true><<<static_cast<unsigned int>(blocks), rope::kThreads, 0, st>>>(p);
-    else
-        rope::rope_append_kernel<T, P, false><<<static_cast<unsigned int>(blocks), rope::kThreads, 0, st>>>(p);
-    return launched();
+    return launch(layout == CSD_ROPE_HALF ? rope::rope_append_kernel<T, P, true> : rope::rope_append_kernel<T, P, false>,
+                  dim3(static_cast<unsigned int>(blocks)), rope::kThreads, 0, st, p);
 }
 
 template <typename T>
@@ -206,8 +221,7 @@ csd_status_t copy_pages(const csd_cache_t *c, const pages::View &v, long long mo
     const long long cap = static_cast<long long>(host::multiprocessors()) * 8;
     if (blocks > cap) blocks = cap;
     if (blocks < 1) return CSD_OK;
-    pages::pages_copy_kernel<<<static_cast<unsigned int>(blocks), pages::kCopyThreads, 0, st>>>(p);
-    return launched();
+    return launch(pages::pages_copy_kernel, dim3(static_cast<unsigned int>(blocks)), pages::kCopyThreads, 0, st, p);
 }
 
 // ---- attention ----------------------------------------------------------------------------------
@@ -235,7 +249,7 @@ AttentionPlan attention_plan(int rows, int B)
     a.dp = C::DP;
     a.row_tiles = (rows + C::kRows - 1) / C::kRows;
     a.grid = attention_grid(C::kBlocksPerSm);
-    a.run_cost = 1;
+    a.run_cost = C::DP == 64 ? 3 : 2;      // measured: 2 to 3 of 64-element tiles, no difference from 1 to 3 beyond
     const int limit = kSmemPerSm / C::kBlocksPerSm - kSmemReserved - kSmemStatic;
     const int fixed = 1024 + C::kQBytes + C::kMlBytes + (B + 1) * 4;
     a.stages = (limit - fixed) / C::kStageBytes;
@@ -269,7 +283,7 @@ AttentionPlan attention_tc_plan(int rows, int dim, int B)
     a.rows = rows;
     a.dp = dim <= 64 ? 64 : (dim <= 128 ? 128 : 256);
     a.grid = attention_grid(tc_blocks(dim));
-    a.run_cost = 2;
+    a.run_cost = a.dp == 64 ? 8 : (a.dp == 128 ? 4 : 2);      // about 5 us: 240 us at 2, 228 at 4, 231 at 6 for 1024 units of 8 to 63 tiles
     const int halves = (dim + 63) / 64, slot = halves * attention::kTcTile * 128;
     const int limit = kSmemPerSm / tc_blocks(dim) - kSmemReserved - kSmemStatic;
     // The kernel's waits want four slots at least; tables of thousands of rows leave room for fewer query rows.
@@ -355,23 +369,10 @@ void fill_plan(attention::Params &p, const AttentionPlan &a, char *ws)
 template <typename T, int DP>
 csd_status_t launch_join(const attention::Params &p, const AttentionPlan &a, cudaStream_t st)
 {
-    cudaLaunchConfig_t cfg;
-    std::memset(&cfg, 0, sizeof cfg);
     const int most = a.rows < a.tile_rows ? a.rows : a.tile_rows;
-    cfg.gridDim = dim3(static_cast<unsigned int>(p.by_unit ? p.B * p.Hkv * a.row_tiles : a.grid),
-                       static_cast<unsigned int>((most + attention::kJoinRows - 1) / attention::kJoinRows));
-    cfg.blockDim = dim3(attention::kJoinThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, attention::attention_join_kernel<T, DP>, p, a.tile_rows) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return CSD_ERR_CUDA;
-    }
-    return CSD_OK;
+    const dim3 grid(static_cast<unsigned int>(p.by_unit ? p.B * p.Hkv * a.row_tiles : a.grid),
+                    static_cast<unsigned int>((most + attention::kJoinRows - 1) / attention::kJoinRows));
+    return launch(attention::attention_join_kernel<T, DP>, grid, attention::kJoinThreads, 0, st, p, a.tile_rows);
 }
 
 template <typename C>
@@ -386,9 +387,8 @@ csd_status_t run_attention(attention::Params p, const csd_cache_t *cache, int la
     p.box_rows = cache->page_size < C::kTile ? cache->page_size : C::kTile;
     CUtensorMap map_k, map_v;
     if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
-    attention::attention_kernel<C><<<static_cast<unsigned int>(a.grid), C::kThreads, static_cast<size_t>(a.smem), st>>>(map_k, map_v, p);
-    if (launched() != CSD_OK) return CSD_ERR_CUDA;
-    return launch_join<typename C::T, C::DP>(p, a, st);
+    const csd_status_t rc = launch(attention::attention_kernel<C>, dim3(static_cast<unsigned int>(a.grid)), C::kThreads, static_cast<size_t>(a.smem), st, map_k, map_v, p);
+    return rc != CSD_OK ? rc : launch_join<typename C::T, C::DP>(p, a, st);
 }
 
 template <typename T, int kBlocks>
@@ -411,8 +411,9 @@ csd_status_t run_attention_tc(attention::Params p, const csd_cache_t *cache, int
     p.pool_token = cache->stride_token;
     CUtensorMap map_k, map_v;
     if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
-    attention::attention_tc_kernel<T, kBlocks><<<static_cast<unsigned int>(a.grid), attention::kTcThreads, static_cast<size_t>(a.smem), st>>>(map_k, map_v, p);
-    if (launched() != CSD_OK) return CSD_ERR_CUDA;
+    const csd_status_t rc = launch(attention::attention_tc_kernel<T, kBlocks>, dim3(static_cast<unsigned int>(a.grid)), attention::kTcThreads,
+                                   static_cast<size_t>(a.smem), st, map_k, map_v, p);
+    if (rc != CSD_OK) return rc;
     if (a.dp == 64) return launch_join<T, 64>(p, a, st);
     if (a.dp == 128) return launch_join<T, 128>(p, a, st);
     return launch_join<T, 256>(p, a, st);
@@ -556,9 +557,9 @@ csd_status_t csd_cache_rebuild(const csd_cache_t *cache, void *stream)
         (void)cudaGetLastError();
         return CSD_ERR_CUDA;
     }
-    pages::rebuild_count_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, st>>>(v);
-    pages::rebuild_bits_kernel<<<static_cast<unsigned int>((v.n_pages + pages::kRowThreads - 1) / pages::kRowThreads), pages::kRowThreads, 0, st>>>(v);
-    return launched();
+    const csd_status_t rc = launch(pages::rebuild_count_kernel, dim3(static_cast<unsigned int>(v.rows)), pages::kRowThreads, 0, st, v);
+    if (rc != CSD_OK) return rc;
+    return launch(pages::rebuild_bits_kernel, dim3(static_cast<unsigned int>((v.n_pages + pages::kRowThreads - 1) / pages::kRowThreads)), pages::kRowThreads, 0, st, v);
 }
 
 csd_status_t csd_cache_extend(const csd_cache_t *cache, int T, const int32_t *n_new, void *stream)
@@ -569,9 +570,8 @@ csd_status_t csd_cache_extend(const csd_cache_t *cache, int T, const int32_t *n_
     host::other_work_enqueued();
     const pages::View v = view_of(cache);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    pages::extend_kernel<<<1, pages::kBlock, 0, st>>>(v, n_new, T);
-    if (launched() != CSD_OK) return CSD_ERR_CUDA;
-    return copy_pages(cache, v, cache->rows, st);
+    const csd_status_t rc = launch(pages::extend_kernel, dim3(1), pages::kBlock, 0, st, v, n_new, T);
+    return rc != CSD_OK ? rc : copy_pages(cache, v, cache->rows, st);
 }
 
 static csd_status_t shorten(const csd_cache_t *cache, const int32_t *new_lens, const int32_t *accept_len, void *stream)
@@ -581,8 +581,7 @@ static csd_status_t shorten(const csd_cache_t *cache, const int32_t *new_lens, c
     if (!new_lens && !accept_len) return CSD_ERR_INVALID_ARG;
     host::other_work_enqueued();
     const pages::View v = view_of(cache);
-    pages::truncate_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, static_cast<cudaStream_t>(stream)>>>(v, new_lens, accept_len);
-    return launched();
+    return launch(pages::truncate_kernel, dim3(static_cast<unsigned int>(v.rows)), pages::kRowThreads, 0, static_cast<cudaStream_t>(stream), v, new_lens, accept_len);
 }
 
 csd_status_t csd_cache_truncate(const csd_cache_t *cache, const int32_t *new_lens, void *stream) { return shorten(cache, new_lens, nullptr, stream); }
@@ -597,9 +596,8 @@ csd_status_t csd_cache_fork(const csd_cache_t *cache, const int32_t *parent, voi
     host::other_work_enqueued();
     const pages::View v = view_of(cache);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    pages::fork_stage_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, st>>>(v, parent);
-    pages::fork_commit_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, st>>>(v, parent);
-    return launched();
+    const csd_status_t rc = launch(pages::fork_stage_kernel, dim3(static_cast<unsigned int>(v.rows)), pages::kRowThreads, 0, st, v, parent);
+    return rc != CSD_OK ? rc : launch(pages::fork_commit_kernel, dim3(static_cast<unsigned int>(v.rows)), pages::kRowThreads, 0, st, v, parent);
 }
 
 csd_status_t csd_cache_compact(const csd_cache_t *cache, void *stream)
@@ -609,10 +607,9 @@ csd_status_t csd_cache_compact(const csd_cache_t *cache, void *stream)
     host::other_work_enqueued();
     const pages::View v = view_of(cache);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    pages::compact_kernel<<<1, pages::kBlock, 0, st>>>(v);
-    pages::rename_kernel<<<static_cast<unsigned int>(v.rows), pages::kRowThreads, 0, st>>>(v);
-    if (launched() != CSD_OK) return CSD_ERR_CUDA;
-    return copy_pages(cache, v, cache->n_pages / 2, st);
+    csd_status_t rc = launch(pages::compact_kernel, dim3(1), pages::kBlock, 0, st, v);
+    if (rc == CSD_OK) rc = launch(pages::rename_kernel, dim3(static_cast<unsigned int>(v.rows)), pages::kRowThreads, 0, st, v);
+    return rc != CSD_OK ? rc : copy_pages(cache, v, cache->n_pages / 2, st);
 }
 
 size_t csd_attention_workspace_bytes(int rows, int T, int q_heads, int heads, int dim)

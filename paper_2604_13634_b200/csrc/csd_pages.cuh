@@ -19,6 +19,7 @@
 
 #include "../../include/csd.h"
 #include "csd_common.cuh"
+#include "csd_ptx.cuh"
 
 namespace csd {
 namespace pages {
@@ -73,6 +74,7 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
 //   take a copy of the same page) > 1; the last of them keeps the page.
 __global__ void __launch_bounds__(kBlock, 1) extend_kernel(const View v, const int *n_new, int uniform)
 {
+    ptx::wait_for_stream();
     __shared__ __align__(16) int tail[kMaxRows];     // the shared last page a row would have to copy, or -1
     __shared__ unsigned long long slots[32];
     __shared__ int bad;
@@ -210,6 +212,7 @@ __device__ __forceinline__ void release(const View &v, int page)
 // not keep: granted - min(granted, accept_len + 1).  A row never grows here.
 __global__ void __launch_bounds__(kRowThreads) truncate_kernel(const View v, const int *new_lens, const int *accept_len)
 {
+    ptx::wait_for_stream();
     const int r = blockIdx.x;
     const int len = v.lens[r];
     int to;
@@ -237,6 +240,7 @@ __global__ void __launch_bounds__(kRowThreads) truncate_kernel(const View v, con
 // after all of them: drop the old ones and put the staged tables in place.  Entries that stay the same are left alone.
 __global__ void __launch_bounds__(kRowThreads) fork_stage_kernel(const View v, const int *parent)
 {
+    ptx::wait_for_stream();
     const int r = blockIdx.x;
     int p = __ldg(parent + r);
     if (p >= v.rows) {
@@ -261,6 +265,7 @@ __global__ void __launch_bounds__(kRowThreads) fork_stage_kernel(const View v, c
 
 __global__ void __launch_bounds__(kRowThreads) fork_commit_kernel(const View v, const int *parent)
 {
+    ptx::wait_for_stream();
     const int r = blockIdx.x;
     const int p = __ldg(parent + r);
     const int *to = v.staged + static_cast<long long>(r) * (v.max_pages + 1);
@@ -283,6 +288,7 @@ __global__ void __launch_bounds__(kRowThreads) fork_commit_kernel(const View v, 
 // With n_live pages in use: the i-th lowest page in use at or above n_live moves to the i-th lowest free page below.
 __global__ void __launch_bounds__(kBlock, 1) compact_kernel(const View v)
 {
+    ptx::wait_for_stream();
     __shared__ unsigned long long slots[32];
     const int tid = threadIdx.x;
     unsigned long long mine = 0, n_free;
@@ -331,6 +337,7 @@ __global__ void __launch_bounds__(kBlock, 1) compact_kernel(const View v)
 // Tables after a compaction: pages from n_live on have moved.
 __global__ void __launch_bounds__(kRowThreads) rename_kernel(const View v)
 {
+    ptx::wait_for_stream();
     const int r = blockIdx.x;
     const int n_live = v.moves[2 * *v.n_moves];
     const int held = pages_of(v.lens[r], v.page_shift);
@@ -344,6 +351,7 @@ __global__ void __launch_bounds__(kRowThreads) rename_kernel(const View v)
 // Counts and free bits from tables and lengths.  Entries beyond a row's length become -1.
 __global__ void __launch_bounds__(kRowThreads) rebuild_count_kernel(const View v)
 {
+    ptx::wait_for_stream();
     const int r = blockIdx.x;
     int len = v.lens[r];
     if (len < 0 || len > static_cast<long long>(v.max_pages) << v.page_shift) {
@@ -370,6 +378,7 @@ __global__ void __launch_bounds__(kRowThreads) rebuild_count_kernel(const View v
 
 __global__ void __launch_bounds__(kRowThreads) rebuild_bits_kernel(const View v)
 {
+    ptx::wait_for_stream();
     const int p = blockIdx.x * kRowThreads + threadIdx.x;
     const unsigned int bits = __ballot_sync(kFull, p < v.n_pages && v.refs[p] == 0);
     if ((threadIdx.x & 31) == 0 && p / 32 < v.words) v.free_bits[p / 32] = bits;
@@ -385,6 +394,7 @@ struct CopyParams {
 // Page contents, all layers, keys and values: a warp moves up to 4 KiB at a time, eight 16-byte loads in flight per lane.
 __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const CopyParams p)
 {
+    ptx::wait_for_stream();
     const int lane = threadIdx.x & 31;
     const long long n = static_cast<long long>(*p.n_moves) * p.layers * 2 * p.pieces;
     const long long warps = static_cast<long long>(gridDim.x) * (kCopyThreads / 32);

@@ -8,6 +8,15 @@ namespace ptx {
 
 constexpr long long kWaitCycles = 4000000000ll;      // about two seconds
 
+// Programmatic launches: a kernel launched with that attribute may start while the one before it on the stream still runs; the
+// wait is the point from which everything before it is complete and visible.  A kernel that waits before its first access to
+// global memory can let its own successor in at once.
+__device__ __forceinline__ void wait_for_stream()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 __device__ __forceinline__ unsigned int smem_u32(const void *p) { return static_cast<unsigned int>(__cvta_generic_to_shared(p)); }
 
 __device__ __forceinline__ void mbar_init(unsigned int bar, unsigned int count)

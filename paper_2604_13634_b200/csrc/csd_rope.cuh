@@ -20,6 +20,7 @@
 #include <stdint.h>
 
 #include "../../include/csd.h"
+#include "csd_ptx.cuh"
 
 namespace csd {
 namespace rope {
@@ -120,6 +121,7 @@ struct RopeParams {
 template <typename T, int P, bool kHalf>
 __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams p)
 {
+    ptx::wait_for_stream();
     const long long at = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
     if (at >= p.threads) return;
     const long long tg = at / p.units;
@@ -175,6 +177,7 @@ struct AppendParams {
 template <typename T, int P, bool kHalf>
 __global__ void __launch_bounds__(kThreads) rope_append_kernel(const AppendParams p)
 {
+    ptx::wait_for_stream();
     const long long at = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
     if (at >= p.threads) return;
     const int groups = p.q_groups + 2 * p.kv_groups;
