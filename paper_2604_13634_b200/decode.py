@@ -11,7 +11,7 @@ from ctypes import POINTER, Structure, byref, c_double, c_float, c_int, c_int64,
 
 import torch
 
-from .binding import CSD_BF16, CSD_F16, CSD_F32, CSD_MAX_K, CsdError, _check, _ptr, _stream_ptr, lib
+from .binding import CSD_BF16, CSD_F16, CSD_F32, CsdError, _check, _ptr, lib
 
 CACHE_FULL, CACHE_ROW_FULL, CACHE_BAD_PAGE, CACHE_BAD_ROW, CACHE_INTERNAL = 1, 2, 4, 8, 16
 
@@ -55,6 +55,12 @@ SIGNATURES = {
     "csd_attention": (c_int, [c_void_p, *_strides3, c_int, c_int, POINTER(CacheStruct), c_int, c_float, c_void_p, c_void_p, c_void_p,
                               c_void_p, c_size_t, c_void_p]),
 }
+
+def _stream_ptr(stream, device) -> int:
+    """The stream asked for, or the device's current one (the raw handle: a Stream object costs 3 us to make, as much as the
+    call that it is made for)."""
+    return torch._C._cuda_getCurrentRawStream(device.index or 0) if stream is None else stream.cuda_stream
+
 
 _typed = None
 
@@ -109,7 +115,7 @@ def csd_rope(x, positions, plan: RopePlan, out=None, inverse: bool = False, stre
     assert tuple(positions.shape) in ((B, S), (S,))
     pb, ps = positions.stride() if positions.dim() == 2 else (0, positions.stride(0))
     rc = _lib().csd_rope(x.data_ptr(), out.data_ptr(), _DTYPES[x.dtype], B, S, H, D, *x.stride()[:3], *out.stride()[:3],
-                         positions.data_ptr(), pb, ps, byref(plan._struct), 1 if inverse else 0, _stream_ptr(stream))
+                         positions.data_ptr(), pb, ps, byref(plan._struct), 1 if inverse else 0, _stream_ptr(stream, x.device))
     _check(rc, "csd_rope")
     return out
 
@@ -194,32 +200,32 @@ def _rows_arg(t, cache: PagedCache, what: str):
 
 def csd_cache_rebuild(cache: PagedCache, stream=None):
     """Counts and free pages from cache.table and cache.lens; clears the flags."""
-    _check(_lib().csd_cache_rebuild(byref(cache._struct), _stream_ptr(stream)), "csd_cache_rebuild")
+    _check(_lib().csd_cache_rebuild(byref(cache._struct), _stream_ptr(stream, cache.k.device)), "csd_cache_rebuild")
 
 
 def csd_cache_extend(cache: PagedCache, T: int, n_new=None, stream=None):
     """Room for T (or n_new[row]) more tokens in every row; cache.granted says how many each row got (all rows or none)."""
-    _check(_lib().csd_cache_extend(byref(cache._struct), T, _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream)), "csd_cache_extend")
+    _check(_lib().csd_cache_extend(byref(cache._struct), T, _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, cache.k.device)), "csd_cache_extend")
 
 
 def csd_cache_truncate(cache: PagedCache, new_lens, stream=None):
     """Rows keep their first new_lens[row] tokens."""
-    _check(_lib().csd_cache_truncate(byref(cache._struct), _rows_arg(new_lens, cache, "new_lens"), _stream_ptr(stream)), "csd_cache_truncate")
+    _check(_lib().csd_cache_truncate(byref(cache._struct), _rows_arg(new_lens, cache, "new_lens"), _stream_ptr(stream, cache.k.device)), "csd_cache_truncate")
 
 
 def csd_cache_commit(cache: PagedCache, accept_len, stream=None):
     """After a verification step: of the last extension's tokens, the first accept_len[row] + 1 stay."""
-    _check(_lib().csd_cache_commit(byref(cache._struct), _rows_arg(accept_len, cache, "accept_len"), _stream_ptr(stream)), "csd_cache_commit")
+    _check(_lib().csd_cache_commit(byref(cache._struct), _rows_arg(accept_len, cache, "accept_len"), _stream_ptr(stream, cache.k.device)), "csd_cache_commit")
 
 
 def csd_cache_fork(cache: PagedCache, parent, stream=None):
     """Row b continues row parent[b]'s tokens (itself: unchanged; negative: empty), sharing its pages."""
-    _check(_lib().csd_cache_fork(byref(cache._struct), _rows_arg(parent, cache, "parent"), _stream_ptr(stream)), "csd_cache_fork")
+    _check(_lib().csd_cache_fork(byref(cache._struct), _rows_arg(parent, cache, "parent"), _stream_ptr(stream, cache.k.device)), "csd_cache_fork")
 
 
 def csd_cache_compact(cache: PagedCache, stream=None):
     """The pages in use become the lowest ones."""
-    _check(_lib().csd_cache_compact(byref(cache._struct), _stream_ptr(stream)), "csd_cache_compact")
+    _check(_lib().csd_cache_compact(byref(cache._struct), _stream_ptr(stream, cache.k.device)), "csd_cache_compact")
 
 
 def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | None, q_out=None, n_new=None, stream=None):
@@ -232,7 +238,7 @@ def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | Non
     assert q.stride(3) == k.stride(3) == v.stride(3) == 1 and tuple(q_out.shape) == (B, T, Hq, D) and q_out.is_contiguous()
     rc = _lib().csd_rope_append(q.data_ptr(), *q.stride()[:3], Hq, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3],
                                 q_out.data_ptr(), T, byref(cache._struct), layer, byref(plan._struct) if plan is not None else None,
-                                _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream))
+                                _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, cache.k.device))
     _check(rc, "csd_rope_append")
     return q_out
 
@@ -249,7 +255,7 @@ class AttentionBuffers:
         self.out = torch.empty(cache.rows, T, q_heads, cache.head_dim, dtype=cache.dtype, device=dev)
         self.lse = torch.empty(cache.rows, T, q_heads, dtype=torch.float32, device=dev)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
-        _check(lib().csd_workspace_init(_ptr(self.workspace), self.ws_bytes, _stream_ptr()), "csd_workspace_init")
+        _check(lib().csd_workspace_init(_ptr(self.workspace), self.ws_bytes, _stream_ptr(None, dev)), "csd_workspace_init")
 
 
 def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale: float | None = None, n_new=None, stream=None):
@@ -259,6 +265,6 @@ def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale
     scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else scale
     rc = _lib().csd_attention(q.data_ptr(), *q.stride()[:3], buf.T, buf.q_heads, byref(cache._struct), layer, c_float(scale),
                               _rows_arg(n_new, cache, "n_new"), buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(),
-                              buf.ws_bytes, _stream_ptr(stream))
+                              buf.ws_bytes, _stream_ptr(stream, cache.k.device))
     _check(rc, "csd_attention")
     return buf.out
