@@ -62,16 +62,25 @@ int units_of(int rot, int D)
     return rot / (2 * P) + (D - rot + 2 * P - 1) / (2 * P);
 }
 
+// Blocks of whole tokens where they fit, blocks of a token's threads where one takes more; false: too many.
+bool place_tokens(long long tokens, long long per_token, rope::Places &at, dim3 &grid)
+{
+    if (tokens > INT_MAX || per_token > (65535ll * rope::kThreads)) return false;
+    at.n_tokens = static_cast<int>(tokens);
+    at.per_token = static_cast<int>(per_token);
+    at.tokens = per_token >= rope::kThreads ? 1 : rope::kThreads / at.per_token;
+    grid = dim3(static_cast<unsigned int>((tokens + at.tokens - 1) / at.tokens),
+                at.tokens > 1 ? 1u : static_cast<unsigned int>((per_token + rope::kThreads - 1) / rope::kThreads));
+    return true;
+}
+
 template <typename T, int P>
 csd_status_t launch_rope(rope::RopeParams p, csd_rope_layout_t layout, cudaStream_t st)
 {
     p.units = units_of<P>(p.turn.rot, p.D);
-    p.groups = (p.H + rope::kHeads - 1) / rope::kHeads;
-    p.threads = static_cast<long long>(p.B) * p.S * p.groups * p.units;
-    const long long blocks = (p.threads + rope::kThreads - 1) / rope::kThreads;
-    if (blocks > INT_MAX) return CSD_ERR_UNSUPPORTED;
-    return launch(layout == CSD_ROPE_HALF ? rope::rope_kernel<T, P, true> : rope::rope_kernel<T, P, false>, dim3(static_cast<unsigned int>(blocks)),
-                  rope::kThreads, 0, st, p);
+    dim3 grid;
+    if (!place_tokens(static_cast<long long>(p.B) * p.S, static_cast<long long>((p.H + rope::kHeads - 1) / rope::kHeads) * p.units, p.at, grid)) return CSD_ERR_UNSUPPORTED;
+    return launch(layout == CSD_ROPE_HALF ? rope::rope_kernel<T, P, true> : rope::rope_kernel<T, P, false>, grid, rope::kThreads, 0, st, p);
 }
 
 template <typename T>
@@ -89,11 +98,9 @@ csd_status_t launch_append(rope::AppendParams p, csd_rope_layout_t layout, cudaS
     p.units = units_of<P>(p.turn.rot, p.D);
     p.q_groups = (p.Hq + rope::kHeads - 1) / rope::kHeads;
     p.kv_groups = (p.Hkv + rope::kHeads - 1) / rope::kHeads;
-    p.threads = static_cast<long long>(p.B) * p.T * (p.q_groups + 2 * p.kv_groups) * p.units;
-    const long long blocks = (p.threads + rope::kThreads - 1) / rope::kThreads;
-    if (blocks > INT_MAX) return CSD_ERR_UNSUPPORTED;
-    return launch(layout == CSD_ROPE_HALF ? rope::rope_append_kernel<T, P, true> : rope::rope_append_kernel<T, P, false>,
-                  dim3(static_cast<unsigned int>(blocks)), rope::kThreads, 0, st, p);
+    dim3 grid;
+    if (!place_tokens(static_cast<long long>(p.B) * p.T, static_cast<long long>(p.q_groups + 2 * p.kv_groups) * p.units, p.at, grid)) return CSD_ERR_UNSUPPORTED;
+    return launch(layout == CSD_ROPE_HALF ? rope::rope_append_kernel<T, P, true> : rope::rope_append_kernel<T, P, false>, grid, rope::kThreads, 0, st, p);
 }
 
 template <typename T>
@@ -469,6 +476,7 @@ csd_status_t csd_rope(const void *x, void *y, csd_dtype_t dtype, int B, int S, i
 {
     if (!rope || B < 0 || S < 0 || H < 0 || D <= 0 || !rope_ok(rope, D)) return CSD_ERR_INVALID_ARG;
     if (dtype != CSD_F32 && dtype != CSD_BF16 && dtype != CSD_F16) return CSD_ERR_INVALID_ARG;
+    if (rope->rot > rope::kMaxRot) return CSD_ERR_UNSUPPORTED;
     if (B == 0 || S == 0 || H == 0) return CSD_OK;
     if (!x || !y || !positions) return CSD_ERR_INVALID_ARG;
     host::other_work_enqueued();
