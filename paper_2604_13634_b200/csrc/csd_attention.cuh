@@ -1197,20 +1197,24 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         }
                     }
                     __syncwarp();
-                    // lanes_row lanes a row, 16 bytes each
+                    // `chunks` lanes a row, 16 bytes each
                     const int d = whole ? ch * 8 : pass * cols + ch * 4;
-#pragma unroll 4
-                    for (int w0 = 0; w0 < warp_rows; w0 += rows_at_once) {
-                        const int wr = w0 + sub;
-                        const long long to = __shfl_sync(kFull, whole ? row * p.D : static_cast<long long>(r) * p.part_stride, wr & 31);
-                        if (sub >= rows_at_once || wr >= warp_rows || d >= p.D) continue;
-                        const int r2 = 32 * warp + wr;
-                        uint4 v;
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(q_smem + r2 * pitch + ((ch ^ (r2 & 7)) << 4)) : "memory");
-                        if (whole)
-                            *reinterpret_cast<uint4 *>(static_cast<T *>(p.out) + to + d) = v;
-                        else
-                            __stcg(reinterpret_cast<uint4 *>(part + to + d), v);
+                    const bool mine = sub < rows_at_once && d < p.D;
+                    char *to = whole ? reinterpret_cast<char *>(static_cast<T *>(p.out) + d) : reinterpret_cast<char *>(part + (32 * warp) * p.part_stride + d);
+                    const long long row_bytes = whole ? row * p.D * static_cast<long long>(sizeof(T)) : static_cast<long long>(lane) * p.part_stride * 4;
+                    for (int w0 = 0; w0 < warp_rows; w0 += 4 * rows_at_once) {
+                        uint4 v[4];
+                        long long off[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int wr = w0 + k * rows_at_once + sub, r2 = 32 * warp + wr;
+                            off[k] = __shfl_sync(kFull, row_bytes, wr & 31);
+                            if (mine && wr < warp_rows)
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[k].x), "=r"(v[k].y), "=r"(v[k].z), "=r"(v[k].w) : "r"(q_smem + r2 * pitch + ((ch ^ (r2 & 7)) << 4)) : "memory");
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (mine && w0 + k * rows_at_once + sub < warp_rows) __stcg(reinterpret_cast<uint4 *>(to + off[k]), v[k]);
                     }
                     __syncwarp();
                 }
@@ -1231,12 +1235,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     if (*give_up && lane == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);
 }
 
-// Joins the parts of split units: block (x, y) four query rows of one of them.  The weights of all parts and rows first (a
-// thread per part and row), then each warp sums every fourth part, four rows side by side, so that a row of 40 parts costs a
-// few memory latencies and not forty; the four sums are added in order.
-constexpr int kJoinThreads = 128, kJoinRows = 4, kMaxGrid = 512;
+// Joins the parts of split units: block (x, y) kJoinRows query rows of one of them.  The weights of all parts and rows first (a
+// thread per part and row), then each warp sums every fourth part, the rows side by side, so that a row of 40 parts costs a
+// few memory latencies and not forty; the four sums are added in order.  Four rows to a block where there are many rows
+// (blocks are what costs then), one where there are few.
+constexpr int kJoinThreads = 128, kMaxGrid = 512;
 
-template <typename T, int DP>
+template <typename T, int DP, int kJoinRows>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Params p, int tile_rows)
 {
     __shared__ float2 part_ml[kMaxGrid][kJoinRows];                     // (m, l), then (weight, l)
@@ -1252,27 +1257,27 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Para
     if (here <= 0) return;
     const long long slot_floats = static_cast<long long>(tile_rows) * (DP + 2);
     auto slot = [&](int i) { return p.parts + slot_floats * (i == 0 ? 2 * sp.first + 1 : 2 * (sp.first + i)); };
-    const int row = tid & 3;
+    const int row = tid % kJoinRows;
     float M = -INFINITY, L = 0.f;
-    for (int i = tid >> 2; i < n; i += kJoinThreads / 4) {
+    for (int i = tid / kJoinRows; i < n; i += kJoinThreads / kJoinRows) {
         const float2 ml = row < here ? __ldcg(reinterpret_cast<const float2 *>(slot(i) + tile_rows * DP + 2 * (r0 + row))) : make_float2(-INFINITY, 0.f);
         part_ml[i][row] = ml;
         M = fmaxf(M, ml.x);
     }
 #pragma unroll
-    for (int d = 4; d < 32; d <<= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, d));
-    if (lane < 4) red[warp][row] = M;
+    for (int d = kJoinRows; d < 32; d <<= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, d));
+    if (lane < kJoinRows) red[warp][row] = M;
     __syncthreads();
     M = fmaxf(fmaxf(red[0][row], red[1][row]), fmaxf(red[2][row], red[3][row]));
-    for (int i = tid >> 2; i < n; i += kJoinThreads / 4) {
+    for (int i = tid / kJoinRows; i < n; i += kJoinThreads / kJoinRows) {
         const float2 ml = part_ml[i][row];
         const float w = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
         part_ml[i][row].x = w;
         L += w * ml.y;
     }
 #pragma unroll
-    for (int d = 4; d < 32; d <<= 1) L += __shfl_xor_sync(kFull, L, d);
-    if (lane < 4) sums[warp][row] = L;
+    for (int d = kJoinRows; d < 32; d <<= 1) L += __shfl_xor_sync(kFull, L, d);
+    if (lane < kJoinRows) sums[warp][row] = L;
     __syncthreads();
     constexpr int E = DP / 32;                                          // columns of a lane: 2, 4 or 8, side by side
     float o[kJoinRows][E];
@@ -1281,7 +1286,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Para
 #pragma unroll
         for (int e = 0; e < E; ++e) o[k][e] = 0.f;
     const bool mine = lane * E < p.D;
-#pragma unroll 4
+#pragma unroll (kJoinRows == 1 ? 8 : 4)
     for (int i = warp; i < n; i += 4) {
         const float *from = slot(i) + r0 * DP + lane * E;
 #pragma unroll

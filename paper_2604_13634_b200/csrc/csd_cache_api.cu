@@ -377,9 +377,11 @@ template <typename T, int DP>
 csd_status_t launch_join(const attention::Params &p, const AttentionPlan &a, cudaStream_t st)
 {
     const int most = a.rows < a.tile_rows ? a.rows : a.tile_rows;
-    const dim3 grid(static_cast<unsigned int>(p.by_unit ? p.B * p.Hkv * a.row_tiles : a.grid),
-                    static_cast<unsigned int>((most + attention::kJoinRows - 1) / attention::kJoinRows));
-    return launch(attention::attention_join_kernel<T, DP>, grid, attention::kJoinThreads, 0, st, p, a.tile_rows);
+    const unsigned int units = static_cast<unsigned int>(p.by_unit ? p.B * p.Hkv * a.row_tiles : a.grid);
+    // a block per row while all of them are on the GPU at once
+    if (static_cast<long long>(units) * most <= host::multiprocessors() * 8ll)
+        return launch(attention::attention_join_kernel<T, DP, 1>, dim3(units, static_cast<unsigned int>(most)), attention::kJoinThreads, 0, st, p, a.tile_rows);
+    return launch(attention::attention_join_kernel<T, DP, 4>, dim3(units, static_cast<unsigned int>((most + 3) / 4)), attention::kJoinThreads, 0, st, p, a.tile_rows);
 }
 
 template <typename C>
