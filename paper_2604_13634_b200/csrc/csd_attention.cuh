@@ -405,6 +405,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             int it = 0;
             bool ok = true;
             while (more && ok) {
+                if (lane == 0) note_split(p, share, r);
                 const bool follows = runs.next(rn);
                 const int len_next = follows ? row_len(p, rn.b) : 0;
                 for (int i = 0; i < r.ns && ok; ++i, ++it) {
@@ -796,7 +797,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                             if (qd == 0) __stcg(reinterpret_cast<float2 *>(part + C::kRows * DP + 2 * r), make_float2(m[mt][hh], L));
                         }
                     }
-                if (tid == 0) note_split(p, share, run);
             }
             if constexpr (KG == 1) consumer_barrier(cthreads);          // the query rows in shared memory are done with
         }
@@ -942,6 +942,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         int len = more ? row_len(p, r.b) : 0;
         int id = more ? tile_page<kTcTile>(p, r.b, r.j0, len, lane, per_tile) : -1;      // fetched a tile ahead
         while (more && ok) {
+            if (lane == 0) note_split(p, share, r);
             const bool follows = runs.next(rn);
             const int len_next = follows ? row_len(p, rn.b) : 0;
             int before = -1;
@@ -1225,7 +1226,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         p.lse[row] = seen ? (m + log2f(l)) * kLn2 : -INFINITY;
                 }
             }
-            if (tid == 0) note_split(p, share, ru);
             items += 2 * ns;
         }
         ptx::tc_fence_before();

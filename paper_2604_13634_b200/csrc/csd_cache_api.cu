@@ -256,7 +256,7 @@ AttentionPlan attention_plan(int rows, int B)
     a.dp = C::DP;
     a.row_tiles = (rows + C::kRows - 1) / C::kRows;
     a.grid = attention_grid(C::kBlocksPerSm);
-    a.run_cost = C::DP == 64 ? 3 : 2;      // measured: 2 to 3 of 64-element tiles, no difference from 1 to 3 beyond
+    a.run_cost = 2;      // measured: 2 to 3 of 64-element tiles, no difference from 1 to 3 beyond
     const int limit = kSmemPerSm / C::kBlocksPerSm - kSmemReserved - kSmemStatic;
     const int fixed = 1024 + C::kQBytes + C::kMlBytes + (B + 1) * 4;
     a.stages = (limit - fixed) / C::kStageBytes;
@@ -272,7 +272,7 @@ template <typename T, typename F>
 auto with_config(int dim, F f)
 {
     using attention::Config;
-    if (dim <= 64) return f(Config<T, 64, 1, 1, 4, 1, 2>());
+    if (dim <= 64) return f(Config<T, 64, 1, 2, 4, 1, 2>());
     if (dim <= 128) return f(Config<T, 128, 1, 1, 4, 1, 2>());
     return f(Config<T, 256, 1, 1, 4, 1, 1>());
 }

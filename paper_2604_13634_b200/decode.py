@@ -5,8 +5,6 @@ Like binding.py: argument marshalling only, one function per entry point of incl
 
 from __future__ import annotations
 
-import ctypes
-import math
 from ctypes import POINTER, Structure, byref, c_double, c_float, c_int, c_int64, c_size_t, c_uint64, c_void_p
 
 import torch
@@ -56,10 +54,10 @@ SIGNATURES = {
                               c_void_p, c_size_t, c_void_p]),
 }
 
-def _stream_ptr(stream, device) -> int:
+def _stream_ptr(stream, device: int) -> int:
     """The stream asked for, or the device's current one (the raw handle: a Stream object costs 3 us to make, as much as the
     call that it is made for)."""
-    return torch._C._cuda_getCurrentRawStream(device.index or 0) if stream is None else stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 _typed = None
@@ -101,22 +99,29 @@ class RopePlan:
         self.rot, self.layout = rot, layout
         self.steps = steps.to(device)
         self._struct = RopeStruct(self.steps.data_ptr(), rot, _LAYOUTS[layout], self.magnitude)
+        self._ref = byref(self._struct)
 
 
 def csd_rope(x, positions, plan: RopePlan, out=None, inverse: bool = False, stream=None):
     """x [B, S, H, D] turned by positions [B, S] int32 (or [S], shared by the batch); `inverse` turns back, which is the
     gradient.  `out` may be x itself.  Returns out."""
-    assert x.is_cuda and x.dim() == 4 and x.stride(3) == 1 and positions.is_cuda and positions.dtype == torch.int32
-    if x.dtype not in _DTYPES:
+    code = _DTYPES.get(x.dtype)
+    if code is None:
         raise CsdError(f"x must be float32, bfloat16 or float16, got {x.dtype}")
     out = torch.empty_like(x) if out is None else out
-    B, S, H, D = x.shape
-    assert out.shape == x.shape and out.dtype == x.dtype and out.stride(3) == 1 and out.is_cuda
-    assert tuple(positions.shape) in ((B, S), (S,))
-    pb, ps = positions.stride() if positions.dim() == 2 else (0, positions.stride(0))
-    rc = _lib().csd_rope(x.data_ptr(), out.data_ptr(), _DTYPES[x.dtype], B, S, H, D, *x.stride()[:3], *out.stride()[:3],
-                         positions.data_ptr(), pb, ps, byref(plan._struct), 1 if inverse else 0, _stream_ptr(stream, x.device))
-    _check(rc, "csd_rope")
+    B, S, H, D = shape = x.shape
+    xs, ys, ps = x.stride(), out.stride(), positions.stride()
+    assert x.is_cuda and positions.is_cuda and positions.dtype == torch.int32 and xs[3] == 1
+    assert out.shape == shape and out.dtype == x.dtype and ys[3] == 1 and out.is_cuda
+    if len(ps) == 1:
+        assert positions.shape[0] == S
+        ps = (0, ps[0])
+    else:
+        assert positions.shape == (B, S)
+    rc = _lib().csd_rope(x.data_ptr(), out.data_ptr(), code, B, S, H, D, xs[0], xs[1], xs[2], ys[0], ys[1], ys[2], positions.data_ptr(),
+                         ps[0], ps[1], plan._ref, 1 if inverse else 0, _stream_ptr(stream, x.get_device()))
+    if rc:
+        _check(rc, "csd_rope")
     return out
 
 
@@ -168,6 +173,8 @@ class PagedCache:
             st[1] = kv_heads * page_size * head_dim
         self._struct = CacheStruct(k.data_ptr(), v.data_ptr(), _DTYPES[dtype], layers, n_pages, page_size, kv_heads, head_dim, st[0],
                                    st[1], st[2], st[3], rows, self.max_pages, self.meta.data_ptr(), self.scratch.data_ptr())
+        self._ref = byref(self._struct)
+        self._device = dev.index if dev.index is not None else torch.cuda.current_device()
         csd_cache_rebuild(self)
 
     def load(self, table: torch.Tensor, lens: torch.Tensor, stream=None):
@@ -194,52 +201,55 @@ class PagedCache:
 def _rows_arg(t, cache: PagedCache, what: str):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == (cache.rows,), what
+    assert t.is_cuda and t.dtype == torch.int32 and t.shape == (cache.rows,) and t.is_contiguous(), what
     return t.data_ptr()
 
 
 def csd_cache_rebuild(cache: PagedCache, stream=None):
     """Counts and free pages from cache.table and cache.lens; clears the flags."""
-    _check(_lib().csd_cache_rebuild(byref(cache._struct), _stream_ptr(stream, cache.k.device)), "csd_cache_rebuild")
+    _check(_lib().csd_cache_rebuild(cache._ref, _stream_ptr(stream, cache._device)), "csd_cache_rebuild")
 
 
 def csd_cache_extend(cache: PagedCache, T: int, n_new=None, stream=None):
     """Room for T (or n_new[row]) more tokens in every row; cache.granted says how many each row got (all rows or none)."""
-    _check(_lib().csd_cache_extend(byref(cache._struct), T, _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, cache.k.device)), "csd_cache_extend")
+    _check(_lib().csd_cache_extend(cache._ref, T, _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, cache._device)), "csd_cache_extend")
 
 
 def csd_cache_truncate(cache: PagedCache, new_lens, stream=None):
     """Rows keep their first new_lens[row] tokens."""
-    _check(_lib().csd_cache_truncate(byref(cache._struct), _rows_arg(new_lens, cache, "new_lens"), _stream_ptr(stream, cache.k.device)), "csd_cache_truncate")
+    _check(_lib().csd_cache_truncate(cache._ref, _rows_arg(new_lens, cache, "new_lens"), _stream_ptr(stream, cache._device)), "csd_cache_truncate")
 
 
 def csd_cache_commit(cache: PagedCache, accept_len, stream=None):
     """After a verification step: of the last extension's tokens, the first accept_len[row] + 1 stay."""
-    _check(_lib().csd_cache_commit(byref(cache._struct), _rows_arg(accept_len, cache, "accept_len"), _stream_ptr(stream, cache.k.device)), "csd_cache_commit")
+    _check(_lib().csd_cache_commit(cache._ref, _rows_arg(accept_len, cache, "accept_len"), _stream_ptr(stream, cache._device)), "csd_cache_commit")
 
 
 def csd_cache_fork(cache: PagedCache, parent, stream=None):
     """Row b continues row parent[b]'s tokens (itself: unchanged; negative: empty), sharing its pages."""
-    _check(_lib().csd_cache_fork(byref(cache._struct), _rows_arg(parent, cache, "parent"), _stream_ptr(stream, cache.k.device)), "csd_cache_fork")
+    _check(_lib().csd_cache_fork(cache._ref, _rows_arg(parent, cache, "parent"), _stream_ptr(stream, cache._device)), "csd_cache_fork")
 
 
 def csd_cache_compact(cache: PagedCache, stream=None):
     """The pages in use become the lowest ones."""
-    _check(_lib().csd_cache_compact(byref(cache._struct), _stream_ptr(stream, cache.k.device)), "csd_cache_compact")
+    _check(_lib().csd_cache_compact(cache._ref, _stream_ptr(stream, cache._device)), "csd_cache_compact")
 
 
 def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | None, q_out=None, n_new=None, stream=None):
     """The new tokens of a layer: q [rows, T, q_heads, D] turned into q_out (dense; returned), k turned and v as it is into
     their page slots.  plan None: no rotation."""
-    B, T, Hq, D = q.shape
-    q_out = torch.empty((B, T, Hq, D), dtype=q.dtype, device=q.device) if q_out is None else q_out
+    B, T, Hq, D = shape = q.shape
+    if q_out is None:
+        q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
     assert q.is_cuda and k.is_cuda and v.is_cuda and q.dtype == k.dtype == v.dtype == q_out.dtype == cache.dtype
-    assert B == cache.rows and D == cache.head_dim and tuple(k.shape) == tuple(v.shape) == (B, T, cache.kv_heads, D)
-    assert q.stride(3) == k.stride(3) == v.stride(3) == 1 and tuple(q_out.shape) == (B, T, Hq, D) and q_out.is_contiguous()
-    rc = _lib().csd_rope_append(q.data_ptr(), *q.stride()[:3], Hq, k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3],
-                                q_out.data_ptr(), T, byref(cache._struct), layer, byref(plan._struct) if plan is not None else None,
-                                _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, cache.k.device))
-    _check(rc, "csd_rope_append")
+    assert B == cache.rows and D == cache.head_dim and k.shape == v.shape == (B, T, cache.kv_heads, D)
+    assert qs[3] == ks[3] == vs[3] == 1 and q_out.shape == shape and q_out.is_cuda and q_out.is_contiguous()
+    rc = _lib().csd_rope_append(q.data_ptr(), qs[0], qs[1], qs[2], Hq, k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1], vs[2],
+                                q_out.data_ptr(), T, cache._ref, layer, None if plan is None else plan._ref,
+                                None if n_new is None else _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, cache._device))
+    if rc:
+        _check(rc, "csd_rope_append")
     return q_out
 
 
@@ -255,16 +265,17 @@ class AttentionBuffers:
         self.out = torch.empty(cache.rows, T, q_heads, cache.head_dim, dtype=cache.dtype, device=dev)
         self.lse = torch.empty(cache.rows, T, q_heads, dtype=torch.float32, device=dev)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
-        _check(lib().csd_workspace_init(_ptr(self.workspace), self.ws_bytes, _stream_ptr(None, dev)), "csd_workspace_init")
+        _check(lib().csd_workspace_init(_ptr(self.workspace), self.ws_bytes, _stream_ptr(None, cache._device)), "csd_workspace_init")
 
 
 def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale: float | None = None, n_new=None, stream=None):
     """buf.out, buf.lse: attention of the T newest tokens of every row, q [rows, T, q_heads, D], over its cache."""
-    assert q.is_cuda and q.dtype == cache.dtype and q.stride(3) == 1
-    assert tuple(q.shape) == (cache.rows, buf.T, buf.q_heads, cache.head_dim)
-    scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else scale
-    rc = _lib().csd_attention(q.data_ptr(), *q.stride()[:3], buf.T, buf.q_heads, byref(cache._struct), layer, c_float(scale),
-                              _rows_arg(n_new, cache, "n_new"), buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(),
-                              buf.ws_bytes, _stream_ptr(stream, cache.k.device))
-    _check(rc, "csd_attention")
+    qs = q.stride()
+    assert q.is_cuda and q.dtype == cache.dtype and qs[3] == 1 and q.shape == buf.out.shape
+    assert q.shape[0] == cache.rows and q.shape[3] == cache.head_dim
+    rc = _lib().csd_attention(q.data_ptr(), qs[0], qs[1], qs[2], buf.T, buf.q_heads, cache._ref, layer,
+                              cache.head_dim ** -0.5 if scale is None else scale, None if n_new is None else _rows_arg(n_new, cache, "n_new"),
+                              buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(), buf.ws_bytes, _stream_ptr(stream, cache._device))
+    if rc:
+        _check(rc, "csd_attention")
     return buf.out
