@@ -74,31 +74,48 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
 //   take a copy of the same page) > 1; the last of them keeps the page.
 __global__ void __launch_bounds__(kBlock, 1) extend_kernel(const View v, const int *n_new, int uniform)
 {
-    ptx::wait_for_stream();
-    __shared__ __align__(16) int tail[kMaxRows];     // the shared last page a row would have to copy, or -1
+    constexpr int kRowsEach = kMaxRows / kBlock;     // rows of a thread: consecutive, so that scans follow the rows
+    constexpr int kListed = 4096;                    // pages handed out that stay in shared memory; a longer list goes to scratch
+    __shared__ __align__(16) int tail[kMaxRows];     // the shared last page a row would have to copy, or -1; later: its first page in the list
     __shared__ unsigned long long slots[32];
+    __shared__ int short_list[kListed];
     __shared__ int bad;
+    ptx::wait_for_stream();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (v.rows + kBlock - 1) / kBlock;  // rows of a thread: consecutive, so that scans follow the rows
-    const int r0 = tid * per, r1 = min(v.rows, r0 + per);
+    const int per = (v.rows + kBlock - 1) / kBlock, r0 = tid * per;
+    // everything that is needed and does not depend on anything, at once
+    const unsigned int first_bits = tid < v.words ? v.free_bits[tid] : 0u;
+    int len[kRowsEach], n[kRowsEach], page[kRowsEach];
+#pragma unroll
+    for (int k = 0; k < kRowsEach; ++k) {
+        const bool there = k < per && r0 + k < v.rows;
+        len[k] = there ? v.lens[r0 + k] : 0;
+        n[k] = there ? max(n_new ? __ldg(n_new + r0 + k) : uniform, 0) : 0;
+    }
     if (tid == 0) bad = 0;
     for (int r = tid; r < ((v.rows + 3) & ~3); r += kBlock) tail[r] = -1;
     __syncthreads();
     unsigned int complaint = 0;
-    for (int r = r0; r < r1; ++r) {
-        const int len = v.lens[r], n = max(n_new ? __ldg(n_new + r) : uniform, 0);
-        if (n == 0) continue;
-        if (static_cast<long long>(len) + n > (static_cast<long long>(v.max_pages) << v.page_shift)) {
+#pragma unroll
+    for (int k = 0; k < kRowsEach; ++k) {
+        page[k] = -1;
+        if (n[k] == 0) continue;
+        if (static_cast<long long>(len[k]) + n[k] > (static_cast<long long>(v.max_pages) << v.page_shift))
             complaint |= CSD_CACHE_ROW_FULL;
+        else if (len[k] & (v.page_size - 1))
+            page[k] = v.table[static_cast<long long>(r0 + k) * v.max_pages + (len[k] >> v.page_shift)];
+    }
+    int users[kRowsEach];
+#pragma unroll
+    for (int k = 0; k < kRowsEach; ++k) {
+        users[k] = 0;
+        if (n[k] == 0 || !(len[k] & (v.page_size - 1)) || (complaint & CSD_CACHE_ROW_FULL)) continue;
+        if (page[k] < 0 || page[k] >= v.n_pages) {
+            complaint |= CSD_CACHE_BAD_PAGE;
             continue;
         }
-        if (len & (v.page_size - 1)) {
-            const int page = v.table[static_cast<long long>(r) * v.max_pages + (len >> v.page_shift)];
-            if (page < 0 || page >= v.n_pages)
-                complaint |= CSD_CACHE_BAD_PAGE;
-            else if (v.refs[page] > 1)
-                tail[r] = page;
-        }
+        users[k] = v.refs[page[k]];
+        if (users[k] > 1) tail[r0 + k] = page[k];
     }
     if (complaint) {
         atomicOr(v.flags, complaint);
@@ -106,48 +123,49 @@ __global__ void __launch_bounds__(kBlock, 1) extend_kernel(const View v, const i
     }
     __syncthreads();
     const bool refuse_shape = bad != 0;
-    // rows with a shared last page: how many before it have the same one
     unsigned long long mine = 0;                     // pages wanted | page copies << 32
-    unsigned int copied = 0;                         // bit k: row r0 + k copies (per <= 4)
-    for (int r = r0; r < r1; ++r) {
-        const int len = v.lens[r], n = max(n_new ? __ldg(n_new + r) : uniform, 0);
-        if (n == 0 || refuse_shape) continue;
-        int need = pages_of(len + n, v.page_shift) - pages_of(len, v.page_shift);
-        const int page = tail[r];
-        if (page >= 0) {
+    int need[kRowsEach];
+    unsigned int copied = 0;                         // bit k: row r0 + k copies
+#pragma unroll
+    for (int k = 0; k < kRowsEach; ++k) {
+        need[k] = 0;
+        if (n[k] == 0 || refuse_shape) continue;
+        const int r = r0 + k;
+        need[k] = pages_of(len[k] + n[k], v.page_shift) - pages_of(len[k], v.page_shift);
+        if (users[k] > 1) {                          // how many rows before it have the same last page
             int before = 0;
             const int4 *t4 = reinterpret_cast<const int4 *>(tail);
             for (int j = 0; j < (r >> 2); ++j) {
                 const int4 q = t4[j];
-                before += (q.x == page) + (q.y == page) + (q.z == page) + (q.w == page);
+                before += (q.x == page[k]) + (q.y == page[k]) + (q.z == page[k]) + (q.w == page[k]);
             }
-            for (int j = r & ~3; j < r; ++j) before += tail[j] == page;
-            if (v.refs[page] - before > 1) {
-                copied |= 1u << (r - r0);
-                ++need;
-                mine += 1ull << 32;
+            for (int j = r & ~3; j < r; ++j) before += tail[j] == page[k];
+            if (users[k] - before > 1) {
+                copied |= 1u << k;
+                mine += 1ull + (1ull << 32);
             }
         }
-        mine += static_cast<unsigned int>(need);
+        mine += static_cast<unsigned int>(need[k]);
     }
     unsigned long long total2;
     const unsigned long long first2 = block_scan(mine, slots, total2);
     const int total = static_cast<int>(total2 & 0xffffffffu), total_moves = static_cast<int>(total2 >> 32);
+    int *list = total <= kListed ? short_list : v.list;
     // the `total` lowest free pages, in order
     int found = 0;
     for (int w0 = 0; w0 < v.words && found < total; w0 += kBlock) {
         const int w = w0 + tid;
-        unsigned int bits = w < v.words ? v.free_bits[w] : 0u;
+        unsigned int bits = w0 == 0 ? first_bits : (w < v.words ? v.free_bits[w] : 0u);
         unsigned long long sum;
         int at = found + static_cast<int>(block_scan(static_cast<unsigned long long>(__popc(bits)), slots, sum));
         while (bits && at < total) {
-            v.list[at++] = w * 32 + __ffs(bits) - 1;
+            list[at++] = w * 32 + __ffs(bits) - 1;
             bits &= bits - 1;
         }
         found += static_cast<int>(sum);
     }
     const bool refuse = refuse_shape || found < total;
-    __syncthreads();                                 // list is complete; tail has been read
+    __syncthreads();                                 // the list is complete; tail has been read
     if (refuse) {
         if (tid == 0) {
             if (!refuse_shape) atomicOr(v.flags, CSD_CACHE_FULL);
@@ -156,46 +174,43 @@ __global__ void __launch_bounds__(kBlock, 1) extend_kernel(const View v, const i
         for (int r = tid; r < v.rows; r += kBlock) v.granted[r] = 0;
         return;
     }
-    // where a row's pages begin in the list goes into `tail`, with the copy marked in the sign
     {
         int at = static_cast<int>(first2 & 0xffffffffu), mv = static_cast<int>(first2 >> 32);
-        for (int r = r0; r < r1; ++r) {
-            const int len = v.lens[r], n = max(n_new ? __ldg(n_new + r) : uniform, 0);
-            const bool c = (copied >> (r - r0)) & 1u;
-            tail[r] = c ? ~at : at;
-            if (c) {
-                const long long e = static_cast<long long>(r) * v.max_pages + (len >> v.page_shift);
-                const int src = v.table[e], dst = v.list[at];
-                v.moves[2 * mv] = src;
+#pragma unroll
+        for (int k = 0; k < kRowsEach; ++k) {
+            if (k >= per || r0 + k >= v.rows) continue;
+            const int r = r0 + k;
+            if ((copied >> k) & 1u) {
+                const int dst = list[at++];
+                v.moves[2 * mv] = page[k];
                 v.moves[2 * mv + 1] = dst;
                 ++mv;
-                v.table[e] = dst;
-                atomicSub(v.refs + src, 1);
-                ++at;
+                v.table[static_cast<long long>(r) * v.max_pages + (len[k] >> v.page_shift)] = dst;
+                atomicSub(v.refs + page[k], 1);
             }
-            if (n > 0) at += pages_of(len + n, v.page_shift) - pages_of(len, v.page_shift);
+            v.lens[r] = len[k] + n[k];
+            v.granted[r] = n[k];
+            tail[r] = at;
+            at += need[k];
+            // a few new pages: here; more: a warp per row, below
+            if (need[k] <= 2)
+                for (int j = 0; j < need[k]; ++j) v.table[static_cast<long long>(r) * v.max_pages + pages_of(len[k], v.page_shift) + j] = list[at - need[k] + j];
         }
     }
     if (tid == 0) *v.n_moves = total_moves;
     for (int j = tid; j < total; j += kBlock) {
-        const int page = v.list[j];
-        v.refs[page] = 1;
-        atomicAnd(v.free_bits + (page >> 5), ~(1u << (page & 31)));
+        const int p = list[j];
+        v.refs[p] = 1;
+        atomicAnd(v.free_bits + (p >> 5), ~(1u << (p & 31)));
     }
-    __syncthreads();
-    // a warp per row: the new entries of its table, its length
+    bool many = false;
+#pragma unroll
+    for (int k = 0; k < kRowsEach; ++k) many |= need[k] > 2;
+    if (__syncthreads_or(many ? 1 : 0) == 0) return;
     for (int r = warp; r < v.rows; r += kBlock / 32) {
-        const int len = v.lens[r], n = max(n_new ? __ldg(n_new + r) : uniform, 0);
-        if (n > 0) {
-            const int at = tail[r] < 0 ? ~tail[r] + 1 : tail[r];
-            const int held = pages_of(len, v.page_shift), more = pages_of(len + n, v.page_shift) - held;
-            for (int j = lane; j < more; j += 32) v.table[static_cast<long long>(r) * v.max_pages + held + j] = v.list[at + j];
-        }
-        __syncwarp();
-        if (lane == 0) {
-            v.lens[r] = len + n;
-            v.granted[r] = n;
-        }
+        const int more_to = v.granted[r], now = v.lens[r], held = pages_of(now - more_to, v.page_shift), more = pages_of(now, v.page_shift) - held;
+        if (more <= 2) continue;
+        for (int j = lane; j < more; j += 32) v.table[static_cast<long long>(r) * v.max_pages + held + j] = list[tail[r] + j];
     }
 }
 
