@@ -223,12 +223,13 @@ csd_status_t copy_pages(const csd_cache_t *c, const pages::View &v, long long mo
     p.pieces = (p.page_bytes + pages::kCopyBytes - 1) / pages::kCopyBytes;
     p.n_moves = v.n_moves;
     p.moves = v.moves;
-    const long long items = most * p.layers * 2 * p.pieces, per_block = pages::kCopyThreads / 32;
-    long long blocks = (items + per_block - 1) / per_block;
-    const long long cap = static_cast<long long>(host::multiprocessors()) * 8;
+    if (most * p.pieces > INT_MAX || p.layers > 32767) return CSD_ERR_UNSUPPORTED;
+    const long long per_block = pages::kCopyThreads / 32, planes = 2ll * p.layers;
+    long long blocks = (most * p.pieces + per_block - 1) / per_block;
+    const long long cap = (static_cast<long long>(host::multiprocessors()) * 8 + planes - 1) / planes;
     if (blocks > cap) blocks = cap;
     if (blocks < 1) return CSD_OK;
-    return launch(pages::pages_copy_kernel, dim3(static_cast<unsigned int>(blocks)), pages::kCopyThreads, 0, st, p);
+    return launch(pages::pages_copy_kernel, dim3(static_cast<unsigned int>(blocks), static_cast<unsigned int>(planes)), pages::kCopyThreads, 0, st, p);
 }
 
 // ---- attention ----------------------------------------------------------------------------------

@@ -406,32 +406,29 @@ struct CopyParams {
     const int *n_moves, *moves;
 };
 
-// Page contents, all layers, keys and values: a warp moves up to 4 KiB at a time, eight 16-byte loads in flight per lane.
+// Page contents: grid.y is a layer's keys or values.  A warp moves up to 4 KiB at a time, eight 16-byte loads in flight per
+// lane, neighbouring warps neighbouring pieces of a page.
 __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const CopyParams p)
 {
     ptx::wait_for_stream();
     const int lane = threadIdx.x & 31;
-    const long long n = static_cast<long long>(*p.n_moves) * p.layers * 2 * p.pieces;
-    const long long warps = static_cast<long long>(gridDim.x) * (kCopyThreads / 32);
-    for (long long it = static_cast<long long>(blockIdx.x) * (kCopyThreads / 32) + (threadIdx.x >> 5); it < n; it += warps) {
-        const int piece = static_cast<int>(it % p.pieces);
-        long long rest = it / p.pieces;
-        char *pool = (rest & 1) ? p.v : p.k;
-        rest >>= 1;
-        const int layer = static_cast<int>(rest % p.layers);
-        const int move = static_cast<int>(rest / p.layers);
-        const int src = __ldg(p.moves + 2 * move), dst = __ldg(p.moves + 2 * move + 1);
-        char *base = pool + layer * p.layer_bytes + static_cast<long long>(piece) * kCopyBytes;
-        const char *from = base + src * p.page_stride_bytes;
-        char *to = base + dst * p.page_stride_bytes;
-        const int left = p.page_bytes - piece * kCopyBytes;
+    const int n = *p.n_moves * p.pieces;             // (the host has seen to it that this fits)
+    char *pool = ((blockIdx.y & 1) ? p.v : p.k) + static_cast<long long>(blockIdx.y >> 1) * p.layer_bytes + lane * 16;
+    const int warps = gridDim.x * (kCopyThreads / 32);
+    for (int it = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); it < n; it += warps) {
+        const int move = it / p.pieces, piece = it - move * p.pieces;
+        const int2 m = __ldg(reinterpret_cast<const int2 *>(p.moves) + move);
+        char *base = pool + static_cast<long long>(piece) * kCopyBytes;
+        const char *from = base + m.x * p.page_stride_bytes;
+        char *to = base + m.y * p.page_stride_bytes;
+        const int left = p.page_bytes - piece * kCopyBytes - lane * 16;
         uint4 x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (lane * 16 + j * 512 < left) x[j] = ld_stream16(from + lane * 16 + j * 512);
+            if (j * 512 < left) x[j] = ld_stream16(from + j * 512);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (lane * 16 + j * 512 < left) *reinterpret_cast<uint4 *>(to + lane * 16 + j * 512) = x[j];
+            if (j * 512 < left) __stcs(reinterpret_cast<uint4 *>(to + j * 512), x[j]);
     }
 }
 
