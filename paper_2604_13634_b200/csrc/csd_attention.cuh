@@ -74,9 +74,9 @@ struct Params {
     float *parts;                          // [2 gridDim.x] slots of kRows * (DP + 2) floats
     // the tensor-memory kernel alone
     int tile_rows;                         // query rows of a row tile: a multiple of 8, at most 128
+    int q_buffers;                         // sets of query rows: 2, or 1 where they would leave too few slots
     int halves, d16;                       // 64-element columns of a tile; dim rounded up to 16
     int part_stride;                       // floats between rows of a part
-    unsigned int tmem_cols;
     const void *k_pool, *v_pool;           // of this layer
     long long pool_page, pool_head, pool_token;
 };
@@ -175,6 +175,19 @@ __device__ __forceinline__ unsigned int finite_only(unsigned int two)
 }
 
 __device__ __forceinline__ void consumer_barrier(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+
+// A place in a ring of slots that are taken in order: the slot, and the parity of the round.
+struct Cursor {
+    int slot;
+    unsigned int round;
+    __device__ __forceinline__ void next(int slots)
+    {
+        if (++slot == slots) {
+            slot = 0;
+            round ^= 1u;
+        }
+    }
+};
 
 // The split.  A unit of n tiles counts n + run_cost positions, the first run_cost of them empty: what its beginning and its end
 // cost a block.  The positions of all units are split evenly over the blocks; a block's share [x, x1) is a few runs of tiles.
@@ -402,20 +415,20 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             int len = more ? row_len(p, r.b) : 0;
             // page ids are fetched a tile ahead
             int id = more ? tile_page<kTile>(p, r.b, r.j0, len, lane, per_tile) : -1;
-            int it = 0;
+            Cursor at_ring = {0, 0u};
             bool ok = true;
             while (more && ok) {
                 if (lane == 0) note_split(p, share, r);
                 const bool follows = runs.next(rn);
                 const int len_next = follows ? row_len(p, rn.b) : 0;
-                for (int i = 0; i < r.ns && ok; ++i, ++it) {
+                for (int i = 0; i < r.ns && ok; ++i) {
                     const int page = id, j = r.j0 + i;
                     id = i + 1 < r.ns ? tile_page<kTile>(p, r.b, j + 1, len, lane, per_tile)
                                       : (follows ? tile_page<kTile>(p, rn.b, rn.j0, len_next, lane, per_tile) : -1);
-                    const int s = it % p.n_stages;
+                    const int s = at_ring.slot;
                     const unsigned int there = __ballot_sync(kFull, page >= 0);
                     if (lane == 0) {
-                        ok = mbar_wait(empty(s), ((it / p.n_stages) & 1) ^ 1, give_up);
+                        ok = mbar_wait(empty(s), at_ring.round ^ 1u, give_up);
                         if (ok) {
                             const unsigned int bytes = static_cast<unsigned int>(__popc(there)) * box_bytes * C::kHalves;
                             mbar_expect_tx(full_k(s), bytes);
@@ -432,17 +445,18 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                         for (int hf = 0; hf < C::kHalves; ++hf)
                             tma_load_page(at + C::kTileBytes + hf * (kTile * 128), &map_v, full_v(s), hf * 64, in_page, r.h, page);
                     }
+                    at_ring.next(p.n_stages);
                 }
                 if (ok) {                                            // the consumers join through the next stage
-                    const int sj = it % p.n_stages;
+                    const int sj = at_ring.slot;
                     if (lane == 0) {
-                        ok = mbar_wait(empty(sj), ((it / p.n_stages) & 1) ^ 1, give_up);
+                        ok = mbar_wait(empty(sj), at_ring.round ^ 1u, give_up);
                         if (ok) {
                             mbar_arrive(full_k(sj));
                             mbar_arrive(full_v(sj));
                         }
                     }
-                    ++it;
+                    at_ring.next(p.n_stages);
                     ok = __shfl_sync(kFull, ok ? 1 : 0, 0) != 0;
                 }
                 r = rn;
@@ -460,7 +474,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         Runs runs;
         runs.begin(p, base, share.x0, share.x1);
         Run run;
-        int it = 0;
+        Cursor at_ring = {0, 0u};
         const int swz = lane & 7;
         const unsigned int k_lane = (16 * NK * kg + ((lane >> 4) << 3) + swz) * 128u, k_chunk = (lane >> 3) & 1;
         const unsigned int v_lane = (16 * NK * kg + (((lane >> 3) & 1) << 3) + swz) * 128u, v_chunk = lane >> 4;
@@ -509,9 +523,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 l[mt][0] = l[mt][1] = 0.f;
             }
 
-            for (int j = j0; j < j1; ++j, ++it) {
-                const int s = it % p.n_stages;
-                const unsigned int parity = (it / p.n_stages) & 1;
+            for (int j = j0; j < j1; ++j, at_ring.next(p.n_stages)) {
+                const int s = at_ring.slot;
+                const unsigned int parity = at_ring.round;
                 const unsigned int k_at = ring + s * C::kStageBytes, v_at = k_at + C::kTileBytes;
                 const int key0 = j * kTile + 16 * NK * kg;          // the warp's first place
                 float x[MT][2 * NK][4];
@@ -707,7 +721,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 }
             if constexpr (KG > 1) {
                 consumer_barrier(cthreads);                           // also: every warp is done with the tiles before
-                const unsigned int buf = ring + (it % p.n_stages) * C::kStageBytes;
+                const unsigned int buf = ring + at_ring.slot * C::kStageBytes;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -766,8 +780,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(empty(it % p.n_stages));
-                ++it;
+                if (lane == 0) mbar_arrive(empty(at_ring.slot));
+                at_ring.next(p.n_stages);
             }
             const bool whole = run.ns == run.n;
             if (kg == 0) {
@@ -807,11 +821,15 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 // ---- more than 16 query rows per key head: products on the tensor-memory path -------------------------------------------
 //
 // The same split over the blocks, parts and join; inside a block
-//   warps 0..3  softmax: thread r owns query row r of the row tile.  It reads the row's 64 scores of a tile from tensor
-//               memory, writes the weights back there in the cache's type, and keeps (m, l) in registers
+//   warps 0..3  softmax: thread r owns query row r of the row tile.  It reads the row's 64 scores of a tile from tensor memory,
+//               writes the weights back there in the cache's type, and keeps (m, l) in registers
 //   warp 4      one thread issues the products: S = Q K^T (tcgen05.mma, M = 128 query rows, N = 64 places, both operands from
 //               shared memory) into one of two score buffers, O += P V (P from tensor memory, V read with places as its K)
 //   warp 5      the page loads
+// Two blocks per SM (one beyond dim 128, whose accumulators take more than half of the tensor memory): while one waits for its scores
+// or ends a unit, the other keeps the memory busy.  One block with two such sets that took a run's tiles in turn was slower, 247 us
+// against 221 for 1024 units of 8 to 63 tiles: both sets stop at a unit's end together.
+// The next run's query rows are fetched, and its first scores computed, while this one ends (where two sets of query rows fit).
 // A row tile is always computed as 128 rows: rows that do not exist read whatever follows in shared memory and feed accumulator
 // rows that nobody reads.
 // The reference m of a row only moves when a tile's maximum exceeds it by 2^8 (weights up to 2^8 are harmless in float32 sums
@@ -850,31 +868,54 @@ __device__ __forceinline__ void tc_mma_ts(unsigned int d, unsigned int a, unsign
                  "r"(idesc), "r"(accumulate)
                  : "memory");
 }
-// Order of the loads of a run of n tiles of one unit: K0, K1, V0, K2, V1, ..., K(n-1), V(n-2), V(n-1).
-__device__ __forceinline__ int k_item(int i) { return i == 0 ? 0 : 2 * i - 1; }
-__device__ __forceinline__ int v_item(int i, int n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; }
+// Order of the loads of a run of n tiles, and of the products: K0, K1, V0, K2, V1, ..., K(n-1), V(n-2), V(n-1).  The
+// number of V(k) among them:
+__device__ __forceinline__ int v_item(int k, int n) { return k == n - 1 ? 2 * n - 1 : 2 * k + 2; }
+
+// The query rows of a unit into shared memory, asynchronously: rows of 128 bytes, swizzled, 64 elements of all rows after one another.
+template <typename T>
+__device__ __forceinline__ void fetch_rows(const Params &p, const Run &ru, unsigned int to, int warp, int warps, int lane)
+{
+    const int rows_here = min(p.tile_rows, p.rows - ru.rt * p.tile_rows);
+    const int chunks = p.halves * 8, at_once = 32 / chunks, sub = lane / chunks, ch = lane - sub * chunks;
+    if (sub >= at_once) return;                                    // (24 pieces leave lanes over)
+    for (int r = warp * at_once + sub; r < rows_here; r += warps * at_once) {
+        const int rr = ru.rt * p.tile_rows + r, tok = rr / p.group, head = ru.h * p.group + rr - tok * p.group;
+        const unsigned int at = to + (ch >> 3) * (p.tile_rows * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
+        const bool there = ch * 8 < p.D;                            // elements beyond dim: zeros
+        const T *from = static_cast<const T *>(p.q) + ru.b * p.qb + tok * p.qt + head * p.qh + (there ? ch * 8 : 0);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(there ? 16 : 0) : "memory");
+    }
+}
 
 template <typename T, int kBlocksPerSm>
 __global__ void __launch_bounds__(kTcThreads, kBlocksPerSm)
 attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p)
 {
+    constexpr unsigned int kCols = kBlocksPerSm == 2 ? 256 : 512;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) unsigned long long bar_words[2 * kTcMaxSlots + 6];
+    __shared__ __align__(8) unsigned long long bar_words[2 * kTcMaxSlots + 7];
     __shared__ unsigned int tmem_base_slot;
     __shared__ int give_up_flag, odd_run;
     volatile int *give_up = &give_up_flag;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const unsigned int q_smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const unsigned int ring = q_smem + p.halves * p.tile_rows * 128;
+    const unsigned int rows_bytes = static_cast<unsigned int>(p.halves * p.tile_rows * 128);
+    const unsigned int q_smem = (smem_u32(smem_raw) + 1023u) & ~1023u;              // one or two sets of query rows
+    const unsigned int ring = q_smem + p.q_buffers * rows_bytes;
     const unsigned int slot_bytes = static_cast<unsigned int>(p.halves) * (kTcTile * 128);
     int *base = reinterpret_cast<int *>(smem_raw + (ring - smem_u32(smem_raw)) + p.n_stages * slot_bytes);      // [B + 1]
     const unsigned int bars = smem_u32(bar_words);
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (kTcMaxSlots + s); };
-    auto s_full = [&](int i) { return bars + 8u * (2 * kTcMaxSlots + i); };
-    auto p_ready = [&](int i) { return bars + 8u * (2 * kTcMaxSlots + 2 + i); };
-    const unsigned int pv_done = bars + 8u * (2 * kTcMaxSlots + 4), q_ready = bars + 8u * (2 * kTcMaxSlots + 5);
+    auto s_full = [&](int k) { return bars + 8u * (2 * kTcMaxSlots + (k & 1)); };
+    auto p_ready = [&](int k) { return bars + 8u * (2 * kTcMaxSlots + 2 + (k & 1)); };
+    // (two, taken in turn: a wait by parity is sound while the barrier is in the phase waited for or the one after it, and the scores
+    // of tile k, whose product is issued after the output product of tile k - 2, say that the barrier's phase before is over)
+    auto pv_done = [&](int k) { return bars + 8u * (2 * kTcMaxSlots + 4 + (k & 1)); };
+    const unsigned int q_ready = bars + 8u * (2 * kTcMaxSlots + 6);
+    auto slot_at = [&](int s) { return ring + s * slot_bytes; };
+    auto q_at = [&](int run) { return q_smem + (p.q_buffers == 2 ? run & 1 : 0) * rows_bytes; };
 
     if (tid == 0) {
         give_up_flag = 0;
@@ -883,18 +924,18 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(s_full(i), 1);
-            mbar_init(p_ready(i), 4);
+        for (int k = 0; k < 2; ++k) {
+            mbar_init(s_full(k), 1);
+            mbar_init(p_ready(k), 4);
+            mbar_init(pv_done(k), 1);
         }
-        mbar_init(pv_done, 1);
         mbar_init(q_ready, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     }
     if (warp == 1) {
-        ptx::tmem_alloc(smem_u32(&tmem_base_slot), p.tmem_cols);
+        ptx::tmem_alloc(smem_u32(&tmem_base_slot), kCols);
         ptx::tmem_relinquish();
     }
     ptx::wait_for_stream();
@@ -910,49 +951,48 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     __syncthreads();
     const unsigned int tmem = tmem_base_slot;
     const Share share(p, base);
-    auto slot_of = [&](int item) { return item % p.n_stages; };
-    auto phase_of = [&](int item) { return static_cast<unsigned int>(item / p.n_stages) & 1u; };
 
     if (warp == 5) {
         // ---- page loads ----
         Runs runs;
         runs.begin(p, base, share.x0, share.x1);
         Run r, rn;
-        bool more = runs.next(r), ok = true;
+        bool ok = true;
         const int per_tile = kTcTile / p.box_rows;               // pages of a tile (1 where a page is larger)
         const unsigned int box_bytes = static_cast<unsigned int>(p.box_rows) * 128u;
-        int item = 0;
+        Cursor at = {0, 0u};
         auto load = [&](const CUtensorMap *map, int h, int j, int page) {
-            const int s = slot_of(item);
             const unsigned int there = __ballot_sync(kFull, page >= 0);
             int fine = 1;
             if (lane == 0) {
-                fine = mbar_wait(empty(s), phase_of(item) ^ 1u, give_up) ? 1 : 0;
-                if (fine) mbar_expect_tx(full(s), static_cast<unsigned int>(__popc(there)) * box_bytes * p.halves);
+                fine = mbar_wait(empty(at.slot), at.round ^ 1u, give_up) ? 1 : 0;
+                if (fine) mbar_expect_tx(full(at.slot), static_cast<unsigned int>(__popc(there)) * box_bytes * p.halves);
             }
             fine = __shfl_sync(kFull, fine, 0);
             if (fine && page >= 0) {
                 const int in_page = p.box_rows == kTcTile ? (j * kTcTile) & ((1 << p.page_shift) - 1) : 0;
-                const unsigned int at = ring + s * slot_bytes + lane * box_bytes;
-                for (int hf = 0; hf < p.halves; ++hf) tma_load_page(at + hf * (kTcTile * 128), map, full(s), hf * 64, in_page, h, page);
+                const unsigned int to = slot_at(at.slot) + lane * box_bytes;
+                for (int hf = 0; hf < p.halves; ++hf) tma_load_page(to + hf * (kTcTile * 128), map, full(at.slot), hf * 64, in_page, h, page);
             }
-            ++item;
+            at.next(p.n_stages);
             return fine != 0;
         };
+        bool more = runs.next(r);
         int len = more ? row_len(p, r.b) : 0;
         int id = more ? tile_page<kTcTile>(p, r.b, r.j0, len, lane, per_tile) : -1;      // fetched a tile ahead
         while (more && ok) {
             if (lane == 0) note_split(p, share, r);
             const bool follows = runs.next(rn);
             const int len_next = follows ? row_len(p, rn.b) : 0;
-            int before = -1;
+            int before = -1;                                      // the page of the tile whose values are still to be loaded
             for (int i = 0; i < r.ns && ok; ++i) {
                 const int page = id, j = r.j0 + i;
-                id = i + 1 < r.ns ? tile_page<kTcTile>(p, r.b, j + 1, len, lane, per_tile)
-                                  : (follows ? tile_page<kTcTile>(p, rn.b, rn.j0, len_next, lane, per_tile) : -1);
+                const bool last = i + 1 == r.ns;
+                id = !last ? tile_page<kTcTile>(p, r.b, j + 1, len, lane, per_tile)
+                           : (follows ? tile_page<kTcTile>(p, rn.b, rn.j0, len_next, lane, per_tile) : -1);
                 ok = load(&map_k, r.h, j, page);
                 if (ok && i > 0) ok = load(&map_v, r.h, j - 1, before);
-                if (ok && i + 1 == r.ns) ok = load(&map_v, r.h, j, page);
+                if (ok && last) ok = load(&map_v, r.h, j, page);
                 before = page;
             }
             r = rn;
@@ -961,7 +1001,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         }
         // every commit aimed at the slots' barriers has landed before the block ends
         if (lane == 0)
-            for (int k = 0; k < p.n_stages && ok; ++k, ++item) ok = mbar_wait(empty(slot_of(item)), phase_of(item) ^ 1u, give_up);
+            for (int k = 0; k < p.n_stages && ok; ++k, at.next(p.n_stages)) ok = mbar_wait(empty(at.slot), at.round ^ 1u, give_up);
     } else if (warp == 4) {
         // ---- products ----
         if (lane == 0) {
@@ -969,80 +1009,100 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             runs.begin(p, base, share.x0, share.x1);
             Run r;
             const unsigned int idesc_qk = tc_instr<T>(kTcTile, false), idesc_pv = tc_instr<T>(p.d16, true);
-            int n0 = 0, items = 0;                             // tiles and loads of the runs before
+            const unsigned long long half_q = static_cast<unsigned long long>((p.tile_rows * 128) >> 4), half_k = (kTcTile * 128) >> 4;
+            Cursor at = {0, 0u};                               // the loads are used in the order in which they are made
+            int mine = 0;                                      // tiles of the runs before
             bool ok = true;
             for (int run = 0; ok && runs.next(r); ++run) {
-                const int ns = r.ns;
+                const int n = r.ns;
+                const unsigned long long q_desc = ptx::operand_desc(q_at(run));
                 ok = mbar_wait(q_ready, run & 1, give_up);
-                for (int i = 0; i <= ns && ok; ++i) {
-                    if (i < ns) {
-                        const int item = items + k_item(i), s = slot_of(item), x = n0 + i;
-                        if (!(ok = mbar_wait(full(s), phase_of(item), give_up))) break;
+                for (int i = 0; i <= n && ok; ++i) {
+                    if (i < n) {
+                        const int k = mine + i;
+                        if (!(ok = mbar_wait(full(at.slot), at.round, give_up))) break;
                         ptx::tc_fence_after();
-                        const unsigned int k_at = ring + s * slot_bytes;
-                        for (int ks = 0; ks < p.d16 / 16; ++ks)
-                            tc_mma_ss(tmem + (x & 1) * kTcScoreCols, ptx::operand_desc(q_smem + (ks >> 2) * (p.tile_rows * 128)) + 2ull * (ks & 3),
-                                      ptx::operand_desc(k_at + (ks >> 2) * (kTcTile * 128)) + 2ull * (ks & 3), idesc_qk, ks != 0);
-                        ptx::tc_commit(empty(s));
-                        ptx::tc_commit(s_full(x & 1));
+                        const unsigned int d = tmem + (k & 1) * kTcScoreCols;
+                        unsigned long long qd = q_desc, kd = ptx::operand_desc(slot_at(at.slot));
+                        for (int left = p.d16; left > 0; left -= 64, qd += half_q, kd += half_k) {
+                            tc_mma_ss(d, qd, kd, idesc_qk, left == p.d16 ? 0u : 1u);      // 16 elements further: 32 bytes
+                            if (left > 16) tc_mma_ss(d, qd + 2, kd + 2, idesc_qk, 1u);
+                            if (left > 32) tc_mma_ss(d, qd + 4, kd + 4, idesc_qk, 1u);
+                            if (left > 48) tc_mma_ss(d, qd + 6, kd + 6, idesc_qk, 1u);
+                        }
+                        ptx::tc_commit(empty(at.slot));
+                        ptx::tc_commit(s_full(k));
+                        at.next(p.n_stages);
                     }
                     if (i > 0) {
-                        const int u = i - 1, x = n0 + u, item = items + v_item(u, ns), s = slot_of(item);
-                        if (!(ok = mbar_wait(p_ready(x & 1), (x >> 1) & 1, give_up))) break;
-                        if (!(ok = mbar_wait(full(s), phase_of(item), give_up))) break;
+                        const int k = mine + i - 1;
+                        if (!(ok = mbar_wait(p_ready(k), (k >> 1) & 1, give_up))) break;
+                        if (!(ok = mbar_wait(full(at.slot), at.round, give_up))) break;
                         ptx::tc_fence_after();
-                        const unsigned int v_at = ring + s * slot_bytes;
-#pragma unroll
-                        for (int kk = 0; kk < kTcTile / 16; ++kk)
-                            tc_mma_ts(tmem + kTcOutCol, tmem + (x & 1) * kTcScoreCols + 8 * kk, value_desc(v_at + kk * (16 * 128), kTcTile * 128), idesc_pv,
-                                      (u | kk) != 0);
-                        ptx::tc_commit(empty(s));
-                        ptx::tc_commit(pv_done);
+                        const unsigned int d = tmem + kTcOutCol, w = tmem + (k & 1) * kTcScoreCols;
+                        const unsigned long long vd = value_desc(slot_at(at.slot), kTcTile * 128);
+                        tc_mma_ts(d, w, vd, idesc_pv, i > 1 ? 1u : 0u);                  // 16 places further: 2 KiB
+                        tc_mma_ts(d, w + 8, vd + 128, idesc_pv, 1u);
+                        tc_mma_ts(d, w + 16, vd + 256, idesc_pv, 1u);
+                        tc_mma_ts(d, w + 24, vd + 384, idesc_pv, 1u);
+                        ptx::tc_commit(empty(at.slot));
+                        ptx::tc_commit(pv_done(k));
+                        at.next(p.n_stages);
                     }
                 }
-                n0 += ns;
-                items += 2 * ns;
+                mine += n;
             }
         }
     } else {
         // ---- softmax, rows in and out ----
+        const int r = tid;                                        // the thread's query row of the row tile
         zero_empty_rows<T>(p, base, tid, 128);
         Runs runs;
         runs.begin(p, base, share.x0, share.x1);
-        Run ru;
-        const unsigned int my_lanes = static_cast<unsigned int>(32 * warp) << 16;
-        int n = 0, items = 0;
-        const int chunks = p.halves * 8;                          // 16-byte pieces of a query row, or of a row of the result
-        const int rows_at_once = 32 / chunks, sub = lane / chunks, ch = lane - sub * chunks;
-        for (int run = 0; runs.next(ru); ++run) {
+        Run ru, next;
+        bool more = runs.next(next);
+        const unsigned int my_lanes = static_cast<unsigned int>(32 * warp) << 16, my_out = tmem + my_lanes + kTcOutCol;
+        // query rows on their way; and: they are there, scores may be computed
+        auto fetch = [&](const Run &x, int run) { fetch_rows<T>(p, x, q_at(run), warp, 4, lane); };
+        auto fetched = [&]() {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_ready);
+        };
+        const bool ahead = p.q_buffers == 2;
+        if (more && ahead) {
+            fetch(next, 0);
+            fetched();
+        }
+        int items = 0, mine = 0;                                    // loads of the runs before; tiles so far
+        for (int run = 0; more; ++run) {
+            ru = next;
+            more = runs.next(next);
             const int b = ru.b, h = ru.h, rt = ru.rt, j0 = ru.j0, ns = ru.ns;
             const int len = row_len(p, b), news = row_news(p, b);
             const int rows_here = min(p.tile_rows, p.rows - rt * p.tile_rows);
-            consumer_barrier(128);                               // rows of the run before have left through the same memory
-            for (int r = warp * rows_at_once + sub; r < rows_here; r += 4 * rows_at_once) {
-                if (sub >= rows_at_once) break;                   // (24 pieces leave lanes over)
-                const int rr = rt * p.tile_rows + r, tok = rr / p.group, hh = h * p.group + rr - tok * p.group;
-                const unsigned int at = q_smem + (ch >> 3) * (p.tile_rows * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
-                const bool there = ch * 8 < p.D;                  // elements beyond dim: zeros
-                const T *from = static_cast<const T *>(p.q) + b * p.qb + tok * p.qt + hh * p.qh + (there ? ch * 8 : 0);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(there ? 16 : 0) : "memory");
+            ptx::tc_fence_before();
+            consumer_barrier(128);                                   // the accumulators and staged rows of the run before have been read
+            ptx::tc_fence_after();
+            if (!ahead) {
+                fetch(ru, run);
+                fetched();
+            } else if (more) {
+                fetch(next, run + 1);
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            ptx::tc_fence_before();                              // the output of the run before has been read
-            __syncwarp();
-            if (lane == 0) mbar_arrive(q_ready);
-            const int r = tid, rr = rt * p.tile_rows + r, tok = rr / p.group;
+            const int rr = rt * p.tile_rows + r, tok = rr / p.group;
             const int limit = r < rows_here && tok < news ? len - news + tok : -1;
             const bool warp_has = 32 * warp < rows_here;
             float m = 0.f, l = 0.f;                              // l == 0: nothing seen yet, m is arbitrary
 
-            for (int i = 0; i < ns; ++i, ++n) {
+            for (int i = 0; i < ns; ++i, ++mine) {
                 const int key0 = (j0 + i) * kTcTile;
                 const bool edge = key0 + kTcTile - 1 > len - news;
-                const unsigned int s_at = tmem + my_lanes + (n & 1) * kTcScoreCols;
-                mbar_wait(s_full(n & 1), (n >> 1) & 1, give_up);
+                const unsigned int s_at = tmem + my_lanes + (mine & 1) * kTcScoreCols;
+                mbar_wait(s_full(mine), (mine >> 1) & 1, give_up);
                 ptx::tc_fence_after();
+                float f = 1.f;                                   // on what has been accumulated
                 if (warp_has) {
                     float x[32], y[32];
                     ptx::tmem_ld64(s_at, x, y);
@@ -1067,7 +1127,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         my = fmaxf(my, fmaxf(x[j + 1], y[j + 1]));
                     }
                     mx = fmaxf(mx, my);
-                    float up = 0.f, f = 1.f;
+                    float up = 0.f;
                     if (limit >= 0) {
                         if (l == 0.f) {
                             up = mx == -INFINITY ? 0.f : mx;
@@ -1101,16 +1161,19 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     unpack2(add2(sum0, sum1), s0, s1);
                     l += s0 + s1;
                     ptx::tmem_st32(s_at, w2);
+                }
+                if (warp_has) {
                     if (__any_sync(kFull, f != 1.f)) {
-                        // the products before have to be complete; the next one waits for these weights
-                        mbar_wait(pv_done, (n - 1) & 1, give_up);
+                        // the product before has to be complete; the next one waits for these weights
+                        mbar_wait(pv_done(mine - 1), ((mine - 1) >> 1) & 1, give_up);
                         ptx::tc_fence_after();
                         for (int c0 = 0; c0 < p.d16; c0 += 32) {
                             float o[32];
-                            ptx::tmem_ld32(tmem + my_lanes + kTcOutCol + c0, o);
+                            unsigned int w2[32];
+                            ptx::tmem_ld32(my_out + c0, o);
 #pragma unroll
                             for (int j = 0; j < 32; ++j) w2[j] = __float_as_uint(o[j] * f);
-                            ptx::tmem_st32(tmem + my_lanes + kTcOutCol + c0, w2);
+                            ptx::tmem_st32(my_out + c0, w2);
                         }
                     }
                     ptx::tmem_wait_st();
@@ -1118,13 +1181,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 if (edge) {
                     // A weight of zero does not silence an infinity or NaN in the values.  Places beyond the row hold anything:
                     // zeroed.  Such a value in a place of a later new token is left out here and handed to the rows that see it at the end.
-                    // (the loads up to the tile's keys have been consumed: with four slots that includes this slot's load before)
-                    const int item = items + v_item(i, ns), s = slot_of(item);
-                    mbar_wait(full(s), phase_of(item), give_up);
-                    const unsigned int v_at = ring + s * slot_bytes;
-                    const int from = max(len - news + 1 - key0, 0);
-                    for (int k = tid; k < (kTcTile - from) * chunks; k += 128) {
-                        const int kr = from + k / chunks, ch = k % chunks;
+                    // (The loads up to the tile's keys have been consumed: with four slots that includes this slot's load before.)
+                    const int item = items + v_item(i, ns), s = item % p.n_stages;
+                    mbar_wait(full(s), (item / p.n_stages) & 1, give_up);
+                    const unsigned int v_at = slot_at(s);
+                    const int from = max(len - news + 1 - key0, 0), chunks = p.halves * 8;
+                    for (int c = r; c < (kTcTile - from) * chunks; c += 128) {
+                        const int kr = from + c / chunks, ch = c % chunks;
                         const unsigned int at = v_at + (ch >> 3) * (kTcTile * 128) + kr * 128 + (((ch & 7) ^ (kr & 7)) << 4);
                         unsigned int v[4] = {0u, 0u, 0u, 0u}, z[4] = {0u, 0u, 0u, 0u};
                         bool store = key0 + kr >= len;
@@ -1143,33 +1206,34 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 }
                 ptx::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_ready(n & 1));
+                if (lane == 0) mbar_arrive(p_ready(mine));
             }
+            if (ahead && more) fetched();
 
             // ---- the run's rows ----
-            // (a wait by parity is only sound one phase ahead: the last scores are complete, hence the output products up to the
-            // last but two)
-            if (ns > 1) mbar_wait(pv_done, n & 1, give_up);
-            mbar_wait(pv_done, (n - 1) & 1, give_up);
+            if (ns > 1) mbar_wait(pv_done(mine - 2), ((mine - 2) >> 1) & 1, give_up);
+            mbar_wait(pv_done(mine - 1), ((mine - 1) >> 1) & 1, give_up);
             ptx::tc_fence_after();
-            consumer_barrier(128);                              // odd_run of all four warps
+            consumer_barrier(128);                                   // odd_run of all four warps
             const bool odd = *static_cast<volatile int *>(&odd_run) == run + 1;
             const bool whole = ns == ru.n;
-            const bool seen = limit >= 0 && l != 0.f;            // (NaN counts as seen)
+            const bool seen = limit >= 0 && l != 0.f;                // (NaN counts as seen)
             const int head = h * p.group + rr - tok * p.group;
             const long long row = (static_cast<long long>(b) * p.T + tok) * p.Hq + head;
             float *part = p.parts + static_cast<long long>(2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0)) * p.tile_rows * (p.part_stride + 2);
             if (warp_has) {
-                // A thread has a row, memory wants rows side by side: each warp turns its 32 rows round in the memory of its query
-                // rows, which every product has read.  A row of it holds dim elements of the result, or half a row of a part.
+                // A thread has a row, memory wants rows side by side: each warp turns its 32 rows round in shared memory, where the
+                // run's query rows were, which every product has read.
                 const float inv = seen ? (whole ? 1.f / l : 1.f) : 0.f;
                 const int pitch = p.halves * 128, warp_rows = min(32, rows_here - 32 * warp);
-                const unsigned int my_row = q_smem + r * pitch;
-                const int passes = whole ? 1 : 2, cols = whole ? p.halves * 64 : p.halves * 32;
-                for (int pass = 0; pass < passes && pass * cols < p.D; ++pass) {
-                    for (int c0 = pass * cols; c0 < min((pass + 1) * cols, p.D); c0 += 32) {
+                const unsigned int out_smem = q_at(run), my_row = out_smem + r * pitch;
+                const int cols = whole ? p.halves * 64 : p.halves * 32;                        // of a pass: what a staged row holds
+                const int lanes_row = p.halves * 8, at_once = 32 / lanes_row, sub = lane / lanes_row, ch = lane - sub * lanes_row;
+                for (int pass0 = 0; pass0 < p.D; pass0 += cols) {
+                    const int pass1 = min(pass0 + cols, p.D);
+                    for (int c0 = pass0; c0 < pass1; c0 += 32) {
                         float o[32];
-                        ptx::tmem_ld32(tmem + my_lanes + kTcOutCol + c0, o);
+                        ptx::tmem_ld32(my_out + c0, o);
                         if (odd && seen) {
                             float z[32];
 #pragma unroll
@@ -1184,38 +1248,38 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                             if (whole) {
 #pragma unroll
                                 for (int e = 0; e < 4; ++e)
-                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(my_row + (((c0 / 8 + e) ^ (r & 7)) << 4)),
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(my_row + ((((c0 - pass0) / 8 + e) ^ (r & 7)) << 4)),
                                                  "r"(pack_pair<T>(o[8 * e], o[8 * e + 1])), "r"(pack_pair<T>(o[8 * e + 2], o[8 * e + 3])),
                                                  "r"(pack_pair<T>(o[8 * e + 4], o[8 * e + 5])), "r"(pack_pair<T>(o[8 * e + 6], o[8 * e + 7]))
                                                  : "memory");
                             } else {
 #pragma unroll
                                 for (int e = 0; e < 8; ++e)
-                                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(my_row + ((((c0 - pass * cols) / 4 + e) ^ (r & 7)) << 4)),
+                                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(my_row + ((((c0 - pass0) / 4 + e) ^ (r & 7)) << 4)),
                                                  "f"(o[4 * e]), "f"(o[4 * e + 1]), "f"(o[4 * e + 2]), "f"(o[4 * e + 3])
                                                  : "memory");
                             }
                         }
                     }
                     __syncwarp();
-                    // `chunks` lanes a row, 16 bytes each
-                    const int d = whole ? ch * 8 : pass * cols + ch * 4;
-                    const bool mine = sub < rows_at_once && d < p.D;
+                    // lanes_row lanes a row, 16 bytes each
+                    const int d = pass0 + (whole ? ch * 8 : ch * 4);
+                    const bool do_it = sub < at_once && d < pass1;
                     char *to = whole ? reinterpret_cast<char *>(static_cast<T *>(p.out) + d) : reinterpret_cast<char *>(part + (32 * warp) * p.part_stride + d);
                     const long long row_bytes = whole ? row * p.D * static_cast<long long>(sizeof(T)) : static_cast<long long>(lane) * p.part_stride * 4;
-                    for (int w0 = 0; w0 < warp_rows; w0 += 4 * rows_at_once) {
+                    for (int w0 = 0; w0 < warp_rows; w0 += 4 * at_once) {
                         uint4 v[4];
                         long long off[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const int wr = w0 + k * rows_at_once + sub, r2 = 32 * warp + wr;
+                            const int wr = w0 + k * at_once + sub, r2 = 32 * warp + wr;
                             off[k] = __shfl_sync(kFull, row_bytes, wr & 31);
-                            if (mine && wr < warp_rows)
-                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[k].x), "=r"(v[k].y), "=r"(v[k].z), "=r"(v[k].w) : "r"(q_smem + r2 * pitch + ((ch ^ (r2 & 7)) << 4)) : "memory");
+                            if (do_it && wr < warp_rows)
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[k].x), "=r"(v[k].y), "=r"(v[k].z), "=r"(v[k].w) : "r"(out_smem + r2 * pitch + ((ch ^ (r2 & 7)) << 4)) : "memory");
                         }
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            if (mine && w0 + k * rows_at_once + sub < warp_rows) __stcg(reinterpret_cast<uint4 *>(to + off[k]), v[k]);
+                            if (do_it && w0 + k * at_once + sub < warp_rows) __stcg(reinterpret_cast<uint4 *>(to + off[k]), v[k]);
                     }
                     __syncwarp();
                 }
@@ -1231,7 +1295,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         ptx::tc_fence_before();
     }
     __syncthreads();
-    if (warp == 1) ptx::tmem_dealloc(tmem, p.tmem_cols);
+    if (warp == 1) ptx::tmem_dealloc(tmem, kCols);
     if (*give_up && lane == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);
 }
 

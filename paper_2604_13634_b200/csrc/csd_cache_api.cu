@@ -238,7 +238,7 @@ constexpr int kMaxDevices = 64;
 constexpr int kSmemPerSm = 228 * 1024, kSmemReserved = 1024, kSmemStatic = 1024;     // per block: the system's, and the kernel's own
 
 struct AttentionPlan {
-    int rows, row_tiles, tile_rows, dp, grid, stages, smem, run_cost;
+    int rows, row_tiles, tile_rows, dp, grid, stages, smem, run_cost, q_buffers;
     size_t splits_off, parts_off, total;
 };
 
@@ -294,15 +294,19 @@ AttentionPlan attention_tc_plan(int rows, int dim, int B)
     a.run_cost = a.dp == 64 ? 8 : (a.dp == 128 ? 4 : 2);      // about 5 us: 240 us at 2, 228 at 4, 231 at 6 for 1024 units of 8 to 63 tiles
     const int halves = (dim + 63) / 64, slot = halves * attention::kTcTile * 128;
     const int limit = kSmemPerSm / tc_blocks(dim) - kSmemReserved - kSmemStatic;
-    // The kernel's waits want four slots at least; tables of thousands of rows leave room for fewer query rows.
+    // The kernel's waits want four slots at least: two sets of query rows give way to one for them, and where tables of thousands
+    // of rows leave little, a row tile holds fewer query rows.
     for (int most = 128;; most /= 2) {
         a.row_tiles = (rows + most - 1) / most;
         a.tile_rows = ((rows + a.row_tiles - 1) / a.row_tiles + 7) / 8 * 8;
         a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
-        const int fixed = 1024 + halves * a.tile_rows * 128 + (B + 1) * 4;
-        a.stages = (limit - fixed) / slot;
-        if (a.stages > attention::kTcMaxSlots) a.stages = attention::kTcMaxSlots;
-        a.smem = fixed + a.stages * slot;
+        for (a.q_buffers = 2; a.q_buffers >= 1; --a.q_buffers) {
+            const int fixed = 1024 + a.q_buffers * halves * a.tile_rows * 128 + (B + 1) * 4;
+            a.stages = (limit - fixed) / slot;
+            if (a.stages > attention::kTcMaxSlots) a.stages = attention::kTcMaxSlots;
+            a.smem = fixed + a.stages * slot;
+            if (a.stages >= 4) break;
+        }
         if (a.stages >= 4 || most == 16) break;
     }
     a.splits_off = 0;
@@ -409,10 +413,10 @@ csd_status_t run_attention_tc(attention::Params p, const csd_cache_t *cache, int
     const AttentionPlan a = attention_tc_plan(p.T * p.group, p.D, p.B);
     fill_plan(p, a, ws);
     p.tile_rows = a.tile_rows;
+    p.q_buffers = a.q_buffers;
     p.part_stride = a.dp;
     p.halves = (p.D + 63) / 64;
     p.d16 = (p.D + 15) / 16 * 16;
-    p.tmem_cols = kBlocks == 2 ? 256u : 512u;
     p.box_rows = cache->page_size < attention::kTcTile ? cache->page_size : attention::kTcTile;
     p.k_pool = static_cast<char *>(cache->k) + layer * cache->stride_layer * 2;
     p.v_pool = static_cast<char *>(cache->v) + layer * cache->stride_layer * 2;

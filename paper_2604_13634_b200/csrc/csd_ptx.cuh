@@ -43,6 +43,7 @@ __device__ __forceinline__ bool mbar_try_wait(unsigned int bar, unsigned int par
 // Bounded wait.  False if the wait ran out or another role of the CTA has given up.
 __device__ __forceinline__ bool mbar_wait(unsigned int bar, unsigned int parity, volatile int *give_up)
 {
+    if (mbar_try_wait(bar, parity)) return true;
     const long long t0 = clock64();
     while (!mbar_try_wait(bar, parity)) {
         if (*give_up) return false;
