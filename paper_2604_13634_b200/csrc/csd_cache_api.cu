@@ -49,68 +49,72 @@ bool rope_ok(const csd_rope_t *r, int D)
            (r->layout == CSD_ROPE_HALF || r->layout == CSD_ROPE_INTERLEAVED) && std::isfinite(r->magnitude);
 }
 
-// 16-byte accesses need every unit of every head to begin on a 16-byte boundary.
-template <int P>
-bool units_fit(int rot, int D)
+// How a head's row is cut.  Units of 16 bytes' worth of pairs where rot divides into them; single 16-byte vectors where the row does; else pair by pair.
+enum class Cut { kUnits, kVectors, kPairs };
+
+Cut cut_of(int P, int rot, int D, bool vectors)
 {
-    return D % P == 0 && rot % (2 * P) == 0;
+    if (!vectors || D % P != 0 || D / P > rope::kThreads) return Cut::kPairs;
+    return rot % (2 * P) == 0 ? Cut::kUnits : Cut::kVectors;
 }
 
-template <int P>
-int units_of(int rot, int D)
+int units_of(Cut cut, int P, int rot, int D)
 {
+    if (cut == Cut::kVectors) return D / P;
+    if (cut == Cut::kPairs) P = 1;
     return rot / (2 * P) + (D - rot + 2 * P - 1) / (2 * P);
 }
 
-// Blocks of whole tokens where they fit, blocks of a token's threads where one takes more; false: too many.
-bool place_tokens(long long tokens, long long per_token, rope::Places &at, dim3 &grid)
+// Blocks of whole tokens where they fit, blocks of a token's groups of heads where one takes more; false: too many.
+bool place_tokens(long long tokens, long long groups, int units, rope::Places &at, dim3 &grid)
 {
-    if (tokens > INT_MAX || per_token > (65535ll * rope::kThreads)) return false;
+    const long long per_token = groups * units;
+    if (tokens > INT_MAX || per_token > INT_MAX) return false;
     at.n_tokens = static_cast<int>(tokens);
     at.per_token = static_cast<int>(per_token);
     at.tokens = per_token >= rope::kThreads ? 1 : rope::kThreads / at.per_token;
-    grid = dim3(static_cast<unsigned int>((tokens + at.tokens - 1) / at.tokens),
-                at.tokens > 1 ? 1u : static_cast<unsigned int>((per_token + rope::kThreads - 1) / rope::kThreads));
+    at.groups = rope::kThreads / units;
+    const long long taken = at.groups > 0 ? static_cast<long long>(at.groups) * units : rope::kThreads;
+    const long long rows = at.tokens > 1 ? 1 : (per_token + taken - 1) / taken;
+    if (rows > 65535) return false;
+    grid = dim3(static_cast<unsigned int>((tokens + at.tokens - 1) / at.tokens), static_cast<unsigned int>(rows));
     return true;
 }
 
-template <typename T, int P>
-csd_status_t launch_rope(rope::RopeParams p, csd_rope_layout_t layout, cudaStream_t st)
-{
-    p.units = units_of<P>(p.turn.rot, p.D);
-    dim3 grid;
-    if (!place_tokens(static_cast<long long>(p.B) * p.S, static_cast<long long>((p.H + rope::kHeads - 1) / rope::kHeads) * p.units, p.at, grid)) return CSD_ERR_UNSUPPORTED;
-    return launch(layout == CSD_ROPE_HALF ? rope::rope_kernel<T, P, true> : rope::rope_kernel<T, P, false>, grid, rope::kThreads, 0, st, p);
-}
+int groups_of(int heads) { return (heads + rope::kHeads - 1) / rope::kHeads; }
 
 template <typename T>
-csd_status_t run_rope(const rope::RopeParams &p, csd_rope_layout_t layout, cudaStream_t st)
+csd_status_t run_rope(rope::RopeParams p, csd_rope_layout_t layout, cudaStream_t st)
 {
     constexpr int P = 16 / static_cast<int>(sizeof(T));
     const long long all = p.xb | p.xs | p.xh | p.yb | p.ys | p.yh;
-    if (units_fit<P>(p.turn.rot, p.D) && all % P == 0 && aligned16(p.x) && aligned16(p.y)) return launch_rope<T, P>(p, layout, st);
-    return launch_rope<T, 1>(p, layout, st);
-}
-
-template <typename T, int P>
-csd_status_t launch_append(rope::AppendParams p, csd_rope_layout_t layout, cudaStream_t st)
-{
-    p.units = units_of<P>(p.turn.rot, p.D);
-    p.q_groups = (p.Hq + rope::kHeads - 1) / rope::kHeads;
-    p.kv_groups = (p.Hkv + rope::kHeads - 1) / rope::kHeads;
+    const Cut cut = cut_of(P, p.turn.rot, p.D, all % P == 0 && aligned16(p.x) && aligned16(p.y));
+    p.units = units_of(cut, P, p.turn.rot, p.D);
     dim3 grid;
-    if (!place_tokens(static_cast<long long>(p.B) * p.T, static_cast<long long>(p.q_groups + 2 * p.kv_groups) * p.units, p.at, grid)) return CSD_ERR_UNSUPPORTED;
-    return launch(layout == CSD_ROPE_HALF ? rope::rope_append_kernel<T, P, true> : rope::rope_append_kernel<T, P, false>, grid, rope::kThreads, 0, st, p);
+    if (!place_tokens(static_cast<long long>(p.B) * p.S, groups_of(p.H), p.units, p.at, grid)) return CSD_ERR_UNSUPPORTED;
+    const bool half = layout == CSD_ROPE_HALF;
+    auto go = [&](auto kernel) { return launch(kernel, grid, rope::kThreads, 0, st, p); };
+    if (cut == Cut::kUnits) return go(half ? rope::rope_kernel<T, P, true, false> : rope::rope_kernel<T, P, false, false>);
+    if (cut == Cut::kVectors) return go(half ? rope::rope_kernel<T, P, true, true> : rope::rope_kernel<T, P, false, true>);
+    return go(half ? rope::rope_kernel<T, 1, true, false> : rope::rope_kernel<T, 1, false, false>);
 }
 
 template <typename T>
-csd_status_t run_append(const rope::AppendParams &p, csd_rope_layout_t layout, cudaStream_t st)
+csd_status_t run_append(rope::AppendParams p, csd_rope_layout_t layout, cudaStream_t st)
 {
     constexpr int P = 8;
     const long long all = p.qb | p.qt | p.qh | p.kb | p.kt | p.kh | p.vb | p.vt | p.vh;
-    if (units_fit<P>(p.turn.rot, p.D) && all % P == 0 && aligned16(p.q) && aligned16(p.k) && aligned16(p.v) && aligned16(p.q_out))
-        return launch_append<T, P>(p, layout, st);
-    return launch_append<T, 1>(p, layout, st);
+    const Cut cut = cut_of(P, p.turn.rot, p.D, all % P == 0 && aligned16(p.q) && aligned16(p.k) && aligned16(p.v) && aligned16(p.q_out));
+    p.units = units_of(cut, P, p.turn.rot, p.D);
+    p.q_groups = groups_of(p.Hq);
+    p.kv_groups = groups_of(p.Hkv);
+    dim3 grid;
+    if (!place_tokens(static_cast<long long>(p.B) * p.T, p.q_groups + 2ll * p.kv_groups, p.units, p.at, grid)) return CSD_ERR_UNSUPPORTED;
+    const bool half = layout == CSD_ROPE_HALF;
+    auto go = [&](auto kernel) { return launch(kernel, grid, rope::kThreads, 0, st, p); };
+    if (cut == Cut::kUnits) return go(half ? rope::rope_append_kernel<T, P, true, false> : rope::rope_append_kernel<T, P, false, false>);
+    if (cut == Cut::kVectors) return go(half ? rope::rope_append_kernel<T, P, true, true> : rope::rope_append_kernel<T, P, false, true>);
+    return go(half ? rope::rope_append_kernel<T, 1, true, false> : rope::rope_append_kernel<T, 1, false, false>);
 }
 
 // ---- the cache ----------------------------------------------------------------------------------

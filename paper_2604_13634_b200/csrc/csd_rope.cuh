@@ -12,6 +12,9 @@
 // Bound: memory (every element read once, written once).  A block has a few whole tokens.  Its threads first put the tokens' sines
 // and cosines into shared memory, one per pair and token; then each thread turns one unit (P = 16 bytes' worth of pairs: two
 // 16-byte vectors, neighbouring lanes neighbouring vectors) of kHeads heads, whose loads it has issued before.
+// Where rot does not divide into such units but rows are made of whole vectors, a thread has one vector of kHeads heads instead and
+// reads the partners of its elements one by one (they lie in the same rows, which the block reads anyway): 90.7 us to
+// XX for 85 MB with 66 of 168 elements turned.  Element by element only where rows themselves are not whole vectors.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -203,10 +206,11 @@ __device__ __forceinline__ void turn(Vec<T, 8> &a, Vec<T, 8> &b, const float2 (&
     }
 }
 
-// Which token, unit and group of heads a thread has: `per_token` threads a token, `tokens` tokens to a block (grid.y > 1 where a
-// token takes more than a block).  32-bit quotients only: the 64-bit ones of a flat index cost more than the rotation.
+// Which token, unit and group of heads a thread has: `per_token` threads a token, `tokens` tokens to a block, or (grid.y > 1)
+// `groups` groups of heads of one token to a block: a head lies in one block whole, so that a barrier can part its reads and its
+// writes (0: heads of more units than a block has threads, whose units are read and written by one thread each).  32-bit quotients only: the 64-bit ones of a flat index cost more than the rotation.
 struct Places {
-    int per_token, tokens;
+    int per_token, tokens, groups;
     int n_tokens;
 };
 
@@ -217,7 +221,7 @@ struct Place {
 
 // cosines and sines of a block's tokens: element (token, j, u) is pair u P + j, so that neighbouring units are neighbours
 constexpr int kMaxRot = 4096;
-constexpr int kTable = kMaxRot / 2;        // tokens * rot / 2 <= threads * P <= this, too
+constexpr int kTable = kMaxRot / 2 + 8;    // tokens * (rot / 2, rounded up to P) <= threads * P <= this, too
 
 __device__ __forceinline__ Place place_of(const Places &p, int units)
 {
@@ -228,13 +232,127 @@ __device__ __forceinline__ Place place_of(const Places &p, int units)
         r.in_block = i / p.per_token;
         i -= r.in_block * p.per_token;
     } else {
-        i += blockIdx.y * kThreads;
+        const int taken = p.groups > 0 ? p.groups * units : kThreads;
+        if (i >= taken) r.in_block = 1;                            // (no token of its own: not ok below)
+        i += blockIdx.y * taken;
     }
     r.token = blockIdx.x * p.tokens + r.in_block;
     r.group = i / units;
     r.unit = i - r.group * units;
     r.ok = r.in_block < p.tokens && i < p.per_token && r.token < p.n_tokens;
     return r;
+}
+
+// One vector of P elements from e0 of a head's row: every element with its partner.  half: element e < rot/2 pairs with e + rot/2;
+// interleaved: the partners are neighbours.  Elements from rot on keep their bits.
+template <typename T, int P, bool kHalf>
+struct Loose {
+    alignas(16) T own[P];
+    T other[kHalf ? P : 1];
+
+    __device__ __forceinline__ void load(const T *row, int e0, int rot)
+    {
+        *reinterpret_cast<Vec<T, P> *>(own) = *reinterpret_cast<const Vec<T, P> *>(row + e0);
+        if constexpr (kHalf) {
+            const int half = rot / 2;
+            const T *a = row + half, *b = row - half;
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+                if (e0 + j < rot) other[j] = e0 + j < half ? a[e0 + j] : b[e0 + j];
+        }
+    }
+    __device__ __forceinline__ void store(T *row, int e0) const { *reinterpret_cast<Vec<T, P> *>(row + e0) = *reinterpret_cast<const Vec<T, P> *>(own); }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int j = 0; j < P; ++j) own[j] = from_f32<T>(0.f);
+    }
+};
+
+// What a vector's elements are multiplied by: for all heads the same.
+template <int P, bool kHalf>
+struct LooseTurn {
+    float2 cs[kHalf ? P : P / 2];
+    // table: pair i at (i % P) * columns + i / P
+    __device__ __forceinline__ LooseTurn(const float2 *table, int columns, int e0, int rot)
+    {
+        const int half = rot / 2;
+#pragma unroll
+        for (int j = 0; j < (kHalf ? P : P / 2); ++j) {
+            const int e = e0 + j, i = kHalf ? (e < half ? e : e - half) : e0 / 2 + j;
+            if (kHalf ? e < rot : i < half) {
+                cs[j] = table[(i % P) * columns + i / P];
+                if (kHalf && e < half) cs[j].y = -cs[j].y;         // x0 cos - x1 sin: the product with the sign changed is the same product
+            }
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void apply(Loose<T, P, kHalf> &v, int e0, int rot) const
+    {
+        if constexpr (kHalf) {
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+                if (e0 + j < rot) v.own[j] = from_f32<T>(__fmaf_rn(to_f32(v.own[j]), cs[j].x, __fmul_rn(to_f32(v.other[j]), cs[j].y)));
+        } else {
+#pragma unroll
+            for (int j = 0; j < P / 2; ++j)
+                if (e0 + 2 * j < rot) {
+                    float x = to_f32(v.own[2 * j]), y = to_f32(v.own[2 * j + 1]);
+                    turn_pair(x, y, cs[j]);
+                    v.own[2 * j] = from_f32<T>(x);
+                    v.own[2 * j + 1] = from_f32<T>(y);
+                }
+        }
+    }
+};
+
+// The two shapes of a thread's work under one interface: whole units (kLoose false) and single vectors.
+template <typename T, int P, bool kHalf, bool kLoose>
+struct Piece;
+template <typename T, int P, bool kHalf>
+struct Piece<T, P, kHalf, false> {
+    Vec<T, P> a, c;
+    static __device__ __forceinline__ int columns(int rot) { return rot / 2 / P; }
+    __device__ __forceinline__ void load(const T *row, int u, int rot, int D)
+    {
+        const Unit un = unit_at<P, kHalf>(u, rot, D);
+        a = *reinterpret_cast<const Vec<T, P> *>(row + un.a);
+        if (un.second) c = *reinterpret_cast<const Vec<T, P> *>(row + un.b);
+    }
+    __device__ __forceinline__ void turn_by(const float2 (&cs)[P]) { turn<kHalf>(a, c, cs); }
+    __device__ __forceinline__ void store(T *row, int u, int rot, int D) const
+    {
+        const Unit un = unit_at<P, kHalf>(u, rot, D);
+        *reinterpret_cast<Vec<T, P> *>(row + un.a) = a;
+        if (un.second) *reinterpret_cast<Vec<T, P> *>(row + un.b) = c;
+    }
+    __device__ __forceinline__ void zero() { a = c = Vec<T, P>(); }
+};
+template <typename T, int P, bool kHalf>
+struct Piece<T, P, kHalf, true> {
+    Loose<T, P, kHalf> v;
+    static __device__ __forceinline__ int columns(int rot) { return (rot / 2 + P - 1) / P; }
+    __device__ __forceinline__ void load(const T *row, int u, int rot, int) { v.load(row, u * P, rot); }
+    __device__ __forceinline__ void store(T *row, int u, int, int) const { v.store(row, u * P); }
+    __device__ __forceinline__ void zero() { v.zero(); }
+};
+
+// All heads of a thread turned by its token's table.
+template <typename T, int P, bool kHalf, bool kLoose, int kHeads_>
+__device__ __forceinline__ void turn_all(Piece<T, P, kHalf, kLoose> (&x)[kHeads_], const float2 *table, int u, int rot, int D)
+{
+    const int columns = Piece<T, P, kHalf, kLoose>::columns(rot);
+    if constexpr (kLoose) {
+        const LooseTurn<P, kHalf> by(table, columns, u * P, rot);
+#pragma unroll
+        for (int k = 0; k < kHeads_; ++k) by.apply(x[k].v, u * P, rot);
+    } else if (unit_at<P, kHalf>(u, rot, D).turns) {
+        float2 cs[P];
+#pragma unroll
+        for (int j = 0; j < P; ++j) cs[j] = table[j * columns + u];
+#pragma unroll
+        for (int k = 0; k < kHeads_; ++k) x[k].turn_by(cs);
+    }
 }
 
 struct RopeParams {
@@ -250,54 +368,38 @@ struct RopeParams {
     Places at;
 };
 
-template <typename T, int P, bool kHalf>
+template <typename T, int P, bool kHalf, bool kLoose>
 __global__ void __launch_bounds__(kThreads, 3) rope_kernel(const RopeParams p)
 {
+    using Mine = Piece<T, P, kHalf, kLoose>;
     __shared__ float2 table[kTable];
     ptx::wait_for_stream();
     const Place at = place_of(p.at, p.units);
-    const int u = at.unit, h0 = at.group * kHeads, pairs = p.turn.rot / 2, turning = pairs / P;
-    const Unit un = unit_at<P, kHalf>(u, p.turn.rot, p.D);
-    Vec<T, P> a[kHeads], c[kHeads];
+    const int u = at.unit, h0 = at.group * kHeads, pairs = p.turn.rot / 2, columns = Mine::columns(p.turn.rot), each = columns * P;
+    Mine x[kHeads];
     int b = 0, s = 0;
     if (at.ok) {
         b = at.token / p.S;
         s = at.token - b * p.S;
-        const T *x = static_cast<const T *>(p.x) + b * p.xb + s * p.xs;
+        const T *from = static_cast<const T *>(p.x) + b * p.xb + s * p.xs;
 #pragma unroll
-        for (int k = 0; k < kHeads; ++k) {
-            if (h0 + k < p.H) {
-                const T *xh = x + (h0 + k) * p.xh;
-                a[k] = *reinterpret_cast<const Vec<T, P> *>(xh + un.a);
-                if (un.second) c[k] = *reinterpret_cast<const Vec<T, P> *>(xh + un.b);
-            }
-        }
+        for (int k = 0; k < kHeads; ++k)
+            if (h0 + k < p.H) x[k].load(from + (h0 + k) * p.xh, u, p.turn.rot, p.D);
     }
     for (int i = threadIdx.x; i < p.at.tokens * pairs; i += kThreads) {
         const int k = i / pairs, pair = i - k * pairs, token = blockIdx.x * p.at.tokens + k;
         if (token < p.at.n_tokens) {
             const int tb = token / p.S, ts = token - tb * p.S;
-            table[k * pairs + (pair % P) * turning + pair / P] = angle(p.turn, pair, __ldg(p.positions + tb * p.pb + ts * p.ps), p.inverse != 0);
+            table[k * each + (pair % P) * columns + pair / P] = angle(p.turn, pair, __ldg(p.positions + tb * p.pb + ts * p.ps), p.inverse != 0);
         }
     }
-    __syncthreads();
+    __syncthreads();                       // the table is complete; and every element has been read (y may be x)
     if (!at.ok) return;
-    if (un.turns) {
-        float2 cs[P];
+    turn_all<T, P, kHalf, kLoose>(x, table + at.in_block * each, u, p.turn.rot, p.D);
+    T *to = static_cast<T *>(p.y) + b * p.yb + s * p.ys;
 #pragma unroll
-        for (int j = 0; j < P; ++j) cs[j] = table[at.in_block * pairs + j * turning + u];
-#pragma unroll
-        for (int k = 0; k < kHeads; ++k) turn<kHalf>(a[k], c[k], cs);
-    }
-    T *y = static_cast<T *>(p.y) + b * p.yb + s * p.ys;
-#pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-        if (h0 + k < p.H) {
-            T *yh = y + (h0 + k) * p.yh;
-            *reinterpret_cast<Vec<T, P> *>(yh + un.a) = a[k];
-            if (un.second) *reinterpret_cast<Vec<T, P> *>(yh + un.b) = c[k];
-        }
-    }
+    for (int k = 0; k < kHeads; ++k)
+        if (h0 + k < p.H) x[k].store(to + (h0 + k) * p.yh, u, p.turn.rot, p.D);
 }
 
 struct AppendParams {
@@ -317,34 +419,29 @@ struct AppendParams {
 // One launch for the new tokens' queries (turned, to q_out), keys (turned, to their page slots) and values (to their
 // page slots).  Token t of row b lies at place lens[b] - n_new[b] + t; one that does not exist (t >= n_new[b], or a
 // negative place) gets a zero query and touches no page.
-template <typename T, int P, bool kHalf>
+template <typename T, int P, bool kHalf, bool kLoose>
 __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const AppendParams p)
 {
+    using Mine = Piece<T, P, kHalf, kLoose>;
     __shared__ float2 table[kTable];
     ptx::wait_for_stream();
     const Place at = place_of(p.at, p.units);
-    const int u = at.unit, pairs = p.turn.rot / 2, turning = pairs / P;
-    const Unit un = unit_at<P, kHalf>(u, p.turn.rot, p.D);
+    const int u = at.unit, pairs = p.turn.rot / 2, columns = Mine::columns(p.turn.rot), each = columns * P;
     const int b = at.token / p.T, t = at.token - b * p.T;
     const int which = at.group < p.q_groups ? 0 : (at.group < p.q_groups + p.kv_groups ? 1 : 2);
     const int h0 = (at.group - (which == 0 ? 0 : (which == 1 ? p.q_groups : p.q_groups + p.kv_groups))) * kHeads;
     const int H = which == 0 ? p.Hq : p.Hkv;
-    Vec<T, P> a[kHeads], c[kHeads];
+    Mine x[kHeads];
     int place = 0, page = -1;
     bool real = false;
     if (at.ok) {
-        const T *x = which == 0 ? static_cast<const T *>(p.q) + b * p.qb + t * p.qt
-                                : (which == 1 ? static_cast<const T *>(p.k) + b * p.kb + t * p.kt : static_cast<const T *>(p.v) + b * p.vb + t * p.vt);
-        const long long xh = which == 0 ? p.qh : (which == 1 ? p.kh : p.vh);
+        const T *from = which == 0 ? static_cast<const T *>(p.q) + b * p.qb + t * p.qt
+                                   : (which == 1 ? static_cast<const T *>(p.k) + b * p.kb + t * p.kt : static_cast<const T *>(p.v) + b * p.vb + t * p.vt);
+        const long long head = which == 0 ? p.qh : (which == 1 ? p.kh : p.vh);
         // (rows and tokens that do not exist are read too: they lie in the caller's tensor)
 #pragma unroll
-        for (int k = 0; k < kHeads; ++k) {
-            if (h0 + k < H) {
-                const T *xr = x + (h0 + k) * xh;
-                a[k] = *reinterpret_cast<const Vec<T, P> *>(xr + un.a);
-                if (un.second) c[k] = *reinterpret_cast<const Vec<T, P> *>(xr + un.b);
-            }
-        }
+        for (int k = 0; k < kHeads; ++k)
+            if (h0 + k < H) x[k].load(from + (h0 + k) * head, u, which == 2 && kLoose ? 0 : p.turn.rot, p.D);
         const int news = p.n_new ? __ldg(p.n_new + b) : p.T;
         place = __ldg(p.lens + b) - news + t;
         real = t < news && place >= 0;
@@ -357,44 +454,33 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const AppendPa
         const int k = i / pairs, pair = i - k * pairs, token = blockIdx.x * p.at.tokens + k;
         if (token < p.at.n_tokens) {
             const int tb = token / p.T, tt = token - tb * p.T;
-            table[k * pairs + (pair % P) * turning + pair / P] =
+            table[k * each + (pair % P) * columns + pair / P] =
                 angle(p.turn, pair, __ldg(p.lens + tb) - (p.n_new ? __ldg(p.n_new + tb) : p.T) + tt, false);
         }
     }
-    __syncthreads();
+    __syncthreads();                       // the table is complete; and every element has been read (q_out may be q)
     if (!at.ok || (which != 0 && !real)) return;
-    T *y;
-    long long yh;
+    T *to;
+    long long head;
     if (which == 0) {
-        y = static_cast<T *>(p.q_out) + static_cast<long long>(at.token) * p.Hq * p.D;
-        yh = p.D;
+        to = static_cast<T *>(p.q_out) + static_cast<long long>(at.token) * p.Hq * p.D;
+        head = p.D;
     } else {
         if (page < 0 || page >= p.n_pages) {                      // a table that does not hold its row's tokens
             atomicOr(p.flags, CSD_CACHE_BAD_PAGE);
             return;
         }
-        y = static_cast<T *>(which == 1 ? p.k_pool : p.v_pool) + page * p.pool_page + (place & ((1 << p.page_shift) - 1)) * p.pool_token;
-        yh = p.pool_head;
+        to = static_cast<T *>(which == 1 ? p.k_pool : p.v_pool) + page * p.pool_page + (place & ((1 << p.page_shift) - 1)) * p.pool_token;
+        head = p.pool_head;
     }
-    if (un.turns && which != 2) {
-        float2 cs[P];
-#pragma unroll
-        for (int j = 0; j < P; ++j) cs[j] = table[at.in_block * pairs + j * turning + u];
-#pragma unroll
-        for (int k = 0; k < kHeads; ++k) turn<kHalf>(a[k], c[k], cs);
-    }
+    if (which != 2) turn_all<T, P, kHalf, kLoose>(x, table + at.in_block * each, u, p.turn.rot, p.D);
     if (!real) {
 #pragma unroll
-        for (int k = 0; k < kHeads; ++k) a[k] = c[k] = Vec<T, P>();
+        for (int k = 0; k < kHeads; ++k) x[k].zero();
     }
 #pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-        if (h0 + k < H) {
-            T *yr = y + (h0 + k) * yh;
-            *reinterpret_cast<Vec<T, P> *>(yr + un.a) = a[k];
-            if (un.second) *reinterpret_cast<Vec<T, P> *>(yr + un.b) = c[k];
-        }
-    }
+    for (int k = 0; k < kHeads; ++k)
+        if (h0 + k < H) x[k].store(to + (h0 + k) * head, u, p.turn.rot, p.D);
 }
 
 }  // namespace rope

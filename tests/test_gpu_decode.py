@@ -56,7 +56,8 @@ def check_rope(y, x, positions, plan, th, dtype, inverse=False):
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("B,S,H,D,rot,scaling", [(2, 5, 3, 64, 64, "none"), (1, 1, 1, 128, 128, "parts"), (3, 7, 5, 80, 32, "yarn"),
                                                  (2, 3, 4, 72, 34, "linear"), (1, 4, 2, 7, 6, "base"), (1, 2, 9, 256, 2, "none"),
-                                                 (2, 33, 8, 96, 96, "base")])
+                                                 (2, 33, 8, 96, 96, "base"), (2, 3, 3, 168, 66, "none"), (1, 2, 2, 601, 70, "linear"), (2, 2, 7, 1024, 1002, "parts"),
+                                                 (1, 3, 2, 4104, 4096, "none"), (2, 40, 1, 8, 2, "none")])
 def test_rope(dtype, layout, B, S, H, D, rot, scaling):
     gen = gen_of(1)
     x = rand(gen, B, S, H, D, dtype=dtype, scale=2.0)
