@@ -12,9 +12,9 @@
 // Bound: memory (every element read once, written once).  A block has a few whole tokens.  Its threads first put the tokens' sines
 // and cosines into shared memory, one per pair and token; then each thread turns one unit (P = 16 bytes' worth of pairs: two
 // 16-byte vectors, neighbouring lanes neighbouring vectors) of kHeads heads, whose loads it has issued before.
-// Where rot does not divide into such units but rows are made of whole vectors, a thread has one vector of kHeads heads instead and
-// reads the partners of its elements one by one (they lie in the same rows, which the block reads anyway): 90.7 us to
-// XX for 85 MB with 66 of 168 elements turned.  Element by element only where rows themselves are not whole vectors.
+// Where rot does not divide into such units but rows are made of whole vectors, a thread has one vector of kHeads heads instead:
+// 38.4 us (interleaved; 90.7 pair by pair) for 170 MB with 66 of 168 elements turned; 268 MB with 126 of 128 turned in 45.9 us
+// interleaved and 72 us half, where 128 of 128 take 44.0.  Pair by pair only where rows themselves are not whole vectors.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -243,40 +243,45 @@ __device__ __forceinline__ Place place_of(const Places &p, int units)
     return r;
 }
 
-// One vector of P elements from e0 of a head's row: every element with its partner.  half: element e < rot/2 pairs with e + rot/2;
-// interleaved: the partners are neighbours.  Elements from rot on keep their bits.
-template <typename T, int P, bool kHalf>
+// One 16-byte vector of a head's row, from element e0, as four words of W = 1 (float32) or 2 elements.  Its elements' partners: in
+// the interleaved layout their neighbours; in the half layout other threads' elements (e < rot/2 pairs with e + rot/2), handed over in
+// shared memory, word j of every thread's vector of head k in plane (k, j), so that lanes read neighbours.  Elements from rot on
+// keep their bits.  With W = 2 and rot/2 odd a word's partners lie in two words, the upper half of one and the lower of another.
+template <typename T>
 struct Loose {
-    alignas(16) T own[P];
-    T other[kHalf ? P : 1];
+    static constexpr int W = 4 / static_cast<int>(sizeof(T));
+    unsigned int w[4];
 
-    __device__ __forceinline__ void load(const T *row, int e0, int rot)
+    __device__ __forceinline__ void load(const T *row, int e0)
     {
-        *reinterpret_cast<Vec<T, P> *>(own) = *reinterpret_cast<const Vec<T, P> *>(row + e0);
-        if constexpr (kHalf) {
-            const int half = rot / 2;
-            const T *a = row + half, *b = row - half;
-#pragma unroll
-            for (int j = 0; j < P; ++j)
-                if (e0 + j < rot) other[j] = e0 + j < half ? a[e0 + j] : b[e0 + j];
-        }
+        const uint4 v = *reinterpret_cast<const uint4 *>(row + e0);
+        w[0] = v.x;
+        w[1] = v.y;
+        w[2] = v.z;
+        w[3] = v.w;
     }
-    __device__ __forceinline__ void store(T *row, int e0) const { *reinterpret_cast<Vec<T, P> *>(row + e0) = *reinterpret_cast<const Vec<T, P> *>(own); }
-    __device__ __forceinline__ void zero()
+    __device__ __forceinline__ void store(T *row, int e0) const { *reinterpret_cast<uint4 *>(row + e0) = make_uint4(w[0], w[1], w[2], w[3]); }
+    __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0u; }
+    __device__ __forceinline__ void hand_over(unsigned int *planes, int k) const
     {
 #pragma unroll
-        for (int j = 0; j < P; ++j) own[j] = from_f32<T>(0.f);
+        for (int j = 0; j < 4; ++j) planes[(k * 4 + j) * kThreads + threadIdx.x] = w[j];
     }
 };
 
-// What a vector's elements are multiplied by: for all heads the same.
-template <int P, bool kHalf>
+// What a vector's elements are multiplied by, and where their partners lie: for all heads the same.
+template <typename T, bool kHalf>
 struct LooseTurn {
+    static constexpr int W = Loose<T>::W, P = 4 * W;
     float2 cs[kHalf ? P : P / 2];
+    int at[kHalf ? 4 : 1], at_next[kHalf && W == 2 ? 4 : 1];
+
+    static __device__ __forceinline__ int place(int element, int first) { return element / W % 4 * kThreads + first + element / P; }
+
     // table: pair i at (i % P) * columns + i / P
     __device__ __forceinline__ LooseTurn(const float2 *table, int columns, int e0, int rot)
     {
-        const int half = rot / 2;
+        const int half = rot / 2, first = static_cast<int>(threadIdx.x) - e0 / P;           // the thread with the row's first vector
 #pragma unroll
         for (int j = 0; j < (kHalf ? P : P / 2); ++j) {
             const int e = e0 + j, i = kHalf ? (e < half ? e : e - half) : e0 / 2 + j;
@@ -285,22 +290,49 @@ struct LooseTurn {
                 if (kHalf && e < half) cs[j].y = -cs[j].y;         // x0 cos - x1 sin: the product with the sign changed is the same product
             }
         }
-    }
-    template <typename T>
-    __device__ __forceinline__ void apply(Loose<T, P, kHalf> &v, int e0, int rot) const
-    {
         if constexpr (kHalf) {
 #pragma unroll
-            for (int j = 0; j < P; ++j)
-                if (e0 + j < rot) v.own[j] = from_f32<T>(__fmaf_rn(to_f32(v.own[j]), cs[j].x, __fmul_rn(to_f32(v.other[j]), cs[j].y)));
+            for (int j = 0; j < 4; ++j) {
+                const int e = e0 + j * W;
+                if (e < rot) {
+                    at[j] = place(e < half ? e + half : e - half, first);
+                    if constexpr (W == 2) at_next[j] = place(e + 1 < half ? e + 1 + half : e + 1 - half, first);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void apply(Loose<T> &v, const unsigned int *planes, int k, int e0, int rot) const
+    {
+        if constexpr (kHalf) {
+            const unsigned int *of_head = planes + k * 4 * kThreads;
+            const bool odd = (rot / 2) & 1;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (e0 + j * W < rot) {
+                    unsigned int y = of_head[at[j]];
+                    if constexpr (W == 1) {
+                        v.w[j] = __float_as_uint(__fmaf_rn(__uint_as_float(v.w[j]), cs[j].x, __fmul_rn(__uint_as_float(y), cs[j].y)));
+                    } else {
+                        if (odd) y = __funnelshift_r(y, of_head[at_next[j]], 16);
+                        const float2 fx = unpack_word<T>(v.w[j]), fy = unpack_word<T>(y);
+                        float r0, r1;
+                        unpack2(fma2(pack2(fx.x, fx.y), pack2(cs[2 * j].x, cs[2 * j + 1].x), mul2(pack2(fy.x, fy.y), pack2(cs[2 * j].y, cs[2 * j + 1].y))), r0, r1);
+                        v.w[j] = pack_word<T>(r0, r1);
+                    }
+                }
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < P / 2; ++j)
                 if (e0 + 2 * j < rot) {
-                    float x = to_f32(v.own[2 * j]), y = to_f32(v.own[2 * j + 1]);
-                    turn_pair(x, y, cs[j]);
-                    v.own[2 * j] = from_f32<T>(x);
-                    v.own[2 * j + 1] = from_f32<T>(y);
+                    if constexpr (W == 1) {
+                        float x = __uint_as_float(v.w[2 * j]), y = __uint_as_float(v.w[2 * j + 1]);
+                        turn_pair(x, y, cs[j]);
+                        v.w[2 * j] = __float_as_uint(x);
+                        v.w[2 * j + 1] = __float_as_uint(y);
+                    } else {
+                        turn_word_interleaved<T>(v.w[j], cs[j]);
+                    }
                 }
         }
     }
@@ -330,22 +362,22 @@ struct Piece<T, P, kHalf, false> {
 };
 template <typename T, int P, bool kHalf>
 struct Piece<T, P, kHalf, true> {
-    Loose<T, P, kHalf> v;
+    Loose<T> v;
     static __device__ __forceinline__ int columns(int rot) { return (rot / 2 + P - 1) / P; }
-    __device__ __forceinline__ void load(const T *row, int u, int rot, int) { v.load(row, u * P, rot); }
+    __device__ __forceinline__ void load(const T *row, int u, int, int) { v.load(row, u * P); }
     __device__ __forceinline__ void store(T *row, int u, int, int) const { v.store(row, u * P); }
     __device__ __forceinline__ void zero() { v.zero(); }
 };
 
 // All heads of a thread turned by its token's table.
 template <typename T, int P, bool kHalf, bool kLoose, int kHeads_>
-__device__ __forceinline__ void turn_all(Piece<T, P, kHalf, kLoose> (&x)[kHeads_], const float2 *table, int u, int rot, int D)
+__device__ __forceinline__ void turn_all(Piece<T, P, kHalf, kLoose> (&x)[kHeads_], const float2 *table, const unsigned int *planes, int u, int rot, int D)
 {
     const int columns = Piece<T, P, kHalf, kLoose>::columns(rot);
     if constexpr (kLoose) {
-        const LooseTurn<P, kHalf> by(table, columns, u * P, rot);
+        const LooseTurn<T, kHalf> by(table, columns, u * P, rot);
 #pragma unroll
-        for (int k = 0; k < kHeads_; ++k) by.apply(x[k].v, u * P, rot);
+        for (int k = 0; k < kHeads_; ++k) by.apply(x[k].v, planes, k, u * P, rot);
     } else if (unit_at<P, kHalf>(u, rot, D).turns) {
         float2 cs[P];
 #pragma unroll
@@ -373,6 +405,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_kernel(const RopeParams p)
 {
     using Mine = Piece<T, P, kHalf, kLoose>;
     __shared__ float2 table[kTable];
+    __shared__ unsigned int planes[kLoose && kHalf ? kThreads * kHeads * 4 : 1];
     ptx::wait_for_stream();
     const Place at = place_of(p.at, p.units);
     const int u = at.unit, h0 = at.group * kHeads, pairs = p.turn.rot / 2, columns = Mine::columns(p.turn.rot), each = columns * P;
@@ -384,7 +417,10 @@ __global__ void __launch_bounds__(kThreads, 3) rope_kernel(const RopeParams p)
         const T *from = static_cast<const T *>(p.x) + b * p.xb + s * p.xs;
 #pragma unroll
         for (int k = 0; k < kHeads; ++k)
-            if (h0 + k < p.H) x[k].load(from + (h0 + k) * p.xh, u, p.turn.rot, p.D);
+            if (h0 + k < p.H) {
+                x[k].load(from + (h0 + k) * p.xh, u, p.turn.rot, p.D);
+                if constexpr (kLoose && kHalf) x[k].v.hand_over(planes, k);
+            }
     }
     for (int i = threadIdx.x; i < p.at.tokens * pairs; i += kThreads) {
         const int k = i / pairs, pair = i - k * pairs, token = blockIdx.x * p.at.tokens + k;
@@ -395,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_kernel(const RopeParams p)
     }
     __syncthreads();                       // the table is complete; and every element has been read (y may be x)
     if (!at.ok) return;
-    turn_all<T, P, kHalf, kLoose>(x, table + at.in_block * each, u, p.turn.rot, p.D);
+    turn_all<T, P, kHalf, kLoose>(x, table + at.in_block * each, planes, u, p.turn.rot, p.D);
     T *to = static_cast<T *>(p.y) + b * p.yb + s * p.ys;
 #pragma unroll
     for (int k = 0; k < kHeads; ++k)
@@ -424,6 +460,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const AppendPa
 {
     using Mine = Piece<T, P, kHalf, kLoose>;
     __shared__ float2 table[kTable];
+    __shared__ unsigned int planes[kLoose && kHalf ? kThreads * kHeads * 4 : 1];
     ptx::wait_for_stream();
     const Place at = place_of(p.at, p.units);
     const int u = at.unit, pairs = p.turn.rot / 2, columns = Mine::columns(p.turn.rot), each = columns * P;
@@ -441,7 +478,10 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const AppendPa
         // (rows and tokens that do not exist are read too: they lie in the caller's tensor)
 #pragma unroll
         for (int k = 0; k < kHeads; ++k)
-            if (h0 + k < H) x[k].load(from + (h0 + k) * head, u, which == 2 && kLoose ? 0 : p.turn.rot, p.D);
+            if (h0 + k < H) {
+                x[k].load(from + (h0 + k) * head, u, p.turn.rot, p.D);
+                if constexpr (kLoose && kHalf) x[k].v.hand_over(planes, k);
+            }
         const int news = p.n_new ? __ldg(p.n_new + b) : p.T;
         place = __ldg(p.lens + b) - news + t;
         real = t < news && place >= 0;
@@ -473,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const AppendPa
         to = static_cast<T *>(which == 1 ? p.k_pool : p.v_pool) + page * p.pool_page + (place & ((1 << p.page_shift) - 1)) * p.pool_token;
         head = p.pool_head;
     }
-    if (which != 2) turn_all<T, P, kHalf, kLoose>(x, table + at.in_block * each, u, p.turn.rot, p.D);
+    if (which != 2) turn_all<T, P, kHalf, kLoose>(x, table + at.in_block * each, planes, u, p.turn.rot, p.D);
     if (!real) {
 #pragma unroll
         for (int k = 0; k < kHeads; ++k) x[k].zero();
