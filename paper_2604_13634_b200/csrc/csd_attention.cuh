@@ -13,12 +13,12 @@
 //                     device), so a block works on a run of tiles of a few (row, head) units.
 //       producer warp  puts the tile's keys and values, page by page, into a ring of shared-memory stages by TMA (boxes of
 //                     64 elements x the places of one page, 128-byte swizzle; elements beyond dim read as zero)
-//       consumer warps KG x RG of them: a warp owns 16 MT of the unit's query rows and 16 NK of a tile's places, with
-//                     its own running (m, l, O) in registers: no exchange between warps until the unit ends.  Products
-//                     are mma.sync m16n8k16 (16 x 8 x 16) with float32 accumulators: a tile has at most 128 query rows, the
-//                     tensor pipe is far from its limit while the tiles stream.
-//     At the end of a unit the KG warps of a row group join through a ring stage; a unit that lies in one block whole is
-//     written out, otherwise the part goes to the workspace.
+//       consumer warps four: a warp owns 16 NK of a tile's places, against all of the unit's query rows (at most 16), with its
+//                     own running (m, l, O) in registers: no exchange between warps until the unit ends.  Products are
+//                     mma.sync m16n8k16 with float32 accumulators: with 16 query rows the tensor pipe is at a tenth of its
+//                     limit while the tiles stream.
+//     At the end of a unit the warps join through a ring stage; a unit that lies in one block whole is written out, otherwise
+//     the part goes to the workspace.
 //   attention_join_kernel  joins the parts of the units that were split (at most one begins in each block), a warp per query row, in
 //                     the order of the places.
 // No block waits for another; waits inside a block are bounded.
@@ -81,13 +81,14 @@ struct Params {
     long long pool_page, pool_head, pool_token;
 };
 
-template <typename T_, int DP_, int MT_, int NK_, int KG_, int RG_, int kBlocksPerSm_>
+// A variant of the mma.sync kernel: dim padded to DP, 16 NK places to a warp and tile.
+template <typename T_, int DP_, int NK_, int kBlocksPerSm_>
 struct Config {
     using T = T_;
-    static constexpr int DP = DP_, MT = MT_, NK = NK_, KG = KG_, RG = RG_, kBlocksPerSm = kBlocksPerSm_;
-    static constexpr int kTile = 16 * NK * KG;
-    static constexpr int kRows = 16 * MT * RG;
-    static constexpr int kWarps = KG * RG;
+    static constexpr int DP = DP_, NK = NK_, kBlocksPerSm = kBlocksPerSm_;
+    static constexpr int kWarps = 4;
+    static constexpr int kTile = 16 * NK * kWarps;
+    static constexpr int kRows = 16;
     // Registers move between warpgroups of four warps: the producer's gives up what it does not need.
     static constexpr int kThreads = 32 * (kWarps + 4);
     static constexpr int kGroups = kWarps / 4 + 1;
@@ -95,21 +96,16 @@ struct Config {
     static constexpr bool kMoveRegs = kLaunchRegs < 232;
     static constexpr int kProducerRegs = 40;
     static constexpr int kConsumerRegs = (kGroups * kLaunchRegs - kProducerRegs) / (kGroups - 1) / 8 * 8;
-    static_assert(kWarps % 4 == 0 && (!kMoveRegs || (kConsumerRegs <= 240 && kConsumerRegs * (kGroups - 1) + kProducerRegs <= kGroups * kLaunchRegs)),
-                  "register split");
+    static_assert(!kMoveRegs || (kConsumerRegs <= 240 && kConsumerRegs * (kGroups - 1) + kProducerRegs <= kGroups * kLaunchRegs), "register split");
     static constexpr int kHalves = DP / 64;                        // 128-byte columns of a tile
     static constexpr int kTileBytes = kTile * DP * 2;               // keys or values of a stage
     static constexpr int kStageBytes = 2 * kTileBytes;
     static constexpr int kQBytes = kRows * DP * 2;
-    static constexpr int kMlBytes = KG * kRows * 8;
+    static constexpr int kMlBytes = kWarps * kRows * 8;
     static constexpr int kSlotFloats = kRows * (DP + 2);
-    static constexpr bool kQInRegisters = MT == 1 && DP <= 128;
-    // joining warps: KG / 2 buffers of the block's rows fit in a stage, column by column block if need be
-    static constexpr int kJoinBytes = KG / 2 * kRows * DP * 4;
-    static constexpr int kJoinPasses = KG == 1 ? 1 : (kJoinBytes + kStageBytes - 1) / kStageBytes;
+    static constexpr bool kQInRegisters = DP <= 128;
     static constexpr int kNt = DP / 8;                              // column tiles of 8
-    static constexpr int kNtPass = kNt / kJoinPasses;
-    static_assert(kNt % kJoinPasses == 0, "column passes");
+    static_assert(kWarps * kRows * DP * 4 <= kStageBytes, "the warps' sums fit in a stage");
 };
 
 __device__ __forceinline__ void tma_load_page(unsigned int dst, const CUtensorMap *map, unsigned int bar, int d, int place, int head, int page)
@@ -362,7 +358,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kBlocksPerSm)
 attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p)
 {
     using T = typename C::T;
-    constexpr int DP = C::DP, MT = C::MT, NK = C::NK, KG = C::KG, RG = C::RG, kTile = C::kTile;
+    constexpr int DP = C::DP, NK = C::NK, kTile = C::kTile;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bar_words[3 * kMaxStages];
     __shared__ int give_up_flag;
@@ -372,7 +368,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     const unsigned int ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const unsigned int q_smem = ring + p.n_stages * C::kStageBytes;
     unsigned char *after_q = smem_raw + (q_smem - smem_u32(smem_raw)) + C::kQBytes;
-    float2 *ml = reinterpret_cast<float2 *>(after_q);                              // [KG][kRows]
+    float2 *ml = reinterpret_cast<float2 *>(after_q);                              // [kWarps][kRows]
     int *base = reinterpret_cast<int *>(after_q + C::kMlBytes);                    // [B + 1]
     const unsigned int bars = smem_u32(bar_words);
     auto full_k = [&](int s) { return bars + 8u * s; };
@@ -467,7 +463,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     } else {
         // ---- consumers ----
         if constexpr (C::kMoveRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kConsumerRegs));
-        const int rg = warp / KG, kg = warp % KG;
         const int g = lane >> 2, qd = lane & 3;
         const int cthreads = C::kWarps * 32;
         zero_empty_rows<T>(p, base, tid, cthreads);
@@ -476,9 +471,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         Run run;
         Cursor at_ring = {0, 0u};
         const int swz = lane & 7;
-        const unsigned int k_lane = (16 * NK * kg + ((lane >> 4) << 3) + swz) * 128u, k_chunk = (lane >> 3) & 1;
-        const unsigned int v_lane = (16 * NK * kg + (((lane >> 3) & 1) << 3) + swz) * 128u, v_chunk = lane >> 4;
-        const unsigned int q_lane = (16 * MT * rg + (((lane >> 3) & 1) << 3) + swz) * 128u, q_chunk = lane >> 4;
+        const unsigned int k_lane = (16 * NK * warp + ((lane >> 4) << 3) + swz) * 128u, k_chunk = (lane >> 3) & 1;
+        const unsigned int v_lane = (16 * NK * warp + (((lane >> 3) & 1) << 3) + swz) * 128u, v_chunk = lane >> 4;
+        const unsigned int q_lane = ((((lane >> 3) & 1) << 3) + swz) * 128u, q_chunk = lane >> 4;
 
         while (runs.next(run)) {
             // ---- a unit, or the part of one that lies in this block ----
@@ -497,129 +492,109 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
             }
             consumer_barrier(cthreads);
-            int limit[MT][2];                                       // last place that the thread's rows see; -1: none
+            int limit[2];                                           // last place that the thread's rows see; -1: none
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const int r = 16 * (MT * rg + mt) + g + 8 * hh, rr = rt * C::kRows + r;
-                    const int tok = rr / p.group;
-                    limit[mt][hh] = r < rows_here && tok < news ? len - news + tok : -1;
-                }
+            for (int hh = 0; hh < 2; ++hh) {
+                const int r = g + 8 * hh, rr = rt * C::kRows + r, tok = rr / p.group;
+                limit[hh] = r < rows_here && tok < news ? len - news + tok : -1;
+            }
             unsigned int qf[C::kQInRegisters ? DP / 16 : 1][4];
             if constexpr (C::kQInRegisters) {
 #pragma unroll
                 for (int ks = 0; ks < DP / 16; ++ks)
                     ldsm4(qf[ks], q_smem + (ks >> 2) * (C::kRows * 128) + q_lane + ((((ks & 3) * 2 + q_chunk) ^ swz) << 4));
             }
-            float o[MT][C::kNt][4], m[MT][2], l[MT][2];
+            float o[C::kNt][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
+            for (int nt = 0; nt < C::kNt; ++nt)
 #pragma unroll
-                for (int nt = 0; nt < C::kNt; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[mt][nt][e] = 0.f;
-                m[mt][0] = m[mt][1] = -INFINITY;
-                l[mt][0] = l[mt][1] = 0.f;
-            }
+                for (int e = 0; e < 4; ++e) o[nt][e] = 0.f;
 
             for (int j = j0; j < j1; ++j, at_ring.next(p.n_stages)) {
                 const int s = at_ring.slot;
                 const unsigned int parity = at_ring.round;
                 const unsigned int k_at = ring + s * C::kStageBytes, v_at = k_at + C::kTileBytes;
-                const int key0 = j * kTile + 16 * NK * kg;          // the warp's first place
-                float x[MT][2 * NK][4];
+                const int key0 = j * kTile + 16 * NK * warp;          // the warp's first place
+                float x[2 * NK][4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int n = 0; n < 2 * NK; ++n)
 #pragma unroll
-                    for (int n = 0; n < 2 * NK; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[mt][n][e] = 0.f;
+                    for (int e = 0; e < 4; ++e) x[n][e] = 0.f;
                 mbar_wait(full_k(s), parity, give_up);
                 const bool any = key0 < len;                         // nothing of the warp's places exists otherwise
                 if (any) {
 #pragma unroll
                     for (int ks = 0; ks < DP / 16; ++ks) {
-                        unsigned int qa[MT][4];
+                        unsigned int qa[4];
+                        if constexpr (C::kQInRegisters) {
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            if constexpr (C::kQInRegisters) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) qa[mt][e] = qf[ks][e];
-                            } else {
-                                ldsm4(qa[mt], q_smem + (ks >> 2) * (C::kRows * 128) + q_lane + mt * (16 * 128) + ((((ks & 3) * 2 + q_chunk) ^ swz) << 4));
-                            }
+                            for (int e = 0; e < 4; ++e) qa[e] = qf[ks][e];
+                        } else {
+                            ldsm4(qa, q_smem + (ks >> 2) * (C::kRows * 128) + q_lane + ((((ks & 3) * 2 + q_chunk) ^ swz) << 4));
                         }
 #pragma unroll
                         for (int nk = 0; nk < NK; ++nk) {
                             unsigned int kb[4];
                             ldsm4(kb, k_at + (ks >> 2) * (kTile * 128) + k_lane + nk * (16 * 128) + ((((ks & 3) * 2 + k_chunk) ^ swz) << 4));
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) {
-                                mma16816<T>(x[mt][2 * nk], qa[mt], kb[0], kb[1]);
-                                mma16816<T>(x[mt][2 * nk + 1], qa[mt], kb[2], kb[3]);
-                            }
+                            mma16816<T>(x[2 * nk], qa, kb[0], kb[1]);
+                            mma16816<T>(x[2 * nk + 1], qa, kb[2], kb[3]);
                         }
                     }
                 }
                 // scores in powers of two; places that a row does not see become -inf whatever was computed for them
                 const bool edge = key0 + 16 * NK - 1 > len - news;   // some row does not see all of the warp's places
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int n = 0; n < 2 * NK; ++n)
 #pragma unroll
-                    for (int n = 0; n < 2 * NK; ++n)
+                    for (int e = 0; e < 4; ++e) {
+                        x[n][e] *= p.scale_log2;
+                        if (edge && key0 + 8 * n + 2 * qd + (e & 1) > limit[e >> 1]) x[n][e] = -INFINITY;
+                    }
+                float mx[2], at0[2];
+                bool grew = false;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            x[mt][n][e] *= p.scale_log2;
-                            if (edge && key0 + 8 * n + 2 * qd + (e & 1) > limit[mt][e >> 1]) x[mt][n][e] = -INFINITY;
-                        }
-                unsigned int pa[MT][NK][4];
+                for (int hh = 0; hh < 2; ++hh) {
+                    float v = x[0][2 * hh];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    float mx[2], f[2], at0[2];
-                    bool grew = false;
+                    for (int n = 0; n < 2 * NK; ++n) v = fmaxf(v, fmaxf(x[n][2 * hh], x[n][2 * hh + 1]));
+                    v = fmaxf(v, __shfl_xor_sync(kFull, v, 1));
+                    v = fmaxf(v, __shfl_xor_sync(kFull, v, 2));
+                    mx[hh] = fmaxf(m[hh], v);
+                    grew |= mx[hh] > m[hh];
+                    at0[hh] = mx[hh] == -INFINITY ? 0.f : mx[hh];
+                }
+                if (__any_sync(kFull, grew)) {
+                    float f[2];
 #pragma unroll
                     for (int hh = 0; hh < 2; ++hh) {
-                        float v = x[mt][0][2 * hh];
-#pragma unroll
-                        for (int n = 0; n < 2 * NK; ++n) v = fmaxf(v, fmaxf(x[mt][n][2 * hh], x[mt][n][2 * hh + 1]));
-                        v = fmaxf(v, __shfl_xor_sync(kFull, v, 1));
-                        v = fmaxf(v, __shfl_xor_sync(kFull, v, 2));
-                        mx[hh] = fmaxf(m[mt][hh], v);
-                        grew |= mx[hh] > m[mt][hh];
-                        at0[hh] = mx[hh] == -INFINITY ? 0.f : mx[hh];
-                    }
-                    if (__any_sync(kFull, grew)) {
-#pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-                            f[hh] = ex2_approx(m[mt][hh] - at0[hh]);
-                            l[mt][hh] *= f[hh];
-                            m[mt][hh] = mx[hh];
-                        }
-#pragma unroll
-                        for (int nt = 0; nt < C::kNt; ++nt) {
-                            o[mt][nt][0] *= f[0];
-                            o[mt][nt][1] *= f[0];
-                            o[mt][nt][2] *= f[1];
-                            o[mt][nt][3] *= f[1];
-                        }
+                        f[hh] = ex2_approx(m[hh] - at0[hh]);
+                        l[hh] *= f[hh];
+                        m[hh] = mx[hh];
                     }
 #pragma unroll
-                    for (int n = 0; n < 2 * NK; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            x[mt][n][e] = ex2_approx(x[mt][n][e] - at0[e >> 1]);
-                            l[mt][e >> 1] += x[mt][n][e];
-                        }
-                    // the weights go into the second product in the cache's type: relative error 2^-9 (2^-12) of each, of random
-                    // sign, where the result itself is rounded to that type; the sum l is taken before the rounding
-#pragma unroll
-                    for (int nk = 0; nk < NK; ++nk) {
-                        pa[mt][nk][0] = pack_pair<T>(x[mt][2 * nk][0], x[mt][2 * nk][1]);
-                        pa[mt][nk][1] = pack_pair<T>(x[mt][2 * nk][2], x[mt][2 * nk][3]);
-                        pa[mt][nk][2] = pack_pair<T>(x[mt][2 * nk + 1][0], x[mt][2 * nk + 1][1]);
-                        pa[mt][nk][3] = pack_pair<T>(x[mt][2 * nk + 1][2], x[mt][2 * nk + 1][3]);
+                    for (int nt = 0; nt < C::kNt; ++nt) {
+                        o[nt][0] *= f[0];
+                        o[nt][1] *= f[0];
+                        o[nt][2] *= f[1];
+                        o[nt][3] *= f[1];
                     }
+                }
+#pragma unroll
+                for (int n = 0; n < 2 * NK; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[n][e] = ex2_approx(x[n][e] - at0[e >> 1]);
+                        l[e >> 1] += x[n][e];
+                    }
+                // the weights go into the second product in the cache's type: relative error 2^-9 (2^-12) of each, of random sign,
+                // where the result itself is rounded to that type; the sum l is taken before the rounding
+                unsigned int pa[NK][4];
+#pragma unroll
+                for (int nk = 0; nk < NK; ++nk) {
+                    pa[nk][0] = pack_pair<T>(x[2 * nk][0], x[2 * nk][1]);
+                    pa[nk][1] = pack_pair<T>(x[2 * nk][2], x[2 * nk][3]);
+                    pa[nk][2] = pack_pair<T>(x[2 * nk + 1][0], x[2 * nk + 1][1]);
+                    pa[nk][3] = pack_pair<T>(x[2 * nk + 1][2], x[2 * nk + 1][3]);
                 }
                 mbar_wait(full_v(s), parity, give_up);
                 bool odd_values = false, wrote = false;
@@ -630,7 +605,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     bool odd = false;
                     for (int i = lane; i < 16 * NK * (DP / 8); i += 32) {
                         const int r = i / (DP / 8), ch = i % (DP / 8), key = key0 + r;
-                        const unsigned int at = v_at + (ch >> 3) * (kTile * 128) + (16 * NK * kg + r) * 128 + (((ch & 7) ^ (r & 7)) << 4);
+                        const unsigned int at = v_at + (ch >> 3) * (kTile * 128) + (16 * NK * warp + r) * 128 + (((ch & 7) ^ (r & 7)) << 4);
                         if (key >= len) {
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
                             wrote = true;
@@ -654,33 +629,28 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) vb[e] = finite_only<T>(vb[e]);
                             }
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) {
-                                mma16816<T>(o[mt][2 * n2], pa[mt][nk], vb[0], vb[1]);
-                                mma16816<T>(o[mt][2 * n2 + 1], pa[mt][nk], vb[2], vb[3]);
-                            }
+                            mma16816<T>(o[2 * n2], pa[nk], vb[0], vb[1]);
+                            mma16816<T>(o[2 * n2 + 1], pa[nk], vb[2], vb[3]);
                         }
                 }
                 if (odd_values) {                                    // what was left out, for the rows that see it
                     for (int r = 0; r < 16 * NK && key0 + r < len; ++r) {
                         const int src = (lane & ~3) | ((r & 7) >> 1);
-                        float wt[MT][2];
+                        float wt[2];
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
+                        for (int hh = 0; hh < 2; ++hh) {
+                            wt[hh] = 0.f;
 #pragma unroll
-                            for (int hh = 0; hh < 2; ++hh) {
-                                wt[mt][hh] = 0.f;
+                            for (int n = 0; n < 2 * NK; ++n)
 #pragma unroll
-                                for (int n = 0; n < 2 * NK; ++n)
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e) {
-                                        const float y = __shfl_sync(kFull, x[mt][n][2 * hh + e], src);
-                                        if (n == (r >> 3) && e == (r & 1)) wt[mt][hh] = y;
-                                    }
-                            }
+                                for (int e = 0; e < 2; ++e) {
+                                    const float y = __shfl_sync(kFull, x[n][2 * hh + e], src);
+                                    if (n == (r >> 3) && e == (r & 1)) wt[hh] = y;
+                                }
+                        }
 #pragma unroll
                         for (int nt = 0; nt < C::kNt; ++nt) {
-                            const unsigned int at = v_at + (nt >> 3) * (kTile * 128) + (16 * NK * kg + r) * 128 + (((nt & 7) ^ (r & 7)) << 4) + 4 * qd;
+                            const unsigned int at = v_at + (nt >> 3) * (kTile * 128) + (16 * NK * warp + r) * 128 + (((nt & 7) ^ (r & 7)) << 4) + 4 * qd;
                             unsigned int two;
                             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(two) : "r"(at) : "memory");
                             const unsigned int kept = finite_only<T>(two);
@@ -688,13 +658,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                             const float v0 = rope::to_f32(pair[0]), v1 = rope::to_f32(pair[1]);
                             const bool odd0 = (two ^ kept) & 0xffffu, odd1 = (two ^ kept) & 0xffff0000u;
 #pragma unroll
-                            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                                for (int hh = 0; hh < 2; ++hh)
-                                    if (key0 + r <= limit[mt][hh]) {
-                                        if (odd0) o[mt][nt][2 * hh] += wt[mt][hh] * v0;
-                                        if (odd1) o[mt][nt][2 * hh + 1] += wt[mt][hh] * v1;
-                                    }
+                            for (int hh = 0; hh < 2; ++hh)
+                                if (key0 + r <= limit[hh]) {
+                                    if (odd0) o[nt][2 * hh] += wt[hh] * v0;
+                                    if (odd1) o[nt][2 * hh + 1] += wt[hh] * v1;
+                                }
                         }
                     }
                 }
@@ -704,115 +672,73 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 if (lane == 0) mbar_arrive(empty(s));
             }
 
-            // ---- the unit's rows: join the KG warps of a row group ----
+            // ---- the unit's rows: the warps' sums meet in the next stage, and the rows leave from there side by side ----
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    l[mt][hh] += __shfl_xor_sync(kFull, l[mt][hh], 1);
-                    l[mt][hh] += __shfl_xor_sync(kFull, l[mt][hh], 2);
-                    if (limit[mt][hh] < 0) {                          // a row without a token, or one that sees nothing
-                        m[mt][hh] = -INFINITY;
-                        l[mt][hh] = 0.f;
-#pragma unroll
-                        for (int nt = 0; nt < C::kNt; ++nt) o[mt][nt][2 * hh] = o[mt][nt][2 * hh + 1] = 0.f;
-                    }
-                    if (KG > 1 && qd == 0) ml[kg * C::kRows + 16 * (MT * rg + mt) + g + 8 * hh] = make_float2(m[mt][hh], l[mt][hh]);
+            for (int hh = 0; hh < 2; ++hh) {
+                l[hh] += __shfl_xor_sync(kFull, l[hh], 1);
+                l[hh] += __shfl_xor_sync(kFull, l[hh], 2);
+                if (limit[hh] < 0) {                                  // a row without a token, or one that sees nothing
+                    m[hh] = -INFINITY;
+                    l[hh] = 0.f;
                 }
-            if constexpr (KG > 1) {
-                consumer_barrier(cthreads);                           // also: every warp is done with the tiles before
-                const unsigned int buf = ring + at_ring.slot * C::kStageBytes;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        const int r = 16 * (MT * rg + mt) + g + 8 * hh;
-                        float M = -INFINITY, L = 0.f;
-#pragma unroll
-                        for (int k = 0; k < KG; ++k) M = fmaxf(M, ml[k * C::kRows + r].x);
-#pragma unroll
-                        for (int k = 0; k < KG; ++k) {
-                            const float2 y = ml[k * C::kRows + r];
-                            L += y.y * (y.x == -INFINITY ? 0.f : ex2_approx(y.x - M));
-                        }
-                        const float f = m[mt][hh] == -INFINITY ? 0.f : ex2_approx(m[mt][hh] - M);
-#pragma unroll
-                        for (int nt = 0; nt < C::kNt; ++nt) {
-                            o[mt][nt][2 * hh] *= f;
-                            o[mt][nt][2 * hh + 1] *= f;
-                        }
-                        m[mt][hh] = M;
-                        l[mt][hh] = L;
-                    }
-#pragma unroll
-                for (int pass = 0; pass < C::kJoinPasses; ++pass)
-#pragma unroll
-                    for (int half = KG / 2; half >= 1; half /= 2) {
-                        if (pass > 0 || half < KG / 2) consumer_barrier(cthreads);
-                        const int pair = kg % half;
-                        const unsigned int at = buf + ((pair * RG + rg) * MT * C::kNtPass * 32 + lane) * 16;
-                        if (kg >= half && kg < 2 * half) {
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                                for (int nt = 0; nt < C::kNtPass; ++nt) {
-                                    const float(&y)[4] = o[mt][pass * C::kNtPass + nt];
-                                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at + (mt * C::kNtPass + nt) * 512), "f"(y[0]), "f"(y[1]),
-                                                 "f"(y[2]), "f"(y[3])
-                                                 : "memory");
-                                }
-                        }
-                        consumer_barrier(cthreads);
-                        if (kg < half) {
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                                for (int nt = 0; nt < C::kNtPass; ++nt) {
-                                    float y[4];
-                                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                                                 : "=f"(y[0]), "=f"(y[1]), "=f"(y[2]), "=f"(y[3])
-                                                 : "r"(at + (mt * C::kNtPass + nt) * 512)
-                                                 : "memory");
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) o[mt][pass * C::kNtPass + nt][e] += y[e];
-                                }
-                        }
-                    }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(empty(at_ring.slot));
-                at_ring.next(p.n_stages);
+                if (qd == 0) ml[warp * C::kRows + g + 8 * hh] = make_float2(m[hh], l[hh]);
             }
+            consumer_barrier(cthreads);                               // every warp is done with the tiles before: the stage is free
+            // element (row, column) of a warp's sums; the columns' order within a row is turned by the row, so that the eight rows a
+            // warp writes at once fall on different banks
+            float *sums = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw)) + at_ring.slot * C::kStageBytes);
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const int r = g + 8 * hh;
+                if (r < rows_here) {
+#pragma unroll
+                    for (int nt = 0; nt < C::kNt; ++nt)
+                        *reinterpret_cast<float2 *>(sums + (warp * C::kRows + r) * DP + ((nt * 8) ^ ((r & 3) << 3)) + 2 * qd) =
+                            limit[hh] < 0 ? make_float2(0.f, 0.f) : make_float2(o[nt][2 * hh], o[nt][2 * hh + 1]);
+                }
+            }
+            consumer_barrier(cthreads);
             const bool whole = run.ns == run.n;
-            if (kg == 0) {
-                const int slot = 2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0);
-                float *part = p.parts + static_cast<long long>(slot) * C::kSlotFloats;
+            float *part = p.parts + static_cast<long long>(2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0)) * C::kSlotFloats;
+            for (int i = tid; i < rows_here * (DP / 4); i += cthreads) {
+                const int r = i / (DP / 4), c = i % (DP / 4) * 4;
+                float2 y[C::kWarps];
+                float M = -INFINITY, L = 0.f;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int k = 0; k < C::kWarps; ++k) {
+                    y[k] = ml[k * C::kRows + r];
+                    M = fmaxf(M, y[k].x);
+                }
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        const int r = 16 * (MT * rg + mt) + g + 8 * hh;
-                        if (r >= rows_here) continue;
-                        const float L = l[mt][hh];
-                        if (whole) {
-                            const int rr = rt * C::kRows + r, tok = rr / p.group, head = h * p.group + rr - tok * p.group;
-                            const long long row = (static_cast<long long>(b) * p.T + tok) * p.Hq + head;
-                            const float inv = L == 0.f ? 0.f : 1.f / L;
-                            unsigned int *out = reinterpret_cast<unsigned int *>(static_cast<T *>(p.out) + row * p.D);
-#pragma unroll
-                            for (int nt = 0; nt < C::kNt; ++nt)
-                                if (nt * 8 < p.D) out[nt * 4 + qd] = pack_pair<T>(o[mt][nt][2 * hh] * inv, o[mt][nt][2 * hh + 1] * inv);
-                            if (p.lse && qd == 0) p.lse[row] = L == 0.f ? -INFINITY : (fmaxf(m[mt][hh], -3e38f) + log2f(L)) * kLn2;
-                        } else {
-#pragma unroll
-                            for (int nt = 0; nt < C::kNt; ++nt)
-                                if (nt * 8 < p.D)
-                                    __stcg(reinterpret_cast<float2 *>(part + r * DP + nt * 8 + 2 * qd), make_float2(o[mt][nt][2 * hh], o[mt][nt][2 * hh + 1]));
-                            if (qd == 0) __stcg(reinterpret_cast<float2 *>(part + C::kRows * DP + 2 * r), make_float2(m[mt][hh], L));
-                        }
+                for (int k = 0; k < C::kWarps; ++k) {
+                    // (a warp that has seen nothing adds nothing; one whose scores were all NaN keeps its NaN)
+                    const float f = y[k].x == -INFINITY ? (y[k].y == 0.f ? 0.f : y[k].y) : ex2_approx(y[k].x - M);
+                    const float4 z = *reinterpret_cast<const float4 *>(sums + (k * C::kRows + r) * DP + (c ^ ((r & 3) << 3)));
+                    L += y[k].y * f;
+                    sum.x += z.x * f;
+                    sum.y += z.y * f;
+                    sum.z += z.z * f;
+                    sum.w += z.w * f;
+                }
+                if (c < p.D) {
+                    if (whole) {
+                        const int rr = rt * C::kRows + r, tok = rr / p.group, head = h * p.group + rr - tok * p.group;
+                        const long long row = (static_cast<long long>(b) * p.T + tok) * p.Hq + head;
+                        const float inv = L == 0.f ? 0.f : 1.f / L;
+                        *reinterpret_cast<uint2 *>(static_cast<T *>(p.out) + row * p.D + c) =
+                            make_uint2(pack_pair<T>(sum.x * inv, sum.y * inv), pack_pair<T>(sum.z * inv, sum.w * inv));
+                        if (p.lse && c == 0) p.lse[row] = L == 0.f ? -INFINITY : (fmaxf(M, -3e38f) + log2f(L)) * kLn2;
+                    } else {
+                        __stcg(reinterpret_cast<float4 *>(part + r * DP + c), sum);
+                        if (c == 0) __stcg(reinterpret_cast<float2 *>(part + C::kRows * DP + 2 * r), make_float2(M, L));
                     }
+                }
             }
-            if constexpr (KG == 1) consumer_barrier(cthreads);          // the query rows in shared memory are done with
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty(at_ring.slot));
+            at_ring.next(p.n_stages);
         }
     }
     if (*give_up && tid % 32 == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);

@@ -277,9 +277,9 @@ template <typename T, typename F>
 auto with_config(int dim, F f)
 {
     using attention::Config;
-    if (dim <= 64) return f(Config<T, 64, 1, 2, 4, 1, 2>());
-    if (dim <= 128) return f(Config<T, 128, 1, 1, 4, 1, 2>());
-    return f(Config<T, 256, 1, 1, 4, 1, 1>());
+    if (dim <= 64) return f(Config<T, 64, 2, 2>());
+    if (dim <= 128) return f(Config<T, 128, 1, 2>());
+    return f(Config<T, 256, 1, 1>());
 }
 
 // Which kernel: up to 16 query rows per (row, key head) fit the register tiles of the mma.sync kernel; beyond, the tensor-memory
