@@ -468,29 +468,44 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         zero_empty_rows<T>(p, base, tid, cthreads);
         Runs runs;
         runs.begin(p, base, share.x0, share.x1);
-        Run run;
+        Run run, next;
         Cursor at_ring = {0, 0u};
+        constexpr int kFetch = C::kRows * (DP / 8) / (C::kWarps * 32);       // 16-byte pieces of the query rows for a thread
+        uint4 fetched[kFetch];
+        auto fetch = [&](const Run &x) {
+            const int here = min(C::kRows, p.rows - x.rt * C::kRows);
+#pragma unroll
+            for (int k = 0; k < kFetch; ++k) {
+                const int i = tid + k * C::kWarps * 32, r = i / (DP / 8), ch = i % (DP / 8);
+                fetched[k] = make_uint4(0, 0, 0, 0);
+                if (r < here && ch * 8 < p.D) {
+                    const int rr = x.rt * C::kRows + r, tok = rr / p.group, head = x.h * p.group + rr - tok * p.group;
+                    fetched[k] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + x.b * p.qb + tok * p.qt + head * p.qh + ch * 8));
+                }
+            }
+        };
+        bool more = runs.next(next);
+        if (more) fetch(next);
         const int swz = lane & 7;
         const unsigned int k_lane = (16 * NK * warp + ((lane >> 4) << 3) + swz) * 128u, k_chunk = (lane >> 3) & 1;
         const unsigned int v_lane = (16 * NK * warp + (((lane >> 3) & 1) << 3) + swz) * 128u, v_chunk = lane >> 4;
         const unsigned int q_lane = ((((lane >> 3) & 1) << 3) + swz) * 128u, q_chunk = lane >> 4;
 
-        while (runs.next(run)) {
+        while (more) {
+            run = next;
+            more = runs.next(next);
             // ---- a unit, or the part of one that lies in this block ----
             const int b = run.b, h = run.h, rt = run.rt, j0 = run.j0, j1 = run.j0 + run.ns;
             const int len = row_len(p, b), news = row_news(p, b);
             const int rows_here = min(C::kRows, p.rows - rt * C::kRows);
-            // its query rows: row r is token r / group, query head h * group + r % group
-            for (int i = tid; i < C::kRows * (DP / 8); i += cthreads) {
-                const int r = i / (DP / 8), ch = i % (DP / 8);
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (r < rows_here && ch * 8 < p.D) {
-                    const int rr = rt * C::kRows + r, tok = rr / p.group, hh = h * p.group + rr - tok * p.group;
-                    x = __ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + b * p.qb + tok * p.qt + hh * p.qh + ch * 8));
-                }
+            // its query rows, on their way since the run before began: row r is token r / group, query head h * group + r % group
+#pragma unroll
+            for (int k = 0; k < kFetch; ++k) {
+                const int i = tid + k * C::kWarps * 32, r = i / (DP / 8), ch = i % (DP / 8);
                 const unsigned int at = q_smem + (ch >> 3) * (C::kRows * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(fetched[k].x), "r"(fetched[k].y), "r"(fetched[k].z), "r"(fetched[k].w) : "memory");
             }
+            if (more) fetch(next);
             consumer_barrier(cthreads);
             int limit[2];                                           // last place that the thread's rows see; -1: none
 #pragma unroll
