@@ -190,16 +190,16 @@ struct Cursor {
 struct Run {
     int b, h, rt;             // row, key head, row tile
     int j0, ns, n;            // first tile, tiles here, tiles of the unit
-    long long at;             // position of the unit's first tile
+    int at;                   // position of the unit's first tile
 };
 
 struct Runs {
     const int *base;          // base[b]: positions of the rows before b (one head, one row tile)
     int B, Hkv, row_tiles, cost;
     int b, h, rt;
-    long long x, x1, unit;    // next position, end of the share, first position of the unit
+    int x, x1, unit;          // next position, end of the share, first position of the unit
 
-    __device__ __forceinline__ void begin(const Params &p, const int *base_, long long x0, long long end)
+    __device__ __forceinline__ void begin(const Params &p, const int *base_, int x0, int end)
     {
         base = base_;
         B = p.B;
@@ -211,7 +211,7 @@ struct Runs {
         b = h = rt = 0;
         unit = 0;
         if (x >= x1) return;
-        const long long hr = static_cast<long long>(Hkv) * row_tiles;
+        const int hr = Hkv * row_tiles;
         int lo = 0, hi = B - 1;                              // the last row whose positions begin at or before x has some
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -219,8 +219,8 @@ struct Runs {
         }
         b = lo;
         const int each = base[b + 1] - base[b];
-        const int hrt = static_cast<int>((x - base[b] * hr) / each);
-        unit = base[b] * hr + static_cast<long long>(hrt) * each;
+        const int hrt = static_cast<int>(static_cast<unsigned int>(x - base[b] * hr) / static_cast<unsigned int>(each));
+        unit = base[b] * hr + hrt * each;
         h = hrt / row_tiles;
         rt = hrt - h * row_tiles;
     }
@@ -234,8 +234,8 @@ struct Runs {
             r.rt = rt;
             r.n = each - cost;
             r.at = unit + cost;
-            r.j0 = max(static_cast<int>(x - r.at), 0);
-            r.ns = static_cast<int>(min(static_cast<long long>(r.n), x1 - r.at)) - r.j0;
+            r.j0 = max(x - r.at, 0);
+            r.ns = min(r.n, x1 - r.at) - r.j0;
             unit += each;
             x = unit;
             if (++rt == row_tiles) {
@@ -286,18 +286,28 @@ __device__ __forceinline__ int tile_page(const Params &p, int b, int j, int len,
     return p.n_pages;                                    // outside the tensor map: reads as zeros
 }
 
-// This block's share of the positions, and the block that a position belongs to.
+// This block's share of the positions, and the block that a position belongs to.  The host sees to it that positions fit in 31 bits:
+// divisions of 64 bits here and in Runs cost a microsecond before the first load.
 struct Share {
-    long long total, G, x0, x1;
+    unsigned int total, blocks, each, more;              // total = each blocks + more; every one of these blocks has a position at least
+    int x0, x1;
     __device__ __forceinline__ Share(const Params &p, const int *base)
     {
-        total = static_cast<long long>(base[p.B]) * p.Hkv * p.row_tiles;
-        G = max(1ll, min(static_cast<long long>(gridDim.x), total));
-        const long long c = blockIdx.x;
-        x0 = c < G ? c * total / G : total;
-        x1 = c < G ? (c + 1) * total / G : total;
+        total = static_cast<unsigned int>(base[p.B] * p.Hkv * p.row_tiles);
+        blocks = max(min(gridDim.x, total), 1u);
+        each = total / blocks;
+        more = total - each * blocks;
+        x0 = from(min(blockIdx.x, blocks));
+        x1 = from(min(blockIdx.x + 1, blocks));
     }
-    __device__ __forceinline__ int owner(long long x) const { return static_cast<int>(((x + 1) * G - 1) / total); }
+    __device__ __forceinline__ int from(unsigned int c) const { return static_cast<int>(c * each + c * more / blocks); }
+    __device__ __forceinline__ int owner(int x) const
+    {
+        unsigned int c = static_cast<unsigned int>(static_cast<float>(x) / static_cast<float>(total) * static_cast<float>(blocks));
+        while (c > 0 && from(c) > x) --c;                // at most a step or two: the quotient is good to 2^-22 of the blocks
+        while (from(c + 1) <= x) ++c;
+        return static_cast<int>(c);
+    }
 };
 
 // The block with a unit's first tile says whether it was split.
@@ -414,7 +424,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             Cursor at_ring = {0, 0u};
             bool ok = true;
             while (more && ok) {
-                if (lane == 0) note_split(p, share, r);
                 const bool follows = runs.next(rn);
                 const int len_next = follows ? row_len(p, rn.b) : 0;
                 for (int i = 0; i < r.ns && ok; ++i) {
@@ -455,6 +464,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     at_ring.next(p.n_stages);
                     ok = __shfl_sync(kFull, ok ? 1 : 0, 0) != 0;
                 }
+                if (lane == 0) note_split(p, share, r);
                 r = rn;
                 len = len_next;
                 more = follows;
@@ -922,7 +932,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         int len = more ? row_len(p, r.b) : 0;
         int id = more ? tile_page<kTcTile>(p, r.b, r.j0, len, lane, per_tile) : -1;      // fetched a tile ahead
         while (more && ok) {
-            if (lane == 0) note_split(p, share, r);
             const bool follows = runs.next(rn);
             const int len_next = follows ? row_len(p, rn.b) : 0;
             int before = -1;                                      // the page of the tile whose values are still to be loaded
@@ -936,6 +945,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 if (ok && last) ok = load(&map_v, r.h, j, page);
                 before = page;
             }
+            if (lane == 0) note_split(p, share, r);
             r = rn;
             len = len_next;
             more = follows;

@@ -646,9 +646,12 @@ csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t
     const csd_status_t ok = check_cache(cache);
     if (ok != CSD_OK) return ok;
     if (!q || !out || !workspace || T <= 0 || q_heads <= 0 || layer < 0 || layer >= cache->layers || !std::isfinite(scale)) return CSD_ERR_INVALID_ARG;
-    if (static_cast<long long>(cache->rows) * cache->max_pages * cache->page_size > (1ll << 35)) return CSD_ERR_UNSUPPORTED;   // tiles are counted in 32 bits
-    const size_t need = csd_attention_workspace_bytes(cache->rows, T, q_heads, cache->heads, cache->dim);
-    if (need == 0) return CSD_ERR_UNSUPPORTED;
+    if (!attention_shape_ok(cache->rows, T, q_heads, cache->heads, cache->dim)) return CSD_ERR_UNSUPPORTED;
+    const AttentionPlan plan = attention_plan_of(T, q_heads / cache->heads, cache->dim, cache->rows);
+    // positions are counted in 31 bits: tiles of 64 places at least, and what a unit costs beside its tiles
+    const double row_positions = (static_cast<double>(cache->max_pages) * cache->page_size + 63) / 64 + plan.run_cost;
+    if (row_positions * cache->rows * cache->heads * plan.row_tiles >= 2147483648.0) return CSD_ERR_UNSUPPORTED;
+    const size_t need = plan.total;
     if (!aligned16(q) || !aligned16(out) || (q_stride_b | q_stride_t | q_stride_h) % 8 != 0) return CSD_ERR_INVALID_ARG;
     if (workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return CSD_ERR_WORKSPACE;
     host::other_work_enqueued();
