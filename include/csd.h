@@ -583,7 +583,7 @@ csd_status_t csd_cache_meta_layout(int rows, int max_pages, int n_pages, csd_cac
 size_t csd_cache_scratch_bytes(int rows, int max_pages, int n_pages);
 
 /* Counts and free pages from the tables and lengths in meta, flags cleared: after the caller has written those (zeroed
- * meta and rebuild: an empty cache).  Table entries beyond a row's length become -1.  Three launches; asynchronous. */
+ * meta and rebuild: an empty cache).  Table entries beyond a row's length become -1.  Two launches and two fills; asynchronous. */
 csd_status_t csd_cache_rebuild(const csd_cache_t *cache, void *stream);
 
 /* Room for T more tokens in every row, or n_new[row] (DEVICE [rows]; negative counts as 0).  All rows or none: where the
@@ -629,11 +629,14 @@ csd_status_t csd_rope_append(const void *q, int64_t q_stride_b, int64_t q_stride
  * strides); T <= CSD_MAX_K + 1; out: dense, the cache's type, 16-byte aligned; lse: float [rows, T, q_heads] or NULL.
  * scale: finite.  Scores, maxima and sums are float32; the weights are rounded to the cache's type for the second product
  * and counted in the sum before that rounding.
- * The places of all rows and heads are split evenly over the GPU; a (row, head) that several blocks read is joined by the
- * last of them to finish, in a fixed order, so results are bit-reproducible for given lengths.
- * workspace: csd_attention_workspace_bytes bytes, 256-byte aligned, initialised once with csd_workspace_init; one call at a
- * time; any shape that it is large enough for.
- * One launch; asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (q_heads not a multiple of heads, T), WORKSPACE, CUDA. */
+ * The places of all rows and heads are split evenly over the GPU; what several blocks have read of a (row, head) is joined by
+ * a second launch, in the order of the places, so results are bit-reproducible for given lengths.  More than 16 query rows to
+ * a key head (T * g > 16) take the tensor-memory products: there the maximum that the weights refer to follows the scores
+ * by powers of two up to 2^8, which moves their rounding but no bound on it.
+ * workspace: csd_attention_workspace_bytes bytes, 256-byte aligned, no initialisation; one call at a time; any shape that it
+ * is large enough for.
+ * Two launches; asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (q_heads not a multiple of heads, T, more than 2^31 tiles of
+ * 64 places if every row were full), WORKSPACE, CUDA. */
 size_t csd_attention_workspace_bytes(int rows, int T, int q_heads, int heads, int dim);
 csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads,
                            const csd_cache_t *cache, int layer, float scale, const int32_t *n_new,

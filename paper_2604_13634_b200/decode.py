@@ -265,7 +265,6 @@ class AttentionBuffers:
         self.out = torch.empty(cache.rows, T, q_heads, cache.head_dim, dtype=cache.dtype, device=dev)
         self.lse = torch.empty(cache.rows, T, q_heads, dtype=torch.float32, device=dev)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
-        _check(lib().csd_workspace_init(_ptr(self.workspace), self.ws_bytes, _stream_ptr(None, cache._device)), "csd_workspace_init")
 
 
 def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale: float | None = None, n_new=None, stream=None):

@@ -480,3 +480,18 @@ def test_unsupported_python_arguments_are_refused():
     with pytest.raises(AssertionError):
         csd_attention(torch.zeros(1, 1, 2, 64, device="cuda"), cache, 0, buf)
     assert StepBuffers(1, 4, 100, torch.bfloat16).ws_bytes > 0
+
+
+def test_more_tiles_than_can_be_counted_are_refused():
+    from ctypes import byref
+    cache = PagedCache(2, 4, 16, 1, 2, 64, torch.bfloat16, 64)
+    many = decode.CacheStruct()
+    for name, _ in decode.CacheStruct._fields_:
+        setattr(many, name, getattr(cache._struct, name))
+    many.rows, many.max_pages = 4096, 1 << 19                         # 2^29 tiles of 64 places for each head, 9 row tiles of T * 32 query rows
+    q = torch.zeros(2, 33, 64, 64, dtype=torch.bfloat16, device="cuda")
+    call = lambda c, ws: decode._lib().csd_attention(q.data_ptr(), *q.stride()[:3], 33, 64, byref(c), 0, 0.125, None, q.data_ptr(), None, q.data_ptr(), ws, None)  # noqa: E731
+    for c, ws, why in ((many, 1 << 40, "unsupported"), (cache._struct, 16, "workspace")):
+        with pytest.raises(decode.CsdError, match=why):
+            decode._check(call(c, ws), "csd_attention")
+    assert not q.any()
