@@ -6,7 +6,15 @@
 // A run of places gives a part (m, l, O) = (max_j x_j, sum_j 2^(x_j - m), sum_j 2^(x_j - m) v_j) with x = scale log2(e) q.k, and
 // parts join as M = max m_i, L = sum l_i 2^(m_i - M), O = sum O_i 2^(m_i - M) / L.
 //
-// Bound: memory (each key and value is read once; T g query rows share it, g = query heads per key head).
+// Bound: memory (each key and value is read once; T g query rows share it, g = query heads per key head); for a short cache the
+// latency of the chain lengths -> page ids -> tiles -> join, 9.7 us with one row of 700 tokens.
+// Measured with keys and values of 0.1 to 1.2 GB, bf16, 8 key heads of 128: 5.9 TB/s for one row of 131071 tokens and one new token
+// (90.9 us, 32 query heads), 5.8 for 128 rows of 500 to 4000 with nine (206 us), 5.2 for 32 ragged rows up to 8191 with six (104 us),
+// 3.1 for one row of 30001 with 72 query rows to a key head (39.9 us: half of it is the start, the parts' way out and the join).
+//
+// Two kernels, by query rows to a key head and row of the cache: up to 16 fit one mma.sync tile held in registers; beyond, 128 rows
+// share a tensor-memory tile.  32 rows of 8191 tokens with 30 query rows took 182 us as two row tiles of the first kernel, which
+// reads its keys twice, and take 104 with the second; with 16 rows or fewer most of the second's 128-row products are for nobody.
 //
 //   attention_kernel  persistent.  The tiles (kTile places of one row and key head) of all rows and heads, laid out row after
 //                     row, are split evenly and contiguously over the blocks, whatever the rows' lengths are (read on the
@@ -19,8 +27,9 @@
 //                     limit while the tiles stream.
 //     At the end of a unit the warps join through a ring stage; a unit that lies in one block whole is written out, otherwise
 //     the part goes to the workspace.
-//   attention_join_kernel  joins the parts of the units that were split (at most one begins in each block), a warp per query row, in
-//                     the order of the places.
+//   attention_join_kernel  joins the parts of the units that were split (at most one begins in each block).  A launch of its own: joining
+//                     in the last block to finish a unit was slower (103.6 us against 94 for one row of 131071 tokens, 36.9
+//                     against 30.6 for 16 rows with a key head to every query head), a chain of cold reads at the end of the slowest block.
 // No block waits for another; waits inside a block are bounded.
 #pragma once
 
@@ -779,7 +788,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 //   warp 5      the page loads
 // Two blocks per SM (one beyond dim 128, whose accumulators take more than half of the tensor memory): while one waits for its scores
 // or ends a unit, the other keeps the memory busy.  One block with two such sets that took a run's tiles in turn was slower, 247 us
-// against 221 for 1024 units of 8 to 63 tiles: both sets stop at a unit's end together.
+// against 221 at that time for 1024 units of 8 to 63 tiles: both sets stop at a unit's end together.
 // The next run's query rows are fetched, and its first scores computed, while this one ends (where two sets of query rows fit).
 // A row tile is always computed as 128 rows: rows that do not exist read whatever follows in shared memory and feed accumulator
 // rows that nobody reads.
