@@ -13,8 +13,9 @@
 // 3.1 for one row of 30001 with 72 query rows to a key head (39.9 us: half of it is the start, the parts' way out and the join).
 //
 // Two kernels, by query rows to a key head and row of the cache: up to 16 fit one mma.sync tile held in registers; beyond, 128 rows
-// share a tensor-memory tile.  32 rows of 8191 tokens with 30 query rows took 182 us as two row tiles of the first kernel, which
-// reads its keys twice, and take 104 with the second; with 16 rows or fewer most of the second's 128-row products are for nobody.
+// share a tensor-memory tile.  32 ragged rows up to 8191 tokens, dim 128: 93 us (first kernel) and 101 (second) with 10 query rows, 94
+// and 102 with 15, 155 and 103 with 20, 163 and 104 with 30; 128 rows of 500 to 4000, dim 64: 100 and 131 with 8, 102 and 132 with 16,
+// 185 and 135 with 32.  Beyond 16 the first kernel has a second row tile, which reads every key again.
 //
 //   attention_kernel  persistent.  The tiles (kTile places of one row and key head) of all rows and heads, laid out row after
 //                     row, are split evenly and contiguously over the blocks, whatever the rows' lengths are (read on the
@@ -791,7 +792,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 // against 221 at that time for 1024 units of 8 to 63 tiles: both sets stop at a unit's end together.
 // The next run's query rows are fetched, and its first scores computed, while this one ends (where two sets of query rows fit).
 // A row tile is always computed as 128 rows: rows that do not exist read whatever follows in shared memory and feed accumulator
-// rows that nobody reads.
+// rows that nobody reads.  Products of 64 rows where these suffice gave the same times, and 159 us against 140 with 64 query rows of
+// 64 elements; each query row twice, against either half of a tile's places, 225 us against 206 (36 query rows of 128).  The
+// products' issue and reads, not the weights, are what a tile waits for: with dim 64 the pipe is busy for half of the time.
 // The reference m of a row only moves when a tile's maximum exceeds it by 2^8 (weights up to 2^8 are harmless in float32 sums
 // and in either cache type), so the accumulators in tensor memory are rescaled a few times per unit, not per tile.
 constexpr int kTcTile = 64;
@@ -1261,8 +1264,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
 
 // Joins the parts of split units: block (x, y) kJoinRows query rows of one of them.  The weights of all parts and rows first (a
 // thread per part and row), then each warp sums every fourth part, the rows side by side, so that a row of 40 parts costs a
-// few memory latencies and not forty; the four sums are added in order.  Four rows to a block where there are many rows
-// (blocks are what costs then), one where there are few.
+// few memory latencies and not forty; the four sums are added in order.  Four rows to a block, or one where units have many parts.
 constexpr int kJoinThreads = 128, kMaxGrid = 512;
 
 template <typename T, int DP, int kJoinRows>

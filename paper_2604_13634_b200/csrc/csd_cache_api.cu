@@ -282,8 +282,8 @@ auto with_config(int dim, F f)
     return f(Config<T, 256, 1, 1>());
 }
 
-// Which kernel: up to 16 query rows per (row, key head) fit the register tiles of the mma.sync kernel; beyond, the tensor-memory
-// kernel, with row tiles of at most 128.
+// Which kernel: up to 16 query rows per (row, key head) fit the register tiles of the mma.sync kernel (94 us where the other takes 102,
+// 15 query rows of 128 elements); beyond, the tensor-memory kernel, with row tiles of at most 128 (103 us against 155 with 20 rows).
 bool attention_uses_tc(int rows) { return rows > 16; }
 
 // Two blocks per SM while their accumulators fit in half of the tensor memory each (128 + dim columns of 512).
@@ -389,8 +389,9 @@ csd_status_t launch_join(const attention::Params &p, const AttentionPlan &a, cud
 {
     const int most = a.rows < a.tile_rows ? a.rows : a.tile_rows;
     const unsigned int units = static_cast<unsigned int>(p.by_unit ? p.B * p.Hkv * a.row_tiles : a.grid);
-    // a block per row while all of them are on the GPU at once
-    if (static_cast<long long>(units) * most <= host::multiprocessors() * 8ll)
+    // a block per row where a unit may have 32 parts or more (8 units of 37: 90.1 us against 91.5 with four rows to a block, 40.0
+    // against 41.6 with 72 rows; with four: 39.3 against 41.3 for 16 units of 18, 28.0 against 29.8 for 256, 206 against 212 for 1024)
+    if (a.grid >= 32ll * units)
         return launch(attention::attention_join_kernel<T, DP, 1>, dim3(units, static_cast<unsigned int>(most)), attention::kJoinThreads, 0, st, p, a.tile_rows);
     return launch(attention::attention_join_kernel<T, DP, 4>, dim3(units, static_cast<unsigned int>((most + 3) / 4)), attention::kJoinThreads, 0, st, p, a.tile_rows);
 }
