@@ -623,7 +623,7 @@ csd_status_t csd_rope_append(const void *q, int64_t q_stride_b, int64_t q_stride
 /* Attention of the T newest tokens of every row over its cache: with g = q_heads / heads,
  *     out[b,t,h] = sum_j w_j v_j,  w = softmax_j(scale q[b,t,h].k_j),  lse[b,t,h] = ln sum_j exp(scale q[b,t,h].k_j)
  * over the places j <= lens[b] - n_new[b] + t of key head h / g.  A token that sees nothing (an empty row, t >= n_new[b], a
- * negative place) gives zeros and lse = -inf; what lies in places that a token does not see, infinities and NaN included,
+ * negative place), or whose scores are all -inf, gives zeros and lse = -inf; what lies in places that a token does not see, infinities and NaN included,
  * does not reach its result.
  * q: [rows, T, q_heads, dim] of the cache's type, strides in elements, dim contiguous, 16-byte aligned (base and
  * strides); T <= CSD_MAX_K + 1; out: dense, the cache's type, 16-byte aligned; lse: float [rows, T, q_heads] or NULL.
