@@ -782,19 +782,20 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 // ---- more than 16 query rows per key head: products on the tensor-memory path -------------------------------------------
 //
 // The same split over the blocks, parts and join; inside a block
-//   warps 0..3  softmax: thread r owns query row r of the row tile.  It reads the row's 64 scores of a tile from tensor memory,
+//   warps 0..3  softmax: a thread owns a query row of the row tile.  It reads the row's 64 scores of a tile from tensor memory,
 //               writes the weights back there in the cache's type, and keeps (m, l) in registers
-//   warp 4      one thread issues the products: S = Q K^T (tcgen05.mma, M = 128 query rows, N = 64 places, both operands from
+//   warp 4      one thread issues the products: S = Q K^T (tcgen05.mma, M = 128 or 64 query rows, N = 64 places, both operands from
 //               shared memory) into one of two score buffers, O += P V (P from tensor memory, V read with places as its K)
 //   warp 5      the page loads
 // Two blocks per SM (one beyond dim 128, whose accumulators take more than half of the tensor memory): while one waits for its scores
 // or ends a unit, the other keeps the memory busy.  One block with two such sets that took a run's tiles in turn was slower, 247 us
 // against 221 at that time for 1024 units of 8 to 63 tiles: both sets stop at a unit's end together.
 // The next run's query rows are fetched, and its first scores computed, while this one ends (where two sets of query rows fit).
-// A row tile is always computed as 128 rows: rows that do not exist read whatever follows in shared memory and feed accumulator
-// rows that nobody reads.  Products of 64 rows where these suffice gave the same times, and 159 us against 140 with 64 query rows of
-// 64 elements; each query row twice, against either half of a tile's places, 225 us against 206 (36 query rows of 128).  The
-// products' issue and reads, not the weights, are what a tile waits for: with dim 64 the pipe is busy for half of the time.
+// A row tile is always computed as 128 rows (kM), or 64 where these suffice and pay: rows that do not exist read whatever follows in
+// shared memory and feed accumulator rows that nobody reads.  Of 128 rows a softmax warp's quarter of the tensor memory holds 32, of
+// 64 it holds 16, in its first 16 lanes.  Each query row twice, against either half of a tile's places, took 225 us against 206 (36
+// query rows of 128): the products' issue and reads, not the weights, are what a tile waits for (with dim 64 the pipe is busy for
+// half of the time).
 // The reference m of a row only moves when a tile's maximum exceeds it by 2^8 (weights up to 2^8 are harmless in float32 sums
 // and in either cache type), so the accumulators in tensor memory are rescaled a few times per unit, not per tile.
 constexpr int kTcTile = 64;
@@ -803,10 +804,10 @@ constexpr int kTcMaxSlots = 16;
 constexpr unsigned int kTcScoreCols = 64, kTcOutCol = 128;     // tensor memory: scores at 0 and 64 (weights over them), output from 128
 
 template <typename T>
-__device__ __forceinline__ unsigned int tc_instr(int n, bool b_mn_major)
+__device__ __forceinline__ unsigned int tc_instr(int m, int n, bool b_mn_major)
 {
     constexpr unsigned int type = sizeof(T) == 2 && ExponentBits<T>::value == 0x7f80u ? 1u : 0u;     // 1: bf16, 0: f16
-    return (1u << 4) | (type << 7) | (type << 10) | (b_mn_major ? 1u << 16 : 0u) | (static_cast<unsigned int>(n >> 3) << 17) | ((128u >> 4) << 24);
+    return (1u << 4) | (type << 7) | (type << 10) | (b_mn_major ? 1u << 16 : 0u) | (static_cast<unsigned int>(n >> 3) << 17) | (static_cast<unsigned int>(m >> 4) << 24);
 }
 // Values as the second operand: rows of 64 elements (128 bytes, swizzled) are K, the elements within them N.
 __device__ __forceinline__ unsigned long long value_desc(unsigned int smem_addr, unsigned int column_bytes)
@@ -851,10 +852,12 @@ __device__ __forceinline__ void fetch_rows(const Params &p, const Run &ru, unsig
     }
 }
 
-template <typename T, int kBlocksPerSm>
+template <typename T, int kBlocksPerSm, int kM>
 __global__ void __launch_bounds__(kTcThreads, kBlocksPerSm)
 attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p)
 {
+    static_assert(kM == 64 || kM == 128, "rows of a product");
+    constexpr int kWarpRows = kM / 4;                            // query rows of a softmax warp, in its first lanes
     constexpr unsigned int kCols = kBlocksPerSm == 2 ? 256 : 512;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bar_words[2 * kTcMaxSlots + 7];
@@ -971,7 +974,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             Runs runs;
             runs.begin(p, base, share.x0, share.x1);
             Run r;
-            const unsigned int idesc_qk = tc_instr<T>(kTcTile, false), idesc_pv = tc_instr<T>(p.d16, true);
+            const unsigned int idesc_qk = tc_instr<T>(kM, kTcTile, false), idesc_pv = tc_instr<T>(kM, p.d16, true);
             const unsigned long long half_q = static_cast<unsigned long long>((p.tile_rows * 128) >> 4), half_k = (kTcTile * 128) >> 4;
             Cursor at = {0, 0u};                               // the loads are used in the order in which they are made
             int mine = 0;                                      // tiles of the runs before
@@ -1018,7 +1021,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         }
     } else {
         // ---- softmax, rows in and out ----
-        const int r = tid;                                        // the thread's query row of the row tile
+        const int warp_row = kWarpRows * warp, r = lane < kWarpRows ? warp_row + lane : kM;      // the thread's query row of the row tile
         zero_empty_rows<T>(p, base, tid, 128);
         Runs runs;
         runs.begin(p, base, share.x0, share.x1);
@@ -1056,7 +1059,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             }
             const int rr = rt * p.tile_rows + r, tok = rr / p.group;
             const int limit = r < rows_here && tok < news ? len - news + tok : -1;
-            const bool warp_has = 32 * warp < rows_here;
+            const bool warp_has = warp_row < rows_here;
             float m = 0.f, l = 0.f;                              // l == 0: nothing seen yet, m is arbitrary
 
             for (int i = 0; i < ns; ++i, ++mine) {
@@ -1149,7 +1152,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     mbar_wait(full(s), (item / p.n_stages) & 1, give_up);
                     const unsigned int v_at = slot_at(s);
                     const int from = max(len - news + 1 - key0, 0), chunks = p.halves * 8;
-                    for (int c = r; c < (kTcTile - from) * chunks; c += 128) {
+                    for (int c = tid; c < (kTcTile - from) * chunks; c += 128) {
                         const int kr = from + c / chunks, ch = c % chunks;
                         const unsigned int at = v_at + (ch >> 3) * (kTcTile * 128) + kr * 128 + (((ch & 7) ^ (kr & 7)) << 4);
                         unsigned int v[4] = {0u, 0u, 0u, 0u}, z[4] = {0u, 0u, 0u, 0u};
@@ -1188,7 +1191,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 // A thread has a row, memory wants rows side by side: each warp turns its 32 rows round in shared memory, where the
                 // run's query rows were, which every product has read.
                 const float inv = seen ? (whole ? 1.f / l : 1.f) : 0.f;
-                const int pitch = p.halves * 128, warp_rows = min(32, rows_here - 32 * warp);
+                const int pitch = p.halves * 128, warp_rows = min(kWarpRows, rows_here - warp_row);
                 const unsigned int out_smem = q_at(run), my_row = out_smem + r * pitch;
                 const int cols = whole ? p.halves * 64 : p.halves * 32;                        // of a pass: what a staged row holds
                 const int lanes_row = p.halves * 8, at_once = 32 / lanes_row, sub = lane / lanes_row, ch = lane - sub * lanes_row;
@@ -1228,14 +1231,14 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     // lanes_row lanes a row, 16 bytes each
                     const int d = pass0 + (whole ? ch * 8 : ch * 4);
                     const bool do_it = sub < at_once && d < pass1;
-                    char *to = whole ? reinterpret_cast<char *>(static_cast<T *>(p.out) + d) : reinterpret_cast<char *>(part + (32 * warp) * p.part_stride + d);
+                    char *to = whole ? reinterpret_cast<char *>(static_cast<T *>(p.out) + d) : reinterpret_cast<char *>(part + warp_row * p.part_stride + d);
                     const long long row_bytes = whole ? row * p.D * static_cast<long long>(sizeof(T)) : static_cast<long long>(lane) * p.part_stride * 4;
                     for (int w0 = 0; w0 < warp_rows; w0 += 4 * at_once) {
                         uint4 v[4];
                         long long off[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const int wr = w0 + k * at_once + sub, r2 = 32 * warp + wr;
+                            const int wr = w0 + k * at_once + sub, r2 = warp_row + wr;
                             off[k] = __shfl_sync(kFull, row_bytes, wr & 31);
                             if (do_it && wr < warp_rows)
                                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[k].x), "=r"(v[k].y), "=r"(v[k].z), "=r"(v[k].w) : "r"(out_smem + r2 * pitch + ((ch ^ (r2 & 7)) << 4)) : "memory");

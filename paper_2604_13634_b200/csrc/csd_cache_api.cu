@@ -289,6 +289,12 @@ bool attention_uses_tc(int rows) { return rows > 16; }
 // Two blocks per SM while their accumulators fit in half of the tensor memory each (128 + dim columns of 512).
 int tc_blocks(int dim) { return dim <= 128 ? 2 : 1; }
 
+// Products of 64 rows: a warp of the softmax then has 16 query rows, not 32.  Same time on a cool GPU, but the products draw less, and
+// kept busy the clock stays higher: 222 us against 235 for 128 rows of 500 to 4000 (36 query rows of 128 elements), 112 against 120
+// (30), 236 against 245 (64); with 64 elements 145 against 153 (32), but 161 against 159 (48) and 159 against 140 (64, cool), where
+// twice the warps' work counts.
+bool tc_products_of_64(int tile_rows, int dim) { return tile_rows <= (dim <= 64 ? 32 : 64); }
+
 AttentionPlan attention_tc_plan(int rows, int dim, int B)
 {
     AttentionPlan a;
@@ -412,12 +418,11 @@ csd_status_t run_attention(attention::Params p, const csd_cache_t *cache, int la
     return rc != CSD_OK ? rc : launch_join<typename C::T, C::DP>(p, a, st);
 }
 
-template <typename T, int kBlocks>
-csd_status_t run_attention_tc(attention::Params p, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
+template <typename T, int kBlocks, int kM>
+csd_status_t run_attention_tc(attention::Params p, const AttentionPlan &a, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
 {
     static std::atomic<bool> ready[kMaxDevices];
-    if (!kernel_ready(attention::attention_tc_kernel<T, kBlocks>, ready, kSmemPerSm / kBlocks - kSmemReserved - kSmemStatic, 1, 0)) return CSD_ERR_CUDA;
-    const AttentionPlan a = attention_tc_plan(p.T * p.group, p.D, p.B);
+    if (!kernel_ready(attention::attention_tc_kernel<T, kBlocks, kM>, ready, kSmemPerSm / kBlocks - kSmemReserved - kSmemStatic, 1, 0)) return CSD_ERR_CUDA;
     fill_plan(p, a, ws);
     p.tile_rows = a.tile_rows;
     p.q_buffers = a.q_buffers;
@@ -432,7 +437,7 @@ csd_status_t run_attention_tc(attention::Params p, const csd_cache_t *cache, int
     p.pool_token = cache->stride_token;
     CUtensorMap map_k, map_v;
     if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
-    const csd_status_t rc = launch(attention::attention_tc_kernel<T, kBlocks>, dim3(static_cast<unsigned int>(a.grid)), attention::kTcThreads,
+    const csd_status_t rc = launch(attention::attention_tc_kernel<T, kBlocks, kM>, dim3(static_cast<unsigned int>(a.grid)), attention::kTcThreads,
                                    static_cast<size_t>(a.smem), st, map_k, map_v, p);
     if (rc != CSD_OK) return rc;
     if (a.dp == 64) return launch_join<T, 64>(p, a, st);
@@ -443,8 +448,12 @@ csd_status_t run_attention_tc(attention::Params p, const csd_cache_t *cache, int
 template <typename T>
 csd_status_t run_attention_any(const attention::Params &p, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
 {
-    if (attention_uses_tc(p.T * p.group))
-        return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2>(p, cache, layer, ws, st) : run_attention_tc<T, 1>(p, cache, layer, ws, st);
+    if (attention_uses_tc(p.T * p.group)) {
+        const AttentionPlan a = attention_tc_plan(p.T * p.group, p.D, p.B);
+        if (tc_products_of_64(a.tile_rows, p.D))
+            return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 64>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 64>(p, a, cache, layer, ws, st);
+        return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 128>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 128>(p, a, cache, layer, ws, st);
+    }
     return with_config<T>(p.D, [&](auto cfg) { return run_attention<decltype(cfg)>(p, cache, layer, ws, st); });
 }
 
