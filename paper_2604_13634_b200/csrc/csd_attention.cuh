@@ -462,7 +462,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     }
                     at_ring.next(p.n_stages);
                 }
-                if (ok) {                                            // the consumers join through the next stage
+                if (ok) {                                            // the consumers join through the next stage, once it is theirs
                     const int sj = at_ring.slot;
                     if (lane == 0) {
                         ok = mbar_wait(empty(sj), at_ring.round ^ 1u, give_up);
@@ -718,7 +718,10 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 }
                 if (qd == 0) ml[warp * C::kRows + g + 8 * hh] = make_float2(m[hh], l[hh]);
             }
-            consumer_barrier(cthreads);                               // every warp is done with the tiles before: the stage is free
+            // The stage is handed over by the producer: without this wait the arrivals on empty() below could come before the producer's
+            // test of the phase before, which by parity then reads as still open.
+            mbar_wait(full_k(at_ring.slot), at_ring.round, give_up);
+            consumer_barrier(cthreads);                               // every warp is done with the tiles before
             // element (row, column) of a warp's sums; the columns' order within a row is turned by the row, so that the eight rows a
             // warp writes at once fall on different banks
             float *sums = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw)) + at_ring.slot * C::kStageBytes);
