@@ -263,8 +263,8 @@ struct Runs {
     }
 };
 
-__device__ __forceinline__ int row_len(const Params &p, int b) { return min(max(__ldg(p.lens + b), 0), p.max_pages << p.page_shift); }
-__device__ __forceinline__ int row_news(const Params &p, int b) { return p.n_new ? min(max(__ldg(p.n_new + b), 0), p.T) : p.T; }
+__device__ __forceinline__ int row_len(const Params &p, int b) { return min(max(ptx::ld_written(p.lens + b), 0), p.max_pages << p.page_shift); }
+__device__ __forceinline__ int row_news(const Params &p, int b) { return p.n_new ? min(max(ptx::ld_written(p.n_new + b), 0), p.T) : p.T; }
 
 // base[b + 1] holds the positions of row b; becomes base[b] = positions of the rows before b.  One warp.
 __device__ __forceinline__ void scan_tiles(int *base, int B)
@@ -290,7 +290,7 @@ __device__ __forceinline__ int tile_page(const Params &p, int b, int j, int len,
 {
     const int place = j * kTile + lane * p.box_rows;
     if (lane >= per_tile || place >= len) return -1;
-    const int id = __ldg(p.table + static_cast<long long>(b) * p.max_pages + (place >> p.page_shift));
+    const int id = ptx::ld_written(p.table + static_cast<long long>(b) * p.max_pages + (place >> p.page_shift));
     if (id >= 0 && id < p.n_pages) return id;
     atomicOr(p.flags, CSD_CACHE_BAD_PAGE);
     return p.n_pages;                                    // outside the tensor map: reads as zeros
@@ -357,7 +357,7 @@ __device__ __noinline__ void add_left_out(const Params &p, int b, int h, int tok
 {
     const T *q = static_cast<const T *>(p.q) + b * p.qb + tok * p.qt + head * p.qh;
     for (int key = from; key <= to; ++key) {
-        const int page = __ldg(p.table + static_cast<long long>(b) * p.max_pages + (key >> p.page_shift));
+        const int page = ptx::ld_written(p.table + static_cast<long long>(b) * p.max_pages + (key >> p.page_shift));
         if (page < 0 || page >= p.n_pages) continue;
         const long long at = page * p.pool_page + h * p.pool_head + (key & ((1 << p.page_shift) - 1)) * p.pool_token;
         const T *k = static_cast<const T *>(p.k_pool) + at, *v = static_cast<const T *>(p.v_pool) + at;
@@ -500,7 +500,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 fetched[k] = make_uint4(0, 0, 0, 0);
                 if (r < here && ch * 8 < p.D) {
                     const int rr = x.rt * C::kRows + r, tok = rr / p.group, head = x.h * p.group + rr - tok * p.group;
-                    fetched[k] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + x.b * p.qb + tok * p.qt + head * p.qh + ch * 8));
+                    fetched[k] = ptx::ld_written(reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + x.b * p.qb + tok * p.qt + head * p.qh + ch * 8));
                 }
             }
         };
@@ -1281,7 +1281,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Para
     __shared__ __align__(16) float rows[4][kJoinRows][DP];
     ptx::wait_for_stream();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const Split sp = {__ldcg(&p.splits[blockIdx.x].unit), __ldcg(&p.splits[blockIdx.x].first), __ldcg(&p.splits[blockIdx.x].parts)};
+    const Split sp = {ptx::ld_written(&p.splits[blockIdx.x].unit), ptx::ld_written(&p.splits[blockIdx.x].first), ptx::ld_written(&p.splits[blockIdx.x].parts)};
     const int n = sp.parts;
     if (n == 0) return;
     const int rt = sp.unit % p.row_tiles, bh = sp.unit / p.row_tiles, b = bh / p.Hkv, h = bh - b * p.Hkv;

@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kBlock, 1) extend_kernel(const View v, const i
     for (int k = 0; k < kRowsEach; ++k) {
         const bool there = k < per && r0 + k < v.rows;
         len[k] = there ? v.lens[r0 + k] : 0;
-        n[k] = there ? max(n_new ? __ldg(n_new + r0 + k) : uniform, 0) : 0;
+        n[k] = there ? max(n_new ? ptx::ld_written(n_new + r0 + k) : uniform, 0) : 0;
     }
     if (tid == 0) bad = 0;
     for (int r = tid; r < ((v.rows + 3) & ~3); r += kBlock) tail[r] = -1;
@@ -233,10 +233,10 @@ __global__ void __launch_bounds__(kRowThreads) truncate_kernel(const View v, con
     const int len = v.lens[r];
     int to;
     if (accept_len) {
-        const int n = v.granted[r], kept = min(n, max(__ldg(accept_len + r), -1) + 1);
+        const int n = v.granted[r], kept = min(n, max(ptx::ld_written(accept_len + r), -1) + 1);
         to = len - (n - kept);
     } else {
-        to = __ldg(new_lens + r);
+        to = ptx::ld_written(new_lens + r);
     }
     to = min(max(to, 0), len);
     const int first = pages_of(to, v.page_shift), held = pages_of(len, v.page_shift);
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kRowThreads) fork_stage_kernel(const View v, c
 {
     ptx::wait_for_stream();
     const int r = blockIdx.x;
-    int p = __ldg(parent + r);
+    int p = ptx::ld_written(parent + r);
     if (p >= v.rows) {
         if (threadIdx.x == 0) atomicOr(v.flags, CSD_CACHE_BAD_ROW);
         p = r;
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(kRowThreads) fork_commit_kernel(const View v, 
 {
     ptx::wait_for_stream();
     const int r = blockIdx.x;
-    const int p = __ldg(parent + r);
+    const int p = ptx::ld_written(parent + r);
     const int *to = v.staged + static_cast<long long>(r) * (v.max_pages + 1);
     if (p != r && p < v.rows) {
         int *own = v.table + static_cast<long long>(r) * v.max_pages;
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const CopyPara
     const int warps = gridDim.x * (kCopyThreads / 32);
     for (int it = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); it < n; it += warps) {
         const int move = it / p.pieces, piece = it - move * p.pieces;
-        const int2 m = __ldg(reinterpret_cast<const int2 *>(p.moves) + move);
+        const int2 m = ptx::ld_written(reinterpret_cast<const int2 *>(p.moves) + move);
         char *base = pool + static_cast<long long>(piece) * kCopyBytes;
         const char *from = base + m.x * p.page_stride_bytes;
         char *to = base + m.y * p.page_stride_bytes;
@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const CopyPara
         uint4 x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j * 512 < left) x[j] = ld_stream16(from + j * 512);
+            if (j * 512 < left) x[j] = ptx::ld_written_once(from + j * 512);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j * 512 < left) __stcs(reinterpret_cast<uint4 *>(to + j * 512), x[j]);

@@ -17,6 +17,35 @@ __device__ __forceinline__ void wait_for_stream()
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// Loads of what a kernel before this one on the stream may have written.  Such data changes while the kernel waits, so it is not
+// read-only for the kernel's lifetime and must not go through ld.global.nc (__ldg), which also lets a compiler move the load above the
+// wait.  These are coherent, and volatile like the wait, so they stay behind it.
+__device__ __forceinline__ int ld_written(const int *p)
+{
+    int v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ int2 ld_written(const int2 *p)
+{
+    int2 v;
+    asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint4 ld_written(const uint4 *p)
+{
+    uint4 v;
+    asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+// ... 16 bytes that are read once
+__device__ __forceinline__ uint4 ld_written_once(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
 __device__ __forceinline__ unsigned int smem_u32(const void *p) { return static_cast<unsigned int>(__cvta_generic_to_shared(p)); }
 
 __device__ __forceinline__ void mbar_init(unsigned int bar, unsigned int count)

@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_kernel(const RopeParams p)
         const int k = i / pairs, pair = i - k * pairs, token = blockIdx.x * p.at.tokens + k;
         if (token < p.at.n_tokens) {
             const int tb = token / p.S, ts = token - tb * p.S;
-            table[k * each + (pair % P) * columns + pair / P] = angle(p.turn, pair, __ldg(p.positions + tb * p.pb + ts * p.ps), p.inverse != 0);
+            table[k * each + (pair % P) * columns + pair / P] = angle(p.turn, pair, ptx::ld_written(p.positions + tb * p.pb + ts * p.ps), p.inverse != 0);
         }
     }
     __syncthreads();                       // the table is complete; and every element has been read (y may be x)
@@ -486,12 +486,12 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const AppendPa
                 x[k].load(from + (h0 + k) * head, u, p.turn.rot, p.D);
                 if constexpr (kLoose && kHalf) x[k].v.hand_over(planes, k);
             }
-        const int news = p.n_new ? __ldg(p.n_new + b) : p.T;
-        place = __ldg(p.lens + b) - news + t;
+        const int news = p.n_new ? ptx::ld_written(p.n_new + b) : p.T;
+        place = ptx::ld_written(p.lens + b) - news + t;
         real = t < news && place >= 0;
         if (which != 0 && real) {
             const int slot = place >> p.page_shift;
-            page = slot < p.max_pages ? __ldg(p.table + static_cast<long long>(b) * p.max_pages + slot) : -1;
+            page = slot < p.max_pages ? ptx::ld_written(p.table + static_cast<long long>(b) * p.max_pages + slot) : -1;
         }
     }
     for (int i = threadIdx.x; i < p.at.tokens * pairs; i += kThreads) {
@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const AppendPa
         if (token < p.at.n_tokens) {
             const int tb = token / p.T, tt = token - tb * p.T;
             table[k * each + (pair % P) * columns + pair / P] =
-                angle(p.turn, pair, __ldg(p.lens + tb) - (p.n_new ? __ldg(p.n_new + tb) : p.T) + tt, false);
+                angle(p.turn, pair, ptx::ld_written(p.lens + tb) - (p.n_new ? ptx::ld_written(p.n_new + tb) : p.T) + tt, false);
         }
     }
     __syncthreads();                       // the table is complete; and every element has been read (q_out may be q)
