@@ -533,7 +533,7 @@ csd_status_t csd_rope_steps(int rot, double base, csd_rope_scaling_t scaling, do
  * products in float32, rounded once.  16-byte accesses where base, strides, rot/2 and D allow, element-wise otherwise.
  * One launch; asynchronous.  B, S or H of 0 does nothing.
  * Errors: INVALID_ARG (null, negative size, rot odd or outside 2 .. D, unknown type or layout), UNSUPPORTED (rot
- * beyond 4096, 2^31 tokens or more), CUDA. */
+ * beyond 4096, more than 2^31 - 257 tokens), CUDA. */
 csd_status_t csd_rope(const void *x, void *y, csd_dtype_t dtype, int B, int S, int H, int D,
                       int64_t x_stride_b, int64_t x_stride_s, int64_t x_stride_h,
                       int64_t y_stride_b, int64_t y_stride_s, int64_t y_stride_h,

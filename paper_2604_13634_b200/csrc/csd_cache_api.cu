@@ -69,7 +69,7 @@ int units_of(Cut cut, int P, int rot, int D)
 bool place_tokens(long long tokens, long long groups, int units, rope::Places &at, dim3 &grid)
 {
     const long long per_token = groups * units;
-    if (tokens > INT_MAX || per_token > INT_MAX) return false;
+    if (tokens > INT_MAX - rope::kThreads || per_token > INT_MAX) return false;      // the last block's tokens are counted past the end
     at.n_tokens = static_cast<int>(tokens);
     at.per_token = static_cast<int>(per_token);
     at.tokens = per_token >= rope::kThreads ? 1 : rope::kThreads / at.per_token;

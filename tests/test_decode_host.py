@@ -2,10 +2,11 @@
 
 import os
 import re
+from ctypes import byref
 
 import pytest
 
-from paper_2604_13634_b200 import build
+from paper_2604_13634_b200 import binding, build, decode
 
 CSRC = os.path.join(os.path.dirname(os.path.abspath(build.__file__)), "csrc")
 
@@ -22,3 +23,17 @@ def test_only_constants_are_loaded_as_read_only(name):
         code = re.sub(r"//[^\n]*", "", f.read())
     loads = re.findall(r"__ldg\(([^)]*)\)|(ld_stream16|\.nc\b)", code)
     assert [a for a, _ in loads] == (["t.steps + pair"] if name == "csd_rope.cuh" else [])
+
+
+INVALID_ARG, UNSUPPORTED = 1, 4
+SOMEWHERE = 1 << 20                                                  # an aligned address that nothing may follow
+
+
+@pytest.mark.parametrize("B,S", [(1, 2 ** 31 - 1), (2 ** 31 - 1, 1), (1, 2 ** 31 - 256)])
+def test_token_counts_whose_last_block_passes_31_bits_are_refused(B, S):
+    """Blocks of several tokens count up to a block's tokens beyond the last: 85 to a block (three units of one head) make
+    25264515 blocks of 2^31 - 1 tokens, whose last index is 2^31 + 126."""
+    assert -(-(2 ** 31 - 1) // 85) * 85 - 1 > 2 ** 31 - 1
+    plan = decode.RopeStruct(SOMEWHERE, 2, 0, 1.0)
+    rc = decode._lib().csd_rope(SOMEWHERE, SOMEWHERE, binding.CSD_F32, B, S, 1, 6, 6 * S, 6, 6, 6 * S, 6, 6, SOMEWHERE, S, 1, byref(plan), 0, None)
+    assert rc == UNSUPPORTED
