@@ -54,10 +54,24 @@ SIGNATURES = {
                               c_void_p, c_size_t, c_void_p]),
 }
 
-def _stream_ptr(stream, device: int) -> int:
+def _current_device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _stream_ptr(stream, device: int, *others: int) -> int:
     """The stream asked for, or the device's current one (the raw handle: a Stream object costs 3 us to make, as much as the
-    call that it is made for)."""
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    call that it is made for).  `device` has to be the current one and that of all `others` (-1: host memory): a kernel given
+    addresses of another device's memory, or the host's, would fault."""
+    for d in others:
+        if d != device:
+            raise CsdError(f"tensors on different devices: {device} and {d} (-1: the host)")
+    if device != _current_device():
+        raise CsdError(f"tensors on device {device}, but the current device is {_current_device()}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise CsdError(f"tensors on device {device}, but a stream of device {stream.device_index}")
+    return stream.cuda_stream
 
 
 _typed = None
@@ -98,6 +112,7 @@ class RopePlan:
         steps, self.magnitude = csd_rope_steps(rot, base, scaling, factor, original_len, low, high)
         self.rot, self.layout = rot, layout
         self.steps = steps.to(device)
+        self._device = self.steps.get_device()
         self._struct = RopeStruct(self.steps.data_ptr(), rot, _LAYOUTS[layout], self.magnitude)
         self._ref = byref(self._struct)
 
@@ -119,7 +134,8 @@ def csd_rope(x, positions, plan: RopePlan, out=None, inverse: bool = False, stre
     else:
         assert positions.shape == (B, S)
     rc = _lib().csd_rope(x.data_ptr(), out.data_ptr(), code, B, S, H, D, xs[0], xs[1], xs[2], ys[0], ys[1], ys[2], positions.data_ptr(),
-                         ps[0], ps[1], plan._ref, 1 if inverse else 0, _stream_ptr(stream, x.get_device()))
+                         ps[0], ps[1], plan._ref, 1 if inverse else 0,
+                         _stream_ptr(stream, x.get_device(), out.get_device(), positions.get_device(), plan._device))
     if rc:
         _check(rc, "csd_rope")
     return out
@@ -174,7 +190,7 @@ class PagedCache:
         self._struct = CacheStruct(k.data_ptr(), v.data_ptr(), _DTYPES[dtype], layers, n_pages, page_size, kv_heads, head_dim, st[0],
                                    st[1], st[2], st[3], rows, self.max_pages, self.meta.data_ptr(), self.scratch.data_ptr())
         self._ref = byref(self._struct)
-        self._device = dev.index if dev.index is not None else torch.cuda.current_device()
+        self._device = self.k.get_device()
         csd_cache_rebuild(self)
 
     def load(self, table: torch.Tensor, lens: torch.Tensor, stream=None):
@@ -201,7 +217,7 @@ class PagedCache:
 def _rows_arg(t, cache: PagedCache, what: str):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == torch.int32 and t.shape == (cache.rows,) and t.is_contiguous(), what
+    assert t.get_device() == cache._device and t.dtype == torch.int32 and t.shape == (cache.rows,) and t.is_contiguous(), what
     return t.data_ptr()
 
 
@@ -247,7 +263,9 @@ def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | Non
     assert qs[3] == ks[3] == vs[3] == 1 and q_out.shape == shape and q_out.is_cuda and q_out.is_contiguous()
     rc = _lib().csd_rope_append(q.data_ptr(), qs[0], qs[1], qs[2], Hq, k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1], vs[2],
                                 q_out.data_ptr(), T, cache._ref, layer, None if plan is None else plan._ref,
-                                None if n_new is None else _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, cache._device))
+                                None if n_new is None else _rows_arg(n_new, cache, "n_new"),
+                                _stream_ptr(stream, cache._device, q.get_device(), k.get_device(), v.get_device(), q_out.get_device(),
+                                            cache._device if plan is None else plan._device))
     if rc:
         _check(rc, "csd_rope_append")
     return q_out
@@ -265,6 +283,7 @@ class AttentionBuffers:
         self.out = torch.empty(cache.rows, T, q_heads, cache.head_dim, dtype=cache.dtype, device=dev)
         self.lse = torch.empty(cache.rows, T, q_heads, dtype=torch.float32, device=dev)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+        self._device = self.workspace.get_device()
 
 
 def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale: float | None = None, n_new=None, stream=None):
@@ -274,7 +293,8 @@ def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale
     assert q.shape[0] == cache.rows and q.shape[3] == cache.head_dim
     rc = _lib().csd_attention(q.data_ptr(), qs[0], qs[1], qs[2], buf.T, buf.q_heads, cache._ref, layer,
                               cache.head_dim ** -0.5 if scale is None else scale, None if n_new is None else _rows_arg(n_new, cache, "n_new"),
-                              buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(), buf.ws_bytes, _stream_ptr(stream, cache._device))
+                              buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(), buf.ws_bytes,
+                              _stream_ptr(stream, cache._device, q.get_device(), buf._device))
     if rc:
         _check(rc, "csd_attention")
     return buf.out

@@ -37,3 +37,16 @@ def test_token_counts_whose_last_block_passes_31_bits_are_refused(B, S):
     plan = decode.RopeStruct(SOMEWHERE, 2, 0, 1.0)
     rc = decode._lib().csd_rope(SOMEWHERE, SOMEWHERE, binding.CSD_F32, B, S, 1, 6, 6 * S, 6, 6, 6 * S, 6, 6, SOMEWHERE, S, 1, byref(plan), 0, None)
     assert rc == UNSUPPORTED
+
+
+class _Stream:
+    def __init__(self, device_index):
+        self.device_index, self.cuda_stream = device_index, 5
+
+
+def test_addresses_of_another_device_are_refused(monkeypatch):
+    monkeypatch.setattr(decode, "_current_device", lambda: 0)
+    assert decode._stream_ptr(_Stream(0), 0, 0, 0) == 5
+    for stream, device, others in ((_Stream(0), 0, (0, -1)), (_Stream(0), 0, (1,)), (_Stream(1), 0, (0,)), (_Stream(1), 1, (1,)), (None, 1, ())):
+        with pytest.raises(binding.CsdError, match="device"):
+            decode._stream_ptr(stream, device, *others)
