@@ -620,9 +620,10 @@ csd_status_t csd_rope_append(const void *q, int64_t q_stride_b, int64_t q_stride
                              void *q_out, int T, const csd_cache_t *cache, int layer, const csd_rope_t *rope,
                              const int32_t *n_new, void *stream);
 
-/* Attention of the T newest tokens of every row over its cache: with g = q_heads / heads,
+/* Attention of T new tokens of every row over its cache: with g = q_heads / heads,
  *     out[b,t,h] = sum_j w_j v_j,  w = softmax_j(scale q[b,t,h].k_j),  lse[b,t,h] = ln sum_j exp(scale q[b,t,h].k_j)
- * over the places j <= lens[b] - n_new[b] + t of key head h / g.  A token that sees nothing (an empty row, t >= n_new[b], a
+ * over the places j <= lens[b] - n_new[b] + t of key head h / g (n_new NULL: T for every row; n_new[b] > T: the first T of that many new
+ * tokens, whose followers' places are not seen).  A token that sees nothing (an empty row, t >= n_new[b], a
  * negative place), or whose scores are all -inf, gives zeros and lse = -inf; what lies in places that a token does not see, infinities and NaN included,
  * does not reach its result.
  * q: [rows, T, q_heads, dim] of the cache's type, strides in elements, dim contiguous, 16-byte aligned (base and

@@ -264,7 +264,8 @@ struct Runs {
 };
 
 __device__ __forceinline__ int row_len(const Params &p, int b) { return min(max(ptx::ld_written(p.lens + b), 0), p.max_pages << p.page_shift); }
-__device__ __forceinline__ int row_news(const Params &p, int b) { return p.n_new ? min(max(ptx::ld_written(p.n_new + b), 0), p.T) : p.T; }
+// (may be more than T: a pass over the first T of them)
+__device__ __forceinline__ int row_news(const Params &p, int b) { return p.n_new ? max(ptx::ld_written(p.n_new + b), 0) : p.T; }
 
 // base[b + 1] holds the positions of row b; becomes base[b] = positions of the rows before b.  One warp.
 __device__ __forceinline__ void scan_tiles(int *base, int B)

@@ -287,7 +287,8 @@ class AttentionBuffers:
 
 
 def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale: float | None = None, n_new=None, stream=None):
-    """buf.out, buf.lse: attention of the T newest tokens of every row, q [rows, T, q_heads, D], over its cache."""
+    """buf.out, buf.lse: attention of T new tokens of every row, q [rows, T, q_heads, D], over its cache (n_new[row] > T: the first T
+    of that many)."""
     qs = q.stride()
     assert q.is_cuda and q.dtype == cache.dtype and qs[3] == 1 and q.shape == buf.out.shape
     assert q.shape[0] == cache.rows and q.shape[3] == cache.head_dim

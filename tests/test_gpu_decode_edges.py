@@ -1,11 +1,18 @@
 """Edges of the decode-pass operators: arguments that have to be refused, and places where a result could go wrong silently."""
 
+import math
+import os
+import sys
+
 import pytest
 import torch
 
 from paper_2604_13634_b200 import AttentionBuffers, CsdError, PagedCache, RopePlan, csd_attention, csd_rope, csd_rope_append, decode
 
 pytestmark = pytest.mark.gpu
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+from test_gpu_decode import check_attention, filled_cache, rand  # noqa: E402
 
 
 def test_a_plan_in_host_memory_or_another_current_device_is_refused(monkeypatch):
@@ -22,3 +29,51 @@ def test_a_plan_in_host_memory_or_another_current_device_is_refused(monkeypatch)
                  lambda: decode.csd_cache_extend(cache, 1), lambda: decode.csd_cache_compact(cache)):
         with pytest.raises(CsdError, match="device"):
             call()
+
+
+@pytest.mark.parametrize("poison", [math.nan, math.inf])
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,T,page", [(torch.bfloat16, 4, 2, 64, 3, 16), (torch.float16, 16, 2, 256, 2, 64), (torch.bfloat16, 8, 1, 128, 9, 16),
+                                                   (torch.float16, 24, 1, 64, 1, 32), (torch.bfloat16, 20, 2, 256, 4, 128)])
+def test_a_pass_over_the_first_of_many_new_tokens(poison, dtype, Hq, Hkv, D, T, page):
+    """n_new > T: token t lies at lens - n_new + t, and sees neither the places after it nor what they hold (nothing is written there yet)."""
+    lens, news = [400, 130, 64, 20, 700, 65], [300, T + 1, 64, 25, T, 2 ** 31 - 1]
+    cache, gen = filled_cache(50, lens, page, Hkv, D, dtype, False)
+    for b, n in enumerate(lens):
+        for at in range(max(0, n - news[b] + T), n):
+            page_id = int(cache.table[b, at // page])
+            cache.k[0, page_id, :, at % page] = poison
+            cache.v[0, page_id, :, at % page] = poison
+    q = rand(gen, len(lens), T, Hq, D, dtype=dtype, scale=2.0)
+    buf = AttentionBuffers(cache, T, Hq)
+    csd_attention(q, cache, 0, buf, n_new=torch.tensor(news, dtype=torch.int32, device="cuda"))
+    check_attention(buf, q, cache, lens, news, 1 / math.sqrt(D))
+    assert cache.stats()["flags"] == 0
+
+
+def test_a_prompt_in_pieces_after_one_extension():
+    """Room for the whole prompt once, then pieces of T tokens with n_new = what is left: each token sees what it would see alone."""
+    n, T, Hq, Hkv, D = 150, 33, 8, 2, 64
+    caches = [PagedCache(2, 24, 16, 1, Hkv, D, torch.bfloat16, 192) for _ in range(2)]
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    qkv = rand(gen, 2, 5 * T, Hq + 2 * Hkv, D)
+    plan = RopePlan(D)
+    outs = []
+    for whole, cache in zip((True, False), caches):
+        cache.k.fill_(math.nan), cache.v.fill_(math.nan)
+        buf, got = AttentionBuffers(cache, T, Hq), []
+        if whole:
+            decode.csd_cache_extend(cache, n)
+        for at in range(0, n, T):
+            left = torch.full((2,), n - at if whole else min(T, n - at), dtype=torch.int32, device="cuda")
+            if not whole:
+                decode.csd_cache_extend(cache, T, left)
+            q, k, v = qkv[:, at:at + T].split([Hq, Hkv, Hkv], dim=2)
+            q = csd_rope_append(q, k, v, cache, 0, plan, n_new=left)
+            got.append(csd_attention(q, cache, 0, buf, n_new=left).clone())
+        outs.append(torch.cat(got, dim=1))
+        assert cache.stats()["flags"] == 0 and cache.lens.tolist() == [n, n]
+    assert torch.isfinite(outs[0].float()).all() and not outs[0][:, n:].any()
+    for a, b in zip(caches[0].table[0].tolist(), caches[1].table[0].tolist()):
+        assert a < 0 or torch.equal(caches[0].k[0, a].nan_to_num(), caches[1].k[0, b].nan_to_num())
+    # the splits differ with the lengths, so the sums' order does: two roundings of bf16
+    assert (outs[0] - outs[1]).abs().max() <= 2 * 2.0 ** -8 * qkv[..., Hq + Hkv:, :].abs().max()
