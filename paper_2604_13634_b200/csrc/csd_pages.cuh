@@ -233,7 +233,8 @@ __global__ void __launch_bounds__(kRowThreads) truncate_kernel(const View v, con
     const int len = v.lens[r];
     int to;
     if (accept_len) {
-        const int n = v.granted[r], kept = min(n, max(ptx::ld_written(accept_len + r), -1) + 1);
+        // (bounded before one is added: any accepted count will do, 2^31 - 1 for "all" among them)
+        const int n = v.granted[r], kept = min(max(ptx::ld_written(accept_len + r), -1), n - 1) + 1;
         to = len - (n - kept);
     } else {
         to = ptx::ld_written(new_lens + r);

@@ -7,7 +7,8 @@ import sys
 import pytest
 import torch
 
-from paper_2604_13634_b200 import AttentionBuffers, CsdError, PagedCache, RopePlan, csd_attention, csd_rope, csd_rope_append, decode
+from paper_2604_13634_b200 import (AttentionBuffers, CsdError, PagedCache, RopePlan, csd_attention, csd_cache_commit, csd_cache_extend, csd_rope,
+                                   csd_rope_append, decode)
 
 pytestmark = pytest.mark.gpu
 
@@ -26,7 +27,7 @@ def test_a_plan_in_host_memory_or_another_current_device_is_refused(monkeypatch)
     buf, plan = AttentionBuffers(cache, 1, 2), RopePlan(64)
     monkeypatch.setattr(decode, "_current_device", lambda: 1)
     for call in (lambda: csd_rope(x, pos, plan), lambda: csd_rope_append(q, q, q, cache, 0, None), lambda: csd_attention(q, cache, 0, buf),
-                 lambda: decode.csd_cache_extend(cache, 1), lambda: decode.csd_cache_compact(cache)):
+                 lambda: csd_cache_extend(cache, 1), lambda: decode.csd_cache_compact(cache)):
         with pytest.raises(CsdError, match="device"):
             call()
 
@@ -62,11 +63,11 @@ def test_a_prompt_in_pieces_after_one_extension():
         cache.k.fill_(math.nan), cache.v.fill_(math.nan)
         buf, got = AttentionBuffers(cache, T, Hq), []
         if whole:
-            decode.csd_cache_extend(cache, n)
+            csd_cache_extend(cache, n)
         for at in range(0, n, T):
             left = torch.full((2,), n - at if whole else min(T, n - at), dtype=torch.int32, device="cuda")
             if not whole:
-                decode.csd_cache_extend(cache, T, left)
+                csd_cache_extend(cache, T, left)
             q, k, v = qkv[:, at:at + T].split([Hq, Hkv, Hkv], dim=2)
             q = csd_rope_append(q, k, v, cache, 0, plan, n_new=left)
             got.append(csd_attention(q, cache, 0, buf, n_new=left).clone())
@@ -77,3 +78,13 @@ def test_a_prompt_in_pieces_after_one_extension():
         assert a < 0 or torch.equal(caches[0].k[0, a].nan_to_num(), caches[1].k[0, b].nan_to_num())
     # the splits differ with the lengths, so the sums' order does: two roundings of bf16
     assert (outs[0] - outs[1]).abs().max() <= 2 * 2.0 ** -8 * qkv[..., Hq + Hkv:, :].abs().max()
+
+
+@pytest.mark.parametrize("extreme,kept", [(2 ** 31 - 1, 5), (-2 ** 31, 0)])
+def test_commit_takes_any_accepted_count(extreme, kept):
+    cache = PagedCache(3, 12, 8, 1, 1, 64, torch.bfloat16, 64)
+    csd_cache_extend(cache, 20)
+    csd_cache_commit(cache, torch.full((3,), 19, dtype=torch.int32, device="cuda"))
+    csd_cache_extend(cache, 5)
+    csd_cache_commit(cache, torch.tensor([extreme, 1, extreme], dtype=torch.int32, device="cuda"))
+    assert cache.lens.tolist() == [20 + kept, 22, 20 + kept]
