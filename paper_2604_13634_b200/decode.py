@@ -184,7 +184,7 @@ class PagedCache:
         # strides of dimensions of size 1 mean nothing to torch; the library reads them
         st = list(k.stride())
         if kv_heads == 1:
-            st[2], st[3] = page_size * head_dim, head_dim
+            st[2] = page_size * head_dim
         if n_pages == 1:
             st[1] = kv_heads * page_size * head_dim
         self._struct = CacheStruct(k.data_ptr(), v.data_ptr(), _DTYPES[dtype], layers, n_pages, page_size, kv_heads, head_dim, st[0],

@@ -88,3 +88,18 @@ def test_commit_takes_any_accepted_count(extreme, kept):
     csd_cache_extend(cache, 5)
     csd_cache_commit(cache, torch.tensor([extreme, 1, extreme], dtype=torch.int32, device="cuda"))
     assert cache.lens.tolist() == [20 + kept, 22, 20 + kept]
+
+
+def test_a_pool_of_one_head_keeps_its_token_stride():
+    for shape, halves in (((2, 4, 1, 16, 128), 4), ((2, 4, 1, 32, 64), 3)):
+        kv = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+        k, v = kv.split(64, dim=4) if halves == 4 else (kv[:, :, :, 0::2], kv[:, :, :, 1::2])
+        with pytest.raises(CsdError):
+            PagedCache(1, 4, 16, 2, 1, 64, torch.bfloat16, 64, k=k, v=v)
+    for shape in ((2, 4, 1, 16, 64), (2, 4, 16, 1, 64)):
+        k, v = (torch.zeros(shape, dtype=torch.bfloat16, device="cuda").view(2, 4, 1, 16, 64) for _ in range(2))
+        cache = PagedCache(1, 4, 16, 2, 1, 64, torch.bfloat16, 64, k=k, v=v)
+        csd_cache_extend(cache, 3)
+        new = torch.arange(3, device="cuda").view(1, 3, 1, 1).expand(1, 3, 1, 64).to(torch.bfloat16)
+        csd_rope_append(new, new, new, cache, 1, None)
+        assert torch.equal(cache.k[1, 0, 0, :3], new[0, :, 0]) and torch.equal(cache.v[1, 0, 0, :3], new[0, :, 0])
