@@ -8,8 +8,9 @@ the cache once, in pieces, and every row shares its pages (csd_cache_fork).  Eac
     csd_step_lmhead      verification straight from the hidden states
     csd_cache_commit     keep the last token and the accepted drafts, free the rest
 
-with nothing read back to the host between.  The drafts come from a table of the last successor of every token, which stands in
-for a draft model.  `--check` recomputes the hidden states of a row's whole sequence without a cache.
+with nothing read back to the host between.  The tokens that a pass stores and attends to are those that the extension granted
+(cache.granted, on the device): one that finds no room grants none and leaves a flag, and the pass then touches no page.  The drafts
+come from a table of the last successor of every token, which stands in for a draft model.  `--check` recomputes the hidden states of a row's whole sequence without a cache.
 
     python examples/decode_with_cache.py --rows 8 --steps 40 --check
 """
@@ -45,15 +46,16 @@ class Target:
         y = x.float()
         return (y * torch.rsqrt(y.square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
 
-    def hidden(self, tokens, cache, buffers, n_new=None):
-        """tokens [rows, T]: the newest tokens of every row, for which the cache has room -> [rows, T, H]."""
+    def hidden(self, tokens, cache, buffers):
+        """tokens [rows, T]: new tokens of every row, of which the last extension of the cache granted the first cache.granted[row]
+        -> [rows, T, H].  After an extension that found no room that is none of them: nothing is stored, nothing attended to."""
         rows, T = tokens.shape
         x = self.embedding[tokens.long()]
         for layer in range(self.layers):
             qkv = (self.normed(x) @ self.qkv[layer].T).view(rows, T, -1, self.D)
             q, k, v = qkv.split([self.q_heads, self.kv_heads, self.kv_heads], dim=2)
-            q = csd.csd_rope_append(q, k, v, cache, layer, self.rope, n_new=n_new)
-            seen = csd.csd_attention(q, cache, layer, buffers, n_new=n_new)
+            q = csd.csd_rope_append(q, k, v, cache, layer, self.rope, n_new=cache.granted)
+            seen = csd.csd_attention(q, cache, layer, buffers, n_new=cache.granted)
             x = x + seen.view(rows, T, -1) @ self.out[layer].T
         return self.normed(x)
 
@@ -97,7 +99,7 @@ def decode(target: Target, rows=8, K=4, steps=40, prompt_len=100, page_size=16, 
         tokens = torch.zeros(rows, piece, dtype=torch.int32, device=dev)
         tokens[0, :part.numel()] = part
         csd.csd_cache_extend(cache, piece, only_first)
-        target.hidden(tokens, cache, buffers, n_new=only_first)
+        target.hidden(tokens, cache, buffers)
     csd.csd_cache_fork(cache, torch.zeros(rows, dtype=torch.int32, device=dev))
 
     # rows begin with different tokens, or all would say the same
@@ -121,7 +123,8 @@ def decode(target: Target, rows=8, K=4, steps=40, prompt_len=100, page_size=16, 
         emitted = tokens.gather(1, buf.accept_len[:, None].long())[:, 0]
         last = buf.next_token.clone()
         successor[emitted.long()] = last
-    torch.cuda.synchronize()
+    if cache.stats()["flags"]:                                    # an extension found no room, or worse
+        raise RuntimeError(f"cache flags {cache.stats()['flags']:#x}")
     sequences = [prompt[:-1].tolist() for _ in range(rows)]
     for tokens, kept in said:
         for r, (row, n) in enumerate(zip(tokens.tolist(), kept.tolist())):

@@ -492,11 +492,13 @@ csd_status_t csd_ocm_stats(const csd_ocm_t *ocm, csd_stats_t *host_out, void *st
  * and keys are turned by their positions, keys and values join the row's cache, and the queries read the whole cache.
  * The entry points below are that part of the pass and the cache's bookkeeping between steps:
  *     csd_cache_extend (cache, T = K + 1)                 room for the last token and the K drafted ones
- *     per layer:  csd_rope_append(q, k, v, ...)           turn, store
- *                 csd_attention(q', ...)                  read
+ *     per layer:  csd_rope_append(q, k, v, ..., granted)  turn, store
+ *                 csd_attention(q', ..., granted)         read
  *     csd_step / csd_step_lmhead                          accept_len
  *     csd_cache_commit(cache, accept_len)                 keep the last token and the accepted ones, free the rest
- * with csd_cache_fork where rows continue other rows (beams, shared prompts) and csd_cache_compact where a pool has to
+ * n_new of the two calls per layer is the cache's own array `granted` (csd_cache_meta_layout): an extension that finds no room
+ * grants nothing and leaves the lengths, and tokens stored without that room would lie over the newest ones of every row.
+ * And csd_cache_fork where rows continue other rows (beams, shared prompts) and csd_cache_compact where a pool has to
  * shrink.  Nothing here synchronises unless it says so; lengths, page tables and counts stay on the device.
  */
 
@@ -611,7 +613,8 @@ csd_status_t csd_cache_compact(const csd_cache_t *cache, void *stream);
 /* One launch for the new tokens of a layer, turned at their places and stored: token t of row b lies at place
  * lens[b] - n_new[b] + t (n_new NULL: T for every row).  q' to q_out [rows, T, q_heads, dim] (dense; may be q itself), k'
  * and v to their page slots.  A token that does not exist (t >= n_new[b], or a negative place) gets a zero query and
- * stores nothing.  q, k, v: [rows, T, heads, dim] of the cache's type, strides in elements, dim contiguous (slices of one projection's
+ * stores nothing.  n_new says which places are written, not the counts of the last extension: after one that granted nothing, NULL
+ * writes over the row's T newest tokens; pass `granted`.  q, k, v: [rows, T, heads, dim] of the cache's type, strides in elements, dim contiguous (slices of one projection's
  * output qualify).  rope NULL: no rotation.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 csd_status_t csd_rope_append(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int q_heads,

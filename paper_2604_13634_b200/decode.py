@@ -227,7 +227,8 @@ def csd_cache_rebuild(cache: PagedCache, stream=None):
 
 
 def csd_cache_extend(cache: PagedCache, T: int, n_new=None, stream=None):
-    """Room for T (or n_new[row]) more tokens in every row; cache.granted says how many each row got (all rows or none)."""
+    """Room for T (or n_new[row]) more tokens in every row; cache.granted says how many each row got (all rows or none) and is the
+    n_new of the calls that store and read them."""
     _check(_lib().csd_cache_extend(cache._ref, T, _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, cache._device)), "csd_cache_extend")
 
 
@@ -253,7 +254,8 @@ def csd_cache_compact(cache: PagedCache, stream=None):
 
 def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | None, q_out=None, n_new=None, stream=None):
     """The new tokens of a layer: q [rows, T, q_heads, D] turned into q_out (dense; returned), k turned and v as it is into
-    their page slots.  plan None: no rotation."""
+    their page slots.  plan None: no rotation.  After csd_cache_extend pass n_new=cache.granted: where that found no room it
+    granted nothing, and T tokens (n_new None) would go over the newest ones of the row."""
     B, T, Hq, D = shape = q.shape
     if q_out is None:
         q_out = torch.empty(shape, dtype=q.dtype, device=q.device)

@@ -7,12 +7,13 @@ import sys
 import pytest
 import torch
 
-from paper_2604_13634_b200 import (AttentionBuffers, CsdError, PagedCache, RopePlan, csd_attention, csd_cache_commit, csd_cache_extend, csd_rope,
-                                   csd_rope_append, decode)
+from paper_2604_13634_b200 import (AttentionBuffers, CsdError, PagedCache, RopePlan, csd_attention, csd_cache_commit, csd_cache_extend, csd_cache_fork,
+                                   csd_rope, csd_rope_append, decode)
 
 pytestmark = pytest.mark.gpu
 
-sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+HERE = os.path.dirname(os.path.abspath(__file__))
+sys.path.insert(0, HERE)
 from test_gpu_decode import check_attention, filled_cache, rand  # noqa: E402
 
 
@@ -103,3 +104,24 @@ def test_a_pool_of_one_head_keeps_its_token_stride():
         new = torch.arange(3, device="cuda").view(1, 3, 1, 1).expand(1, 3, 1, 64).to(torch.bfloat16)
         csd_rope_append(new, new, new, cache, 1, None)
         assert torch.equal(cache.k[1, 0, 0, :3], new[0, :, 0]) and torch.equal(cache.v[1, 0, 0, :3], new[0, :, 0])
+
+
+def test_a_refused_extension_leaves_every_page_as_it_was():
+    sys.path.insert(0, os.path.join(os.path.dirname(HERE), "examples"))
+    import decode_with_cache as example
+    target = example.Target()
+    cache = PagedCache(3, 3, 16, target.layers, target.kv_heads, target.D, torch.bfloat16, 64)
+    buffers = AttentionBuffers(cache, 5, target.q_heads)
+    tokens = torch.arange(15, dtype=torch.int32, device="cuda").view(3, 5)
+    n = torch.tensor([5, 0, 0], dtype=torch.int32, device="cuda")
+    for _ in range(4):
+        csd_cache_extend(cache, 5, n)
+        target.hidden(tokens, cache, buffers)
+    csd_cache_fork(cache, torch.zeros(3, dtype=torch.int32, device="cuda"))
+    assert cache.lens.tolist() == [20] * 3 and cache.stats() == dict(flags=0, pages=2, shared=2, tokens=60)
+    k, v, table = cache.k.clone(), cache.v.clone(), cache.table.clone()
+    csd_cache_extend(cache, 5)                                        # two copies of the shared last page are wanted, one page is free
+    target.hidden(tokens, cache, buffers)
+    csd_cache_commit(cache, torch.full((3,), 2, dtype=torch.int32, device="cuda"))
+    assert torch.equal(cache.k, k) and torch.equal(cache.v, v) and torch.equal(cache.table, table)
+    assert cache.lens.tolist() == [20] * 3 and cache.stats()["flags"] == decode.CACHE_FULL
