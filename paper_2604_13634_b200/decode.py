@@ -199,6 +199,7 @@ class PagedCache:
         assert table.shape[1] <= self.max_pages
         with torch.cuda.stream(torch.cuda.current_stream() if stream is None else stream):
             self.table[:, :table.shape[1]].copy_(table)
+            self.table[:, table.shape[1]:].fill_(-1)              # a length beyond the table given is flagged, not read from the one before
             self.lens.copy_(lens)
         csd_cache_rebuild(self, stream)
 

@@ -125,3 +125,12 @@ def test_a_refused_extension_leaves_every_page_as_it_was():
     csd_cache_commit(cache, torch.full((3,), 2, dtype=torch.int32, device="cuda"))
     assert torch.equal(cache.k, k) and torch.equal(cache.v, v) and torch.equal(cache.table, table)
     assert cache.lens.tolist() == [20] * 3 and cache.stats()["flags"] == decode.CACHE_FULL
+
+
+def test_load_of_a_narrower_table_keeps_nothing_of_the_one_before():
+    cache = PagedCache(2, 20, 8, 1, 1, 64, torch.bfloat16, 64)
+    table = torch.arange(16, dtype=torch.int32).view(2, 8)
+    cache.load(table, torch.tensor([64, 64], dtype=torch.int32))
+    cache.load(table[:, :2].contiguous(), torch.tensor([40, 16], dtype=torch.int32))
+    assert cache.stats()["flags"] == decode.CACHE_BAD_PAGE and (cache.table[:, 2:] == -1).all()
+    assert cache.refs.tolist() == [1, 1] + [0] * 6 + [1, 1] + [0] * 10
