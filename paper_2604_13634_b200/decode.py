@@ -293,7 +293,7 @@ def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale
     """buf.out, buf.lse: attention of T new tokens of every row, q [rows, T, q_heads, D], over its cache (n_new[row] > T: the first T
     of that many)."""
     qs = q.stride()
-    assert q.is_cuda and q.dtype == cache.dtype and qs[3] == 1 and q.shape == buf.out.shape
+    assert q.is_cuda and q.dtype == cache.dtype == buf.out.dtype and qs[3] == 1 and q.shape == buf.out.shape
     assert q.shape[0] == cache.rows and q.shape[3] == cache.head_dim
     rc = _lib().csd_attention(q.data_ptr(), qs[0], qs[1], qs[2], buf.T, buf.q_heads, cache._ref, layer,
                               cache.head_dim ** -0.5 if scale is None else scale, None if n_new is None else _rows_arg(n_new, cache, "n_new"),

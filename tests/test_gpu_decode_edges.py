@@ -134,3 +134,10 @@ def test_load_of_a_narrower_table_keeps_nothing_of_the_one_before():
     cache.load(table[:, :2].contiguous(), torch.tensor([40, 16], dtype=torch.int32))
     assert cache.stats()["flags"] == decode.CACHE_BAD_PAGE and (cache.table[:, 2:] == -1).all()
     assert cache.refs.tolist() == [1, 1] + [0] * 6 + [1, 1] + [0] * 10
+
+
+def test_buffers_of_another_type_are_refused():
+    caches = [PagedCache(1, 4, 16, 1, 2, 64, dtype, 64) for dtype in (torch.bfloat16, torch.float16)]
+    buf = AttentionBuffers(caches[0], 1, 2)
+    with pytest.raises(AssertionError):
+        csd_attention(torch.zeros(1, 1, 2, 64, dtype=torch.float16, device="cuda"), caches[1], 0, buf)
