@@ -74,6 +74,15 @@ def _stream_ptr(stream, device: int, *others: int) -> int:
     return stream.cuda_stream
 
 
+def _result(x, stream, **kw):
+    """An uninitialised result like x, owned by the stream that writes it: memory of the current stream could have been freed by
+    work that is still to run there, and would go back to it while the other stream still writes."""
+    if stream is None:
+        return torch.empty_like(x, **kw)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(x, **kw)
+
+
 _typed = None
 
 
@@ -123,7 +132,7 @@ def csd_rope(x, positions, plan: RopePlan, out=None, inverse: bool = False, stre
     code = _DTYPES.get(x.dtype)
     if code is None:
         raise CsdError(f"x must be float32, bfloat16 or float16, got {x.dtype}")
-    out = torch.empty_like(x) if out is None else out
+    out = _result(x, stream) if out is None else out
     B, S, H, D = shape = x.shape
     xs, ys, ps = x.stride(), out.stride(), positions.stride()
     assert x.is_cuda and positions.is_cuda and positions.dtype == torch.int32 and xs[3] == 1
@@ -259,7 +268,7 @@ def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | Non
     granted nothing, and T tokens (n_new None) would go over the newest ones of the row."""
     B, T, Hq, D = shape = q.shape
     if q_out is None:
-        q_out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        q_out = _result(q, stream, memory_format=torch.contiguous_format)
     qs, ks, vs = q.stride(), k.stride(), v.stride()
     assert q.is_cuda and k.is_cuda and v.is_cuda and q.dtype == k.dtype == v.dtype == q_out.dtype == cache.dtype
     assert B == cache.rows and D == cache.head_dim and k.shape == v.shape == (B, T, cache.kv_heads, D)

@@ -141,3 +141,19 @@ def test_buffers_of_another_type_are_refused():
     buf = AttentionBuffers(caches[0], 1, 2)
     with pytest.raises(AssertionError):
         csd_attention(torch.zeros(1, 1, 2, 64, dtype=torch.float16, device="cuda"), caches[1], 0, buf)
+
+
+def test_results_belong_to_the_stream_that_writes_them():
+    s = torch.cuda.Stream()
+    x, pos, plan = torch.randn(1, 500, 8, 64, device="cuda"), torch.zeros(1, 500, dtype=torch.int32, device="cuda"), RopePlan(64)
+    cache = PagedCache(1, 64, 16, 1, 8, 64, torch.bfloat16, 1024)
+    q = torch.zeros(1, 300, 8, 64, dtype=torch.bfloat16, device="cuda")
+    csd_cache_extend(cache, 300)
+    torch.cuda.synchronize()
+    for call in (lambda: csd_rope(x, pos, plan, stream=s), lambda: csd_rope_append(q, q, q, cache, 0, plan, stream=s)):
+        y = call()
+        torch.cuda.synchronize()
+        at, like = y.data_ptr(), (y.shape, y.dtype)
+        del y
+        again = torch.empty(like[0], dtype=like[1], device="cuda")
+        assert again.data_ptr() != at
