@@ -126,9 +126,29 @@ class RopePlan:
         self._ref = byref(self._struct)
 
 
+class _Rope(torch.autograd.Function):
+    """The rotation is linear: its gradient is the turn back, with the same factor."""
+
+    @staticmethod
+    def forward(ctx, x, positions, plan, inverse, stream):
+        ctx.save_for_backward(positions)
+        ctx.plan, ctx.inverse = plan, inverse
+        return csd_rope(x, positions, plan, inverse=inverse, stream=stream)
+
+    @staticmethod
+    def backward(ctx, g):
+        (positions,) = ctx.saved_tensors
+        g = g if g.stride(3) == 1 else g.contiguous()
+        return csd_rope(g, positions, ctx.plan, inverse=not ctx.inverse), None, None, None, None
+
+
 def csd_rope(x, positions, plan: RopePlan, out=None, inverse: bool = False, stream=None):
     """x [B, S, H, D] turned by positions [B, S] int32 (or [S], shared by the batch); `inverse` turns back, which is the
-    gradient.  `out` may be x itself.  Returns out."""
+    gradient: autograd knows it where x requires one and no `out` is given.  `out` may be x itself.  Returns out."""
+    if x.requires_grad and torch.is_grad_enabled():
+        if out is not None:
+            raise CsdError("csd_rope: a result written into `out` has no gradient; x requires one")
+        return _Rope.apply(x, positions, plan, inverse, stream)
     code = _DTYPES.get(x.dtype)
     if code is None:
         raise CsdError(f"x must be float32, bfloat16 or float16, got {x.dtype}")
@@ -265,7 +285,7 @@ def csd_cache_compact(cache: PagedCache, stream=None):
 def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | None, q_out=None, n_new=None, stream=None):
     """The new tokens of a layer: q [rows, T, q_heads, D] turned into q_out (dense; returned), k turned and v as it is into
     their page slots.  plan None: no rotation.  After csd_cache_extend pass n_new=cache.granted: where that found no room it
-    granted nothing, and T tokens (n_new None) would go over the newest ones of the row."""
+    granted nothing, and T tokens (n_new None) would go over the newest ones of the row.  Serving form: no gradient (csd_rope has one)."""
     B, T, Hq, D = shape = q.shape
     if q_out is None:
         q_out = _result(q, stream, memory_format=torch.contiguous_format)
@@ -300,7 +320,7 @@ class AttentionBuffers:
 
 def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale: float | None = None, n_new=None, stream=None):
     """buf.out, buf.lse: attention of T new tokens of every row, q [rows, T, q_heads, D], over its cache (n_new[row] > T: the first T
-    of that many)."""
+    of that many).  Serving form: no gradient."""
     qs = q.stride()
     assert q.is_cuda and q.dtype == cache.dtype == buf.out.dtype and qs[3] == 1 and q.shape == buf.out.shape
     assert q.shape[0] == cache.rows and q.shape[3] == cache.head_dim

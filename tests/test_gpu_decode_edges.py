@@ -157,3 +157,22 @@ def test_results_belong_to_the_stream_that_writes_them():
         del y
         again = torch.empty(like[0], dtype=like[1], device="cuda")
         assert again.data_ptr() != at
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rope_has_a_gradient(dtype):
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(2, 5, 3, 80, generator=gen, device="cuda").to(dtype).requires_grad_()
+    g = torch.randn(2, 5, 3, 80, generator=gen, device="cuda").to(dtype)
+    pos = torch.randint(0, 5000, (2, 5), generator=gen, device="cuda", dtype=torch.int32)
+    plan = RopePlan(64, layout="interleaved", scaling="yarn", factor=4.0)
+    y = csd_rope(x, pos, plan)
+    assert y.requires_grad and torch.equal(y, csd_rope(x.detach(), pos, plan))
+    (got,) = torch.autograd.grad(y, x, g)
+    assert torch.equal(got, csd_rope(g, pos, plan, inverse=True))
+    (got,) = torch.autograd.grad(csd_rope(x, pos, plan, inverse=True).sum(), x)      # a gradient without strides, of the turn back
+    assert torch.equal(got, csd_rope(torch.ones_like(g), pos, plan))
+    with pytest.raises(CsdError, match="gradient"):
+        csd_rope(x, pos, plan, out=torch.empty_like(x))
+    with torch.no_grad():
+        assert not csd_rope(x, pos, plan, out=torch.empty_like(x)).requires_grad
