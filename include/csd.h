@@ -632,11 +632,13 @@ csd_status_t csd_rope_append(const void *q, int64_t q_stride_b, int64_t q_stride
  * q: [rows, T, q_heads, dim] of the cache's type, strides in elements, dim contiguous, 16-byte aligned (base and
  * strides); T <= CSD_MAX_K + 1; out: dense, the cache's type, 16-byte aligned; lse: float [rows, T, q_heads] or NULL.
  * scale: finite.  Scores, maxima and sums are float32; the weights are rounded to the cache's type for the second product
- * and counted in the sum before that rounding.
+ * and counted in the sum before that rounding (float16: raised by a power of two first, so that what its range drops is at most
+ * 2^-32 of the largest weight per place).
  * The places of all rows and heads are split evenly over the GPU; what several blocks have read of a (row, head) is joined by
  * a second launch, in the order of the places, so results are bit-reproducible for given lengths.  More than 16 query rows to
- * a key head (T * g > 16) take the tensor-memory products: there the maximum that the weights refer to follows the scores
- * by powers of two up to 2^8, which moves their rounding but no bound on it.
+ * a key head (T * g > 16) take the tensor-memory products: there what the weights refer to is a maximum that stays
+ * until a score exceeds it by more than a factor 2^8 and then jumps to the largest score of that tile, which moves their rounding but
+ * no bound on it.
  * workspace: csd_attention_workspace_bytes bytes, 256-byte aligned, no initialisation; one call at a time; any shape that it
  * is large enough for.
  * Two launches; asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (q_heads not a multiple of heads, T, more than 2^31 tiles of

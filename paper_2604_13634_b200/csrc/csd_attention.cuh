@@ -171,6 +171,18 @@ template <>
 struct ExponentBits<__half> {
     static constexpr unsigned int value = 0x7c00u;
 };
+// Weights go into the second product in the cache's type: a relative error of 2^-9 (bfloat16) or 2^-12 (float16) of each, of random
+// sign, where the result itself is rounded to that type; the sum l is taken before the rounding.  Float16 steps by 2^-24 below 2^-14, and
+// what is below 2^-25 of the largest weight would be counted in l and dropped from the product (0.4 % of the result for 131072 places
+// of 2^-25).  So a row's reference m lies this many powers of two below the maximum: O and l carry the factor, their quotient and
+// m + log2 l do not.  Float16 holds 2^15; in the kernel whose reference may lag by 2^kLag that much is left for it.  What remains is
+// at most 2^-39 of the largest weight per place, or 2^-32.
+constexpr int kLag = 8;
+template <typename T>
+__device__ __forceinline__ constexpr float raised(int lag)
+{
+    return ExponentBits<T>::value == 0x7c00u ? static_cast<float>(lag == 0 ? 14 : 15 - lag) : 0.f;
+}
 template <typename T>
 __device__ __forceinline__ unsigned int finite_only(unsigned int two)
 {
@@ -595,7 +607,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     for (int n = 0; n < 2 * NK; ++n) v = fmaxf(v, fmaxf(x[n][2 * hh], x[n][2 * hh + 1]));
                     v = fmaxf(v, __shfl_xor_sync(kFull, v, 1));
                     v = fmaxf(v, __shfl_xor_sync(kFull, v, 2));
-                    mx[hh] = fmaxf(m[hh], v);
+                    mx[hh] = fmaxf(m[hh], v - raised<T>(0));
                     grew |= mx[hh] > m[hh];
                     at0[hh] = mx[hh] == -INFINITY ? 0.f : mx[hh];
                 }
@@ -622,8 +634,6 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                         x[n][e] = ex2_approx(x[n][e] - at0[e >> 1]);
                         l[e >> 1] += x[n][e];
                     }
-                // the weights go into the second product in the cache's type: relative error 2^-9 (2^-12) of each, of random sign,
-                // where the result itself is rounded to that type; the sum l is taken before the rounding
                 unsigned int pa[NK][4];
 #pragma unroll
                 for (int nk = 0; nk < NK; ++nk) {
@@ -800,8 +810,8 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 // 64 it holds 16, in its first 16 lanes.  Each query row twice, against either half of a tile's places, took 225 us against 206 (36
 // query rows of 128): the products' issue and reads, not the weights, are what a tile waits for (with dim 64 the pipe is busy for
 // half of the time).
-// The reference m of a row only moves when a tile's maximum exceeds it by 2^8 (weights up to 2^8 are harmless in float32 sums
-// and in either cache type), so the accumulators in tensor memory are rescaled a few times per unit, not per tile.
+// The reference of a row stays while no score exceeds it by more than kLag powers of two (weights up to 2^kLag, raised as above, are
+// harmless in float32 sums and in either cache type) and jumps to the tile's maximum when one does, so the accumulators in tensor memory are rescaled a few times per unit, not per tile.
 constexpr int kTcTile = 64;
 constexpr int kTcThreads = 192;
 constexpr int kTcMaxSlots = 16;
@@ -1100,10 +1110,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     float up = 0.f;
                     if (limit >= 0) {
                         if (l == 0.f) {
-                            up = mx == -INFINITY ? 0.f : mx;
-                        } else if (mx > 8.f) {
-                            up = mx;
-                            f = ex2_approx(-mx);
+                            up = mx == -INFINITY ? 0.f : mx - raised<T>(kLag);
+                        } else if (mx > raised<T>(kLag) + kLag) {
+                            up = mx - raised<T>(kLag);
+                            f = ex2_approx(-up);
                         }
                     }
                     if (__any_sync(kFull, up != 0.f)) {
@@ -1115,8 +1125,6 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                             y[j] -= up;
                         }
                     }
-                    // the weights go into the second product in the cache's type: relative error 2^-9 (2^-12) of each, of random
-                    // sign, where the result itself is rounded to that type; the sum l is taken before the rounding
                     unsigned int w2[32];
                     unsigned long long sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll

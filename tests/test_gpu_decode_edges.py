@@ -4,9 +4,11 @@ import math
 import os
 import sys
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import decode_oracle as O
 from paper_2604_13634_b200 import (AttentionBuffers, CsdError, PagedCache, RopePlan, csd_attention, csd_cache_commit, csd_cache_extend, csd_cache_fork,
                                    csd_rope, csd_rope_append, decode)
 
@@ -14,7 +16,7 @@ pytestmark = pytest.mark.gpu
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, HERE)
-from test_gpu_decode import check_attention, filled_cache, rand  # noqa: E402
+from test_gpu_decode import ULP, check_attention, f64, filled_cache, rand  # noqa: E402
 
 
 def test_a_plan_in_host_memory_or_another_current_device_is_refused(monkeypatch):
@@ -176,3 +178,29 @@ def test_rope_has_a_gradient(dtype):
         csd_rope(x, pos, plan, out=torch.empty_like(x))
     with torch.no_grad():
         assert not csd_rope(x, pos, plan, out=torch.empty_like(x)).requires_grad
+
+
+@pytest.mark.parametrize("group,T,raised", [(2, 1, 14), (20, 1, 7), (3, 9, 7)])     # 2 query rows to a key head, 20 and 27
+@pytest.mark.parametrize("at", [0, 70000, 131071])
+def test_many_small_weights_in_float16(group, T, raised, at):
+    """One place with most of the weight and 131071 with 2^-25.1 of it each, which a weight rounded to float16 as it is would drop.
+    The rows share their pages; there are more of them than blocks, so that some are read by one block whole."""
+    n, D, rows, heads = 131072, 64, 40, 8
+    cache = PagedCache(rows, n // 64, 64, 1, heads, D, torch.float16, n)
+    cache.load(torch.arange(n // 64, dtype=torch.int32, device="cuda").expand(rows, -1), torch.full((rows,), n, dtype=torch.int32, device="cuda"))
+    cache.v.fill_(1.0)
+    cache.k[0, at // 64, :, at % 64, 0] = 1.0
+    cache.v[0, at // 64, :, at % 64] = 0.0
+    q = torch.zeros(rows, T, heads * group, D, dtype=torch.float16, device="cuda")
+    q[..., 0] = 16.0
+    scale = 25.1 * math.log(2) / 16
+    buf = AttentionBuffers(cache, T, heads * group)
+    csd_attention(q, cache, 0, buf, scale=scale)
+    k, v = (f64(x[0, :, 0]).reshape(1, n, D) for x in (cache.k, cache.v))
+    out, lse, reach, size = O.attention(f64(q[0, :, :1]), k, v, T, scale)                # all heads hold the same
+    e, u = 2 * (D + 8) * 2.0 ** -24 * size, ULP[torch.float16]
+    # a weight is off by half of float16's smallest step at most, in units of the largest weight raised by `raised` powers of two
+    bound = (u + (2 * e + 2.0 ** -20 + n * 2.0 ** -24)[..., None]) * reach + u * np.abs(out) + n * 2.0 ** -(25 + raised) + 2.0 ** -24
+    err = np.abs(f64(buf.out) - out[None])
+    assert (err <= bound[None]).all(), (float(err.max()), float(bound.min()), float(out.max()))
+    assert np.abs(f64(buf.lse) - lse[None]).max() <= e.max() + 2.0 ** -20 + n * 2.0 ** -24 + 2.0 ** -22 * np.abs(lse).max()
