@@ -204,3 +204,27 @@ def test_many_small_weights_in_float16(group, T, raised, at):
     err = np.abs(f64(buf.out) - out[None])
     assert (err <= bound[None]).all(), (float(err.max()), float(bound.min()), float(out.max()))
     assert np.abs(f64(buf.lse) - lse[None]).max() <= e.max() + 2.0 ** -20 + n * 2.0 ** -24 + 2.0 ** -22 * np.abs(lse).max()
+
+
+@pytest.mark.parametrize("Hq", [2, 20])
+@pytest.mark.parametrize("n", [1, 50, 300, 9000])
+def test_scores_of_minus_infinity(Hq, n):
+    D, page = 64, 16
+    cache, gen = filled_cache(51, [n, n, n], page, 1, D, torch.bfloat16, False)
+    q = rand(gen, 3, 1, Hq, D)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    places = {0: range(n), 1: range(n // 2), 2: range(n - n // 2, n)}
+    for b, r in places.items():
+        at = torch.tensor(list(r), dtype=torch.long, device="cuda")
+        cache.k[0, cache.table[b, at // page].long(), 0, at % page, 0] = -math.inf
+    buf = AttentionBuffers(cache, 1, Hq)
+    csd_attention(q, cache, 0, buf)
+    assert not buf.out[0].any() and torch.isneginf(buf.lse[0]).all()
+    for b in (1, 2):
+        keep = [j for j in range(n) if j not in places[b]]
+        k, v = (O.rows_of(f64(x[0]), cache.table[b].tolist(), n, page)[:, keep] for x in (cache.k, cache.v))
+        out, lse, reach, size = O.attention(f64(q[b]), k, v, 1, D ** -0.5)
+        e = 2 * (D + 8) * 2.0 ** -24 * size
+        u = ULP[torch.bfloat16]
+        assert (np.abs(f64(buf.out[b]) - out) <= (u + (2 * e + 2.0 ** -20 + n * 2.0 ** -24)[..., None]) * reach + u * np.abs(out)).all()
+        assert np.abs(f64(buf.lse[b]) - lse).max() <= e.max() + 2.0 ** -20 + n * 2.0 ** -24 + 2.0 ** -22 * np.abs(lse).max()
