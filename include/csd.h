@@ -562,7 +562,7 @@ csd_status_t csd_rope(const void *x, void *y, csd_dtype_t dtype, int B, int S, i
 typedef struct {
     void *k, *v;
     csd_dtype_t dtype;                    /* CSD_BF16 or CSD_F16                                        */
-    int layers, n_pages, page_size;       /* page_size: a power of two, 8 .. 256                         */
+    int layers, n_pages, page_size;       /* layers <= 32767; page_size: a power of two, 8 .. 256        */
     int heads, dim;                       /* key/value heads; dim a multiple of 8, 8 .. 256              */
     int64_t stride_layer, stride_page, stride_head, stride_token;
     int rows, max_pages;                  /* rows <= CSD_CACHE_MAX_ROWS; most pages of a row              */

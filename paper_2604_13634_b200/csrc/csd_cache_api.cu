@@ -169,6 +169,9 @@ csd_status_t check_cache(const csd_cache_t *c)
     if (c->layers <= 0 || c->n_pages <= 0 || c->heads <= 0 || c->dim <= 0 || c->rows <= 0 || c->max_pages <= 0) return CSD_ERR_INVALID_ARG;
     if (c->page_size < 8 || c->page_size > 256 || (c->page_size & (c->page_size - 1)) != 0) return CSD_ERR_UNSUPPORTED;
     if (c->dim % 8 != 0 || c->dim > 256 || c->heads > 4096) return CSD_ERR_UNSUPPORTED;
+    // (a copy of a page has a row of the grid for every layer's keys and values; its pieces are counted in 31 bits)
+    const long long pieces = (static_cast<long long>(c->heads) * c->page_size * c->dim * 2 + pages::kCopyBytes - 1) / pages::kCopyBytes;
+    if (c->layers > 32767 || (c->rows > c->n_pages / 2 ? c->rows : c->n_pages / 2) * pieces > INT_MAX) return CSD_ERR_UNSUPPORTED;
     if (!cache_shape_ok(c->rows, c->max_pages, c->n_pages) || static_cast<long long>(c->max_pages) * c->page_size > (1ll << 30)) return CSD_ERR_UNSUPPORTED;
     if (!aligned16(c->k) || !aligned16(c->v)) return CSD_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(c->meta) & 255u) || (reinterpret_cast<uintptr_t>(c->scratch) & 255u)) return CSD_ERR_INVALID_ARG;
@@ -227,7 +230,6 @@ csd_status_t copy_pages(const csd_cache_t *c, const pages::View &v, long long mo
     p.pieces = (p.page_bytes + pages::kCopyBytes - 1) / pages::kCopyBytes;
     p.n_moves = v.n_moves;
     p.moves = v.moves;
-    if (most * p.pieces > INT_MAX || p.layers > 32767) return CSD_ERR_UNSUPPORTED;
     const long long per_block = pages::kCopyThreads / 32, planes = 2ll * p.layers;
     long long blocks = (most * p.pieces + per_block - 1) / per_block;
     const long long cap = (static_cast<long long>(host::multiprocessors()) * 8 + planes - 1) / planes;

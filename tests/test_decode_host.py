@@ -50,3 +50,10 @@ def test_addresses_of_another_device_are_refused(monkeypatch):
     for stream, device, others in ((_Stream(0), 0, (0, -1)), (_Stream(0), 0, (1,)), (_Stream(1), 0, (0,)), (_Stream(1), 1, (1,)), (None, 1, ())):
         with pytest.raises(binding.CsdError, match="device"):
             decode._stream_ptr(stream, device, *others)
+
+
+def test_more_layers_than_the_page_copies_can_have_are_refused_before_the_bookkeeping():
+    """The copies' grid has a row for every layer's keys and values, at most 65535 of them."""
+    c = decode.CacheStruct(SOMEWHERE, SOMEWHERE, binding.CSD_BF16, 32768, 4, 8, 1, 8, 4 * 64, 64, 64, 8, 1, 4, SOMEWHERE, SOMEWHERE)
+    for call in (lambda L: L.csd_cache_extend(byref(c), 1, None, None), lambda L: L.csd_cache_compact(byref(c), None), lambda L: L.csd_cache_rebuild(byref(c), None)):
+        assert call(decode._lib()) == UNSUPPORTED
