@@ -58,13 +58,10 @@ def _current_device() -> int:
     return torch._C._cuda_getDevice()
 
 
-def _stream_ptr(stream, device: int, *others: int) -> int:
+def _stream_ptr(stream, device: int) -> int:
     """The stream asked for, or the device's current one (the raw handle: a Stream object costs 3 us to make, as much as the
-    call that it is made for).  `device` has to be the current one and that of all `others` (-1: host memory): a kernel given
-    addresses of another device's memory, or the host's, would fault."""
-    for d in others:
-        if d != device:
-            raise CsdError(f"tensors on different devices: {device} and {d} (-1: the host)")
+    call that it is made for).  The device of the call's tensors has to be the current one: a kernel given another device's addresses
+    would fault."""
     if device != _current_device():
         raise CsdError(f"tensors on device {device}, but the current device is {_current_device()}")
     if stream is None:
@@ -72,6 +69,10 @@ def _stream_ptr(stream, device: int, *others: int) -> int:
     if stream.device_index != device:
         raise CsdError(f"tensors on device {device}, but a stream of device {stream.device_index}")
     return stream.cuda_stream
+
+
+def _scattered(what: str, *devices: int):
+    raise CsdError(f"{what}: tensors on different devices: {devices} (-1: the host)")
 
 
 def _result(x, stream, **kw):
@@ -155,16 +156,18 @@ def csd_rope(x, positions, plan: RopePlan, out=None, inverse: bool = False, stre
     out = _result(x, stream) if out is None else out
     B, S, H, D = shape = x.shape
     xs, ys, ps = x.stride(), out.stride(), positions.stride()
-    assert x.is_cuda and positions.is_cuda and positions.dtype == torch.int32 and xs[3] == 1
-    assert out.shape == shape and out.dtype == x.dtype and ys[3] == 1 and out.is_cuda
+    assert positions.dtype == torch.int32 and xs[3] == 1
+    assert out.shape == shape and out.dtype == x.dtype and ys[3] == 1
+    dev = plan._device
+    if not (x.get_device() == out.get_device() == positions.get_device() == dev >= 0):
+        _scattered("csd_rope", x.get_device(), out.get_device(), positions.get_device(), dev)
     if len(ps) == 1:
         assert positions.shape[0] == S
         ps = (0, ps[0])
     else:
         assert positions.shape == (B, S)
     rc = _lib().csd_rope(x.data_ptr(), out.data_ptr(), code, B, S, H, D, xs[0], xs[1], xs[2], ys[0], ys[1], ys[2], positions.data_ptr(),
-                         ps[0], ps[1], plan._ref, 1 if inverse else 0,
-                         _stream_ptr(stream, x.get_device(), out.get_device(), positions.get_device(), plan._device))
+                         ps[0], ps[1], plan._ref, 1 if inverse else 0, _stream_ptr(stream, dev))
     if rc:
         _check(rc, "csd_rope")
     return out
@@ -290,14 +293,15 @@ def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | Non
     if q_out is None:
         q_out = _result(q, stream, memory_format=torch.contiguous_format)
     qs, ks, vs = q.stride(), k.stride(), v.stride()
-    assert q.is_cuda and k.is_cuda and v.is_cuda and q.dtype == k.dtype == v.dtype == q_out.dtype == cache.dtype
+    assert q.dtype == k.dtype == v.dtype == q_out.dtype == cache.dtype
     assert B == cache.rows and D == cache.head_dim and k.shape == v.shape == (B, T, cache.kv_heads, D)
-    assert qs[3] == ks[3] == vs[3] == 1 and q_out.shape == shape and q_out.is_cuda and q_out.is_contiguous()
+    assert qs[3] == ks[3] == vs[3] == 1 and q_out.shape == shape and q_out.is_contiguous()
+    dev = cache._device
+    if not (q.get_device() == k.get_device() == v.get_device() == q_out.get_device() == dev) or plan is not None and plan._device != dev:
+        _scattered("csd_rope_append", q.get_device(), k.get_device(), v.get_device(), q_out.get_device(), dev, plan._device if plan else dev)
     rc = _lib().csd_rope_append(q.data_ptr(), qs[0], qs[1], qs[2], Hq, k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1], vs[2],
                                 q_out.data_ptr(), T, cache._ref, layer, None if plan is None else plan._ref,
-                                None if n_new is None else _rows_arg(n_new, cache, "n_new"),
-                                _stream_ptr(stream, cache._device, q.get_device(), k.get_device(), v.get_device(), q_out.get_device(),
-                                            cache._device if plan is None else plan._device))
+                                None if n_new is None else _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, dev))
     if rc:
         _check(rc, "csd_rope_append")
     return q_out
@@ -322,12 +326,14 @@ def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale
     """buf.out, buf.lse: attention of T new tokens of every row, q [rows, T, q_heads, D], over its cache (n_new[row] > T: the first T
     of that many).  Serving form: no gradient."""
     qs = q.stride()
-    assert q.is_cuda and q.dtype == cache.dtype == buf.out.dtype and qs[3] == 1 and q.shape == buf.out.shape
+    assert q.dtype == cache.dtype == buf.out.dtype and qs[3] == 1 and q.shape == buf.out.shape
     assert q.shape[0] == cache.rows and q.shape[3] == cache.head_dim
+    dev = cache._device
+    if not (q.get_device() == buf._device == dev):
+        _scattered("csd_attention", q.get_device(), buf._device, dev)
     rc = _lib().csd_attention(q.data_ptr(), qs[0], qs[1], qs[2], buf.T, buf.q_heads, cache._ref, layer,
                               cache.head_dim ** -0.5 if scale is None else scale, None if n_new is None else _rows_arg(n_new, cache, "n_new"),
-                              buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(), buf.ws_bytes,
-                              _stream_ptr(stream, cache._device, q.get_device(), buf._device))
+                              buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(), buf.ws_bytes, _stream_ptr(stream, dev))
     if rc:
         _check(rc, "csd_attention")
     return buf.out

@@ -5,6 +5,7 @@ import re
 from ctypes import byref
 
 import pytest
+import torch
 
 from paper_2604_13634_b200 import binding, build, decode
 
@@ -46,10 +47,16 @@ class _Stream:
 
 def test_addresses_of_another_device_are_refused(monkeypatch):
     monkeypatch.setattr(decode, "_current_device", lambda: 0)
-    assert decode._stream_ptr(_Stream(0), 0, 0, 0) == 5
-    for stream, device, others in ((_Stream(0), 0, (0, -1)), (_Stream(0), 0, (1,)), (_Stream(1), 0, (0,)), (_Stream(1), 1, (1,)), (None, 1, ())):
+    assert decode._stream_ptr(_Stream(0), 0) == 5
+    for stream, device in ((_Stream(1), 0), (_Stream(1), 1), (None, 1)):
         with pytest.raises(binding.CsdError, match="device"):
-            decode._stream_ptr(stream, device, *others)
+            decode._stream_ptr(stream, device)
+    x, pos, plan = torch.zeros(1, 3, 2, 64), torch.zeros(1, 3, dtype=torch.int32), decode.RopePlan(64, device="cpu")
+    with pytest.raises(binding.CsdError, match="device"):
+        decode.csd_rope(x, pos, plan)
+    plan._device = 0
+    with pytest.raises(binding.CsdError, match="device"):
+        decode.csd_rope(x, pos, plan)
 
 
 def test_more_layers_than_the_page_copies_can_have_are_refused_before_the_bookkeeping():
