@@ -54,8 +54,7 @@ SIGNATURES = {
                               c_void_p, c_size_t, c_void_p]),
 }
 
-def _current_device() -> int:
-    return torch._C._cuda_getDevice()
+_current_device = torch._C._cuda_getDevice
 
 
 def _stream_ptr(stream, device: int) -> int:
@@ -186,6 +185,8 @@ class PagedCache:
             raise CsdError(f"a cache holds bfloat16 or float16, got {dtype}")
         if page_size <= 0 or max_len <= 0:
             raise CsdError(f"unsupported page_size={page_size} max_len={max_len}")
+        if (k is None) != (v is None):
+            raise CsdError("a pool to adopt is both keys and values")
         shape = (layers, n_pages, kv_heads, page_size, head_dim)
         dev = k.device if k is not None else torch.device(device)
         if k is None:

@@ -64,3 +64,10 @@ def test_more_layers_than_the_page_copies_can_have_are_refused_before_the_bookke
     c = decode.CacheStruct(SOMEWHERE, SOMEWHERE, binding.CSD_BF16, 32768, 4, 8, 1, 8, 4 * 64, 64, 64, 8, 1, 4, SOMEWHERE, SOMEWHERE)
     for call in (lambda L: L.csd_cache_extend(byref(c), 1, None, None), lambda L: L.csd_cache_compact(byref(c), None), lambda L: L.csd_cache_rebuild(byref(c), None)):
         assert call(decode._lib()) == UNSUPPORTED
+
+
+def test_half_a_pool_is_refused():
+    half = torch.zeros(1, 4, 1, 16, 64, dtype=torch.bfloat16)
+    for kw in (dict(k=half), dict(v=half)):
+        with pytest.raises(binding.CsdError, match="both"):
+            decode.PagedCache(1, 4, 16, 1, 1, 64, torch.bfloat16, 64, **kw)
