@@ -81,7 +81,7 @@ bool place_tokens(long long tokens, long long groups, int units, rope::Places &a
     return true;
 }
 
-int groups_of(int heads) { return (heads + rope::kHeads - 1) / rope::kHeads; }
+int groups_of(int heads) { return (heads - 1) / rope::kHeads + 1; }         // (of any positive count: a sum could pass 31 bits)
 
 template <typename T>
 csd_status_t run_rope(rope::RopeParams p, csd_rope_layout_t layout, cudaStream_t st)

@@ -71,3 +71,14 @@ def test_half_a_pool_is_refused():
     for kw in (dict(k=half), dict(v=half)):
         with pytest.raises(binding.CsdError, match="both"):
             decode.PagedCache(1, 4, 16, 1, 1, 64, torch.bfloat16, 64, **kw)
+
+
+@pytest.mark.parametrize("H", [2 ** 31 - 1, 2 ** 31 - 3])
+def test_head_counts_that_pass_31_bits_in_groups_are_refused(H):
+    """Heads are taken four at a time, and the count is rounded up: three more than 2^31 - 1 - 3 wrap."""
+    plan = decode.RopeStruct(SOMEWHERE, 2, 0, 1.0)
+    L = decode._lib()
+    assert L.csd_rope(SOMEWHERE, SOMEWHERE, binding.CSD_F32, 1, 1, H, 6, 6 * H, 6 * H, 6, 6 * H, 6 * H, 6, SOMEWHERE, 1, 1, byref(plan), 0, None) == UNSUPPORTED
+    c = decode.CacheStruct(SOMEWHERE, SOMEWHERE, binding.CSD_BF16, 1, 4, 8, 1, 8, 4 * 64, 64, 64, 8, 1, 4, SOMEWHERE, SOMEWHERE)
+    three = (8, 8, 8)
+    assert L.csd_rope_append(SOMEWHERE, *three, H, SOMEWHERE, *three, SOMEWHERE, *three, SOMEWHERE, 1, byref(c), 0, None, None, None) == UNSUPPORTED
