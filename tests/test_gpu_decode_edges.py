@@ -228,3 +228,43 @@ def test_scores_of_minus_infinity(Hq, n):
         u = ULP[torch.bfloat16]
         assert (np.abs(f64(buf.out[b]) - out) <= (u + (2 * e + 2.0 ** -20 + n * 2.0 ** -24)[..., None]) * reach + u * np.abs(out)).all()
         assert np.abs(f64(buf.lse[b]) - lse).max() <= e.max() + 2.0 ** -20 + n * 2.0 ** -24 + 2.0 ** -22 * np.abs(lse).max()
+
+
+@pytest.mark.parametrize("Hq", [2, 20])
+def test_attention_over_the_most_rows(Hq):
+    """4096 rows: the table of their tiles leaves the fewest stages for keys and values; rows of no tile, one, and several."""
+    rows, page, D = 4096, 8, 64
+    lens = [(i * 7) % 150 if i % 5 else 0 for i in range(rows - 1)] + [3000]
+    cache, gen = filled_cache(52, lens, page, 1, D, torch.bfloat16, False)
+    q = rand(gen, rows, 1, Hq, D, scale=2.0)
+    buf = AttentionBuffers(cache, 1, Hq)
+    csd_attention(q, cache, 0, buf)
+    check_attention(buf, q, cache, lens, [1] * rows, 1 / math.sqrt(D), rows=list(range(0, rows, 61)) + [rows - 1])
+    empty = torch.tensor([n == 0 for n in lens], device="cuda")
+    assert not buf.out[empty].any() and torch.isneginf(buf.lse[empty]).all() and torch.isfinite(buf.lse[~empty]).all()
+    first = buf.out.clone()
+    for _ in range(5):
+        csd_attention(q, cache, 0, buf)
+        assert torch.equal(buf.out, first)
+    assert cache.stats()["flags"] == 0
+
+
+@pytest.mark.parametrize("dtype,token_major,layout,D,rot", [(torch.bfloat16, False, "half", 128, 128), (torch.float16, True, "interleaved", 80, 34)])
+@pytest.mark.parametrize("T", [34, 300, 1001])
+def test_rope_append_of_a_prompt(dtype, token_major, layout, D, rot, T):
+    """Any number of new tokens: queries and keys as csd_rope turns them, values as they are, each at its place."""
+    page, Hq, Hkv, lens = 16, 5, 2, [T, T + 700, T - 1, 40]
+    cache, gen = filled_cache(53, lens, page, Hkv, D, dtype, token_major)
+    news = [T, T, T - 1, 7]
+    qkv = rand(gen, len(lens), T, Hq + 2 * Hkv, D, dtype=dtype)
+    q, k, v = qkv.split([Hq, Hkv, Hkv], dim=2)
+    plan = RopePlan(rot, layout=layout, scaling="parts", factor=8.0)
+    pos = torch.tensor([n - m for n, m in zip(lens, news)], dtype=torch.int32, device="cuda")[:, None] + torch.arange(T, dtype=torch.int32, device="cuda")
+    want_q, want_k = csd_rope(q, pos, plan), csd_rope(k, pos, plan)
+    out = csd_rope_append(q, k, v, cache, 0, plan, n_new=torch.tensor(news, dtype=torch.int32, device="cuda"))
+    for b, m in enumerate(news):
+        assert torch.equal(out[b, :m], want_q[b, :m]) and not out[b, m:].any()
+        at = pos[b, :m].long()
+        pages = cache.table[b, at // page].long()
+        assert torch.equal(cache.k[0, pages, :, at % page], want_k[b, :m]) and torch.equal(cache.v[0, pages, :, at % page], v[b, :m])
+    assert cache.stats()["flags"] == 0
