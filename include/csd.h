@@ -71,7 +71,7 @@ typedef enum { CSD_F32 = 0, CSD_BF16 = 1, CSD_F16 = 2 } csd_dtype_t;   /* CSD_F1
                                          the step's results are unreliable (csd_stats_t.debug_site says
                                          which check).  The access was skipped; nothing trapped.  One
                                          check (a partial-result slot) is always compiled in; a library
-                                         built with -DCSD_DEBUG checks every index it computes.        */
+                                         built with -DCSD_DEBUG checks every index that a step computes. */
 
 /* Optional per-position diagnostics.  Any member may be NULL.  Row arrays have
  * B*(K+1) entries, position arrays B*K, both row-major.  Values are defined for

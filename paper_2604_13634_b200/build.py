@@ -9,7 +9,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcsd.so")
-LIB_DEBUG = os.path.join(HERE, "libcsd_debug.so")     # the same sources with -DCSD_DEBUG: every index checked
+LIB_DEBUG = os.path.join(HERE, "libcsd_debug.so")     # the same sources with -DCSD_DEBUG: the step kernels' indexes checked
 SOURCES = ["csd_api.cu", "csd_cache_api.cu"]
 HEADERS = ["csd_common.cuh", "csd_ocm.cuh", "csd_step.cuh", "csd_sampled.cuh", "csd_lmhead.cuh", "csd_host.h", "csd_ptx.cuh", "csd_rope.cuh", "csd_pages.cuh",
            "csd_attention.cuh", os.path.join("..", "..", "include", "csd.h")]
@@ -34,7 +34,8 @@ def needs_build(lib: str = LIB) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
-    """Compile the library (debug=True: the bounds-checked variant, loaded when CSD_DEBUG=1 is set)."""
+    """Compile the library (debug=True: the variant whose verification-step kernels check every index, loaded when CSD_DEBUG=1 is set;
+    the rotary, page and attention kernels are the same in both)."""
     lib = LIB_DEBUG if debug else LIB
     if not force and not needs_build(lib):
         return lib

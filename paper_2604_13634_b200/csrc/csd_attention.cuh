@@ -8,14 +8,15 @@
 //
 // Bound: memory (each key and value is read once; T g query rows share it, g = query heads per key head); for a short cache the
 // latency of the chain lengths -> page ids -> tiles -> join, 9.7 us with one row of 700 tokens.
-// Measured with keys and values of 0.1 to 1.2 GB, bf16, 8 key heads of 128: 5.9 TB/s for one row of 131071 tokens and one new token
-// (90.9 us, 32 query heads), 5.8 for 128 rows of 500 to 4000 with nine (206 us), 5.2 for 32 ragged rows up to 8191 with six (104 us),
-// 3.1 for one row of 30001 with 72 query rows to a key head (39.9 us: half of it is the start, the parts' way out and the join).
+// Measured with keys and values of 0.1 to 1.2 GB, bf16, 8 key heads of 128: 6.0 TB/s for one row of 131071 tokens and one new token
+// (89.7 us, 32 query heads), 5.9 for 128 rows of 500 to 4000 with nine (203 us), 5.2 for 32 ragged rows up to 8191 with six (104 us),
+// 3.2 for one row of 30001 with 72 query rows to a key head (39.0 us: half of it is the start, the parts' way out and the join).
 //
-// Two kernels, by query rows to a key head and row of the cache: up to 16 fit one mma.sync tile held in registers; beyond, 128 rows
-// share a tensor-memory tile.  32 ragged rows up to 8191 tokens, dim 128: 93 us (first kernel) and 101 (second) with 10 query rows, 94
-// and 102 with 15, 155 and 103 with 20, 163 and 104 with 30; 128 rows of 500 to 4000, dim 64: 100 and 131 with 8, 102 and 132 with 16,
-// 185 and 135 with 32.  Beyond 16 the first kernel has a second row tile, which reads every key again.
+// Two kernels, by query rows to a key head and row of the cache: up to 16 fit one mma.sync tile held in registers; beyond, up to 128 rows
+// share a tensor-memory tile.  With pages of 16 tokens, first kernel and second: 32 ragged rows up to 8191 tokens, dim 128: 97 us and 105
+// with 10 query rows, 96 and 106 with 15, 97 and 107 with 16, 156 and 105 with 20, 166 and 107 with 30; 128 rows of 500 to 4000, dim 64:
+// 110 and 162 with 8 and 16, 194 and 167 with 20, 197 and 171 with 32; 32 rows up to 4095, dim 256: 108 and 128 with 8, 119 and 127 with 16,
+// 202 and 130 with 20.  Beyond 16 the first kernel has a second row tile, which reads every key again.
 //
 //   attention_kernel  persistent.  The tiles (kTile places of one row and key head) of all rows and heads, laid out row after
 //                     row, are split evenly and contiguously over the blocks, whatever the rows' lengths are (read on the
@@ -26,7 +27,7 @@
 //                     own running (m, l, O) in registers: no exchange between warps until the unit ends.  Products are
 //                     mma.sync m16n8k16 with float32 accumulators: with 16 query rows the tensor pipe is at a tenth of its
 //                     limit while the tiles stream.
-//     At the end of a unit the warps join through a ring stage; a unit that lies in one block whole is written out, otherwise
+//     At the end of a unit the warps join through a ring stage that the producer hands over; a unit that lies in one block whole is written out, otherwise
 //     the part goes to the workspace.
 //   attention_join_kernel  joins the parts of the units that were split (at most one begins in each block).  A launch of its own: joining
 //                     in the last block to finish a unit was slower (103.6 us against 94 for one row of 131071 tokens, 36.9

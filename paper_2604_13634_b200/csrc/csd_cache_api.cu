@@ -284,17 +284,18 @@ auto with_config(int dim, F f)
     return f(Config<T, 256, 1, 1>());
 }
 
-// Which kernel: up to 16 query rows per (row, key head) fit the register tiles of the mma.sync kernel (94 us where the other takes 102,
-// 15 query rows of 128 elements); beyond, the tensor-memory kernel, with row tiles of at most 128 (103 us against 155 with 20 rows).
+// Which kernel: up to 16 query rows per (row, key head) fit the register tiles of the mma.sync kernel (97 us where the other takes 107,
+// 16 query rows of 128 elements); beyond, the tensor-memory kernel, with row tiles of at most 128 (105 us against 156 with 20 rows).
 bool attention_uses_tc(int rows) { return rows > 16; }
 
 // Two blocks per SM while their accumulators fit in half of the tensor memory each (128 + dim columns of 512).
 int tc_blocks(int dim) { return dim <= 128 ? 2 : 1; }
 
-// Products of 64 rows: a warp of the softmax then has 16 query rows, not 32.  Same time on a cool GPU, but the products draw less, and
-// kept busy the clock stays higher: 222 us against 235 for 128 rows of 500 to 4000 (36 query rows of 128 elements), 112 against 120
-// (30), 236 against 245 (64); with 64 elements 145 against 153 (32), but 161 against 159 (48) and 159 against 140 (64, cool), where
-// twice the warps' work counts.
+// Products of 64 rows: a warp of the softmax then has 16 query rows, not 32.  On a cool GPU that is 0 to 2 % faster, but the products
+// draw less, and kept busy for a second the clock stays higher.  Busy, 64 rows against 128: 243 us and 262 for 128 rows of 500 to 4000 in
+// pages of 16 (36 query rows of 128 elements), 258 and 269 (64), 113 and 120 for 32 ragged rows up to 8191 (30); 131 and 140 (32 query rows
+// of 256 elements); with 64 elements in pages of 64 tokens 144 and 152 (32), but 159 and 158 (48, cool 160 and 144) and 165 and 161 (64,
+// cool 163 and 147), where twice the warps' work counts; in pages of 16 the loads hide the difference (169 and 170 with 32).
 bool tc_products_of_64(int tile_rows, int dim) { return tile_rows <= (dim <= 64 ? 32 : 64); }
 
 AttentionPlan attention_tc_plan(int rows, int dim, int B)

@@ -12,7 +12,7 @@
 //
 // Bounds: the bookkeeping kernels are latency (a few dependent reads and one block-wide scan); pages_copy_kernel,
 // which moves page contents over all layers, is memory.  Fork, extension and truncation of 64 rows with 48 page copies over 16 layers
-// take 24 us, of which the copies' 101 MB need 15.4.
+// take 23.1 us, of which the copies' 101 MB need 15.4.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -409,8 +409,8 @@ struct CopyParams {
 };
 
 // Page contents: grid.y is a layer's keys or values.  A warp moves up to 4 KiB at a time, eight 16-byte loads in flight per
-// lane, neighbouring warps neighbouring pieces of a page.  2.6 GB (2500 pages of 32 KB in 16 planes, read and written): 412 us, 6.4 TB/s,
-// of the 430 to 445 us of the compaction that asked for them.
+// lane, neighbouring warps neighbouring pieces of a page.  2.6 GB (2500 pages of 32 KB in 16 planes, read and written): 412 to 420 us, 6.2
+// to 6.4 TB/s, of the 430 to 445 us of the compaction that asked for them.
 __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const CopyParams p)
 {
     ptx::wait_for_stream();

@@ -12,7 +12,7 @@
 // Bound: memory (every element read once, written once).  A block has a few whole tokens.  Its threads first put the tokens' sines
 // and cosines into shared memory, one per pair and token; then each thread turns one unit (P = 16 bytes' worth of pairs: two
 // 16-byte vectors, neighbouring lanes neighbouring vectors) of kHeads heads, whose loads it has issued before.
-// 268 MB of bf16 (4 x 4096 tokens, 32 heads of 128): 44.2 us, 6.1 TB/s.  16 MB of float32 (2 x 1023 tokens, 12 heads of 80 of which 32
+// 268 MB of bf16 (4 x 4096 tokens, 32 heads of 128): 44.0 us, 6.1 TB/s.  16 MB of float32 (2 x 1023 tokens, 12 heads of 80 of which 32
 // turn): 5.9 us, start and one pass.
 // Where rot does not divide into such units but rows are made of whole vectors, a thread has one vector of kHeads heads instead:
 // 38.4 us (interleaved; 90.7 pair by pair) for 170 MB with 66 of 168 elements turned; 268 MB with 126 of 128 turned in 45.9 us
@@ -457,8 +457,8 @@ struct AppendParams {
 // One launch for the new tokens' queries (turned, to q_out), keys (turned, to their page slots) and values (to their
 // page slots).  Token t of row b lies at place lens[b] - n_new[b] + t; one that does not exist (t >= n_new[b], or a
 // negative place) gets a zero query and touches no page.
-// Bound: latency for one token (2.7 us: launch, length, page id, store), memory beyond (9.2 us for 28 MB: 128 rows of nine tokens, 32 +
-// 2 x 8 heads of 128, where the chain of those reads is a third).
+// Bound: latency for one token (2.6 us: launch, length, page id, store), memory beyond (9.2 us for 28 MB: 128 rows of nine tokens, 32 +
+// 2 x 8 heads of 128, where the chain of those reads is a third and 132 of the 576 blocks run as a second wave).
 template <typename T, int P, bool kHalf, bool kLoose>
 __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const AppendParams p)
 {
