@@ -791,7 +791,11 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             at_ring.next(p.n_stages);
         }
     }
-    if (*give_up && tid % 32 == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);
+    // a wait ran out (whoever noticed stays, and so does the block)
+    if (*give_up) {
+        if (tid % 32 == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);
+        ptx::linger();
+    }
 }
 
 // ---- more than 16 query rows per key head: products on the tensor-memory path -------------------------------------------
@@ -1274,8 +1278,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         ptx::tc_fence_before();
     }
     __syncthreads();
+    if (*give_up) {                                                  // a wait ran out
+        if (lane == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);
+        ptx::linger();
+        __syncthreads();
+    }
     if (warp == 1) ptx::tmem_dealloc(tmem, kCols);
-    if (*give_up && lane == 0) atomicOr(p.flags, CSD_CACHE_INTERNAL);
 }
 
 // Joins the parts of split units: block (x, y) kJoinRows query rows of one of them.  The weights of all parts and rows first (a

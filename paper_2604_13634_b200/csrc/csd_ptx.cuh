@@ -84,6 +84,15 @@ __device__ __forceinline__ bool mbar_wait(unsigned int bar, unsigned int parity,
     return true;
 }
 
+// After a wait has run out: a millisecond in which copies and products that are still in flight land, before the block's shared and
+// tensor memory go to another block.
+__device__ __forceinline__ void linger()
+{
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000ll) {
+    }
+}
+
 __device__ __forceinline__ void tmem_alloc(unsigned int smem_dst, unsigned int cols)
 {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(cols) : "memory");

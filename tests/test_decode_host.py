@@ -82,3 +82,15 @@ def test_head_counts_that_pass_31_bits_in_groups_are_refused(H):
     c = decode.CacheStruct(SOMEWHERE, SOMEWHERE, binding.CSD_BF16, 1, 4, 8, 1, 8, 4 * 64, 64, 64, 8, 1, 4, SOMEWHERE, SOMEWHERE)
     three = (8, 8, 8)
     assert L.csd_rope_append(SOMEWHERE, *three, H, SOMEWHERE, *three, SOMEWHERE, *three, SOMEWHERE, 1, byref(c), 0, None, None, None) == UNSUPPORTED
+
+
+def test_blocks_that_give_up_stay_until_their_copies_have_landed():
+    """Each kernel with bounded waits sees at its end whether one ran out, and lingers before its memory goes to another block."""
+    with open(os.path.join(CSRC, "csd_attention.cuh")) as f:
+        kernels = re.split(r"__global__", re.sub(r"//[^\n]*", "", f.read()))[1:]
+    waiting = [k for k in kernels if "mbar_wait(" in k]
+    assert len(waiting) == 2
+    for k in waiting:
+        end = k[k.rindex("if (*give_up)"):]
+        assert "CSD_CACHE_INTERNAL" in end and "ptx::linger();" in end
+        assert "tmem_alloc" not in k or end.index("ptx::linger();") < end.index("tmem_dealloc")
