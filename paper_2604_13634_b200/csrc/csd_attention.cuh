@@ -32,7 +32,7 @@
 //   attention_join_kernel  joins the parts of the units that were split (at most one begins in each block).  A launch of its own: joining
 //                     in the last block to finish a unit was slower (103.6 us against 94 for one row of 131071 tokens, 36.9
 //                     against 30.6 for 16 rows with a key head to every query head), a chain of cold reads at the end of the slowest block.
-// No block waits for another; waits inside a block are bounded.
+// No block waits for another; waits inside a block are bounded, and a block whose wait runs out stays until what it sent for has landed.
 #pragma once
 
 #include <cuda.h>

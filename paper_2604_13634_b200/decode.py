@@ -175,8 +175,8 @@ def csd_rope(x, positions, plan: RopePlan, out=None, inverse: bool = False, stre
 class PagedCache:
     """Keys and values of `rows` sequences in pages, with the bookkeeping on the device.
 
-    k, v: [layers, n_pages, kv_heads, page_size, head_dim] views (whatever lies outside within a page); pass your own to
-    adopt them.  table, lens, granted, refs are views of `meta`: copying meta saves or restores the bookkeeping.
+    k, v: [layers, n_pages, kv_heads, page_size, head_dim] views, each page dense (whatever lies outside within
+    it: heads or tokens); pass your own to adopt them.  table, lens, granted, refs are views of `meta`: copying meta saves or restores the bookkeeping.
     """
 
     def __init__(self, rows: int, n_pages: int, page_size: int, layers: int, kv_heads: int, head_dim: int, dtype: torch.dtype,
