@@ -648,6 +648,44 @@ csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t
                            const csd_cache_t *cache, int layer, float scale, const int32_t *n_new,
                            void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- the pass over a tree of drafted tokens ----
+ *
+ * Several alternatives per position, verified in one pass: the T new tokens of a row are the nodes of a tree, node 0 the token emitted
+ * before the step (the root), every other node a drafted token that follows its parent's.
+ *     csd_cache_extend (cache, T)                                    room for all nodes
+ *     csd_tree_plan    (parents, ..., granted, masks, positions)     once per step
+ *     per layer:  csd_rope_append_at(q, k, v, ..., granted, positions)
+ *                 csd_attention_tree(q', ..., granted, masks)
+ */
+#define CSD_TREE_MAX_NODES 64
+
+/* For the T new tokens of every row, masks[b,t]: bit u set where u is t or one of the nodes that t hangs from; and positions[b,t] =
+ * lens[b] - n_new[b] + depth(t) + offset[b].  parents: int32, element (b,t) at b*parent_stride + t (0: one tree for all rows; NULL: a
+ * chain).  A parent that is no earlier node (negative, t itself or later) hangs t directly from the row's history, at depth 0.
+ * offset: NULL, or DEVICE [rows]: what positions are ahead of places (a row that has lost tokens to csd_cache_evict).  Tokens t >= n_new[b]
+ * (NULL: T) get no bits and position 0.  masks: DEVICE uint64 [rows, T], 8-byte aligned; positions: DEVICE int32 [rows, T] or NULL.
+ * One launch; asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (T > CSD_TREE_MAX_NODES), CUDA. */
+csd_status_t csd_tree_plan(const int32_t *parents, int64_t parent_stride, int T, const csd_cache_t *cache, const int32_t *n_new,
+                           const int32_t *offset, uint64_t *masks, int32_t *positions, void *stream);
+
+/* csd_rope_append with the positions given: token t of row b is turned by positions[b,t] (DEVICE int32 [rows, T]; NULL: its place) and
+ * stored at its place lens[b] - n_new[b] + t as ever. */
+csd_status_t csd_rope_append_at(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int q_heads,
+                                const void *k, int64_t k_stride_b, int64_t k_stride_t, int64_t k_stride_h,
+                                const void *v, int64_t v_stride_b, int64_t v_stride_t, int64_t v_stride_h,
+                                void *q_out, int T, const csd_cache_t *cache, int layer, const csd_rope_t *rope,
+                                const int32_t *n_new, const int32_t *positions, void *stream);
+
+/* csd_attention for T <= CSD_TREE_MAX_NODES new tokens that see each other by masks (DEVICE uint64 [rows, T]): token t of row b sees every
+ * place before the new ones, and the place lens[b] - n_new[b] + u of new token u < n_new[b] where bit u of masks[b,t] is set -- its own as well
+ * only where its bit says so.  Any masks will do, a tree's or others.  A token with t >= n_new[b] or a negative place, and one that sees nothing,
+ * gives zeros and lse = -inf; what lies in places that a token does not see does not reach its result.  Everything else is as for
+ * csd_attention; the workspace's size is csd_attention_tree_workspace_bytes. */
+size_t csd_attention_tree_workspace_bytes(int rows, int T, int q_heads, int heads, int dim);
+csd_status_t csd_attention_tree(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads,
+                                const csd_cache_t *cache, int layer, float scale, const int32_t *n_new, const uint64_t *masks,
+                                void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- helpers ---- */
 
 /* (float) log((double) tau): the threshold the gate of Eq. 3 compares against.

@@ -35,6 +35,7 @@ EXPORTS = [
     "csd_rope_steps", "csd_rope", "csd_rope_append", "csd_attention_workspace_bytes", "csd_attention",
     "csd_cache_meta_bytes", "csd_cache_meta_layout", "csd_cache_scratch_bytes", "csd_cache_rebuild", "csd_cache_extend",
     "csd_cache_truncate", "csd_cache_commit", "csd_cache_fork", "csd_cache_compact",
+    "csd_tree_plan", "csd_rope_append_at", "csd_attention_tree_workspace_bytes", "csd_attention_tree",
 ]
 
 

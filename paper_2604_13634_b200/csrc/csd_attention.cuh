@@ -33,6 +33,9 @@
 //                     in the last block to finish a unit was slower (103.6 us against 94 for one row of 131071 tokens, 36.9
 //                     against 30.6 for 16 rows with a key head to every query head), a chain of cold reads at the end of the slowest block.
 // No block waits for another; waits inside a block are bounded, and a block whose wait runs out stays until what it sent for has landed.
+//
+// Trees (kTree): the new tokens are the nodes of a tree, and token t sees every place before the new ones and the new tokens u whose bit is
+// set in masks[b,t].  Only the tiles with new tokens differ: a thread holds its rows' masks and tests a bit where the chain compares places.
 #pragma once
 
 #include <cuda.h>
@@ -76,6 +79,7 @@ struct Params {
     int page_shift, n_pages, max_pages;
     int box_rows;                          // places of a TMA box: min(page, kTile)
     const int *table, *lens, *n_new;
+    const unsigned long long *masks;       // trees: [B, T], bit u: the token sees new token u
     unsigned int *flags;
     float scale_log2;
     int n_stages;
@@ -280,6 +284,22 @@ __device__ __forceinline__ int row_len(const Params &p, int b) { return min(max(
 // (may be more than T: a pass over the first T of them)
 __device__ __forceinline__ int row_news(const Params &p, int b) { return p.n_new ? max(ptx::ld_written(p.n_new + b), 0) : p.T; }
 
+// Trees: which new tokens token tok of row b sees, those that exist alone: bits of the places first + u in [0, len).
+__device__ __forceinline__ unsigned long long token_mask(const Params &p, int b, int tok, int len, int news)
+{
+    const int2 m = ptx::ld_written(reinterpret_cast<const int2 *>(p.masks) + static_cast<long long>(b) * p.T + tok);
+    unsigned long long bits = static_cast<unsigned long long>(static_cast<unsigned int>(m.y)) << 32 | static_cast<unsigned int>(m.x);
+    const int before = news - len;                       // new tokens that have no place (a length below n_new)
+    if (news < 64) bits &= (1ull << news) - 1ull;
+    if (before > 0) bits = before < 64 ? bits >> before << before : 0ull;
+    return bits;
+}
+// Whether a place is seen: every one before `first`, of the others those whose bit is set.
+__device__ __forceinline__ bool tree_sees(unsigned long long bits, int first, int key)
+{
+    return key < first || (key - first < 64 && (bits >> (key - first) & 1ull));
+}
+
 // base[b + 1] holds the positions of row b; becomes base[b] = positions of the rows before b.  One warp.
 __device__ __forceinline__ void scan_tiles(int *base, int B)
 {
@@ -366,11 +386,13 @@ __device__ __forceinline__ void zero_empty_rows(const Params &p, const int *base
 
 // Adds w v for the infinities and NaN among 32 elements (from c0) of the values in places [from, to], which the product left
 // out, to one row's accumulators; w is computed again.  Rare: straight from global memory.
-template <typename T>
-__device__ __noinline__ void add_left_out(const Params &p, int b, int h, int tok, int head, int c0, int from, int to, float m, float (&o)[32])
+template <typename T, bool kTree>
+__device__ __noinline__ void add_left_out(const Params &p, int b, int h, int tok, int head, int c0, int from, int to, float m, float (&o)[32],
+                                          unsigned long long bits, int first)
 {
     const T *q = static_cast<const T *>(p.q) + b * p.qb + tok * p.qt + head * p.qh;
     for (int key = from; key <= to; ++key) {
+        if (kTree && !tree_sees(bits, first, key)) continue;
         const int page = ptx::ld_written(p.table + static_cast<long long>(b) * p.max_pages + (key >> p.page_shift));
         if (page < 0 || page >= p.n_pages) continue;
         const long long at = page * p.pool_page + h * p.pool_head + (key & ((1 << p.page_shift) - 1)) * p.pool_token;
@@ -387,7 +409,7 @@ __device__ __noinline__ void add_left_out(const Params &p, int b, int h, int tok
     }
 }
 
-template <typename C>
+template <typename C, bool kTree>
 __global__ void __launch_bounds__(C::kThreads, C::kBlocksPerSm)
 attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p)
 {
@@ -542,11 +564,24 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             if (more) fetch(next);
             consumer_barrier(cthreads);
             int limit[2];                                           // last place that the thread's rows see; -1: none
+            unsigned long long bits[kTree ? 2 : 1];
+            const int first = len - news;                           // place of the first new token
+            const int shared = kTree ? first - 1 : first;           // last place that all rows see
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
                 const int r = g + 8 * hh, rr = rt * C::kRows + r, tok = rr / p.group;
-                limit[hh] = r < rows_here && tok < news ? len - news + tok : -1;
+                limit[hh] = r < rows_here && tok < news ? first + tok : -1;
+                if constexpr (kTree) {
+                    bits[hh] = limit[hh] >= 0 ? token_mask(p, b, tok, len, news) : 0ull;
+                    if (first <= 0 && bits[hh] == 0ull) limit[hh] = -1;
+                }
             }
+            auto unseen = [&](int key, int hh) {
+                if constexpr (kTree)
+                    return !tree_sees(bits[hh], first, key);
+                else
+                    return key > limit[hh];
+            };
             unsigned int qf[C::kQInRegisters ? DP / 16 : 1][4];
             if constexpr (C::kQInRegisters) {
 #pragma unroll
@@ -591,13 +626,13 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     }
                 }
                 // scores in powers of two; places that a row does not see become -inf whatever was computed for them
-                const bool edge = key0 + 16 * NK - 1 > len - news;   // some row does not see all of the warp's places
+                const bool edge = key0 + 16 * NK - 1 > shared;       // some row does not see all of the warp's places
 #pragma unroll
                 for (int n = 0; n < 2 * NK; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         x[n][e] *= p.scale_log2;
-                        if (edge && key0 + 8 * n + 2 * qd + (e & 1) > limit[e >> 1]) x[n][e] = -INFINITY;
+                        if (edge && unseen(key0 + 8 * n + 2 * qd + (e & 1), e >> 1)) x[n][e] = -INFINITY;
                     }
                 float mx[2], at0[2];
                 bool grew = false;
@@ -656,7 +691,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                         if (key >= len) {
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
                             wrote = true;
-                        } else if (key > len - news) {
+                        } else if (key > shared) {
                             unsigned int y[4];
                             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(at) : "memory");
                             odd |= finite_only<T>(y[0]) != y[0] || finite_only<T>(y[1]) != y[1] || finite_only<T>(y[2]) != y[2] || finite_only<T>(y[3]) != y[3];
@@ -706,7 +741,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                             const bool odd0 = (two ^ kept) & 0xffffu, odd1 = (two ^ kept) & 0xffff0000u;
 #pragma unroll
                             for (int hh = 0; hh < 2; ++hh)
-                                if (key0 + r <= limit[hh]) {
+                                if (!unseen(key0 + r, hh)) {
                                     if (odd0) o[nt][2 * hh] += wt[hh] * v0;
                                     if (odd1) o[nt][2 * hh + 1] += wt[hh] * v1;
                                 }
@@ -871,7 +906,7 @@ __device__ __forceinline__ void fetch_rows(const Params &p, const Run &ru, unsig
     }
 }
 
-template <typename T, int kBlocksPerSm, int kM>
+template <typename T, int kBlocksPerSm, int kM, bool kTree>
 __global__ void __launch_bounds__(kTcThreads, kBlocksPerSm)
 attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p)
 {
@@ -1077,13 +1112,19 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 fetch(next, run + 1);
             }
             const int rr = rt * p.tile_rows + r, tok = rr / p.group;
-            const int limit = r < rows_here && tok < news ? len - news + tok : -1;
+            const int first = len - news, shared = kTree ? first - 1 : first;      // first new token; last place that all rows see
+            int limit = r < rows_here && tok < news ? first + tok : -1;            // the token's own place; -1: it sees nothing
+            unsigned long long bits = 0ull;
+            if constexpr (kTree) {
+                if (limit >= 0) bits = token_mask(p, b, tok, len, news);
+                if (first <= 0 && bits == 0ull) limit = -1;
+            }
             const bool warp_has = warp_row < rows_here;
             float m = 0.f, l = 0.f;                              // l == 0: nothing seen yet, m is arbitrary
 
             for (int i = 0; i < ns; ++i, ++mine) {
                 const int key0 = (j0 + i) * kTcTile;
-                const bool edge = key0 + kTcTile - 1 > len - news;
+                const bool edge = key0 + kTcTile - 1 > shared;
                 const unsigned int s_at = tmem + my_lanes + (mine & 1) * kTcScoreCols;
                 mbar_wait(s_full(mine), (mine >> 1) & 1, give_up);
                 ptx::tc_fence_after();
@@ -1098,11 +1139,22 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         unpack2(fma2(pack2(y[j], y[j + 1]), sc2, m2), y[j], y[j + 1]);
                     }
                     if (edge) {
-                        const int left = limit - key0;
+                        if constexpr (kTree) {
+                            const int old = first - key0;                 // of the tile's places, those before the new tokens (below 64 here)
+                            unsigned long long see = old > 0 ? bits << old | ((1ull << old) - 1ull) : (old > -64 ? bits >> -old : 0ull);
+                            const unsigned int lo = static_cast<unsigned int>(see), hi = static_cast<unsigned int>(see >> 32);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            if (j > left) x[j] = -INFINITY;
-                            if (32 + j > left) y[j] = -INFINITY;
+                            for (int j = 0; j < 32; ++j) {
+                                if (!(lo >> j & 1u)) x[j] = -INFINITY;
+                                if (!(hi >> j & 1u)) y[j] = -INFINITY;
+                            }
+                        } else {
+                            const int left = limit - key0;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                if (j > left) x[j] = -INFINITY;
+                                if (32 + j > left) y[j] = -INFINITY;
+                            }
                         }
                     }
                     float mx = fmaxf(x[0], y[0]), my = fmaxf(x[1], y[1]);
@@ -1168,7 +1220,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     const int item = items + v_item(i, ns), s = item % p.n_stages;
                     mbar_wait(full(s), (item / p.n_stages) & 1, give_up);
                     const unsigned int v_at = slot_at(s);
-                    const int from = max(len - news + 1 - key0, 0), chunks = p.halves * 8;
+                    const int from = max(shared + 1 - key0, 0), chunks = p.halves * 8;
                     for (int c = tid; c < (kTcTile - from) * chunks; c += 128) {
                         const int kr = from + c / chunks, ch = c % chunks;
                         const unsigned int at = v_at + (ch >> 3) * (kTcTile * 128) + kr * 128 + (((ch & 7) ^ (kr & 7)) << 4);
@@ -1221,7 +1273,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                             float z[32];
 #pragma unroll
                             for (int e = 0; e < 32; ++e) z[e] = o[e];
-                            add_left_out<T>(p, b, h, tok, head, c0, max(len - news + 1, j0 * kTcTile), min(limit, (j0 + ns) * kTcTile - 1), m, z);
+                            add_left_out<T, kTree>(p, b, h, tok, head, c0, max(shared + 1, j0 * kTcTile), min(kTree ? len - 1 : limit, (j0 + ns) * kTcTile - 1), m, z,
+                                                   bits, first);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = z[e];
                         }

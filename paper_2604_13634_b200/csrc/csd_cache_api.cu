@@ -9,6 +9,7 @@
 #include "csd_attention.cuh"
 #include "csd_pages.cuh"
 #include "csd_rope.cuh"
+#include "csd_tree.cuh"
 
 using namespace csd;
 
@@ -334,9 +335,9 @@ AttentionPlan attention_plan_of(int T, int group, int dim, int B)
     return with_config<__nv_bfloat16>(dim, [&](auto cfg) { return attention_plan<decltype(cfg)>(T * group, B); });
 }
 
-bool attention_shape_ok(int rows, int T, int q_heads, int heads, int dim)
+bool attention_shape_ok(int rows, int T, int most, int q_heads, int heads, int dim)
 {
-    if (rows <= 0 || rows > CSD_CACHE_MAX_ROWS || T <= 0 || T > CSD_MAX_K + 1 || heads <= 0 || heads > 4096 || q_heads <= 0 || q_heads > (1 << 16) ||
+    if (rows <= 0 || rows > CSD_CACHE_MAX_ROWS || T <= 0 || T > most || heads <= 0 || heads > 4096 || q_heads <= 0 || q_heads > (1 << 16) ||
         q_heads % heads != 0 || dim <= 0 || dim > 256 || dim % 8 != 0)
         return false;
     return static_cast<long long>(rows) * T * q_heads <= (1ll << 27);
@@ -405,11 +406,11 @@ csd_status_t launch_join(const attention::Params &p, const AttentionPlan &a, cud
     return launch(attention::attention_join_kernel<T, DP, 4>, dim3(units, static_cast<unsigned int>((most + 3) / 4)), attention::kJoinThreads, 0, st, p, a.tile_rows);
 }
 
-template <typename C>
+template <typename C, bool kTree>
 csd_status_t run_attention(attention::Params p, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
 {
     static std::atomic<bool> ready[kMaxDevices];
-    if (!kernel_ready(attention::attention_kernel<C>, ready, kSmemPerSm / C::kBlocksPerSm - kSmemReserved - kSmemStatic, C::kGroups,
+    if (!kernel_ready(attention::attention_kernel<C, kTree>, ready, kSmemPerSm / C::kBlocksPerSm - kSmemReserved - kSmemStatic, C::kGroups,
                       C::kMoveRegs ? C::kConsumerRegs * (C::kGroups - 1) + C::kProducerRegs : 0))
         return CSD_ERR_CUDA;
     const AttentionPlan a = attention_plan<C>(p.T * p.group, p.B);
@@ -417,15 +418,15 @@ csd_status_t run_attention(attention::Params p, const csd_cache_t *cache, int la
     p.box_rows = cache->page_size < C::kTile ? cache->page_size : C::kTile;
     CUtensorMap map_k, map_v;
     if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
-    const csd_status_t rc = launch(attention::attention_kernel<C>, dim3(static_cast<unsigned int>(a.grid)), C::kThreads, static_cast<size_t>(a.smem), st, map_k, map_v, p);
+    const csd_status_t rc = launch(attention::attention_kernel<C, kTree>, dim3(static_cast<unsigned int>(a.grid)), C::kThreads, static_cast<size_t>(a.smem), st, map_k, map_v, p);
     return rc != CSD_OK ? rc : launch_join<typename C::T, C::DP>(p, a, st);
 }
 
-template <typename T, int kBlocks, int kM>
+template <typename T, int kBlocks, int kM, bool kTree>
 csd_status_t run_attention_tc(attention::Params p, const AttentionPlan &a, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
 {
     static std::atomic<bool> ready[kMaxDevices];
-    if (!kernel_ready(attention::attention_tc_kernel<T, kBlocks, kM>, ready, kSmemPerSm / kBlocks - kSmemReserved - kSmemStatic, 1, 0)) return CSD_ERR_CUDA;
+    if (!kernel_ready(attention::attention_tc_kernel<T, kBlocks, kM, kTree>, ready, kSmemPerSm / kBlocks - kSmemReserved - kSmemStatic, 1, 0)) return CSD_ERR_CUDA;
     fill_plan(p, a, ws);
     p.tile_rows = a.tile_rows;
     p.q_buffers = a.q_buffers;
@@ -440,7 +441,7 @@ csd_status_t run_attention_tc(attention::Params p, const AttentionPlan &a, const
     p.pool_token = cache->stride_token;
     CUtensorMap map_k, map_v;
     if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
-    const csd_status_t rc = launch(attention::attention_tc_kernel<T, kBlocks, kM>, dim3(static_cast<unsigned int>(a.grid)), attention::kTcThreads,
+    const csd_status_t rc = launch(attention::attention_tc_kernel<T, kBlocks, kM, kTree>, dim3(static_cast<unsigned int>(a.grid)), attention::kTcThreads,
                                    static_cast<size_t>(a.smem), st, map_k, map_v, p);
     if (rc != CSD_OK) return rc;
     if (a.dp == 64) return launch_join<T, 64>(p, a, st);
@@ -448,16 +449,16 @@ csd_status_t run_attention_tc(attention::Params p, const AttentionPlan &a, const
     return launch_join<T, 256>(p, a, st);
 }
 
-template <typename T>
+template <typename T, bool kTree>
 csd_status_t run_attention_any(const attention::Params &p, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
 {
     if (attention_uses_tc(p.T * p.group)) {
         const AttentionPlan a = attention_tc_plan(p.T * p.group, p.D, p.B);
         if (tc_products_of_64(a.tile_rows, p.D))
-            return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 64>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 64>(p, a, cache, layer, ws, st);
-        return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 128>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 128>(p, a, cache, layer, ws, st);
+            return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 64, kTree>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 64, kTree>(p, a, cache, layer, ws, st);
+        return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 128, kTree>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 128, kTree>(p, a, cache, layer, ws, st);
     }
-    return with_config<T>(p.D, [&](auto cfg) { return run_attention<decltype(cfg)>(p, cache, layer, ws, st); });
+    return with_config<T>(p.D, [&](auto cfg) { return run_attention<decltype(cfg), kTree>(p, cache, layer, ws, st); });
 }
 
 }  // namespace
@@ -530,6 +531,15 @@ csd_status_t csd_rope_append(const void *q, int64_t q_stride_b, int64_t q_stride
                              int64_t v_stride_t, int64_t v_stride_h, void *q_out, int T, const csd_cache_t *cache, int layer,
                              const csd_rope_t *rope, const int32_t *n_new, void *stream)
 {
+    return csd_rope_append_at(q, q_stride_b, q_stride_t, q_stride_h, q_heads, k, k_stride_b, k_stride_t, k_stride_h, v, v_stride_b, v_stride_t, v_stride_h,
+                              q_out, T, cache, layer, rope, n_new, nullptr, stream);
+}
+
+csd_status_t csd_rope_append_at(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int q_heads, const void *k,
+                                int64_t k_stride_b, int64_t k_stride_t, int64_t k_stride_h, const void *v, int64_t v_stride_b,
+                                int64_t v_stride_t, int64_t v_stride_h, void *q_out, int T, const csd_cache_t *cache, int layer,
+                                const csd_rope_t *rope, const int32_t *n_new, const int32_t *positions, void *stream)
+{
     const csd_status_t ok = check_cache(cache);
     if (ok != CSD_OK) return ok;
     if (!q || !k || !v || !q_out || T <= 0 || q_heads <= 0 || layer < 0 || layer >= cache->layers) return CSD_ERR_INVALID_ARG;
@@ -551,6 +561,7 @@ csd_status_t csd_rope_append(const void *q, int64_t q_stride_b, int64_t q_stride
     p.n_pages = cache->n_pages;
     p.max_pages = cache->max_pages;
     p.table = pv.table; p.lens = pv.lens; p.n_new = n_new;
+    p.positions = positions;
     p.flags = pv.flags;
     if (rope) {
         p.turn.steps = reinterpret_cast<const unsigned long long *>(rope->steps);
@@ -648,18 +659,25 @@ csd_status_t csd_cache_compact(const csd_cache_t *cache, void *stream)
 
 size_t csd_attention_workspace_bytes(int rows, int T, int q_heads, int heads, int dim)
 {
-    if (!attention_shape_ok(rows, T, q_heads, heads, dim)) return 0;
+    if (!attention_shape_ok(rows, T, CSD_MAX_K + 1, q_heads, heads, dim)) return 0;
     return attention_plan_of(T, q_heads / heads, dim, rows).total;
 }
 
-csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads,
-                           const csd_cache_t *cache, int layer, float scale, const int32_t *n_new, void *out, float *lse,
+size_t csd_attention_tree_workspace_bytes(int rows, int T, int q_heads, int heads, int dim)
+{
+    if (!attention_shape_ok(rows, T, CSD_TREE_MAX_NODES, q_heads, heads, dim)) return 0;
+    return attention_plan_of(T, q_heads / heads, dim, rows).total;
+}
+
+// masks NULL: a chain.
+static csd_status_t attend(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int most, int q_heads,
+                           const csd_cache_t *cache, int layer, float scale, const int32_t *n_new, const uint64_t *masks, void *out, float *lse,
                            void *workspace, size_t workspace_bytes, void *stream)
 {
     const csd_status_t ok = check_cache(cache);
     if (ok != CSD_OK) return ok;
     if (!q || !out || !workspace || T <= 0 || q_heads <= 0 || layer < 0 || layer >= cache->layers || !std::isfinite(scale)) return CSD_ERR_INVALID_ARG;
-    if (!attention_shape_ok(cache->rows, T, q_heads, cache->heads, cache->dim)) return CSD_ERR_UNSUPPORTED;
+    if (!attention_shape_ok(cache->rows, T, most, q_heads, cache->heads, cache->dim)) return CSD_ERR_UNSUPPORTED;
     const AttentionPlan plan = attention_plan_of(T, q_heads / cache->heads, cache->dim, cache->rows);
     // positions are counted in 31 bits: tiles of 64 places at least, and what a unit costs beside its tiles
     const double row_positions = (static_cast<double>(cache->max_pages) * cache->page_size + 63) / 64 + plan.run_cost;
@@ -680,11 +698,50 @@ csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t
     p.n_pages = cache->n_pages;
     p.max_pages = cache->max_pages;
     p.table = pv.table; p.lens = pv.lens; p.n_new = n_new;
+    p.masks = reinterpret_cast<const unsigned long long *>(masks);
     p.flags = pv.flags;
     p.scale_log2 = scale * kLog2e;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
-    return cache->dtype == CSD_BF16 ? run_attention_any<__nv_bfloat16>(p, cache, layer, ws, st) : run_attention_any<__half>(p, cache, layer, ws, st);
+    if (masks) return cache->dtype == CSD_BF16 ? run_attention_any<__nv_bfloat16, true>(p, cache, layer, ws, st) : run_attention_any<__half, true>(p, cache, layer, ws, st);
+    return cache->dtype == CSD_BF16 ? run_attention_any<__nv_bfloat16, false>(p, cache, layer, ws, st) : run_attention_any<__half, false>(p, cache, layer, ws, st);
 }
+
+csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads,
+                           const csd_cache_t *cache, int layer, float scale, const int32_t *n_new, void *out, float *lse,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    return attend(q, q_stride_b, q_stride_t, q_stride_h, T, CSD_MAX_K + 1, q_heads, cache, layer, scale, n_new, nullptr, out, lse, workspace, workspace_bytes, stream);
+}
+
+csd_status_t csd_attention_tree(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads,
+                                const csd_cache_t *cache, int layer, float scale, const int32_t *n_new, const uint64_t *masks, void *out, float *lse,
+                                void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!masks || (reinterpret_cast<uintptr_t>(masks) & 7u)) return CSD_ERR_INVALID_ARG;
+    return attend(q, q_stride_b, q_stride_t, q_stride_h, T, CSD_TREE_MAX_NODES, q_heads, cache, layer, scale, n_new, masks, out, lse, workspace, workspace_bytes, stream);
+}
+
+csd_status_t csd_tree_plan(const int32_t *parents, int64_t parent_stride, int T, const csd_cache_t *cache, const int32_t *n_new, const int32_t *offset,
+                           uint64_t *masks, int32_t *positions, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    if (T <= 0 || !masks || (reinterpret_cast<uintptr_t>(masks) & 7u) || parent_stride < 0) return CSD_ERR_INVALID_ARG;
+    if (T > CSD_TREE_MAX_NODES) return CSD_ERR_UNSUPPORTED;
+    host::other_work_enqueued();
+    tree::PlanParams p;
+    std::memset(&p, 0, sizeof p);
+    p.parents = parents;
+    p.parent_stride = parent_stride;
+    p.T = T;
+    p.lens = view_of(cache).lens;
+    p.n_new = n_new;
+    p.offset = offset;
+    p.masks = reinterpret_cast<unsigned long long *>(masks);
+    p.positions = positions;
+    return launch(tree::plan_kernel, dim3(static_cast<unsigned int>(cache->rows)), CSD_TREE_MAX_NODES, 0, static_cast<cudaStream_t>(stream), p);
+}
+
 
 }  // extern "C"

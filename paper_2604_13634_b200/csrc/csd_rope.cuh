@@ -448,6 +448,7 @@ struct AppendParams {
     long long pool_page, pool_head, pool_token;
     int page_shift, n_pages, max_pages;
     const int *table, *lens, *n_new;
+    const int *positions;                  // [B, T] what the tokens are turned by; null: their places
     unsigned int *flags;
     Turn turn;
     int units, q_groups, kv_groups;
@@ -498,8 +499,9 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const AppendPa
         const int k = i / pairs, pair = i - k * pairs, token = blockIdx.x * p.at.tokens + k;
         if (token < p.at.n_tokens) {
             const int tb = token / p.T, tt = token - tb * p.T;
-            table[k * each + (pair % P) * columns + pair / P] =
-                angle(p.turn, pair, ptx::ld_written(p.lens + tb) - (p.n_new ? ptx::ld_written(p.n_new + tb) : p.T) + tt, false);
+            const int position = p.positions ? ptx::ld_written(p.positions + static_cast<long long>(tb) * p.T + tt)
+                                             : ptx::ld_written(p.lens + tb) - (p.n_new ? ptx::ld_written(p.n_new + tb) : p.T) + tt;
+            table[k * each + (pair % P) * columns + pair / P] = angle(p.turn, pair, position, false);
         }
     }
     __syncthreads();                       // the table is complete; and every element has been read (q_out may be q)

@@ -11,6 +11,7 @@ import torch
 
 from .binding import CSD_BF16, CSD_F16, CSD_F32, CsdError, _check, _ptr, lib
 
+CSD_TREE_MAX_NODES = 64
 CACHE_FULL, CACHE_ROW_FULL, CACHE_BAD_PAGE, CACHE_BAD_ROW, CACHE_INTERNAL = 1, 2, 4, 8, 16
 
 _DTYPES = {torch.float32: CSD_F32, torch.bfloat16: CSD_BF16, torch.float16: CSD_F16}
@@ -49,7 +50,13 @@ SIGNATURES = {
     "csd_cache_commit": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
     "csd_cache_fork": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
     "csd_cache_compact": (c_int, [POINTER(CacheStruct), c_void_p]),
+    "csd_rope_append_at": (c_int, [c_void_p, *_strides3, c_int, c_void_p, *_strides3, c_void_p, *_strides3, c_void_p, c_int,
+                                   POINTER(CacheStruct), c_int, POINTER(RopeStruct), c_void_p, c_void_p, c_void_p]),
+    "csd_tree_plan": (c_int, [c_void_p, c_int64, c_int, POINTER(CacheStruct), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     "csd_attention_workspace_bytes": (c_size_t, [c_int] * 5),
+    "csd_attention_tree_workspace_bytes": (c_size_t, [c_int] * 5),
+    "csd_attention_tree": (c_int, [c_void_p, *_strides3, c_int, c_int, POINTER(CacheStruct), c_int, c_float, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_void_p, c_size_t, c_void_p]),
     "csd_attention": (c_int, [c_void_p, *_strides3, c_int, c_int, POINTER(CacheStruct), c_int, c_float, c_void_p, c_void_p, c_void_p,
                               c_void_p, c_size_t, c_void_p]),
 }
@@ -286,10 +293,11 @@ def csd_cache_compact(cache: PagedCache, stream=None):
     _check(_lib().csd_cache_compact(cache._ref, _stream_ptr(stream, cache._device)), "csd_cache_compact")
 
 
-def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | None, q_out=None, n_new=None, stream=None):
+def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | None, q_out=None, n_new=None, positions=None, stream=None):
     """The new tokens of a layer: q [rows, T, q_heads, D] turned into q_out (dense; returned), k turned and v as it is into
     their page slots.  plan None: no rotation.  After csd_cache_extend pass n_new=cache.granted: where that found no room it
-    granted nothing, and T tokens (n_new None) would go over the newest ones of the row.  Serving form: no gradient (csd_rope has one)."""
+    granted nothing, and T tokens (n_new None) would go over the newest ones of the row.  positions [rows, T] int32 (a TreePlan's): what
+    the tokens are turned by; None: their places.  Serving form: no gradient (csd_rope has one)."""
     B, T, Hq, D = shape = q.shape
     if q_out is None:
         q_out = _result(q, stream, memory_format=torch.contiguous_format)
@@ -300,21 +308,59 @@ def csd_rope_append(q, k, v, cache: PagedCache, layer: int, plan: RopePlan | Non
     dev = cache._device
     if not (q.get_device() == k.get_device() == v.get_device() == q_out.get_device() == dev) or plan is not None and plan._device != dev:
         _scattered("csd_rope_append", q.get_device(), k.get_device(), v.get_device(), q_out.get_device(), dev, plan._device if plan else dev)
-    rc = _lib().csd_rope_append(q.data_ptr(), qs[0], qs[1], qs[2], Hq, k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1], vs[2],
-                                q_out.data_ptr(), T, cache._ref, layer, None if plan is None else plan._ref,
-                                None if n_new is None else _rows_arg(n_new, cache, "n_new"), _stream_ptr(stream, dev))
+    args = (q.data_ptr(), qs[0], qs[1], qs[2], Hq, k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1], vs[2],
+            q_out.data_ptr(), T, cache._ref, layer, None if plan is None else plan._ref,
+            None if n_new is None else _rows_arg(n_new, cache, "n_new"))
+    if positions is None:
+        rc = _lib().csd_rope_append(*args, _stream_ptr(stream, dev))
+    else:
+        rc = _lib().csd_rope_append_at(*args, _nodes_arg(positions, cache, T, torch.int32, "positions"), _stream_ptr(stream, dev))
     if rc:
         _check(rc, "csd_rope_append")
     return q_out
 
 
-class AttentionBuffers:
-    """Caller-owned outputs and workspace of csd_attention for one cache, T new tokens per row and q_heads query heads."""
+def _nodes_arg(t, cache: PagedCache, T: int, dtype, what: str):
+    assert t.get_device() == cache._device and t.dtype == dtype and t.shape == (cache.rows, T) and t.is_contiguous(), what
+    return t.data_ptr()
 
-    def __init__(self, cache: PagedCache, T: int, q_heads: int):
+
+class TreePlan:
+    """Masks [rows, T] (int64 holding 64 bits) and positions [rows, T] (int32) of T <= CSD_TREE_MAX_NODES new tokens per row; see
+    csd_tree_plan, which fills them once per step for all layers."""
+
+    def __init__(self, cache: PagedCache, T: int):
+        if not 0 < T <= CSD_TREE_MAX_NODES:
+            raise CsdError(f"unsupported tree: T={T}")
+        self.T = T
+        self.masks = torch.zeros(cache.rows, T, dtype=torch.int64, device=cache.k.device)
+        self.positions = torch.zeros(cache.rows, T, dtype=torch.int32, device=cache.k.device)
+
+
+def csd_tree_plan(parents, cache: PagedCache, plan: TreePlan, n_new=None, offset=None, stream=None):
+    """plan.masks, plan.positions from parents [rows, T] int32 (or [T]: one tree for all rows; None: a chain): which nodes each node
+    hangs from, itself among them, and lens - n_new + depth + offset.  offset [rows] int32: what positions are ahead of places."""
+    stride = 0
+    if parents is not None:
+        assert parents.dtype == torch.int32 and (parents.shape[-1] == 1 or parents.stride(-1) == 1)
+        assert tuple(parents.shape) in ((plan.T,), (cache.rows, plan.T))
+        if parents.get_device() != cache._device:
+            _scattered("csd_tree_plan", parents.get_device(), cache._device)
+        stride = parents.stride(0) if parents.dim() == 2 else 0
+    _check(_lib().csd_tree_plan(_ptr(parents), stride, plan.T, cache._ref, _rows_arg(n_new, cache, "n_new"), _rows_arg(offset, cache, "offset"),
+                                _nodes_arg(plan.masks, cache, plan.T, torch.int64, "masks"),
+                                _nodes_arg(plan.positions, cache, plan.T, torch.int32, "positions"), _stream_ptr(stream, cache._device)), "csd_tree_plan")
+
+
+class AttentionBuffers:
+    """Caller-owned outputs and workspace of csd_attention, or csd_attention_tree (tree=True), for one cache, T new tokens per row and
+    q_heads query heads."""
+
+    def __init__(self, cache: PagedCache, T: int, q_heads: int, tree: bool = False):
         self.T, self.q_heads = T, q_heads
         dev = cache.k.device
-        self.ws_bytes = int(_lib().csd_attention_workspace_bytes(cache.rows, T, q_heads, cache.kv_heads, cache.head_dim))
+        size = _lib().csd_attention_tree_workspace_bytes if tree else _lib().csd_attention_workspace_bytes
+        self.ws_bytes = int(size(cache.rows, T, q_heads, cache.kv_heads, cache.head_dim))
         if self.ws_bytes == 0:
             raise CsdError(f"unsupported attention: rows={cache.rows} T={T} q_heads={q_heads} kv_heads={cache.kv_heads} dim={cache.head_dim}")
         self.out = torch.empty(cache.rows, T, q_heads, cache.head_dim, dtype=cache.dtype, device=dev)
@@ -326,15 +372,26 @@ class AttentionBuffers:
 def csd_attention(q, cache: PagedCache, layer: int, buf: AttentionBuffers, scale: float | None = None, n_new=None, stream=None):
     """buf.out, buf.lse: attention of T new tokens of every row, q [rows, T, q_heads, D], over its cache (n_new[row] > T: the first T
     of that many).  Serving form: no gradient."""
+    return _attend("csd_attention", q, cache, layer, buf, None, scale, n_new, stream)
+
+
+def csd_attention_tree(q, cache: PagedCache, layer: int, buf: AttentionBuffers, masks, scale: float | None = None, n_new=None, stream=None):
+    """csd_attention where the new tokens see each other by masks [rows, T] int64 (a TreePlan's): bit u of masks[b, t] lets token t see
+    new token u; the places before the new ones are seen by all.  buf: AttentionBuffers(..., tree=True).  Serving form: no gradient."""
+    return _attend("csd_attention_tree", q, cache, layer, buf, _nodes_arg(masks, cache, buf.T, torch.int64, "masks"), scale, n_new, stream)
+
+
+def _attend(what, q, cache, layer, buf, masks, scale, n_new, stream):
     qs = q.stride()
     assert q.dtype == cache.dtype == buf.out.dtype and qs[3] == 1 and q.shape == buf.out.shape
     assert q.shape[0] == cache.rows and q.shape[3] == cache.head_dim
     dev = cache._device
     if not (q.get_device() == buf._device == dev):
-        _scattered("csd_attention", q.get_device(), buf._device, dev)
-    rc = _lib().csd_attention(q.data_ptr(), qs[0], qs[1], qs[2], buf.T, buf.q_heads, cache._ref, layer,
-                              cache.head_dim ** -0.5 if scale is None else scale, None if n_new is None else _rows_arg(n_new, cache, "n_new"),
-                              buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(), buf.ws_bytes, _stream_ptr(stream, dev))
+        _scattered(what, q.get_device(), buf._device, dev)
+    ahead = (q.data_ptr(), qs[0], qs[1], qs[2], buf.T, buf.q_heads, cache._ref, layer,
+             cache.head_dim ** -0.5 if scale is None else scale, None if n_new is None else _rows_arg(n_new, cache, "n_new"))
+    after = (buf.out.data_ptr(), buf.lse.data_ptr(), buf.workspace.data_ptr(), buf.ws_bytes, _stream_ptr(stream, dev))
+    rc = _lib().csd_attention(*ahead, *after) if masks is None else _lib().csd_attention_tree(*ahead, masks, *after)
     if rc:
-        _check(rc, "csd_attention")
+        _check(rc, what)
     return buf.out
