@@ -686,6 +686,31 @@ csd_status_t csd_attention_tree(const void *q, int64_t q_stride_b, int64_t q_str
                                 const csd_cache_t *cache, int layer, float scale, const int32_t *n_new, const uint64_t *masks,
                                 void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
+/* The verification loop of Algorithm 1 (greedy) on a tree: for every row, with z[b,t] the target's logits after node t, begin at node 0 and
+ * repeat at the current node c
+ *     t* = argmax z[b,c,:]                                         (lowest index on ties)
+ *     a child with token t* is accepted (the lowest such index);
+ *     where there is none, of the children d with T[(d, t*)] >= lambda and z[b,c,d] - z[b,c,t*] >= ln tau (csd_verify's memory and gate) the
+ *     one with the largest z[b,c,d] is rescued (the lowest index on ties);
+ *     else the walk ends.
+ * accept_len[b]: nodes accepted after the root; next_token[b]: t* of the last node; path[b,i]: the i-th node of the walk (the root is the 0th), -1
+ * behind the last; rescued_mask[b,t]: 1 for nodes taken by rescue.  rej_draft/rej_target[b,t]: the pair (token of t, t* of its parent) for every
+ * child of a node at which no child had the token t*, -1 elsewhere: what UpdateMemory is told (csd_ocm_update takes the arrays as they
+ * are).  With a chain these are csd_verify's results.  The memory is only read; its statistics count the step, n_nodes - 1 positions a row, matches,
+ * rescues and pairs.
+ * logits: [B, T, V], strides in elements, V contiguous, CSD_F32 or CSD_BF16, of any alignment (16-byte loads between the ragged ends).  Only the
+ * rows of the nodes on the path are read, so only those can raise CSD_FLAG_NAN_LOGIT (a NaN, or a maximum that is not finite; that row's
+ * results are undefined).
+ * tokens: int32 [B, T]; a token outside [0, V) can be neither accepted nor rescued and is not recorded (CSD_FLAG_BAD_DRAFT where its parent
+ * was reached).  parents: as for csd_tree_plan; a node without an earlier parent is never reached.  n_nodes: DEVICE [B] (NULL: T); nodes from
+ * it on do not exist; a row without any gives accept_len 0, next_token -1 and a path of -1.
+ * accept_len and path are the arguments of csd_cache_commit_path.
+ * One launch; asynchronous; no workspace.  Errors: INVALID_ARG, UNSUPPORTED (T > CSD_TREE_MAX_NODES), CUDA. */
+csd_status_t csd_verify_tree(const void *logits, csd_dtype_t dtype, int B, int T, int V, int64_t stride_b, int64_t stride_t,
+                             const int32_t *tokens, const int32_t *parents, int64_t parent_stride, const int32_t *n_nodes,
+                             const csd_ocm_t *ocm, float tau, int32_t *accept_len, int32_t *next_token, int32_t *path,
+                             uint8_t *rescued_mask, int32_t *rej_draft, int32_t *rej_target, void *stream);
+
 /* ---- helpers ---- */
 
 /* (float) log((double) tau): the threshold the gate of Eq. 3 compares against.

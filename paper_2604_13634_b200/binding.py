@@ -35,7 +35,7 @@ EXPORTS = [
     "csd_rope_steps", "csd_rope", "csd_rope_append", "csd_attention_workspace_bytes", "csd_attention",
     "csd_cache_meta_bytes", "csd_cache_meta_layout", "csd_cache_scratch_bytes", "csd_cache_rebuild", "csd_cache_extend",
     "csd_cache_truncate", "csd_cache_commit", "csd_cache_fork", "csd_cache_compact",
-    "csd_tree_plan", "csd_rope_append_at", "csd_attention_tree_workspace_bytes", "csd_attention_tree",
+    "csd_tree_plan", "csd_rope_append_at", "csd_attention_tree_workspace_bytes", "csd_attention_tree", "csd_verify_tree",
 ]
 
 
@@ -116,6 +116,8 @@ def lib():
         "csd_ocm_merge": (c_int, [c_void_p, c_void_p, c_void_p]),
         "csd_ocm_save": (c_int, [c_void_p, c_char_p, c_void_p]),
         "csd_ocm_load": (c_int, [POINTER(c_void_p), c_char_p, c_uint64, c_int]),
+        "csd_verify_tree": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_int64, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_float,
+                                    c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
         "csd_scg_threshold": (c_float, [c_float]),
         "csd_launch_shape": (c_int, [c_int, c_int, c_int, c_int, POINTER(c_int), POINTER(c_int), POINTER(c_int), POINTER(c_int)]),
         "csd_set_tuning": (c_int, [c_int, c_int, c_int]),
@@ -326,6 +328,38 @@ def csd_verify(logits, draft, ocm: Ocm, tau: float, buf: StepBuffers, stream=Non
 def csd_step(logits, draft, ocm: Ocm, tau: float, buf: StepBuffers, stream=None):
     """csd_verify plus the memory update with the step's rejections, in one launch."""
     _step_call("csd_step", logits, draft, ocm, tau, buf, stream)
+
+
+class TreeBuffers:
+    """Caller-owned outputs of csd_verify_tree for B rows of T nodes."""
+
+    def __init__(self, B, T, device="cuda"):
+        self.B, self.T = B, T
+        i = dict(dtype=torch.int32, device=device)
+        self.accept_len, self.next_token = torch.empty(B, **i), torch.empty(B, **i)
+        self.path, self.rej_draft, self.rej_target = (torch.empty(B, T, **i) for _ in range(3))
+        self.rescued_mask = torch.empty(B, T, dtype=torch.uint8, device=device)
+
+
+def csd_verify_tree(logits, tokens, parents, ocm: Ocm, tau: float, buf: TreeBuffers, n_nodes=None, stream=None):
+    """Verification loop of Algorithm 1 (greedy) on trees: logits [B, T, V], tokens [B, T] int32 (node 0 the root), parents [B, T] or [T]
+    int32, n_nodes [B] int32.  buf.accept_len and buf.path go to csd_cache_commit_path, buf.rej_draft and buf.rej_target to Ocm.update;
+    the memory is only read."""
+    B, T, V = logits.shape
+    assert (B, T) == (buf.B, buf.T) and logits.stride(2) == 1
+    assert tokens.dtype == torch.int32 and tokens.shape == (B, T) and tokens.is_contiguous()
+    assert parents.dtype == torch.int32 and tuple(parents.shape) in ((T,), (B, T)) and (T == 1 or parents.stride(-1) == 1)
+    assert n_nodes is None or n_nodes.dtype == torch.int32 and n_nodes.shape == (B,) and n_nodes.is_contiguous()
+    dev = ocm.device.index
+    devices = [t.get_device() for t in (logits, tokens, parents, buf.path) + (() if n_nodes is None else (n_nodes,))]
+    current = torch.cuda.current_device() if stream is None else stream.device_index
+    if any(d != dev for d in devices) or current != dev:
+        raise CsdError(f"csd_verify_tree: tensors on devices {devices}, the memory on {dev}, the stream on {current} (-1: the host)")
+    strides = logits.stride(0), logits.stride(1) if T > 1 else V
+    _check(lib().csd_verify_tree(logits.data_ptr(), _dtype_code(logits), B, T, V, *strides, tokens.data_ptr(), parents.data_ptr(),
+                                 parents.stride(0) if parents.dim() == 2 else 0, _ptr(n_nodes), ocm.handle, c_float(tau),
+                                 buf.accept_len.data_ptr(), buf.next_token.data_ptr(), buf.path.data_ptr(), buf.rescued_mask.data_ptr(),
+                                 buf.rej_draft.data_ptr(), buf.rej_target.data_ptr(), _stream_ptr(stream)), "csd_verify_tree")
 
 
 class HostStep:

@@ -15,6 +15,7 @@
 #include "csd_step.cuh"
 #include "csd_sampled.cuh"
 #include "csd_lmhead.cuh"
+#include "csd_verify_tree.cuh"
 
 using namespace csd;
 
@@ -378,6 +379,14 @@ csd_status_t run_step(const void *logits, csd_dtype_t dtype, int B, int K, int V
         return CSD_ERR_CUDA;
     }
     return cudaGetLastError() == cudaSuccess ? CSD_OK : CSD_ERR_CUDA;
+}
+
+// Blocks of a cluster that share a logit row of the tree's walk.
+unsigned int verify_tree_blocks(int, int V, int elt)
+{
+    unsigned int blocks = 8;
+    while (blocks > 1 && static_cast<long long>(V) * elt < 4096ll * blocks) blocks /= 2;
+    return blocks;
 }
 
 csd_status_t run_update(csd_ocm *ocm, const int32_t *d, const int32_t *t, const uint32_t *w, int64_t n, void *stream,
@@ -775,6 +784,51 @@ csd_status_t csd_step(const void *logits, csd_dtype_t dtype, int B, int K, int V
 {
     return run_step(logits, dtype, B, K, V, stride_b, stride_k, draft, ocm, tau, accept_len, next_token, rescued_mask,
                     rej_draft, rej_target, diag, workspace, workspace_bytes, stream, true);
+}
+
+csd_status_t csd_verify_tree(const void *logits, csd_dtype_t dtype, int B, int T, int V, int64_t stride_b, int64_t stride_t,
+                             const int32_t *tokens, const int32_t *parents, int64_t parent_stride, const int32_t *n_nodes,
+                             const csd_ocm_t *ocm, float tau, int32_t *accept_len, int32_t *next_token, int32_t *path,
+                             uint8_t *rescued_mask, int32_t *rej_draft, int32_t *rej_target, void *stream)
+{
+    if (!logits || !tokens || !parents || !ocm || !accept_len || !next_token || !path || !rescued_mask || !rej_draft || !rej_target) return CSD_ERR_INVALID_ARG;
+    if (B <= 0 || T <= 0 || V <= 0 || (dtype != CSD_F32 && dtype != CSD_BF16)) return CSD_ERR_INVALID_ARG;
+    if (!(tau >= 0.0f) || std::isinf(tau) || parent_stride < 0) return CSD_ERR_INVALID_ARG;
+    if (stride_t < V || (B > 1 && stride_b < stride_t * (T - 1) + V)) return CSD_ERR_INVALID_ARG;
+    if (T > CSD_TREE_MAX_NODES || B > (1 << 26)) return CSD_ERR_UNSUPPORTED;
+    chain_break();
+    verify_tree::Params p;
+    std::memset(&p, 0, sizeof p);
+    p.logits = logits;
+    p.T = T; p.V = V;
+    p.stride_b = stride_b; p.stride_t = stride_t; p.parent_stride = parent_stride;
+    p.tokens = tokens; p.parents = parents; p.n_nodes = n_nodes;
+    p.ocm = view_of(ocm);
+    p.log_tau = csd_scg_threshold(tau);
+    p.accept_len = accept_len; p.next_token = next_token; p.path = path;
+    p.rescued = rescued_mask;
+    p.rej_d = rej_draft; p.rej_t = rej_target;
+    const unsigned int blocks = verify_tree_blocks(B, V, elt_bytes(dtype));
+    cudaLaunchConfig_t cfg;
+    std::memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(static_cast<unsigned int>(B) * blocks);
+    cfg.blockDim = dim3(verify_tree::kThreads);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = blocks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    const cudaError_t rc = dtype == CSD_F32 ? cudaLaunchKernelEx(&cfg, verify_tree::verify_tree_kernel<float>, p)
+                                            : cudaLaunchKernelEx(&cfg, verify_tree::verify_tree_kernel<__nv_bfloat16>, p);
+    if (rc != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CSD_ERR_CUDA;
+    }
+    return CSD_OK;
 }
 
 csd_status_t csd_ocm_update(csd_ocm_t *ocm, const int32_t *rej_draft, const int32_t *rej_target, int64_t n, void *stream)
