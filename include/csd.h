@@ -550,6 +550,7 @@ csd_status_t csd_rope(const void *x, void *y, csd_dtype_t dtype, int B, int S, i
 #define CSD_CACHE_BAD_PAGE  0x4u  /* a table in use holds an id outside the pool: that access was skipped     */
 #define CSD_CACHE_BAD_ROW   0x8u  /* a fork named a parent row that does not exist: the row was left as it is */
 #define CSD_CACHE_INTERNAL  0x10u /* a wait inside a kernel ran out: a bug of the library, results unreliable  */
+#define CSD_CACHE_BAD_PATH  0x20u /* a path to commit was shorter than the accepted count says, or not ascending: cut there */
 
 /* A cache: pages of keys and values, and which page holds what.  HOST struct of caller-owned DEVICE memory.
  * Element (layer, page, head, token, d) of k and of v lies at layer*stride_layer + page*stride_page + head*stride_head +
@@ -656,6 +657,8 @@ csd_status_t csd_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t
  *     csd_tree_plan    (parents, ..., granted, masks, positions)     once per step
  *     per layer:  csd_rope_append_at(q, k, v, ..., granted, positions)
  *                 csd_attention_tree(q', ..., granted, masks)
+ *     csd_verify_tree                                                accept_len and the path
+ *     csd_cache_commit_path(cache, accept_len, path)                 keep the path, free the rest
  */
 #define CSD_TREE_MAX_NODES 64
 
@@ -710,6 +713,14 @@ csd_status_t csd_verify_tree(const void *logits, csd_dtype_t dtype, int B, int T
                              const int32_t *tokens, const int32_t *parents, int64_t parent_stride, const int32_t *n_nodes,
                              const csd_ocm_t *ocm, float tau, int32_t *accept_len, int32_t *next_token, int32_t *path,
                              uint8_t *rescued_mask, int32_t *rej_draft, int32_t *rej_target, void *stream);
+
+/* csd_cache_commit for a tree: of the tokens granted by the last extension, row b keeps path[b,i] for i = 0 .. min(granted[b], accept_len[b] + 1)
+ * - 1 (the root and the accepted nodes, csd_verify_tree's outputs), which become the row's last tokens in that order: their keys and values move
+ * together in every layer, the other new tokens are dropped and pages that nothing uses are free.  path: DEVICE int32 [rows, T], T <=
+ * CSD_TREE_MAX_NODES; ascending within a row, as a path through a tree is: an entry that is not above the one before it, or not among
+ * the granted tokens, ends what is kept (CSD_CACHE_BAD_PATH).  Two launches; asynchronous.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *accept_len, const int32_t *path, int T, void *stream);
 
 /* ---- helpers ---- */
 

@@ -7,6 +7,7 @@
 #include "../../include/csd.h"
 #include "csd_host.h"
 #include "csd_attention.cuh"
+#include "csd_keep.cuh"
 #include "csd_pages.cuh"
 #include "csd_rope.cuh"
 #include "csd_tree.cuh"
@@ -237,6 +238,18 @@ csd_status_t copy_pages(const csd_cache_t *c, const pages::View &v, long long mo
     if (blocks > cap) blocks = cap;
     if (blocks < 1) return CSD_OK;
     return launch(pages::pages_copy_kernel, dim3(static_cast<unsigned int>(blocks), static_cast<unsigned int>(planes)), pages::kCopyThreads, 0, st, p);
+}
+
+keep::Pool pool_of(const csd_cache_t *c)
+{
+    keep::Pool p;
+    p.k = static_cast<char *>(c->k);
+    p.v = static_cast<char *>(c->v);
+    p.layer = c->stride_layer * 2; p.page = c->stride_page * 2; p.head = c->stride_head * 2; p.token = c->stride_token * 2;
+    p.layers = c->layers;
+    p.heads = c->heads;
+    p.vecs = c->dim / 8;
+    return p;
 }
 
 // ---- attention ----------------------------------------------------------------------------------
@@ -632,6 +645,29 @@ static csd_status_t shorten(const csd_cache_t *cache, const int32_t *new_lens, c
 csd_status_t csd_cache_truncate(const csd_cache_t *cache, const int32_t *new_lens, void *stream) { return shorten(cache, new_lens, nullptr, stream); }
 
 csd_status_t csd_cache_commit(const csd_cache_t *cache, const int32_t *accept_len, void *stream) { return shorten(cache, nullptr, accept_len, stream); }
+
+csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *accept_len, const int32_t *path, int T, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    if (!accept_len || !path || T <= 0) return CSD_ERR_INVALID_ARG;
+    if (T > CSD_TREE_MAX_NODES || 2ll * cache->layers * cache->heads * (cache->dim / 8) > INT_MAX) return CSD_ERR_UNSUPPORTED;
+    host::other_work_enqueued();
+    keep::PathParams p;
+    std::memset(&p, 0, sizeof p);
+    p.v = view_of(cache);
+    p.pool = pool_of(cache);
+    p.accept_len = accept_len;
+    p.path = path;
+    p.T = T;
+    // a block per 128 vectors of a token, as long as that is a few waves of blocks
+    long long blocks = (2ll * cache->layers * cache->heads * p.pool.vecs + keep::kPathThreads - 1) / keep::kPathThreads;
+    const long long cap = (64ll * host::multiprocessors() + cache->rows - 1) / cache->rows;
+    if (blocks > cap) blocks = cap;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const csd_status_t rc = launch(keep::path_move_kernel, dim3(static_cast<unsigned int>(blocks), static_cast<unsigned int>(cache->rows)), keep::kPathThreads, 0, st, p);
+    return rc != CSD_OK ? rc : launch(keep::path_commit_kernel, dim3(static_cast<unsigned int>(cache->rows)), pages::kRowThreads, 0, st, p);
+}
 
 csd_status_t csd_cache_fork(const csd_cache_t *cache, const int32_t *parent, void *stream)
 {

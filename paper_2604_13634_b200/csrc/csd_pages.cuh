@@ -224,6 +224,22 @@ __device__ __forceinline__ void release(const View &v, int page)
     if (atomicSub(v.refs + page, 1) == 1) atomicOr(v.free_bits + (page >> 5), 1u << (page & 31));
 }
 
+// A row of len tokens keeps `to` of them.  All threads of a block of kRowThreads.
+__device__ __forceinline__ void shorten(const View &v, int r, int len, int to)
+{
+    const int first = pages_of(to, v.page_shift), held = pages_of(len, v.page_shift);
+    int *row = v.table + static_cast<long long>(r) * v.max_pages;
+    for (int i = first + threadIdx.x; i < held; i += kRowThreads) {
+        release(v, row[i]);
+        row[i] = -1;
+    }
+    __syncthreads();                                 // every thread has read the row's length and grant
+    if (threadIdx.x == 0) {
+        v.lens[r] = to;
+        v.granted[r] = 0;
+    }
+}
+
 // Rows become shorter: to new_lens[row], or (commit) by the tokens of the last extension that the verification did
 // not keep: granted - min(granted, accept_len + 1).  A row never grows here.
 __global__ void __launch_bounds__(kRowThreads) truncate_kernel(const View v, const int *new_lens, const int *accept_len)
@@ -239,18 +255,7 @@ __global__ void __launch_bounds__(kRowThreads) truncate_kernel(const View v, con
     } else {
         to = ptx::ld_written(new_lens + r);
     }
-    to = min(max(to, 0), len);
-    const int first = pages_of(to, v.page_shift), held = pages_of(len, v.page_shift);
-    int *row = v.table + static_cast<long long>(r) * v.max_pages;
-    for (int i = first + threadIdx.x; i < held; i += kRowThreads) {
-        release(v, row[i]);
-        row[i] = -1;
-    }
-    __syncthreads();                                 // every thread has read the row's length and grant
-    if (threadIdx.x == 0) {
-        v.lens[r] = to;
-        v.granted[r] = 0;
-    }
+    shorten(v, r, len, min(max(to, 0), len));
 }
 
 // Rows continue other rows' pages.  First launch: stage the new tables and count the new references; second launch,

@@ -12,7 +12,7 @@ import torch
 from .binding import CSD_BF16, CSD_F16, CSD_F32, CsdError, _check, _ptr, lib
 
 CSD_TREE_MAX_NODES = 64
-CACHE_FULL, CACHE_ROW_FULL, CACHE_BAD_PAGE, CACHE_BAD_ROW, CACHE_INTERNAL = 1, 2, 4, 8, 16
+CACHE_FULL, CACHE_ROW_FULL, CACHE_BAD_PAGE, CACHE_BAD_ROW, CACHE_INTERNAL, CACHE_BAD_PATH = 1, 2, 4, 8, 16, 32
 
 _DTYPES = {torch.float32: CSD_F32, torch.bfloat16: CSD_BF16, torch.float16: CSD_F16}
 _LAYOUTS = {"half": 0, "interleaved": 1}
@@ -48,6 +48,7 @@ SIGNATURES = {
     "csd_cache_extend": (c_int, [POINTER(CacheStruct), c_int, c_void_p, c_void_p]),
     "csd_cache_truncate": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
     "csd_cache_commit": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
+    "csd_cache_commit_path": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p, c_int, c_void_p]),
     "csd_cache_fork": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
     "csd_cache_compact": (c_int, [POINTER(CacheStruct), c_void_p]),
     "csd_rope_append_at": (c_int, [c_void_p, *_strides3, c_int, c_void_p, *_strides3, c_void_p, *_strides3, c_void_p, c_int,
@@ -281,6 +282,14 @@ def csd_cache_truncate(cache: PagedCache, new_lens, stream=None):
 def csd_cache_commit(cache: PagedCache, accept_len, stream=None):
     """After a verification step: of the last extension's tokens, the first accept_len[row] + 1 stay."""
     _check(_lib().csd_cache_commit(cache._ref, _rows_arg(accept_len, cache, "accept_len"), _stream_ptr(stream, cache._device)), "csd_cache_commit")
+
+
+def csd_cache_commit_path(cache: PagedCache, accept_len, path, stream=None):
+    """After the verification of a tree (TreeBuffers' accept_len and path [rows, T]): of the last extension's tokens, path[row, 0 ..
+    accept_len[row]] stay and move together."""
+    assert path.dim() == 2
+    _check(_lib().csd_cache_commit_path(cache._ref, _rows_arg(accept_len, cache, "accept_len"), _nodes_arg(path, cache, path.shape[1], torch.int32, "path"),
+                                        path.shape[1], _stream_ptr(stream, cache._device)), "csd_cache_commit_path")
 
 
 def csd_cache_fork(cache: PagedCache, parent, stream=None):
