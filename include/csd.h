@@ -550,6 +550,7 @@ csd_status_t csd_rope(const void *x, void *y, csd_dtype_t dtype, int B, int S, i
 #define CSD_CACHE_BAD_PAGE  0x4u  /* a table in use holds an id outside the pool: that access was skipped     */
 #define CSD_CACHE_BAD_ROW   0x8u  /* a fork named a parent row that does not exist: the row was left as it is */
 #define CSD_CACHE_INTERNAL  0x10u /* a wait inside a kernel ran out: a bug of the library, results unreliable  */
+#define CSD_CACHE_SHARED    0x40u /* an eviction would have moved tokens within a page that other rows use: that row was left as it is */
 #define CSD_CACHE_BAD_PATH  0x20u /* a path to commit was shorter than the accepted count says, or not ascending: cut there */
 
 /* A cache: pages of keys and values, and which page holds what.  HOST struct of caller-owned DEVICE memory.
@@ -721,6 +722,24 @@ csd_status_t csd_verify_tree(const void *logits, csd_dtype_t dtype, int B, int T
  * the granted tokens, ends what is kept (CSD_CACHE_BAD_PATH).  Two launches; asynchronous.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *accept_len, const int32_t *path, int T, void *stream);
+
+/* ---- a cache kept to a budget ---- */
+
+/* Rows of more than `keep` tokens (or keep_rows[b], DEVICE [rows]) are cut down to that many.  With R = min(recent, keep) and S =
+ * min(sinks, keep - R): the first S and the last R tokens stay, and of those between the keep - S - R with the largest mass[b,place] (the
+ * lowest place on ties; NaN counts as the smallest).  The last R stay the last, in order; of the others, those that lie below place
+ * keep - R stay where they are, and those beyond, in order, fill the places below it that became free, lowest first.  Keys, values (in every
+ * layer) and masses move with their tokens; masses of the places given up become 0; pages that nothing uses are free.  Keys keep the
+ * rotation of their old positions, so positions of later tokens run ahead of places by what the row has lost: csd_tree_plan's offset.
+ * A row that would have to move tokens into a page that other rows use as well is left as it is (CSD_CACHE_SHARED).
+ * mass: DEVICE float, element (b,place) at b*mass_stride + place, with max_pages * page_size places to a row.
+ * kept: DEVICE int32 [rows, width]: the place before of the token now at place i, -1 from the new length on (rows left as they are: i); width >=
+ * keep; keep_rows[b] beyond width counts as width.  evicted: DEVICE int32 [rows], tokens lost.  granted is 0 afterwards.
+ * workspace: csd_cache_evict_workspace_bytes bytes, 256-byte aligned, no initialisation; one call at a time.
+ * Three launches; asynchronous.  Errors: INVALID_ARG (null, negative, keep > width, mass_stride below a row's places), UNSUPPORTED, WORKSPACE, CUDA. */
+size_t csd_cache_evict_workspace_bytes(int rows, int width);
+csd_status_t csd_cache_evict(const csd_cache_t *cache, float *mass, int64_t mass_stride, int keep, const int32_t *keep_rows, int sinks, int recent,
+                             int32_t *kept, int width, int32_t *evicted, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- helpers ---- */
 

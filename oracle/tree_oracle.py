@@ -123,8 +123,9 @@ def evict(mass, n, keep, sinks, recent):
         return list(range(n))
     recent = min(max(recent, 0), keep)
     sinks = min(max(sinks, 0), keep - recent)
-    value = [-math.inf if math.isnan(x) else float(x) for x in mass[:n]]
-    middle = sorted(range(sinks, n - recent), key=lambda j: (-value[j], j))[:keep - recent - sinks]
+    value = [float(x) for x in mass[:n]]
+    below_all = [math.isnan(x) for x in value]                         # NaN is smaller than minus infinity
+    middle = sorted(range(sinks, n - recent), key=lambda j: (below_all[j], 0.0 if below_all[j] else -value[j], j))[:keep - recent - sinks]
     chosen = set(range(sinks)) | set(middle)
     front = keep - recent
     movers = iter(sorted(j for j in chosen if j >= front))

@@ -41,6 +41,31 @@ csd_status_t launch(void (*kernel)(P...), dim3 grid, unsigned int threads, size_
     return CSD_OK;
 }
 
+// ... with blocks in clusters.
+template <typename... P, typename... A>
+csd_status_t launch_clusters(void (*kernel)(P...), dim3 grid, unsigned int threads, size_t smem, cudaStream_t st, unsigned int cluster, const A &...args)
+{
+    cudaLaunchConfig_t cfg;
+    std::memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CSD_ERR_CUDA;
+    }
+    return CSD_OK;
+}
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // ---- rotary positions ---------------------------------------------------------------------------
@@ -239,6 +264,11 @@ csd_status_t copy_pages(const csd_cache_t *c, const pages::View &v, long long mo
     if (blocks < 1) return CSD_OK;
     return launch(pages::pages_copy_kernel, dim3(static_cast<unsigned int>(blocks), static_cast<unsigned int>(planes)), pages::kCopyThreads, 0, st, p);
 }
+
+size_t evict_pairs_off(int rows) { return align_up(static_cast<size_t>(rows) * sizeof(keep::RowPlan), 256); }
+
+// Blocks that share the choice among a row's places: one while a thread has at most 16 of them, else eight.
+unsigned int evict_blocks(long long places) { return places <= 16 * keep::kPickThreads ? 1u : keep::kMostBlocks; }
 
 keep::Pool pool_of(const csd_cache_t *c)
 {
@@ -667,6 +697,48 @@ csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *acce
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const csd_status_t rc = launch(keep::path_move_kernel, dim3(static_cast<unsigned int>(blocks), static_cast<unsigned int>(cache->rows)), keep::kPathThreads, 0, st, p);
     return rc != CSD_OK ? rc : launch(keep::path_commit_kernel, dim3(static_cast<unsigned int>(cache->rows)), pages::kRowThreads, 0, st, p);
+}
+
+size_t csd_cache_evict_workspace_bytes(int rows, int width)
+{
+    if (rows <= 0 || rows > CSD_CACHE_MAX_ROWS || width < 0 || width > (1 << 30)) return 0;
+    return evict_pairs_off(rows) + static_cast<size_t>(rows) * (width > 0 ? width : 1) * sizeof(int2);
+}
+
+csd_status_t csd_cache_evict(const csd_cache_t *cache, float *mass, int64_t mass_stride, int keep, const int32_t *keep_rows, int sinks, int recent,
+                             int32_t *kept, int width, int32_t *evicted, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    if (!mass || !evicted || !workspace || width < 0 || (width > 0 && !kept) || keep < 0 || sinks < 0 || recent < 0) return CSD_ERR_INVALID_ARG;
+    if (!keep_rows && keep > width) return CSD_ERR_INVALID_ARG;
+    const long long places = static_cast<long long>(cache->max_pages) * cache->page_size;
+    if (cache->rows > 1 && mass_stride < places) return CSD_ERR_INVALID_ARG;
+    if (width > (1 << 30)) return CSD_ERR_UNSUPPORTED;
+    if (workspace_bytes < csd_cache_evict_workspace_bytes(cache->rows, width) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return CSD_ERR_WORKSPACE;
+    host::other_work_enqueued();
+    keep::EvictParams p;
+    std::memset(&p, 0, sizeof p);
+    p.v = view_of(cache);
+    p.pool = pool_of(cache);
+    p.mass = mass;
+    p.mass_stride = mass_stride;
+    p.keep = keep;
+    p.keep_rows = keep_rows;
+    p.sinks = sinks;
+    p.recent = recent;
+    p.width = width;
+    p.kept = kept;
+    p.evicted = evicted;
+    p.plans = static_cast<keep::RowPlan *>(workspace);
+    p.pairs = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + evict_pairs_off(cache->rows));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    csd_status_t rc = launch_clusters(keep::evict_pick_kernel, dim3(static_cast<unsigned int>(cache->rows) * evict_blocks(places)), keep::kPickThreads, 0, st, evict_blocks(places), p);
+    if (rc != CSD_OK) return rc;
+    const long long units = 2ll * cache->layers * cache->heads + 1, most = 8ll * host::multiprocessors();
+    const long long blocks = units * cache->rows < most ? units * cache->rows : most;
+    rc = launch(keep::evict_move_kernel, dim3(static_cast<unsigned int>(blocks)), keep::kMoveThreads, 0, st, p);
+    return rc != CSD_OK ? rc : launch(keep::evict_finish_kernel, dim3(static_cast<unsigned int>(cache->rows)), pages::kRowThreads, 0, st, p);
 }
 
 csd_status_t csd_cache_fork(const csd_cache_t *cache, const int32_t *parent, void *stream)

@@ -12,7 +12,7 @@ import torch
 from .binding import CSD_BF16, CSD_F16, CSD_F32, CsdError, _check, _ptr, lib
 
 CSD_TREE_MAX_NODES = 64
-CACHE_FULL, CACHE_ROW_FULL, CACHE_BAD_PAGE, CACHE_BAD_ROW, CACHE_INTERNAL, CACHE_BAD_PATH = 1, 2, 4, 8, 16, 32
+CACHE_FULL, CACHE_ROW_FULL, CACHE_BAD_PAGE, CACHE_BAD_ROW, CACHE_INTERNAL, CACHE_BAD_PATH, CACHE_SHARED = 1, 2, 4, 8, 16, 32, 64
 
 _DTYPES = {torch.float32: CSD_F32, torch.bfloat16: CSD_BF16, torch.float16: CSD_F16}
 _LAYOUTS = {"half": 0, "interleaved": 1}
@@ -49,6 +49,9 @@ SIGNATURES = {
     "csd_cache_truncate": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
     "csd_cache_commit": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
     "csd_cache_commit_path": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p, c_int, c_void_p]),
+    "csd_cache_evict_workspace_bytes": (c_size_t, [c_int, c_int]),
+    "csd_cache_evict": (c_int, [POINTER(CacheStruct), c_void_p, c_int64, c_int, c_void_p, c_int, c_int, c_void_p, c_int, c_void_p, c_void_p, c_size_t,
+                                c_void_p]),
     "csd_cache_fork": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
     "csd_cache_compact": (c_int, [POINTER(CacheStruct), c_void_p]),
     "csd_rope_append_at": (c_int, [c_void_p, *_strides3, c_int, c_void_p, *_strides3, c_void_p, *_strides3, c_void_p, c_int,
@@ -290,6 +293,40 @@ def csd_cache_commit_path(cache: PagedCache, accept_len, path, stream=None):
     assert path.dim() == 2
     _check(_lib().csd_cache_commit_path(cache._ref, _rows_arg(accept_len, cache, "accept_len"), _nodes_arg(path, cache, path.shape[1], torch.int32, "path"),
                                         path.shape[1], _stream_ptr(stream, cache._device)), "csd_cache_commit_path")
+
+
+class EvictBuffers:
+    """Caller-owned outputs and workspace of csd_cache_evict for budgets up to `keep` tokens: kept [rows, keep], evicted [rows]."""
+
+    def __init__(self, cache: PagedCache, keep: int):
+        self.keep, dev = keep, cache.k.device
+        self.ws_bytes = int(_lib().csd_cache_evict_workspace_bytes(cache.rows, keep)) if 0 <= keep < 2 ** 31 else 0
+        if self.ws_bytes == 0:
+            raise CsdError(f"unsupported budget: {keep}")
+        self.kept = torch.empty(cache.rows, keep, dtype=torch.int32, device=dev)
+        self.evicted = torch.empty(cache.rows, dtype=torch.int32, device=dev)
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+
+
+def _mass_arg(mass, cache: PagedCache):
+    assert mass.dtype == torch.float32 and mass.dim() == 2 and mass.shape[0] == cache.rows and mass.shape[1] >= cache.max_pages * cache.page_size
+    assert mass.stride(1) == 1 and (cache.rows == 1 or mass.stride(0) >= mass.shape[1])
+    if mass.get_device() != cache._device:
+        _scattered("mass", mass.get_device(), cache._device)
+    return mass.data_ptr(), max(mass.stride(0), mass.shape[1])
+
+
+def csd_cache_evict(cache: PagedCache, mass, keep, buf: EvictBuffers, sinks: int = 0, recent: int = 0, stream=None):
+    """Rows of more than keep tokens (an int, or int32 [rows] on the device) keep the first `sinks`, the last `recent` and the best by mass
+    [rows, places] of the rest; keys, values and masses move together.  buf.kept: the place before of every place after (-1: none);
+    buf.evicted: tokens lost, what positions of later tokens run ahead of their places (csd_tree_plan's offset is the sum of these)."""
+    rows = None
+    if isinstance(keep, torch.Tensor):
+        rows, keep = _rows_arg(keep, cache, "keep"), 0
+    if not (buf.kept.shape == (cache.rows, buf.keep) and buf.kept.get_device() == cache._device):
+        raise CsdError("csd_cache_evict: buffers of another cache")
+    _check(_lib().csd_cache_evict(cache._ref, *_mass_arg(mass, cache), keep, rows, sinks, recent, buf.kept.data_ptr(), buf.keep, buf.evicted.data_ptr(),
+                                  buf.workspace.data_ptr(), buf.ws_bytes, _stream_ptr(stream, cache._device)), "csd_cache_evict")
 
 
 def csd_cache_fork(cache: PagedCache, parent, stream=None):
