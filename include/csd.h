@@ -725,9 +725,22 @@ csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *acce
 
 /* ---- a cache kept to a budget ---- */
 
+/* How much attention the places of every row get from its T <= CSD_TREE_MAX_NODES newest tokens, added to mass:
+ *     mass[b,j] += sum_{t,h} exp(scale q[b,t,h].k_j - lse[b,t,h])
+ * over the tokens t < n_new[b] (NULL: T) that see place j, with key head h / g: the softmax weights of csd_attention (masks NULL) or
+ * csd_attention_tree, whose q, scale, n_new, masks and lse these are.  A token with lse = -inf, or without a place, adds nothing; rows without new tokens stay
+ * as they are; what lies in places that a token does not see does not matter.  fresh != 0: the places of the new tokens [lens - n_new,
+ * lens) begin at 0 whatever mass held there -- for the first layer of a pass, when mass sums over layers.
+ * q: as for csd_attention.  lse: DEVICE float [rows, T, q_heads].  mass: as for csd_cache_evict.
+ * Scores, exponentials and sums in float32, added in a fixed order.  One launch; asynchronous.
+ * Errors: INVALID_ARG, UNSUPPORTED (as csd_attention), CUDA. */
+csd_status_t csd_attention_mass(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads, const float *lse,
+                                const csd_cache_t *cache, int layer, float scale, const int32_t *n_new, const uint64_t *masks, float *mass,
+                                int64_t mass_stride, int fresh, void *stream);
+
 /* Rows of more than `keep` tokens (or keep_rows[b], DEVICE [rows]) are cut down to that many.  With R = min(recent, keep) and S =
  * min(sinks, keep - R): the first S and the last R tokens stay, and of those between the keep - S - R with the largest mass[b,place] (the
- * lowest place on ties; NaN counts as the smallest).  The last R stay the last, in order; of the others, those that lie below place
+ * lowest place on ties; NaN is below everything).  The last R stay the last, in order; of the others, those that lie below place
  * keep - R stay where they are, and those beyond, in order, fill the places below it that became free, lowest first.  Keys, values (in every
  * layer) and masses move with their tokens; masses of the places given up become 0; pages that nothing uses are free.  Keys keep the
  * rotation of their old positions, so positions of later tokens run ahead of places by what the row has lost: csd_tree_plan's offset.

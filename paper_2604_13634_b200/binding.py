@@ -36,7 +36,7 @@ EXPORTS = [
     "csd_cache_meta_bytes", "csd_cache_meta_layout", "csd_cache_scratch_bytes", "csd_cache_rebuild", "csd_cache_extend",
     "csd_cache_truncate", "csd_cache_commit", "csd_cache_fork", "csd_cache_compact",
     "csd_tree_plan", "csd_rope_append_at", "csd_attention_tree_workspace_bytes", "csd_attention_tree", "csd_verify_tree",
-    "csd_cache_commit_path", "csd_cache_evict_workspace_bytes", "csd_cache_evict",
+    "csd_cache_commit_path", "csd_cache_evict_workspace_bytes", "csd_cache_evict", "csd_attention_mass",
 ]
 
 

@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libcsd.so")
 LIB_DEBUG = os.path.join(HERE, "libcsd_debug.so")     # the same sources with -DCSD_DEBUG: the step kernels' indexes checked
 SOURCES = ["csd_api.cu", "csd_cache_api.cu"]
 HEADERS = ["csd_common.cuh", "csd_ocm.cuh", "csd_step.cuh", "csd_sampled.cuh", "csd_lmhead.cuh", "csd_host.h", "csd_ptx.cuh", "csd_rope.cuh", "csd_pages.cuh",
-           "csd_attention.cuh", "csd_tree.cuh", "csd_verify_tree.cuh", "csd_keep.cuh", os.path.join("..", "..", "include", "csd.h")]
+           "csd_attention.cuh", "csd_tree.cuh", "csd_verify_tree.cuh", "csd_keep.cuh", "csd_mass.cuh", os.path.join("..", "..", "include", "csd.h")]
 
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-shared", "-Xcompiler", "-fPIC", "--threads", "0", "--use_fast_math=false"]

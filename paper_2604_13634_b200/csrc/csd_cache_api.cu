@@ -8,6 +8,7 @@
 #include "csd_host.h"
 #include "csd_attention.cuh"
 #include "csd_keep.cuh"
+#include "csd_mass.cuh"
 #include "csd_pages.cuh"
 #include "csd_rope.cuh"
 #include "csd_tree.cuh"
@@ -285,6 +286,7 @@ keep::Pool pool_of(const csd_cache_t *c)
 // ---- attention ----------------------------------------------------------------------------------
 
 constexpr int kMaxDevices = 64;
+constexpr int kMassStatic = 4096;                    // the mass kernel's own
 constexpr int kSmemPerSm = 228 * 1024, kSmemReserved = 1024, kSmemStatic = 1024;     // per block: the system's, and the kernel's own
 
 struct AttentionPlan {
@@ -490,6 +492,39 @@ csd_status_t run_attention_tc(attention::Params p, const AttentionPlan &a, const
     if (a.dp == 64) return launch_join<T, 64>(p, a, st);
     if (a.dp == 128) return launch_join<T, 128>(p, a, st);
     return launch_join<T, 256>(p, a, st);
+}
+
+// Blocks that share the key heads of a run of places.  More of them finish a short row sooner; fewer meet less often.
+unsigned int mass_blocks(int rows, int heads)
+{
+    unsigned int blocks = rows <= 4 ? 8u : (rows <= 16 ? 4u : (rows <= 48 ? 2u : 1u));
+    while (blocks > static_cast<unsigned int>(heads)) blocks /= 2;
+    return blocks;
+}
+
+template <typename T>
+csd_status_t run_mass(mass::Params p, const csd_cache_t *cache, int layer, cudaStream_t st)
+{
+    static std::atomic<bool> ready[kMaxDevices];
+    constexpr int limit = kSmemPerSm / mass::kBlocksPerSm - kSmemReserved - kMassStatic;
+    if (!kernel_ready(mass::mass_kernel<T>, ready, limit, 1, 0)) return CSD_ERR_CUDA;
+    attention::Params &a = p.a;
+    a.halves = (a.D + 63) / 64;
+    a.d16 = (a.D + 15) / 16 * 16;
+    a.box_rows = cache->page_size < mass::kTile ? cache->page_size : mass::kTile;
+    // Query rows: as many as 32 KiB hold, in two sets where both fit there; the rest of the shared memory is for the ring of keys.
+    const int most = 32768 / (a.halves * 128) / 16 * 16, all = (a.T * a.group + 15) / 16 * 16;
+    p.q_rows = all < most ? all : most;
+    if (p.q_rows > mass::kMostRows) p.q_rows = mass::kMostRows;
+    a.q_buffers = 2 * p.q_rows <= most ? 2 : 1;
+    const int fixed = 1024 + a.q_buffers * a.halves * p.q_rows * 128 + mass::kRunTiles * mass::kTile * 4 + (a.B + 1) * 4;
+    a.n_stages = (limit - fixed) / mass::kSlotBytes;
+    if (a.n_stages > mass::kMaxSlots) a.n_stages = mass::kMaxSlots;
+    if (a.n_stages < 2) return CSD_ERR_UNSUPPORTED;
+    CUtensorMap map_k;
+    if (!make_pool_map(&map_k, cache, cache->k, layer, a.box_rows)) return CSD_ERR_CUDA;
+    const unsigned int blocks = mass_blocks(a.B, a.Hkv), grid = static_cast<unsigned int>(host::multiprocessors()) * mass::kBlocksPerSm / blocks * blocks;
+    return launch_clusters(mass::mass_kernel<T>, dim3(grid), mass::kThreads, static_cast<size_t>(fixed + a.n_stages * mass::kSlotBytes), st, blocks, map_k, p);
 }
 
 template <typename T, bool kTree>
@@ -828,6 +863,41 @@ csd_status_t csd_attention_tree(const void *q, int64_t q_stride_b, int64_t q_str
 {
     if (!masks || (reinterpret_cast<uintptr_t>(masks) & 7u)) return CSD_ERR_INVALID_ARG;
     return attend(q, q_stride_b, q_stride_t, q_stride_h, T, CSD_TREE_MAX_NODES, q_heads, cache, layer, scale, n_new, masks, out, lse, workspace, workspace_bytes, stream);
+}
+
+csd_status_t csd_attention_mass(const void *q, int64_t q_stride_b, int64_t q_stride_t, int64_t q_stride_h, int T, int q_heads, const float *lse,
+                                const csd_cache_t *cache, int layer, float scale, const int32_t *n_new, const uint64_t *masks, float *mass,
+                                int64_t mass_stride, int fresh, void *stream)
+{
+    const csd_status_t ok = check_cache(cache);
+    if (ok != CSD_OK) return ok;
+    if (!q || !lse || !mass || T <= 0 || q_heads <= 0 || layer < 0 || layer >= cache->layers || !std::isfinite(scale)) return CSD_ERR_INVALID_ARG;
+    if (!attention_shape_ok(cache->rows, T, CSD_TREE_MAX_NODES, q_heads, cache->heads, cache->dim)) return CSD_ERR_UNSUPPORTED;
+    const long long places = static_cast<long long>(cache->max_pages) * cache->page_size;
+    if (cache->rows > 1 && mass_stride < places) return CSD_ERR_INVALID_ARG;
+    if ((places + mass::kTile - 1) / mass::kTile * cache->rows > INT_MAX) return CSD_ERR_UNSUPPORTED;       // tiles are counted in 31 bits
+    if (!aligned16(q) || (q_stride_b | q_stride_t | q_stride_h) % 8 != 0 || (reinterpret_cast<uintptr_t>(masks) & 7u)) return CSD_ERR_INVALID_ARG;
+    host::other_work_enqueued();
+    const pages::View pv = view_of(cache);
+    mass::Params p;
+    std::memset(&p, 0, sizeof p);
+    attention::Params &a = p.a;
+    a.q = q;
+    a.B = cache->rows; a.T = T; a.Hq = q_heads; a.Hkv = cache->heads; a.D = cache->dim; a.group = q_heads / cache->heads;
+    a.qb = q_stride_b; a.qt = q_stride_t; a.qh = q_stride_h;
+    a.page_shift = pv.page_shift;
+    a.n_pages = cache->n_pages;
+    a.max_pages = cache->max_pages;
+    a.table = pv.table; a.lens = pv.lens; a.n_new = n_new;
+    a.masks = reinterpret_cast<const unsigned long long *>(masks);
+    a.flags = pv.flags;
+    a.scale_log2 = scale * kLog2e;
+    p.lse = lse;
+    p.mass = mass;
+    p.mass_stride = mass_stride;
+    p.fresh = fresh != 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return cache->dtype == CSD_BF16 ? run_mass<__nv_bfloat16>(p, cache, layer, st) : run_mass<__half>(p, cache, layer, st);
 }
 
 csd_status_t csd_tree_plan(const int32_t *parents, int64_t parent_stride, int T, const csd_cache_t *cache, const int32_t *n_new, const int32_t *offset,

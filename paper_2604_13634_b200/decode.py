@@ -57,6 +57,8 @@ SIGNATURES = {
     "csd_rope_append_at": (c_int, [c_void_p, *_strides3, c_int, c_void_p, *_strides3, c_void_p, *_strides3, c_void_p, c_int,
                                    POINTER(CacheStruct), c_int, POINTER(RopeStruct), c_void_p, c_void_p, c_void_p]),
     "csd_tree_plan": (c_int, [c_void_p, c_int64, c_int, POINTER(CacheStruct), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "csd_attention_mass": (c_int, [c_void_p, *_strides3, c_int, c_int, c_void_p, POINTER(CacheStruct), c_int, c_float, c_void_p, c_void_p, c_void_p,
+                                   c_int64, c_int, c_void_p]),
     "csd_attention_workspace_bytes": (c_size_t, [c_int] * 5),
     "csd_attention_tree_workspace_bytes": (c_size_t, [c_int] * 5),
     "csd_attention_tree": (c_int, [c_void_p, *_strides3, c_int, c_int, POINTER(CacheStruct), c_int, c_float, c_void_p, c_void_p, c_void_p,
@@ -425,6 +427,24 @@ def csd_attention_tree(q, cache: PagedCache, layer: int, buf: AttentionBuffers, 
     """csd_attention where the new tokens see each other by masks [rows, T] int64 (a TreePlan's): bit u of masks[b, t] lets token t see
     new token u; the places before the new ones are seen by all.  buf: AttentionBuffers(..., tree=True).  Serving form: no gradient."""
     return _attend("csd_attention_tree", q, cache, layer, buf, _nodes_arg(masks, cache, buf.T, torch.int64, "masks"), scale, n_new, stream)
+
+
+def csd_attention_mass(q, lse, cache: PagedCache, layer: int, mass, scale: float | None = None, n_new=None, masks=None, fresh: bool = False, stream=None):
+    """mass [rows, places] float32 += the attention weights that the new tokens q [rows, T, q_heads, D] give each place, summed over tokens
+    and heads; lse [rows, T, q_heads] is what csd_attention (masks None) or csd_attention_tree left in buf.lse for the same q, scale, n_new
+    and masks.  fresh: the new tokens' own places begin at 0 (the first layer of a pass).  Returns mass.  Serving form: no gradient."""
+    qs = q.stride()
+    assert q.dtype == cache.dtype and q.dim() == 4 and qs[3] == 1 and q.shape[0] == cache.rows and q.shape[3] == cache.head_dim
+    assert lse.dtype == torch.float32 and lse.shape == q.shape[:3] and lse.is_contiguous()
+    dev = cache._device
+    if not (q.get_device() == lse.get_device() == dev):
+        _scattered("csd_attention_mass", q.get_device(), lse.get_device(), dev)
+    T = q.shape[1]
+    _check(_lib().csd_attention_mass(q.data_ptr(), qs[0], qs[1], qs[2], T, q.shape[2], lse.data_ptr(), cache._ref, layer,
+                                     cache.head_dim ** -0.5 if scale is None else scale, None if n_new is None else _rows_arg(n_new, cache, "n_new"),
+                                     None if masks is None else _nodes_arg(masks, cache, T, torch.int64, "masks"), *_mass_arg(mass, cache),
+                                     1 if fresh else 0, _stream_ptr(stream, dev)), "csd_attention_mass")
+    return mass
 
 
 def _attend(what, q, cache, layer, buf, masks, scale, n_new, stream):
