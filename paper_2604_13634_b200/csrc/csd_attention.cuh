@@ -88,7 +88,7 @@ struct Params {
     Split *splits;                         // [min(units, gridDim.x)]
     float *parts;                          // [2 gridDim.x] slots of kRows * (DP + 2) floats
     // the tensor-memory kernel alone
-    int tile_rows;                         // query rows of a row tile: a multiple of 8, at most 128
+    int tile_rows;                         // query rows of a row tile: a multiple of 8, at most 128 (of a pair: 16, 256)
     int q_buffers;                         // sets of query rows: 2, or 1 where they would leave too few slots
     int halves, d16;                       // 64-element columns of a tile; dim rounded up to 16
     int part_stride;                       // floats between rows of a part
@@ -285,14 +285,17 @@ __device__ __forceinline__ int row_len(const Params &p, int b) { return min(max(
 __device__ __forceinline__ int row_news(const Params &p, int b) { return p.n_new ? max(ptx::ld_written(p.n_new + b), 0) : p.T; }
 
 // Trees: which new tokens token tok of row b sees, those that exist alone: bits of the places first + u in [0, len).
-__device__ __forceinline__ unsigned long long token_mask(const Params &p, int b, int tok, int len, int news)
+__device__ __forceinline__ unsigned long long existing(const int2 &m, int len, int news)
 {
-    const int2 m = ptx::ld_written(reinterpret_cast<const int2 *>(p.masks) + static_cast<long long>(b) * p.T + tok);
     unsigned long long bits = static_cast<unsigned long long>(static_cast<unsigned int>(m.y)) << 32 | static_cast<unsigned int>(m.x);
     const int before = news - len;                       // new tokens that have no place (a length below n_new)
     if (news < 64) bits &= (1ull << news) - 1ull;
     if (before > 0) bits = before < 64 ? bits >> before << before : 0ull;
     return bits;
+}
+__device__ __forceinline__ unsigned long long token_mask(const Params &p, int b, int tok, int len, int news)
+{
+    return existing(ptx::ld_written(reinterpret_cast<const int2 *>(p.masks) + static_cast<long long>(b) * p.T + tok), len, news);
 }
 // Whether a place is seen: every one before `first`, of the others those whose bit is set.
 __device__ __forceinline__ bool tree_sees(unsigned long long bits, int first, int key)
@@ -852,9 +855,14 @@ attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 // half of the time).
 // The reference of a row stays while no score exceeds it by more than kLag powers of two (weights up to 2^kLag, raised as above, are
 // harmless in float32 sums and in either cache type) and jumps to the tile's maximum when one does, so the accumulators in tensor memory are rescaled a few times per unit, not per tile.
+//
+// Pairs of row tiles (kGroups = 2), for more than 128 query rows to a key head: one block per SM with two groups of softmax warps, which share every
+// tile that is loaded; the issuing thread multiplies it with both groups' query rows in turn.  A unit's row tile is then the pair's, of up to
+// 256 rows, group g has its g-th half.
 constexpr int kTcTile = 64;
-constexpr int kTcThreads = 192;
 constexpr int kTcMaxSlots = 16;
+template <int kGroups>
+constexpr int kTcThreads = 128 * kGroups + 64;
 constexpr unsigned int kTcScoreCols = 64, kTcOutCol = 128;     // tensor memory: scores at 0 and 64 (weights over them), output from 128
 
 template <typename T>
@@ -886,6 +894,10 @@ __device__ __forceinline__ void tc_mma_ts(unsigned int d, unsigned int a, unsign
                  "r"(idesc), "r"(accumulate)
                  : "memory");
 }
+template <int N>
+struct Columns {
+    static constexpr int value = N;
+};
 // Order of the loads of a run of n tiles, and of the products: K0, K1, V0, K2, V1, ..., K(n-1), V(n-2), V(n-1).  The
 // number of V(k) among them:
 __device__ __forceinline__ int v_item(int k, int n) { return k == n - 1 ? 2 * n - 1 : 2 * k + 2; }
@@ -906,15 +918,18 @@ __device__ __forceinline__ void fetch_rows(const Params &p, const Run &ru, unsig
     }
 }
 
-template <typename T, int kBlocksPerSm, int kM, bool kTree>
-__global__ void __launch_bounds__(kTcThreads, kBlocksPerSm)
+template <typename T, int kBlocksPerSm, int kM, bool kTree, int kGroups>
+__global__ void __launch_bounds__(kTcThreads<kGroups>, kBlocksPerSm)
 attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p)
 {
     static_assert(kM == 64 || kM == 128, "rows of a product");
+    static_assert(kGroups == 1 || (kGroups == 2 && kBlocksPerSm == 1), "two groups take all of the tensor memory");
+    constexpr int kSoftmax = 128 * kGroups, kIssuer = 4 * kGroups, kLoader = kIssuer + 1;      // threads; warps
+    constexpr unsigned int kGroupCols = 256;                     // between the groups' tensor memory
     constexpr int kWarpRows = kM / 4;                            // query rows of a softmax warp, in its first lanes
     constexpr unsigned int kCols = kBlocksPerSm == 2 ? 256 : 512;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) unsigned long long bar_words[2 * kTcMaxSlots + 7];
+    __shared__ __align__(8) unsigned long long bar_words[2 * kTcMaxSlots + 6 * kGroups + 1];
     __shared__ unsigned int tmem_base_slot;
     __shared__ int give_up_flag, odd_run;
     volatile int *give_up = &give_up_flag;
@@ -928,12 +943,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const unsigned int bars = smem_u32(bar_words);
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (kTcMaxSlots + s); };
-    auto s_full = [&](int k) { return bars + 8u * (2 * kTcMaxSlots + (k & 1)); };
-    auto p_ready = [&](int k) { return bars + 8u * (2 * kTcMaxSlots + 2 + (k & 1)); };
+    auto s_full = [&](int g, int k) { return bars + 8u * (2 * kTcMaxSlots + 6 * g + (k & 1)); };
+    auto p_ready = [&](int g, int k) { return bars + 8u * (2 * kTcMaxSlots + 6 * g + 2 + (k & 1)); };
     // (two, taken in turn: a wait by parity is sound while the barrier is in the phase waited for or the one after it, and the scores
     // of tile k, whose product is issued after the output product of tile k - 2, say that the barrier's phase before is over)
-    auto pv_done = [&](int k) { return bars + 8u * (2 * kTcMaxSlots + 4 + (k & 1)); };
-    const unsigned int q_ready = bars + 8u * (2 * kTcMaxSlots + 6);
+    auto pv_done = [&](int g, int k) { return bars + 8u * (2 * kTcMaxSlots + 6 * g + 4 + (k & 1)); };
+    const unsigned int q_ready = bars + 8u * (2 * kTcMaxSlots + 6 * kGroups);
+    const int group_rows = p.tile_rows / kGroups;                // of a row tile
     auto slot_at = [&](int s) { return ring + s * slot_bytes; };
     auto q_at = [&](int run) { return q_smem + (p.q_buffers == 2 ? run & 1 : 0) * rows_bytes; };
 
@@ -944,12 +960,13 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
-        for (int k = 0; k < 2; ++k) {
-            mbar_init(s_full(k), 1);
-            mbar_init(p_ready(k), 4);
-            mbar_init(pv_done(k), 1);
-        }
-        mbar_init(q_ready, 4);
+        for (int g = 0; g < kGroups; ++g)
+            for (int k = 0; k < 2; ++k) {
+                mbar_init(s_full(g, k), 1);
+                mbar_init(p_ready(g, k), 4);
+                mbar_init(pv_done(g, k), 1);
+            }
+        mbar_init(q_ready, 4 * kGroups);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
@@ -960,7 +977,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     }
     ptx::wait_for_stream();
     if (tid == 0 && !p.by_unit) p.splits[blockIdx.x].parts = 0;
-    for (int b = tid; b < p.B; b += kTcThreads) {
+    for (int b = tid; b < p.B; b += kTcThreads<kGroups>) {
         const int len = row_len(p, b), news = row_news(p, b);
         base[b + 1] = news > 0 && len > 0 ? (len + kTcTile - 1) / kTcTile + p.run_cost : 0;
     }
@@ -972,7 +989,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const unsigned int tmem = tmem_base_slot;
     const Share share(p, base);
 
-    if (warp == 5) {
+    if (warp == kLoader) {
         // ---- page loads ----
         Runs runs;
         runs.begin(p, base, share.x0, share.x1);
@@ -1022,9 +1039,12 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         // every commit aimed at the slots' barriers has landed before the block ends
         if (lane == 0)
             for (int k = 0; k < p.n_stages && ok; ++k, at.next(p.n_stages)) ok = mbar_wait(empty(at.slot), at.round ^ 1u, give_up);
-    } else if (warp == 4) {
+    } else if (warp == kIssuer) {
         // ---- products ----
-        if (lane == 0) {
+        // (written out for each number of 64-element columns: a product whose operands come from loops and tests takes longer to issue than to run;
+        // elements beyond dim are zeros)
+        auto issue = [&](auto columns) {
+            constexpr int kColumns = decltype(columns)::value;
             Runs runs;
             runs.begin(p, base, share.x0, share.x1);
             Run r;
@@ -1042,48 +1062,63 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         const int k = mine + i;
                         if (!(ok = mbar_wait(full(at.slot), at.round, give_up))) break;
                         ptx::tc_fence_after();
-                        const unsigned int d = tmem + (k & 1) * kTcScoreCols;
-                        unsigned long long qd = q_desc, kd = ptx::operand_desc(slot_at(at.slot));
-                        for (int left = p.d16; left > 0; left -= 64, qd += half_q, kd += half_k) {
-                            tc_mma_ss(d, qd, kd, idesc_qk, left == p.d16 ? 0u : 1u);      // 16 elements further: 32 bytes
-                            if (left > 16) tc_mma_ss(d, qd + 2, kd + 2, idesc_qk, 1u);
-                            if (left > 32) tc_mma_ss(d, qd + 4, kd + 4, idesc_qk, 1u);
-                            if (left > 48) tc_mma_ss(d, qd + 6, kd + 6, idesc_qk, 1u);
+                        const unsigned long long k_desc = ptx::operand_desc(slot_at(at.slot));
+#pragma unroll
+                        for (int g = 0; g < kGroups; ++g) {
+                            const unsigned int d = tmem + g * kGroupCols + (k & 1) * kTcScoreCols;
+                            const unsigned long long qd = q_desc + static_cast<unsigned long long>(g * group_rows * 128 >> 4);
+#pragma unroll
+                            for (int c = 0; c < kColumns; ++c)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)                              // 16 elements further: 32 bytes
+                                    tc_mma_ss(d, qd + c * half_q + 2 * e, k_desc + c * half_k + 2 * e, idesc_qk, c == 0 && e == 0 ? 0u : 1u);
+                            if (g + 1 == kGroups) ptx::tc_commit(empty(at.slot));
+                            ptx::tc_commit(s_full(g, k));
                         }
-                        ptx::tc_commit(empty(at.slot));
-                        ptx::tc_commit(s_full(k));
                         at.next(p.n_stages);
                     }
                     if (i > 0) {
                         const int k = mine + i - 1;
-                        if (!(ok = mbar_wait(p_ready(k), (k >> 1) & 1, give_up))) break;
-                        if (!(ok = mbar_wait(full(at.slot), at.round, give_up))) break;
-                        ptx::tc_fence_after();
-                        const unsigned int d = tmem + kTcOutCol, w = tmem + (k & 1) * kTcScoreCols;
                         const unsigned long long vd = value_desc(slot_at(at.slot), kTcTile * 128);
-                        tc_mma_ts(d, w, vd, idesc_pv, i > 1 ? 1u : 0u);                  // 16 places further: 2 KiB
-                        tc_mma_ts(d, w + 8, vd + 128, idesc_pv, 1u);
-                        tc_mma_ts(d, w + 16, vd + 256, idesc_pv, 1u);
-                        tc_mma_ts(d, w + 24, vd + 384, idesc_pv, 1u);
-                        ptx::tc_commit(empty(at.slot));
-                        ptx::tc_commit(pv_done(k));
+#pragma unroll
+                        for (int g = 0; g < kGroups && ok; ++g) {                       // (the first group mends the values for both)
+                            if (!(ok = mbar_wait(p_ready(g, k), (k >> 1) & 1, give_up))) break;
+                            if (g == 0 && !(ok = mbar_wait(full(at.slot), at.round, give_up))) break;
+                            ptx::tc_fence_after();
+                            const unsigned int d = tmem + g * kGroupCols + kTcOutCol, w = tmem + g * kGroupCols + (k & 1) * kTcScoreCols;
+                            tc_mma_ts(d, w, vd, idesc_pv, i > 1 ? 1u : 0u);              // 16 places further: 2 KiB
+                            tc_mma_ts(d, w + 8, vd + 128, idesc_pv, 1u);
+                            tc_mma_ts(d, w + 16, vd + 256, idesc_pv, 1u);
+                            tc_mma_ts(d, w + 24, vd + 384, idesc_pv, 1u);
+                            if (g + 1 == kGroups) ptx::tc_commit(empty(at.slot));
+                            ptx::tc_commit(pv_done(g, k));
+                        }
+                        if (!ok) break;
                         at.next(p.n_stages);
                     }
                 }
                 mine += n;
             }
+        };
+        if (ptx::elect_one()) {
+            if constexpr (kGroups == 2 || kBlocksPerSm == 2) {
+                if (p.halves == 1) issue(Columns<1>()); else issue(Columns<2>());
+            } else {
+                if (p.halves == 3) issue(Columns<3>()); else issue(Columns<4>());
+            }
         }
     } else {
         // ---- softmax, rows in and out ----
-        const int warp_row = kWarpRows * warp, r = lane < kWarpRows ? warp_row + lane : kM;      // the thread's query row of the row tile
-        zero_empty_rows<T>(p, base, tid, 128);
+        const int grp = kGroups == 1 ? 0 : warp >> 2, quarter = kGroups == 1 ? warp : warp & 3;
+        const int warp_row = kWarpRows * quarter, r = lane < kWarpRows ? warp_row + lane : kM;   // the thread's query row of the group's
+        zero_empty_rows<T>(p, base, tid, kSoftmax);
         Runs runs;
         runs.begin(p, base, share.x0, share.x1);
         Run ru, next;
         bool more = runs.next(next);
-        const unsigned int my_lanes = static_cast<unsigned int>(32 * warp) << 16, my_out = tmem + my_lanes + kTcOutCol;
+        const unsigned int my_tmem = tmem + grp * kGroupCols + (static_cast<unsigned int>(32 * quarter) << 16), my_out = my_tmem + kTcOutCol;
         // query rows on their way; and: they are there, scores may be computed
-        auto fetch = [&](const Run &x, int run) { fetch_rows<T>(p, x, q_at(run), warp, 4, lane); };
+        auto fetch = [&](const Run &x, int run) { fetch_rows<T>(p, x, q_at(run), warp, 4 * kGroups, lane); };
         auto fetched = [&]() {
             asm volatile("cp.async.wait_all;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1101,9 +1136,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             more = runs.next(next);
             const int b = ru.b, h = ru.h, rt = ru.rt, j0 = ru.j0, ns = ru.ns;
             const int len = row_len(p, b), news = row_news(p, b);
-            const int rows_here = min(p.tile_rows, p.rows - rt * p.tile_rows);
+            const int rows_here = min(group_rows, p.rows - rt * p.tile_rows - grp * group_rows);
             ptx::tc_fence_before();
-            consumer_barrier(128);                                   // the accumulators and staged rows of the run before have been read
+            consumer_barrier(kSoftmax);                              // the accumulators and staged rows of the run before have been read
             ptx::tc_fence_after();
             if (!ahead) {
                 fetch(ru, run);
@@ -1111,7 +1146,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             } else if (more) {
                 fetch(next, run + 1);
             }
-            const int rr = rt * p.tile_rows + r, tok = rr / p.group;
+            const int rr = rt * p.tile_rows + grp * group_rows + r, tok = rr / p.group;
             const int first = len - news, shared = kTree ? first - 1 : first;      // first new token; last place that all rows see
             int limit = r < rows_here && tok < news ? first + tok : -1;            // the token's own place; -1: it sees nothing
             unsigned long long bits = 0ull;
@@ -1125,8 +1160,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             for (int i = 0; i < ns; ++i, ++mine) {
                 const int key0 = (j0 + i) * kTcTile;
                 const bool edge = key0 + kTcTile - 1 > shared;
-                const unsigned int s_at = tmem + my_lanes + (mine & 1) * kTcScoreCols;
-                mbar_wait(s_full(mine), (mine >> 1) & 1, give_up);
+                const unsigned int s_at = my_tmem + (mine & 1) * kTcScoreCols;
+                mbar_wait(s_full(grp, mine), (mine >> 1) & 1, give_up);
                 ptx::tc_fence_after();
                 float f = 1.f;                                   // on what has been accumulated
                 if (warp_has) {
@@ -1200,7 +1235,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 if (warp_has) {
                     if (__any_sync(kFull, f != 1.f)) {
                         // the product before has to be complete; the next one waits for these weights
-                        mbar_wait(pv_done(mine - 1), ((mine - 1) >> 1) & 1, give_up);
+                        mbar_wait(pv_done(grp, mine - 1), ((mine - 1) >> 1) & 1, give_up);
                         ptx::tc_fence_after();
                         for (int c0 = 0; c0 < p.d16; c0 += 32) {
                             float o[32];
@@ -1213,7 +1248,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     }
                     ptx::tmem_wait_st();
                 }
-                if (edge) {
+                if (edge && grp == 0) {
                     // A weight of zero does not silence an infinity or NaN in the values.  Places beyond the row hold anything:
                     // zeroed.  Such a value in a place of a later new token is left out here and handed to the rows that see it at the end.
                     // (The loads up to the tile's keys have been consumed: with four slots that includes this slot's load before.)
@@ -1241,27 +1276,28 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 }
                 ptx::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_ready(mine));
+                if (lane == 0) mbar_arrive(p_ready(grp, mine));
             }
             if (ahead && more) fetched();
 
             // ---- the run's rows ----
-            if (ns > 1) mbar_wait(pv_done(mine - 2), ((mine - 2) >> 1) & 1, give_up);
-            mbar_wait(pv_done(mine - 1), ((mine - 1) >> 1) & 1, give_up);
+            if (ns > 1) mbar_wait(pv_done(grp, mine - 2), ((mine - 2) >> 1) & 1, give_up);
+            mbar_wait(pv_done(grp, mine - 1), ((mine - 1) >> 1) & 1, give_up);
             ptx::tc_fence_after();
-            consumer_barrier(128);                                   // odd_run of all four warps
+            consumer_barrier(kSoftmax);                              // odd_run of all warps; every product has read the query rows
             const bool odd = *static_cast<volatile int *>(&odd_run) == run + 1;
             const bool whole = ns == ru.n;
             const bool seen = limit >= 0 && l != 0.f;                // (NaN counts as seen)
             const int head = h * p.group + rr - tok * p.group;
             const long long row = (static_cast<long long>(b) * p.T + tok) * p.Hq + head;
-            float *part = p.parts + static_cast<long long>(2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0)) * p.tile_rows * (p.part_stride + 2);
+            float *unit_part = p.parts + static_cast<long long>(2 * static_cast<int>(blockIdx.x) + (j0 == 0 ? 1 : 0)) * p.tile_rows * (p.part_stride + 2);
+            float *part = unit_part + static_cast<long long>(grp * group_rows) * p.part_stride;
             if (warp_has) {
                 // A thread has a row, memory wants rows side by side: each warp turns its 32 rows round in shared memory, where the
                 // run's query rows were, which every product has read.
                 const float inv = seen ? (whole ? 1.f / l : 1.f) : 0.f;
                 const int pitch = p.halves * 128, warp_rows = min(kWarpRows, rows_here - warp_row);
-                const unsigned int out_smem = q_at(run), my_row = out_smem + r * pitch;
+                const unsigned int out_smem = q_at(run) + grp * group_rows * pitch, my_row = out_smem + r * pitch;
                 const int cols = whole ? p.halves * 64 : p.halves * 32;                        // of a pass: what a staged row holds
                 const int lanes_row = p.halves * 8, at_once = 32 / lanes_row, sub = lane / lanes_row, ch = lane - sub * lanes_row;
                 for (int pass0 = 0; pass0 < p.D; pass0 += cols) {
@@ -1321,7 +1357,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 }
                 if (r < rows_here) {
                     if (!whole)
-                        __stcg(reinterpret_cast<float2 *>(part + static_cast<long long>(p.tile_rows) * p.part_stride + 2 * r), make_float2(seen ? m : -INFINITY, seen ? l : 0.f));
+                        __stcg(reinterpret_cast<float2 *>(unit_part + static_cast<long long>(p.tile_rows) * p.part_stride + 2 * (grp * group_rows + r)),
+                               make_float2(seen ? m : -INFINITY, seen ? l : 0.f));
                     else if (p.lse)
                         p.lse[row] = seen ? (m + log2f(l)) * kLn2 : -INFINITY;
                 }

@@ -286,7 +286,7 @@ keep::Pool pool_of(const csd_cache_t *c)
 // ---- attention ----------------------------------------------------------------------------------
 
 constexpr int kMaxDevices = 64;
-constexpr int kMassStatic = 4096;                    // the mass kernel's own
+constexpr int kMassStatic = 6144;                    // the mass kernel's own
 constexpr int kSmemPerSm = 228 * 1024, kSmemReserved = 1024, kSmemStatic = 1024;     // per block: the system's, and the kernel's own
 
 struct AttentionPlan {
@@ -344,20 +344,27 @@ int tc_blocks(int dim) { return dim <= 128 ? 2 : 1; }
 // cool 163 and 147), where twice the warps' work counts; in pages of 16 the loads hide the difference (169 and 170 with 32).
 bool tc_products_of_64(int tile_rows, int dim) { return tile_rows <= (dim <= 64 ? 32 : 64); }
 
-AttentionPlan attention_tc_plan(int rows, int dim, int B)
+// Pairs of row tiles that share their loads: trees whose query rows make an even number of tiles, while two accumulators fit in the tensor
+// memory.  One block per SM with both against two with one each, 32 rows of 4096 in pages of 64, dim 128: 168 us and 202 with 200 query rows,
+// 320 and 373 with 512; with 260 the pairs multiply four tiles where three would do, 298 and 277; dim 64: 271 and 244.
+bool tc_pairs(bool tree, int rows, int dim) { return tree && (rows + 127) / 128 % 2 == 0 && dim > 64 && dim <= 128; }
+
+AttentionPlan attention_tc_plan(bool tree, int rows, int dim, int B)
 {
     AttentionPlan a;
+    const bool pairs = tc_pairs(tree, rows, dim);
+    const int blocks = pairs ? 1 : tc_blocks(dim), unit = pairs ? 16 : 8;
     a.rows = rows;
     a.dp = dim <= 64 ? 64 : (dim <= 128 ? 128 : 256);
-    a.grid = attention_grid(tc_blocks(dim));
+    a.grid = attention_grid(blocks);
     a.run_cost = a.dp == 64 ? 8 : (a.dp == 128 ? 4 : 2);      // about 5 us: 240 us at 2, 228 at 4, 231 at 6 for 1024 units of 8 to 63 tiles
     const int halves = (dim + 63) / 64, slot = halves * attention::kTcTile * 128;
-    const int limit = kSmemPerSm / tc_blocks(dim) - kSmemReserved - kSmemStatic;
+    const int limit = kSmemPerSm / blocks - kSmemReserved - kSmemStatic;
     // The kernel's waits want four slots at least: two sets of query rows give way to one for them, and where tables of thousands
     // of rows leave little, a row tile holds fewer query rows.
-    for (int most = 128;; most /= 2) {
+    for (int most = pairs ? 256 : 128;; most /= 2) {
         a.row_tiles = (rows + most - 1) / most;
-        a.tile_rows = ((rows + a.row_tiles - 1) / a.row_tiles + 7) / 8 * 8;
+        a.tile_rows = ((rows + a.row_tiles - 1) / a.row_tiles + unit - 1) / unit * unit;
         a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
         for (a.q_buffers = 2; a.q_buffers >= 1; --a.q_buffers) {
             const int fixed = 1024 + a.q_buffers * halves * a.tile_rows * 128 + (B + 1) * 4;
@@ -374,9 +381,9 @@ AttentionPlan attention_tc_plan(int rows, int dim, int B)
     return a;
 }
 
-AttentionPlan attention_plan_of(int T, int group, int dim, int B)
+AttentionPlan attention_plan_of(bool tree, int T, int group, int dim, int B)
 {
-    if (attention_uses_tc(T * group)) return attention_tc_plan(T * group, dim, B);
+    if (attention_uses_tc(T * group)) return attention_tc_plan(tree, T * group, dim, B);
     return with_config<__nv_bfloat16>(dim, [&](auto cfg) { return attention_plan<decltype(cfg)>(T * group, B); });
 }
 
@@ -467,11 +474,11 @@ csd_status_t run_attention(attention::Params p, const csd_cache_t *cache, int la
     return rc != CSD_OK ? rc : launch_join<typename C::T, C::DP>(p, a, st);
 }
 
-template <typename T, int kBlocks, int kM, bool kTree>
+template <typename T, int kBlocks, int kM, bool kTree, int kGroups>
 csd_status_t run_attention_tc(attention::Params p, const AttentionPlan &a, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
 {
     static std::atomic<bool> ready[kMaxDevices];
-    if (!kernel_ready(attention::attention_tc_kernel<T, kBlocks, kM, kTree>, ready, kSmemPerSm / kBlocks - kSmemReserved - kSmemStatic, 1, 0)) return CSD_ERR_CUDA;
+    if (!kernel_ready(attention::attention_tc_kernel<T, kBlocks, kM, kTree, kGroups>, ready, kSmemPerSm / kBlocks - kSmemReserved - kSmemStatic, 1, 0)) return CSD_ERR_CUDA;
     fill_plan(p, a, ws);
     p.tile_rows = a.tile_rows;
     p.q_buffers = a.q_buffers;
@@ -486,7 +493,7 @@ csd_status_t run_attention_tc(attention::Params p, const AttentionPlan &a, const
     p.pool_token = cache->stride_token;
     CUtensorMap map_k, map_v;
     if (!make_pool_map(&map_k, cache, cache->k, layer, p.box_rows) || !make_pool_map(&map_v, cache, cache->v, layer, p.box_rows)) return CSD_ERR_CUDA;
-    const csd_status_t rc = launch(attention::attention_tc_kernel<T, kBlocks, kM, kTree>, dim3(static_cast<unsigned int>(a.grid)), attention::kTcThreads,
+    const csd_status_t rc = launch(attention::attention_tc_kernel<T, kBlocks, kM, kTree, kGroups>, dim3(static_cast<unsigned int>(a.grid)), attention::kTcThreads<kGroups>,
                                    static_cast<size_t>(a.smem), st, map_k, map_v, p);
     if (rc != CSD_OK) return rc;
     if (a.dp == 64) return launch_join<T, 64>(p, a, st);
@@ -494,18 +501,57 @@ csd_status_t run_attention_tc(attention::Params p, const AttentionPlan &a, const
     return launch_join<T, 256>(p, a, st);
 }
 
-// Blocks that share the key heads of a run of places.  More of them finish a short row sooner; fewer meet less often.
+// Blocks that share the key heads of a run of places.  More of them finish a few short rows sooner, fewer meet less often: with 1, 2, 4 and 8
+// one row of 700 tokens takes 16.0, 12.5, 10.2 and 9.0 us, one of 131071 54.1, 54.3, 54.8 and 59.6, 32 rows of 500 to 4000 with nine
+// tokens 44.5, 42.2, 43.2 and 42.8, with 33 tokens 108, 77, 73 and 73, 96 rows with nine 82.6, 88.1, 95.7 and 110.
 unsigned int mass_blocks(int rows, int heads)
 {
-    unsigned int blocks = rows <= 4 ? 8u : (rows <= 16 ? 4u : (rows <= 48 ? 2u : 1u));
+    unsigned int blocks = rows <= 4 ? 4u : (rows <= 48 ? 2u : 1u);
     while (blocks > static_cast<unsigned int>(heads)) blocks /= 2;
     return blocks;
+}
+
+// Clusters of 1, 2, 4 or 8 blocks that the GPU holds at a time, asked once per device: fewer than its blocks make, since a cluster stays
+// within a part of the GPU, and clusters too many would run alone at the end (80 us against 60 for one row of 131071 tokens).
+template <typename K>
+int resident_clusters(K kernel, int threads, int smem, int blocks_per_sm, unsigned int blocks, std::atomic<int> (&known)[kMaxDevices][4])
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    std::atomic<int> &mine = known[dev][blocks == 1 ? 0 : (blocks == 2 ? 1 : (blocks == 4 ? 2 : 3))];
+    int n = mine.load();
+    if (n > 0) return n;
+    cudaLaunchConfig_t cfg;
+    std::memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(blocks * 1024u);
+    cfg.blockDim = dim3(static_cast<unsigned int>(threads));
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = blocks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    // (the driver counts one block per SM for kernels that allocate tensor memory, whatever they take of it)
+    int counted = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&counted, kernel, threads, static_cast<size_t>(smem)) != cudaSuccess || counted <= 0) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    n = n / counted * blocks_per_sm;
+    mine.store(n);
+    return n;
 }
 
 template <typename T>
 csd_status_t run_mass(mass::Params p, const csd_cache_t *cache, int layer, cudaStream_t st)
 {
     static std::atomic<bool> ready[kMaxDevices];
+    static std::atomic<int> fitting[kMaxDevices][4];
     constexpr int limit = kSmemPerSm / mass::kBlocksPerSm - kSmemReserved - kMassStatic;
     if (!kernel_ready(mass::mass_kernel<T>, ready, limit, 1, 0)) return CSD_ERR_CUDA;
     attention::Params &a = p.a;
@@ -513,28 +559,33 @@ csd_status_t run_mass(mass::Params p, const csd_cache_t *cache, int layer, cudaS
     a.d16 = (a.D + 15) / 16 * 16;
     a.box_rows = cache->page_size < mass::kTile ? cache->page_size : mass::kTile;
     // Query rows: as many as 32 KiB hold, in two sets where both fit there; the rest of the shared memory is for the ring of keys.
-    const int most = 32768 / (a.halves * 128) / 16 * 16, all = (a.T * a.group + 15) / 16 * 16;
-    p.q_rows = all < most ? all : most;
-    if (p.q_rows > mass::kMostRows) p.q_rows = mass::kMostRows;
-    a.q_buffers = 2 * p.q_rows <= most ? 2 : 1;
+    const int fits = 32768 / (a.halves * 128) / 16 * 16, most = fits < mass::kMostRows ? fits : mass::kMostRows;
+    const int rows = a.T * a.group, passes = (rows + most - 1) / most;
+    p.q_rows = ((rows + passes - 1) / passes + 15) / 16 * 16;
+    a.q_buffers = 2 * p.q_rows <= fits ? 2 : 1;
     const int fixed = 1024 + a.q_buffers * a.halves * p.q_rows * 128 + mass::kRunTiles * mass::kTile * 4 + (a.B + 1) * 4;
     a.n_stages = (limit - fixed) / mass::kSlotBytes;
     if (a.n_stages > mass::kMaxSlots) a.n_stages = mass::kMaxSlots;
     if (a.n_stages < 2) return CSD_ERR_UNSUPPORTED;
     CUtensorMap map_k;
     if (!make_pool_map(&map_k, cache, cache->k, layer, a.box_rows)) return CSD_ERR_CUDA;
-    const unsigned int blocks = mass_blocks(a.B, a.Hkv), grid = static_cast<unsigned int>(host::multiprocessors()) * mass::kBlocksPerSm / blocks * blocks;
-    return launch_clusters(mass::mass_kernel<T>, dim3(grid), mass::kThreads, static_cast<size_t>(fixed + a.n_stages * mass::kSlotBytes), st, blocks, map_k, p);
+    const unsigned int blocks = mass_blocks(a.B, a.Hkv);
+    const int clusters = resident_clusters(mass::mass_kernel<T>, mass::kThreads, limit, mass::kBlocksPerSm, blocks, fitting);
+    if (clusters <= 0) return CSD_ERR_CUDA;
+    return launch_clusters(mass::mass_kernel<T>, dim3(static_cast<unsigned int>(clusters) * blocks), mass::kThreads,
+                           static_cast<size_t>(fixed + a.n_stages * mass::kSlotBytes), st, blocks, map_k, p);
 }
 
 template <typename T, bool kTree>
 csd_status_t run_attention_any(const attention::Params &p, const csd_cache_t *cache, int layer, char *ws, cudaStream_t st)
 {
     if (attention_uses_tc(p.T * p.group)) {
-        const AttentionPlan a = attention_tc_plan(p.T * p.group, p.D, p.B);
+        const AttentionPlan a = attention_tc_plan(kTree, p.T * p.group, p.D, p.B);
+        if constexpr (kTree)
+            if (tc_pairs(true, p.T * p.group, p.D)) return run_attention_tc<T, 1, 128, true, 2>(p, a, cache, layer, ws, st);
         if (tc_products_of_64(a.tile_rows, p.D))
-            return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 64, kTree>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 64, kTree>(p, a, cache, layer, ws, st);
-        return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 128, kTree>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 128, kTree>(p, a, cache, layer, ws, st);
+            return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 64, kTree, 1>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 64, kTree, 1>(p, a, cache, layer, ws, st);
+        return tc_blocks(p.D) == 2 ? run_attention_tc<T, 2, 128, kTree, 1>(p, a, cache, layer, ws, st) : run_attention_tc<T, 1, 128, kTree, 1>(p, a, cache, layer, ws, st);
     }
     return with_config<T>(p.D, [&](auto cfg) { return run_attention<decltype(cfg), kTree>(p, cache, layer, ws, st); });
 }
@@ -803,13 +854,13 @@ csd_status_t csd_cache_compact(const csd_cache_t *cache, void *stream)
 size_t csd_attention_workspace_bytes(int rows, int T, int q_heads, int heads, int dim)
 {
     if (!attention_shape_ok(rows, T, CSD_MAX_K + 1, q_heads, heads, dim)) return 0;
-    return attention_plan_of(T, q_heads / heads, dim, rows).total;
+    return attention_plan_of(false, T, q_heads / heads, dim, rows).total;
 }
 
 size_t csd_attention_tree_workspace_bytes(int rows, int T, int q_heads, int heads, int dim)
 {
     if (!attention_shape_ok(rows, T, CSD_TREE_MAX_NODES, q_heads, heads, dim)) return 0;
-    return attention_plan_of(T, q_heads / heads, dim, rows).total;
+    return attention_plan_of(true, T, q_heads / heads, dim, rows).total;
 }
 
 // masks NULL: a chain.
@@ -821,7 +872,7 @@ static csd_status_t attend(const void *q, int64_t q_stride_b, int64_t q_stride_t
     if (ok != CSD_OK) return ok;
     if (!q || !out || !workspace || T <= 0 || q_heads <= 0 || layer < 0 || layer >= cache->layers || !std::isfinite(scale)) return CSD_ERR_INVALID_ARG;
     if (!attention_shape_ok(cache->rows, T, most, q_heads, cache->heads, cache->dim)) return CSD_ERR_UNSUPPORTED;
-    const AttentionPlan plan = attention_plan_of(T, q_heads / cache->heads, cache->dim, cache->rows);
+    const AttentionPlan plan = attention_plan_of(masks != nullptr, T, q_heads / cache->heads, cache->dim, cache->rows);
     // positions are counted in 31 bits: tiles of 64 places at least, and what a unit costs beside its tiles
     const double row_positions = (static_cast<double>(cache->max_pages) * cache->page_size + 63) / 64 + plan.run_cost;
     if (row_positions * cache->rows * cache->heads * plan.row_tiles >= 2147483648.0) return CSD_ERR_UNSUPPORTED;

@@ -101,7 +101,7 @@ mass_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ P
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long bar_words[2 * kMaxSlots + 5];
     __shared__ __align__(16) float less[2][kMostRows];                   // -lse log2(e) of a pass's query rows; -inf: the row adds nothing
-    __shared__ unsigned long long sees[2][kMostRows];                    // and the new tokens that it sees
+    __shared__ __align__(16) uint4 sees[2][kMostRows];                   // who sees it: new tokens' places 0 .. 31 and 32 .. 63, places before them, none
     __shared__ unsigned int tmem_base_slot;
     __shared__ int give_up_flag;
     volatile int *give_up = &give_up_flag;
@@ -195,34 +195,47 @@ mass_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ P
             for (int k = 0; k < a.n_stages && ok; ++k, at.next(a.n_stages)) ok = mbar_wait(empty(at.slot), at.round ^ 1u, give_up);
     } else if (warp == 4) {
         // ---- products ----
+        // (written out for each number of 64-element columns; elements beyond dim are zeros)
         Cursor at = {0, 0u};
         int k = 0, pass = 0;
         bool ok = true;
+        auto issue = [&](auto columns, int rows) {
+            constexpr int kColumns = decltype(columns)::value;
+            for (int h = static_cast<int>(rank); h < a.Hkv && ok; h += static_cast<int>(blocks))
+                for (int r0 = 0; r0 < rows && ok; r0 += p.q_rows, ++pass) {
+                    const unsigned int idesc = attention::tc_instr<T>(kTile, (min(p.q_rows, rows - r0) + 15) / 16 * 16, false);
+                    ok = mbar_wait(q_ready, pass & 1, give_up);
+                    for (int i = 0; i < n && ok; ++i, ++k) {
+                        if (!(ok = mbar_wait(s_empty(k), ((k >> 1) & 1) ^ 1, give_up))) break;
+                        const unsigned int d = tmem + (k & 1) * kMostRows;
+                        const unsigned long long q_desc = ptx::operand_desc(q_at(pass)), q_column = static_cast<unsigned long long>(p.q_rows * 128 >> 4);
+#pragma unroll
+                        for (int c = 0; c < kColumns; ++c) {
+                            if (!ok || !(ok = mbar_wait(full(at.slot), at.round, give_up))) break;
+                            ptx::tc_fence_after();
+                            const unsigned long long kd = ptx::operand_desc(ring + at.slot * kSlotBytes), qd = q_desc + c * q_column;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)                             // 16 elements further: 32 bytes
+                                attention::tc_mma_ss(d, kd + 2 * e, qd + 2 * e, idesc, c == 0 && e == 0 ? 0u : 1u);
+                            ptx::tc_commit(empty(at.slot));
+                            at.next(a.n_stages);
+                        }
+                        if (ok) ptx::tc_commit(s_full(k));
+                    }
+                }
+        };
+        const bool issuer = ptx::elect_one();
         while (tiles.next(b, j0, n)) {
             const int rows = min(a.T, attention::row_news(a, b)) * a.group;
-            if (lane == 0) {
-                for (int h = static_cast<int>(rank); h < a.Hkv && ok; h += static_cast<int>(blocks))
-                    for (int r0 = 0; r0 < rows && ok; r0 += p.q_rows, ++pass) {
-                        const unsigned int idesc = attention::tc_instr<T>(kTile, (min(p.q_rows, rows - r0) + 15) / 16 * 16, false);
-                        ok = mbar_wait(q_ready, pass & 1, give_up);
-                        for (int i = 0; i < n && ok; ++i, ++k) {
-                            if (!(ok = mbar_wait(s_empty(k), ((k >> 1) & 1) ^ 1, give_up))) break;
-                            const unsigned int d = tmem + (k & 1) * kMostRows;
-                            unsigned long long qd = ptx::operand_desc(q_at(pass));
-                            for (int left = a.d16; left > 0 && ok; left -= 64, qd += static_cast<unsigned long long>(p.q_rows * 128 >> 4)) {
-                                if (!(ok = mbar_wait(full(at.slot), at.round, give_up))) break;
-                                ptx::tc_fence_after();
-                                const unsigned long long kd = ptx::operand_desc(ring + at.slot * kSlotBytes);
-                                attention::tc_mma_ss(d, kd, qd, idesc, left == a.d16 ? 0u : 1u);      // 16 elements further: 32 bytes
-                                if (left > 16) attention::tc_mma_ss(d, kd + 2, qd + 2, idesc, 1u);
-                                if (left > 32) attention::tc_mma_ss(d, kd + 4, qd + 4, idesc, 1u);
-                                if (left > 48) attention::tc_mma_ss(d, kd + 6, qd + 6, idesc, 1u);
-                                ptx::tc_commit(empty(at.slot));
-                                at.next(a.n_stages);
-                            }
-                            if (ok) ptx::tc_commit(s_full(k));
-                        }
-                    }
+            if (issuer) {
+                if (a.halves == 1)
+                    issue(attention::Columns<1>(), rows);
+                else if (a.halves == 2)
+                    issue(attention::Columns<2>(), rows);
+                else if (a.halves == 3)
+                    issue(attention::Columns<3>(), rows);
+                else
+                    issue(attention::Columns<4>(), rows);
             }
             if (blocks > 1) {
                 cluster_meet();
@@ -255,16 +268,21 @@ mass_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ P
             __syncwarp();
             if (lane == 0) mbar_arrive(q_ready);
         };
-        auto column = [&](const Pass &x, float &minus, unsigned long long &bits) {       // what thread r knows of query row r of the pass
-            minus = -INFINITY;
-            bits = 0ull;
-            if (tid >= here_of(x)) return;
+        // thread r looks after query row r of a pass.  Loaded a pass ahead and not looked at before its turn, so that nothing waits here.
+        struct Column {
+            int tok, lse;                                                // tok -1: no row, or a token without a place
+            int2 mask;
+        };
+        auto column = [&](const Pass &x) {
+            Column c = {-1, 0, make_int2(0, 0)};
+            if (tid >= here_of(x)) return c;
             const int rr = x.r0 + tid, tok = rr / a.group, head = x.h * a.group + rr - tok * a.group;
-            if (x.len - x.news + tok < 0) return;                         // a token without a place
-            const float lse = __int_as_float(ptx::ld_written(reinterpret_cast<const int *>(p.lse) + (static_cast<long long>(x.b) * a.T + tok) * a.Hq + head));
-            if (lse == -INFINITY) return;
-            minus = -lse * kLog2e;
-            bits = a.masks ? attention::token_mask(a, x.b, tok, x.len, x.news) : (tok < 63 ? (2ull << tok) - 1ull : ~0ull);
+            if (x.len - x.news + tok < 0) return c;
+            const long long at = static_cast<long long>(x.b) * a.T + tok;
+            c.tok = tok;
+            c.lse = ptx::ld_written(reinterpret_cast<const int *>(p.lse) + at * a.Hq + head);
+            if (a.masks) c.mask = ptx::ld_written(reinterpret_cast<const int2 *>(a.masks) + at);
+            return c;
         };
         // the passes in order, a pass ahead of the work
         Tiles ahead = tiles;
@@ -288,11 +306,10 @@ mass_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ P
             coming.rows = min(a.T, coming.news) * a.group;
         };
         const bool two = a.q_buffers == 2;
-        float minus = 0.f;
-        unsigned long long bits = 0ull;
+        Column mine = {-1, 0, make_int2(0, 0)};
         advance();
         if (more) {
-            column(coming, minus, bits);
+            mine = column(coming);
             if (two) {
                 fetch(coming, 0);
                 fetched();
@@ -310,15 +327,18 @@ mass_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ P
                         fetch(now, pass);
                         fetched();
                     }
+                    const float lse = __int_as_float(mine.lse);
+                    const float minus = mine.tok < 0 || lse == -INFINITY ? -INFINITY : -lse * kLog2e;
                     less[buf][tid] = minus;
-                    sees[buf][tid] = bits;
+                    const bool dead = minus == -INFINITY;
+                    const unsigned long long bits = a.masks ? attention::existing(mine.mask, now.len, now.news) : (mine.tok < 63 ? (2ull << max(mine.tok, 0)) - 1ull : ~0ull);
+                    sees[buf][tid] = dead ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(static_cast<unsigned int>(bits), static_cast<unsigned int>(bits >> 32), ~0u, 0u);
                     // (two sets: a warp may be a pass ahead of another, never two, for every pass has this barrier)
-                    const bool dead = (tid < here && minus == -INFINITY);
                     int any_dead;
-                    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(any_dead) : "r"(dead ? 1 : 0) : "memory");
+                    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(any_dead) : "r"(dead && tid < here ? 1 : 0) : "memory");
                     advance();
                     if (more) {
-                        column(coming, minus, bits);
+                        mine = column(coming);
                         if (two) fetch(coming, pass + 1);
                     }
                     for (int i = 0; i < n; ++i, ++k) {
@@ -348,24 +368,33 @@ mass_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ P
                             unpack2(add2(sum0, sum1), s0, s1);
                             sum = s0 + s1;
                         }
-                        for (; c < here; c += 16) {
+                        // rows that do not exist or add nothing, and places that a row does not see: whatever was computed for them is left out
+                        const int u = key - first;
+                        const unsigned int *const word = reinterpret_cast<const unsigned int *>(&sees[buf][0]) + (u < 0 ? 2 : min(u >> 5, 2) + (u >= 64 ? 1 : 0));
+                        auto picked = [&](int c1, const auto &x, auto width) {
+#pragma unroll
+                            for (int e = 0; e < decltype(width)::value; ++e) {
+                                const float w = ex2_approx(__fmaf_rn(x[e], a.scale_log2, less[buf][c1 + e]));
+                                sum += word[4 * (c1 + e)] >> (u & 31) & 1u ? w : 0.f;
+                            }
+                        };
+                        for (; c + 16 < here; c += 32) {
+                            float x[32];
+                            ptx::tmem_ld32(at + c, x);
+                            picked(c, x, attention::Columns<32>());
+                        }
+                        if (c < here) {
                             float x[16];
                             ptx::tmem_ld16(at + c, x);
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                if (c + e < here) {
-                                    const float l1 = less[buf][c + e], w = ex2_approx(__fmaf_rn(x[e], a.scale_log2, l1));
-                                    if (!careful || (l1 != -INFINITY && attention::tree_sees(sees[buf][c + e], first, key))) sum += w;
-                                }
-                            }
+                            picked(c, x, attention::Columns<16>());
                         }
                         ptx::tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(s_empty(k));
                         float *const to = acc + i * kTile + tid;
                         *to = h == static_cast<int>(rank) && r0 == 0 ? sum : *to + sum;
+                        if (i == 0 && two && more) fetched();             // the products may run on into the next pass
                     }
-                    if (two && more) fetched();
                 }
             // ---- the run's places ----
             float *const mass = p.mass + b * p.mass_stride;

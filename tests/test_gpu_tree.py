@@ -173,7 +173,7 @@ def test_tree_attention(dtype, lens, T, Hq, Hkv, dim, page):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("T,Hq,dim", [(8, 2, 64), (20, 4, 128), (64, 6, 128), (33, 1, 256)])
+@pytest.mark.parametrize("T,Hq,dim", [(8, 2, 64), (20, 4, 128), (64, 6, 128), (33, 1, 256), (64, 8, 128), (40, 4, 96)])
 def test_any_masks(dtype, T, Hq, dim):
     """Bits at random, none at all, all, bits of tokens that do not exist; rows shorter than their new tokens, rows of new tokens alone."""
     rng = np.random.default_rng(T)
@@ -191,7 +191,7 @@ def test_any_masks(dtype, T, Hq, dim):
         check_row(buf.out[b], buf.lse[b], q[b], k, v, masks[b], news[b], 0.3, dtype)
 
 
-@pytest.mark.parametrize("T,Hq", [(8, 2), (40, 3)])
+@pytest.mark.parametrize("T,Hq", [(8, 2), (40, 3), (64, 4)])
 def test_what_a_node_does_not_see_does_not_reach_it(T, Hq):
     """Infinities and NaN in the keys and values of one branch: the other branch keeps its bits, the nodes below get them."""
     cache, table = filled(T, [T + 150, T], 16, 1, 128, torch.bfloat16)
