@@ -268,6 +268,11 @@ csd_status_t copy_pages(const csd_cache_t *c, const pages::View &v, long long mo
 
 size_t evict_pairs_off(int rows) { return align_up(static_cast<size_t>(rows) * sizeof(keep::RowPlan), 256); }
 
+size_t evict_offsets_off(int rows, int width)
+{
+    return evict_pairs_off(rows) + align_up(static_cast<size_t>(rows) * (width > 0 ? width : 1) * sizeof(int2), 256);
+}
+
 // Blocks that share the choice among a row's places: one while a thread has at most 16 of them, else eight.
 unsigned int evict_blocks(long long places) { return places <= 16 * keep::kPickThreads ? 1u : keep::kMostBlocks; }
 
@@ -788,7 +793,7 @@ csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *acce
 size_t csd_cache_evict_workspace_bytes(int rows, int width)
 {
     if (rows <= 0 || rows > CSD_CACHE_MAX_ROWS || width < 0 || width > (1 << 30)) return 0;
-    return evict_pairs_off(rows) + static_cast<size_t>(rows) * (width > 0 ? width : 1) * sizeof(int2);
+    return evict_offsets_off(rows, width) + static_cast<size_t>(rows) * (width > 0 ? width : 1) * sizeof(longlong2);
 }
 
 csd_status_t csd_cache_evict(const csd_cache_t *cache, float *mass, int64_t mass_stride, int keep, const int32_t *keep_rows, int sinks, int recent,
@@ -818,12 +823,15 @@ csd_status_t csd_cache_evict(const csd_cache_t *cache, float *mass, int64_t mass
     p.evicted = evicted;
     p.plans = static_cast<keep::RowPlan *>(workspace);
     p.pairs = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + evict_pairs_off(cache->rows));
+    p.offsets = reinterpret_cast<longlong2 *>(static_cast<char *>(workspace) + evict_offsets_off(cache->rows, width));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     csd_status_t rc = launch_clusters(keep::evict_pick_kernel, dim3(static_cast<unsigned int>(cache->rows) * evict_blocks(places)), keep::kPickThreads, 0, st, evict_blocks(places), p);
     if (rc != CSD_OK) return rc;
-    const long long units = 2ll * cache->layers * cache->heads + 1, most = 8ll * host::multiprocessors();
-    const long long blocks = units * cache->rows < most ? units * cache->rows : most;
-    rc = launch(keep::evict_move_kernel, dim3(static_cast<unsigned int>(blocks)), keep::kMoveThreads, 0, st, p);
+    const long long units = (2ll * cache->layers * cache->heads + 1) * cache->rows;
+    const bool warps = units >= 20ll * host::multiprocessors();
+    const long long most = static_cast<long long>(host::multiprocessors()) * (warps ? keep::kMoveBlocks<32> : keep::kMoveBlocks<keep::kMoveThreads>);
+    const dim3 blocks(static_cast<unsigned int>(units < most ? units : most));
+    rc = launch(warps ? keep::evict_move_kernel<32> : keep::evict_move_kernel<keep::kMoveThreads>, blocks, keep::kMoveThreads, 0, st, p);
     return rc != CSD_OK ? rc : launch(keep::evict_finish_kernel, dim3(static_cast<unsigned int>(cache->rows)), pages::kRowThreads, 0, st, p);
 }
 

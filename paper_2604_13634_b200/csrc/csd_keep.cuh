@@ -146,10 +146,11 @@ __global__ void __launch_bounds__(pages::kRowThreads) path_commit_kernel(const P
 // in ascending order.  So as many tokens move as the row loses at most, and R.
 
 constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32, kBins = 2048, kMostBlocks = 8;
+constexpr int kKeys = 6144;                // keys that a block keeps in shared memory; a larger share is read again
 
 struct RowPlan {
-    int front;                             // movers; pairs[0 .. front)
-    int from, to, recent;                  // the last `recent` tokens go from place `from` to place `to`
+    int early, front;                      // pairs [0, early): movers from places below `keep`; [early, front): the others; then the recent tokens
+    int from, to, recent;                  // which go from place `from` to place `to`
     int len, keep;                         // tokens before and after (equal: nothing happens)
 };
 
@@ -159,10 +160,11 @@ struct EvictParams {
     float *mass;
     long long mass_stride;
     const int *keep_rows;                  // null: `keep` for every row
-    int keep, sinks, recent, width;        // width: columns of kept and of pairs
+    int keep, sinks, recent, width;        // width: columns of kept, pairs and offsets
     int *kept, *evicted;
     RowPlan *plans;                        // [rows]
-    int2 *pairs;                           // [rows, width] mover, hole
+    int2 *pairs;                           // [rows, width] mover, hole: places
+    longlong2 *offsets;                    // [rows, width] where from and where to within a layer's pool, in bytes; -1: no such page
 };
 
 // Masses in descending order are keys in descending order; NaN below everything, one zero.
@@ -198,15 +200,20 @@ __device__ __forceinline__ void add_cluster(unsigned int addr, unsigned int v)
 {
     asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
-// All threads of all blocks of the cluster; also the block's own barrier.
-__device__ __forceinline__ void cluster_meet()
+// All threads of all blocks of the cluster.
+__device__ __forceinline__ void cluster_meet(unsigned int blocks)
 {
+    if (blocks == 1) {
+        __syncthreads();
+        return;
+    }
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 struct PickShared {
+    unsigned int keys[kKeys];
     unsigned int mine[kBins], all[kBins];              // counts of this block; of the cluster (the first block's)
     unsigned int of_warp[kPickWarps][2], of_block[2][kMostBlocks][2];
     unsigned int found[3], refused[kMostBlocks], scan[kPickWarps];      // found: digit, how many with it are chosen, how many have it
@@ -223,29 +230,29 @@ __device__ __forceinline__ void before_me(PickShared &s, int &turn, unsigned int
         s.of_warp[warp][1] = b;
     }
     __syncthreads();
-    if (warp == 0) {
-        const unsigned int x = __reduce_add_sync(kFull, lane < kPickWarps ? s.of_warp[lane][0] : 0u), y = __reduce_add_sync(kFull, lane < kPickWarps ? s.of_warp[lane][1] : 0u);
-        if (lane < static_cast<int>(blocks)) {
-            const unsigned int to = in_block(s.of_block[turn][rank], lane);
-            st_cluster(to, x);
-            st_cluster(to + 4, y);
-        }
+    const unsigned int x = lane < kPickWarps ? s.of_warp[lane][0] : 0u, y = lane < kPickWarps ? s.of_warp[lane][1] : 0u;
+    total[0] = __reduce_add_sync(kFull, x);
+    total[1] = __reduce_add_sync(kFull, y);
+    before[0] = __reduce_add_sync(kFull, lane < warp ? x : 0u);
+    before[1] = __reduce_add_sync(kFull, lane < warp ? y : 0u);
+    if (blocks == 1) return;
+    if (warp == 0 && lane < static_cast<int>(blocks)) {
+        const unsigned int to = in_block(s.of_block[turn][rank], lane);
+        st_cluster(to, total[0]);
+        st_cluster(to + 4, total[1]);
     }
-    cluster_meet();
+    cluster_meet(blocks);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        before[k] = total[k] = 0u;
-        for (unsigned int r = 0; r < blocks; ++r) {
-            total[k] += s.of_block[turn][r][k];
-            if (r < rank) before[k] += s.of_block[turn][r][k];
-        }
-        for (int w = 0; w < warp; ++w) before[k] += s.of_warp[w][k];
+        const unsigned int z = lane < static_cast<int>(blocks) ? s.of_block[turn][lane][k] : 0u;
+        total[k] = __reduce_add_sync(kFull, z);
+        before[k] += __reduce_add_sync(kFull, lane < static_cast<int>(rank) ? z : 0u);
     }
     turn ^= 1;
 }
 
-// Finds the key of the W-th largest of the places [first, first + n) and how many of those that have it are chosen: three rounds over
-// digits of 11, 11 and 10 bits.  A cluster of blocks has the row; each warp of it a run of the places.
+// Finds the key of the W-th largest of the M places from S on, and how many of those that have it are chosen: rounds over digits of 11, 11
+// and 10 bits, fewer where a digit settles it.  A cluster of blocks has the row; each warp of it a run of the places.
 __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictParams p)
 {
     __shared__ PickShared s;
@@ -259,7 +266,7 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
     if (len <= keep) {
         for (int i = my; i < p.width; i += threads) kept[i] = i < len ? i : -1;
         if (my == 0) {
-            p.plans[r] = {0, 0, 0, 0, len, len};
+            p.plans[r] = {0, 0, 0, 0, 0, len, len};
             p.evicted[r] = 0;
         }
         return;
@@ -267,19 +274,35 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
     const int R = min(max(p.recent, 0), keep), S = min(max(p.sinks, 0), keep - R), W = keep - S - R, F = S + W, M = len - R - S;
     const float *const mass = p.mass + r * p.mass_stride;
     const int warps = static_cast<int>(blocks) * kPickWarps, me = static_cast<int>(rank) * kPickWarps + warp;
-    const int p0 = S + static_cast<int>(static_cast<long long>(M) * me / warps), p1 = S + static_cast<int>(static_cast<long long>(M) * (me + 1) / warps);
-    auto key_at = [&](int j) { return mass_key(__int_as_float(ptx::ld_written(reinterpret_cast<const int *>(mass) + j))); };
+    auto run_from = [&](int w) { return S + static_cast<int>(static_cast<long long>(M) * w / warps); };
+    const int p0 = run_from(me), p1 = run_from(me + 1), b0 = run_from(static_cast<int>(rank) * kPickWarps), b1 = run_from(static_cast<int>(rank + 1) * kPickWarps);
+    auto load = [&](int j) { return mass_key(__int_as_float(ptx::ld_written(reinterpret_cast<const int *>(mass) + j))); };
+    const bool cached = b1 - b0 <= kKeys;
+    if (cached && W > 0) {
+        for (int j = p0 + lane; j < p1; j += 32 * 8) {
+            unsigned int k[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) k[e] = j + 32 * e < p1 ? load(j + 32 * e) : 0u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (j + 32 * e < p1) s.keys[j + 32 * e - b0] = k[e];
+        }
+        __syncwarp();                                                  // (a warp reads its own run alone)
+    }
+    auto key_at = [&](int j) { return cached ? s.keys[j - b0] : load(j); };
 
     // ---- the key that decides ----
-    unsigned int prefix = 0u, left = static_cast<unsigned int>(W), ties = 0u;        // of the places with this prefix, `left` are chosen
-    int turn = 0;
+    // places with a key above `prefix` (in the bits above `shift`) are chosen, and `left` of the `ties` that have it
+    unsigned int prefix = 0u, left = static_cast<unsigned int>(W), ties = 0u;
+    int shift = 0, turn = 0;
     if (W > 0) {
 #pragma unroll 1
         for (int round = 0; round < 3; ++round) {
-            const int shift = round == 0 ? 21 : (round == 1 ? 10 : 0), bits = round == 2 ? 10 : 11;
-            const unsigned int above = round == 0 ? 0u : 0xffffffffu << (shift + bits);
+            const int bits = round == 2 ? 10 : 11;
+            const unsigned int above = round == 0 ? 0u : 0xffffffffu << (round == 1 ? 21 : 10);
+            shift = round == 0 ? 21 : (round == 1 ? 10 : 0);
             for (int i = tid; i < kBins; i += kPickThreads) s.mine[i] = s.all[i] = 0u;
-            cluster_meet();
+            cluster_meet(blocks);
             for (int j = p0 + lane; j < p1; j += 32 * 8) {
                 unsigned int k[8];
 #pragma unroll
@@ -289,13 +312,17 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
                     if (j + 32 * e < p1 && (k[e] & above) == prefix) atomicAdd(&s.mine[(k[e] >> shift) & ((1u << bits) - 1u)], 1u);
             }
             __syncthreads();
-            for (int i = tid; i < kBins; i += kPickThreads)
-                if (s.mine[i]) add_cluster(in_block(&s.all[i], 0), s.mine[i]);
-            cluster_meet();
+            if (blocks > 1) {
+                for (int i = tid; i < kBins; i += kPickThreads)
+                    if (s.mine[i]) add_cluster(in_block(&s.all[i], 0), s.mine[i]);
+                cluster_meet(blocks);
+            }
             if (rank == 0) {
                 // from the highest bin down: thread t has bins 4 t' .. 4 t' + 3 with t' = 511 - t
-                const int b0 = 4 * (kPickThreads - 1 - tid);
-                const unsigned int c[4] = {s.all[b0 + 3], s.all[b0 + 2], s.all[b0 + 1], s.all[b0]};
+                const unsigned int *const count = blocks == 1 ? s.mine : s.all;
+                const int c0 = 4 * (kPickThreads - 1 - tid);
+                const uint4 q = *reinterpret_cast<const uint4 *>(count + c0);
+                const unsigned int c[4] = {q.w, q.z, q.y, q.x};
                 const unsigned int sum = c[0] + c[1] + c[2] + c[3];
                 unsigned int inc = sum;
 #pragma unroll
@@ -305,14 +332,13 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
                 }
                 if (lane == 31) s.scan[warp] = inc;
                 __syncthreads();
-                unsigned int at = inc - sum;
-                for (int w = 0; w < warp; ++w) at += s.scan[w];
+                unsigned int at = inc - sum + __reduce_add_sync(kFull, lane < warp ? s.scan[lane] : 0u);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (at < left && left <= at + c[e]) {                      // one thread and bin
-                        for (unsigned int q = 0; q < blocks; ++q) {
-                            const unsigned int to = in_block(s.found, q);
-                            st_cluster(to, static_cast<unsigned int>(b0 + 3 - e));
+                        for (unsigned int b = 0; b < blocks; ++b) {
+                            const unsigned int to = in_block(s.found, b);
+                            st_cluster(to, static_cast<unsigned int>(c0 + 3 - e));
                             st_cluster(to + 4, left - at);
                             st_cluster(to + 8, c[e]);
                         }
@@ -320,30 +346,34 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
                     at += c[e];
                 }
             }
-            cluster_meet();
+            cluster_meet(blocks);
             prefix |= s.found[0] << shift;
             left = s.found[1];
             ties = s.found[2];
+            if (left == ties) break;                                       // all of them: what follows the digit does not matter
         }
     }
-    // a place is chosen if its key is above `prefix`, or is it and fewer than `left` such places come before it
     unsigned int before[2], total[2], first_tie = 0u;
-    const bool all_ties = W > 0 && left == ties;
-    if (W > 0 && !all_ties) {
+    const bool all_ties = left == ties;                                    // (W = 0: nothing is chosen)
+    if (!all_ties) {
         unsigned int mine = 0u;
         for (int j = p0 + lane; j < p1; j += 32) mine += key_at(j) == prefix ? 1u : 0u;
         before_me(s, turn, rank, blocks, __reduce_add_sync(kFull, mine), 0u, before, total);
         first_tie = before[0];
     }
+    const unsigned int digits = prefix >> shift;
     auto walk = [&](auto visit) {
         unsigned int tie = first_tie;
         for (int j0 = p0; j0 < p1; j0 += 32) {
             const int j = j0 + lane;
-            const unsigned int k = j < p1 && W > 0 ? key_at(j) : 0u;
-            const bool same = j < p1 && W > 0 && k == prefix;
-            const unsigned int m = __ballot_sync(kFull, same);
-            const bool chosen = j < p1 && W > 0 && (k > prefix || (same && (all_ties || tie + __popc(m & ((1u << lane) - 1u)) < left)));
-            tie += __popc(m);
+            const unsigned int k = j < p1 && W > 0 ? key_at(j) >> shift : 0u;
+            bool chosen = j < p1 && W > 0 && (all_ties ? k >= digits : k > digits);
+            if (!all_ties) {
+                const bool same = j < p1 && k == digits;
+                const unsigned int m = __ballot_sync(kFull, same);
+                if (same && tie + __popc(m & ((1u << lane) - 1u)) < left) chosen = true;
+                tie += __popc(m);
+            }
             visit(j, j < p1 && !chosen && j < F, chosen && j >= F, chosen && j < F);
         }
     };
@@ -370,40 +400,80 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
         for (int i = my; i < p.width; i += threads) kept[i] = i < len ? i : -1;
         if (my == 0) {
             atomicOr(p.v.flags, CSD_CACHE_SHARED);
-            p.plans[r] = {0, 0, 0, 0, len, len};
+            p.plans[r] = {0, 0, 0, 0, 0, len, len};
             p.evicted[r] = 0;
         }
         return;
     }
     // ---- where everything goes ----
     int2 *const pairs = p.pairs + static_cast<long long>(r) * p.width;
+    longlong2 *const offsets = p.offsets + static_cast<long long>(r) * p.width;
+    const int front = static_cast<int>(total[1]);
+    bool lost = false;
+    auto offset_of = [&](int place) -> long long {
+        const int page = table[place >> p.v.page_shift];
+        if (page < 0 || page >= p.v.n_pages) {
+            lost = true;
+            return -1;
+        }
+        return page * p.pool.page + (place & (p.v.page_size - 1)) * p.pool.token;
+    };
     unsigned int hole_at = before[0], mover_at = before[1];
     walk([&](int j, bool hole, bool mover, bool stays) {
         const unsigned int mh = __ballot_sync(kFull, hole), mm = __ballot_sync(kFull, mover), below = (1u << lane) - 1u;
-        if (hole) __stcg(&pairs[hole_at + __popc(mh & below)].y, j);
-        if (mover) __stcg(&pairs[mover_at + __popc(mm & below)].x, j);
+        if (hole) {
+            const int at = hole_at + __popc(mh & below);
+            __stcg(&pairs[at].y, j);
+            __stcg(&offsets[at].y, offset_of(j));
+        }
+        if (mover) {
+            const int at = mover_at + __popc(mm & below);
+            __stcg(&pairs[at].x, j);
+            __stcg(&offsets[at].x, offset_of(j));
+        }
         if (stays) kept[j] = j;
+        if (j == keep && j < p1) p.plans[r].early = static_cast<int>(mover_at) + __popc(mm & below);     // (the warp whose run has that place)
         hole_at += __popc(mh);
         mover_at += __popc(mm);
     });
     for (int i = my; i < S; i += threads) kept[i] = i;
     for (int i = F + my; i < p.width; i += threads) kept[i] = i < keep ? len - keep + i : -1;
+    for (int i = my; i < R; i += threads) {
+        longlong2 o;
+        o.x = offset_of(len - R + i);
+        o.y = offset_of(F + i);
+        offsets[front + i] = o;
+    }
+    if (lost) atomicOr(p.v.flags, CSD_CACHE_BAD_PAGE);
     if (my == 0) {
-        p.plans[r] = {static_cast<int>(total[1]), len - R, F, R, len, keep};
+        RowPlan *const plan = p.plans + r;
+        if (keep >= len - R) plan->early = front;                           // every mover comes from below `keep`
+        plan->front = front;
+        plan->from = len - R;
+        plan->to = F;
+        plan->recent = R;
+        plan->len = len;
+        plan->keep = keep;
         p.evicted[r] = len - keep;
     }
-    cluster_meet();
-    for (int i = my; i < static_cast<int>(total[1]); i += threads) {
+    cluster_meet(blocks);
+    for (int i = my; i < front; i += threads) {
         const int2 m = __ldcg(pairs + i);
         kept[m.y] = m.x;
     }
 }
 
-// The moves: a block has one head of the keys or values of one layer of one row (or the row's masses) at a time.  First the movers, whose
-// targets nothing else reads; then, after a barrier, the recent tokens in pieces: a piece's loads, a barrier, its stores.
-constexpr int kMoveThreads = 256, kMoveAtOnce = 4;
+// The moves.  Movers from places beyond the row's new end can go at any time, in any number of blocks: nothing else touches where they come
+// from or go to.  The others make room for the recent tokens and go before these: a team of threads does both for one head of the keys or values of one
+// layer of one row, first those movers, then, after a barrier, the recent tokens in pieces: a piece's loads, a barrier, its stores.  A team is a
+// warp where there are warps' worth of such heads (16 rows of 16 layers with 8 heads: 69 us for the call, 81 with blocks), else a block (8 rows of 4
+// layers: 150, with warps 182).  Loads in flight per thread and blocks per SM: 8 and 2, 4 and 4 (exchanged: 74 and 154).
+constexpr int kMoveThreads = 256;
+template <int kTeam>
+constexpr int kMoveBlocks = kTeam == 32 ? 2 : 4;     // per SM
 
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictParams p)
+template <int kTeam>
+__global__ void __launch_bounds__(kMoveThreads, kMoveBlocks<kTeam>) evict_move_kernel(const EvictParams p)
 {
     __shared__ int active[CSD_CACHE_MAX_ROWS];
     __shared__ int of_warp[kMoveThreads / 32];
@@ -426,77 +496,85 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictPar
         __syncthreads();
     }
     const int units = 2 * p.pool.layers * p.pool.heads + 1;
-    const int tokens = kMoveThreads / p.pool.vecs, sub = tid / p.pool.vecs, vec = tid - sub * p.pool.vecs;       // tokens of a piece
-    for (long long w = blockIdx.x; w < static_cast<long long>(n_active) * units; w += gridDim.x) {
-        const int r = active[w / units], unit = static_cast<int>(w % units);
+    const int mine = tid % kTeam;
+    const int tokens = kTeam / p.pool.vecs, sub = mine / p.pool.vecs, vec = mine - sub * p.pool.vecs;       // tokens of a piece
+    const bool works = sub < tokens;
+    auto team_sync = [&]() {
+        if constexpr (kTeam == 32)
+            __syncwarp();
+        else
+            __syncthreads();
+    };
+    // a unit's late movers are shared out over so many teams that all have something to do
+    constexpr int kTeams = kMoveThreads / kTeam, kMoveAtOnce = kTeam == 32 ? 8 : 4;
+    const long long teams = static_cast<long long>(gridDim.x) * kTeams, whole = static_cast<long long>(n_active) * units;
+    const int parts = whole > 0 ? static_cast<int>(min(max(2 * teams / whole, 1ll), 8ll)) : 1;
+    for (long long w = static_cast<long long>(blockIdx.x) * kTeams + tid / kTeam; w < whole * parts; w += teams) {
+        const int part = static_cast<int>(w / whole);
+        const long long w1 = w - part * whole;
+        const int r = active[w1 / units], unit = static_cast<int>(w1 % units);
         const RowPlan plan = p.plans[r];
-        const int2 *const pairs = p.pairs + static_cast<long long>(r) * p.width;
         if (unit == units - 1) {
+            if (part != 0) continue;
+            const int2 *const pairs = p.pairs + static_cast<long long>(r) * p.width;
             float *const mass = p.mass + r * p.mass_stride;
-            for (int i = tid; i < plan.front; i += kMoveThreads) {
+            for (int i = mine; i < plan.front; i += kTeam) {
                 const int2 m = pairs[i];
                 mass[m.y] = mass[m.x];
             }
-            __syncthreads();
-            for (int i0 = 0; i0 < plan.recent; i0 += kMoveThreads) {
-                const int i = i0 + tid;
+            team_sync();
+            for (int i0 = 0; i0 < plan.recent; i0 += kTeam) {
+                const int i = i0 + mine;
                 const float x = i < plan.recent ? mass[plan.from + i] : 0.f;
-                __syncthreads();
+                team_sync();
                 if (i < plan.recent) mass[plan.to + i] = x;
             }
-            __syncthreads();
-            for (int i = plan.keep + tid; i < plan.len; i += kMoveThreads) mass[i] = 0.f;
+            team_sync();
+            for (int i = plan.keep + mine; i < plan.len; i += kTeam) mass[i] = 0.f;
             continue;
         }
         const int plane = unit / p.pool.heads, h = unit - plane * p.pool.heads;
         char *const base = ((plane & 1) ? p.pool.v : p.pool.k) + (plane >> 1) * p.pool.layer + h * p.pool.head + vec * 16;
-        const int *const table = p.v.table + static_cast<long long>(r) * p.v.max_pages;
-        auto slot = [&](int place) -> char * {
-            const int page = table[place >> p.v.page_shift];
-            return page < 0 || page >= p.v.n_pages ? nullptr : base + page * p.pool.page + (place & (p.v.page_size - 1)) * p.pool.token;
-        };
-        bool lost = false;
-        uint4 x[kMoveAtOnce];
-        for (int i0 = 0; i0 < plan.front; i0 += tokens * kMoveAtOnce) {
-            char *to[kMoveAtOnce];
-#pragma unroll
-            for (int k = 0; k < kMoveAtOnce; ++k) {
-                const int i = i0 + k * tokens + sub;
-                to[k] = nullptr;
-                if (sub < tokens && i < plan.front) {
-                    const int2 m = pairs[i];
-                    const char *from = slot(m.x);
-                    to[k] = slot(m.y);
-                    if (!from) to[k] = nullptr;
-                    lost |= !to[k];
-                    if (to[k]) x[k] = ptx::ld_written_once(from);
-                }
+        const longlong2 *const offsets = p.offsets + static_cast<long long>(r) * p.width;
+        // pairs [first, end) in turn: the early movers, the recent tokens, this block's share of the late movers.  The next offsets are fetched ahead; of
+        // the recent tokens no thread stores before all have loaded.
+        for (int phase = part == 0 ? 0 : 2; phase < 3; ++phase) {
+            int first = 0, end = plan.early;
+            if (phase == 1) {
+                team_sync();
+                first = plan.front;
+                end = plan.front + plan.recent;
+            } else if (phase == 2) {
+                const int late = plan.front - plan.early, shares = parts == 1 ? 1 : parts - 1, share = parts == 1 ? 0 : part - 1;
+                if (share < 0) break;
+                first = plan.early + static_cast<int>(static_cast<long long>(late) * share / shares);
+                end = plan.early + static_cast<int>(static_cast<long long>(late) * (share + 1) / shares);
             }
+            longlong2 o[kMoveAtOnce];
+            auto fetch = [&](int i0) {
 #pragma unroll
-            for (int k = 0; k < kMoveAtOnce; ++k)
-                if (to[k]) *reinterpret_cast<uint4 *>(to[k]) = x[k];
-        }
-        __syncthreads();
-        for (int i0 = 0; i0 < plan.recent; i0 += tokens * kMoveAtOnce) {
-            char *to[kMoveAtOnce];
-#pragma unroll
-            for (int k = 0; k < kMoveAtOnce; ++k) {
-                const int i = i0 + k * tokens + sub;
-                to[k] = nullptr;
-                if (sub < tokens && i < plan.recent) {
-                    const char *from = slot(plan.from + i);
-                    to[k] = slot(plan.to + i);
-                    if (!from) to[k] = nullptr;
-                    lost |= !to[k];
-                    if (to[k]) x[k] = ptx::ld_written_once(from);
+                for (int k = 0; k < kMoveAtOnce; ++k) {
+                    const int i = i0 + k * tokens + sub;
+                    o[k] = make_longlong2(-1, -1);
+                    if (works && i < end) o[k] = offsets[i];
                 }
-            }
-            __syncthreads();
+            };
+            fetch(first);
+            for (int i0 = first; i0 < end; i0 += tokens * kMoveAtOnce) {
+                uint4 x[kMoveAtOnce];
+                long long to[kMoveAtOnce];
 #pragma unroll
-            for (int k = 0; k < kMoveAtOnce; ++k)
-                if (to[k]) *reinterpret_cast<uint4 *>(to[k]) = x[k];
+                for (int k = 0; k < kMoveAtOnce; ++k) {
+                    to[k] = o[k].x >= 0 ? o[k].y : -1;
+                    if (to[k] >= 0) x[k] = ptx::ld_written_once(base + o[k].x);
+                }
+                fetch(i0 + tokens * kMoveAtOnce);
+                if (phase == 1) team_sync();
+#pragma unroll
+                for (int k = 0; k < kMoveAtOnce; ++k)
+                    if (to[k] >= 0) *reinterpret_cast<uint4 *>(base + to[k]) = x[k];
+            }
         }
-        if (lost) atomicOr(p.v.flags, CSD_CACHE_BAD_PAGE);
     }
 }
 

@@ -194,3 +194,12 @@ def test_refusals():
     other, _ = filled(1, [40, 40, 40], 16, 1, 1, 64)
     with pytest.raises(CsdError, match="another cache"):
         csd_cache_evict(other, torch.zeros(3, 48, device="cuda"), 5, buf)
+
+
+def test_many_rows_and_layers():
+    """More heads than the GPU has blocks for: a warp moves one of them; rows that lose nothing among those that do, an odd head size."""
+    rng = np.random.default_rng(3)
+    lens = [int(n) for n in rng.integers(30, 400, 40)]
+    cache, table = filled(6, lens, 16, 8, 5, 24)
+    run_and_check(cache, table, lens, masses(8, 40, cache.max_pages * 16, "ties"), 150, 4, 60)
+    assert cache.stats()["flags"] == 0
