@@ -332,7 +332,7 @@ def csd_step(logits, draft, ocm: Ocm, tau: float, buf: StepBuffers, stream=None)
 
 
 class TreeBuffers:
-    """Caller-owned outputs of csd_verify_tree for B rows of T nodes."""
+    """Caller-owned outputs of csd_verify_tree for B rows of T nodes.  The tensors stay the ones made here."""
 
     def __init__(self, B, T, device="cuda"):
         self.B, self.T = B, T
@@ -340,6 +340,8 @@ class TreeBuffers:
         self.accept_len, self.next_token = torch.empty(B, **i), torch.empty(B, **i)
         self.path, self.rej_draft, self.rej_target = (torch.empty(B, T, **i) for _ in range(3))
         self.rescued_mask = torch.empty(B, T, dtype=torch.uint8, device=device)
+        self._device = self.path.get_device()
+        self._out = tuple(x.data_ptr() for x in (self.accept_len, self.next_token, self.path, self.rescued_mask, self.rej_draft, self.rej_target))
 
 
 def csd_verify_tree(logits, tokens, parents, ocm: Ocm, tau: float, buf: TreeBuffers, n_nodes=None, stream=None):
@@ -347,20 +349,26 @@ def csd_verify_tree(logits, tokens, parents, ocm: Ocm, tau: float, buf: TreeBuff
     int32, n_nodes [B] int32.  buf.accept_len and buf.path go to csd_cache_commit_path, buf.rej_draft and buf.rej_target to Ocm.update;
     the memory is only read."""
     B, T, V = logits.shape
-    assert (B, T) == (buf.B, buf.T) and logits.stride(2) == 1
-    assert tokens.dtype == torch.int32 and tokens.shape == (B, T) and tokens.is_contiguous()
-    assert parents.dtype == torch.int32 and tuple(parents.shape) in ((T,), (B, T)) and (T == 1 or parents.stride(-1) == 1)
-    assert n_nodes is None or n_nodes.dtype == torch.int32 and n_nodes.shape == (B,) and n_nodes.is_contiguous()
-    dev = ocm.device.index
-    devices = [t.get_device() for t in (logits, tokens, parents, buf.path) + (() if n_nodes is None else (n_nodes,))]
-    current = torch.cuda.current_device() if stream is None else stream.device_index
-    if any(d != dev for d in devices) or current != dev:
-        raise CsdError(f"csd_verify_tree: tensors on devices {devices}, the memory on {dev}, the stream on {current} (-1: the host)")
-    strides = logits.stride(0), logits.stride(1) if T > 1 else V
-    _check(lib().csd_verify_tree(logits.data_ptr(), _dtype_code(logits), B, T, V, *strides, tokens.data_ptr(), parents.data_ptr(),
-                                 parents.stride(0) if parents.dim() == 2 else 0, _ptr(n_nodes), ocm.handle, c_float(tau),
-                                 buf.accept_len.data_ptr(), buf.next_token.data_ptr(), buf.path.data_ptr(), buf.rescued_mask.data_ptr(),
-                                 buf.rej_draft.data_ptr(), buf.rej_target.data_ptr(), _stream_ptr(stream)), "csd_verify_tree")
+    zs, ps, both = logits.stride(), parents.stride(), (B, T)
+    assert both == (buf.B, buf.T) and zs[2] == 1
+    assert tokens.dtype == parents.dtype == torch.int32 and tokens.shape == both and tokens.is_contiguous()
+    assert parents.shape == (both if len(ps) == 2 else (T,)) and (T == 1 or ps[-1] == 1)
+    nodes, dev, at = None, ocm.device.index, logits.get_device()
+    if n_nodes is not None:
+        assert n_nodes.dtype == torch.int32 and n_nodes.shape == (B,) and n_nodes.is_contiguous()
+        nodes = n_nodes.data_ptr()
+    if not (at == tokens.get_device() == parents.get_device() == buf._device == dev) or n_nodes is not None and n_nodes.get_device() != dev:
+        raise CsdError(f"csd_verify_tree: tensors on different devices: {at}, {tokens.get_device()}, {parents.get_device()}, {buf._device}, "
+                       f"the memory on {dev} (-1: the host)")
+    current = torch._C._cuda_getDevice()
+    if current != dev or stream is not None and stream.device_index != dev:
+        raise CsdError(f"csd_verify_tree: tensors on device {dev}, the current device is {current}, the stream's {stream and stream.device_index}")
+    # (the raw handle: a Stream object costs 3 us to make)
+    to = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    rc = lib().csd_verify_tree(logits.data_ptr(), _dtype_code(logits), B, T, V, zs[0], zs[1] if T > 1 else V, tokens.data_ptr(), parents.data_ptr(),
+                               ps[0] if len(ps) == 2 else 0, nodes, ocm.handle, tau, *buf._out, to)
+    if rc:
+        _check(rc, "csd_verify_tree")
 
 
 class HostStep:

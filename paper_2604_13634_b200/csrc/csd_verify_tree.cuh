@@ -23,8 +23,8 @@
 namespace csd {
 namespace verify_tree {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 16, kNodes = CSD_TREE_MAX_NODES;
-constexpr int kAtOnce = 8;                 // 16-byte loads in flight per thread
+constexpr int kThreads = 512, kWarps = kThreads / 32, kMaxCluster = 8, kNodes = CSD_TREE_MAX_NODES;
+constexpr int kAtOnce = 8;                 // 16-byte loads in flight per thread: all of a row of 262144 bf16 logits, shared by eight blocks
 
 struct Params {
     const void *logits;
@@ -143,9 +143,9 @@ __device__ __forceinline__ void cluster_meet()
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// This block's share of a logit row: (max, lowest index) of it, in every thread of warp 0.
+// This warp's share of a logit row: (max, lowest index) of it.
 template <typename T>
-__device__ __forceinline__ Best row_share(const T *row, int V, unsigned int rank, unsigned int blocks, Best (&of_warp)[kWarps])
+__device__ __forceinline__ Best row_share(const T *row, int V, unsigned int rank, unsigned int blocks)
 {
     constexpr int N = Lane<T>::kN;
     const int tid = threadIdx.x;
@@ -188,24 +188,15 @@ __device__ __forceinline__ Best row_share(const T *row, int V, unsigned int rank
     };
     if (rank == 0 && tid < head) single(tid);
     if (rank == blocks - 1 && head + n_vec * N + tid < V) single(head + n_vec * N + tid);
-    Best mine = {ordered(m), index, odd ? 1 : 0};
-    mine = warp_best(mine);
-    if ((tid & 31) == 0) of_warp[tid >> 5] = mine;
-    __syncthreads();
-    const int lane = tid & 31;
-    mine = {0u, 0x7fffffff, 0};
-    if (tid < 32) {
-        if (lane < kWarps) mine = of_warp[lane];
-        mine = warp_best(mine);
-    }
-    return mine;
+    const Best mine = {ordered(m), index, odd ? 1 : 0};
+    return warp_best(mine);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 4) verify_tree_kernel(const Params p)
+__global__ void __launch_bounds__(kThreads, 2) verify_tree_kernel(const Params p)
 {
     __shared__ int token[kNodes], parent[kNodes];
-    __shared__ Best of_warp[kWarps], of_block[2][kMaxCluster];
+    __shared__ Best of_warps[2][kMaxCluster * kWarps];                  // of all warps of the cluster, this block's copy
     __shared__ int decision;
     __shared__ int path[kNodes], rec_d[kNodes], rec_t[kNodes], rescued[kNodes];        // the first block's
     ptx::wait_for_stream();
@@ -225,17 +216,24 @@ __global__ void __launch_bounds__(kThreads, 4) verify_tree_kernel(const Params p
     while (cur >= 0) {
         if (tid == 0) path[length] = cur;
         const T *row = static_cast<const T *>(p.logits) + b * p.stride_b + cur * p.stride_t;
-        const Best share = row_share<T>(row, p.V, rank, blocks, of_warp);
-        Best *const slots = of_block[length & 1];                       // (read by all before the barrier after the next one)
-        if (tid < 32 && lane < static_cast<int>(blocks)) {
-            const unsigned int to = in_block(ptx::smem_u32(&slots[rank]), lane);
+        const Best share = row_share<T>(row, p.V, rank, blocks);
+        Best *const slots = of_warps[length & 1];                       // (read by all before the barrier after the next one)
+        if (lane < static_cast<int>(blocks)) {
+            const unsigned int to = in_block(ptx::smem_u32(&slots[rank * kWarps + (tid >> 5)]), lane);
             st_cluster(to, share.key);
             st_cluster(to + 4, static_cast<unsigned int>(share.index));
             st_cluster(to + 8, static_cast<unsigned int>(share.odd));
         }
         cluster_meet();
         Best all = {0u, 0x7fffffff, 0};
-        if (lane < static_cast<int>(blocks)) all = slots[lane];
+        for (int w = lane; w < static_cast<int>(blocks) * kWarps; w += 32) {
+            const Best x = slots[w];
+            if (x.key > all.key || (x.key == all.key && x.index < all.index)) {
+                all.key = x.key;
+                all.index = x.index;
+            }
+            all.odd |= x.odd;
+        }
         all = warp_best(all);
         const float m = unordered(all.key);
         star = all.index == 0x7fffffff ? 0 : all.index;                 // (nothing above minus infinity: the lowest)

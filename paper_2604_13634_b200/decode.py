@@ -292,9 +292,11 @@ def csd_cache_commit(cache: PagedCache, accept_len, stream=None):
 def csd_cache_commit_path(cache: PagedCache, accept_len, path, stream=None):
     """After the verification of a tree (TreeBuffers' accept_len and path [rows, T]): of the last extension's tokens, path[row, 0 ..
     accept_len[row]] stay and move together."""
-    assert path.dim() == 2
-    _check(_lib().csd_cache_commit_path(cache._ref, _rows_arg(accept_len, cache, "accept_len"), _nodes_arg(path, cache, path.shape[1], torch.int32, "path"),
-                                        path.shape[1], _stream_ptr(stream, cache._device)), "csd_cache_commit_path")
+    _, T = path.shape
+    rc = _lib().csd_cache_commit_path(cache._ref, _rows_arg(accept_len, cache, "accept_len"), _nodes_arg(path, cache, T, torch.int32, "path"), T,
+                                      _stream_ptr(stream, cache._device))
+    if rc:
+        _check(rc, "csd_cache_commit_path")
 
 
 class EvictBuffers:
@@ -311,11 +313,13 @@ class EvictBuffers:
 
 
 def _mass_arg(mass, cache: PagedCache):
-    assert mass.dtype == torch.float32 and mass.dim() == 2 and mass.shape[0] == cache.rows and mass.shape[1] >= cache.max_pages * cache.page_size
-    assert mass.stride(1) == 1 and (cache.rows == 1 or mass.stride(0) >= mass.shape[1])
+    rows, places = mass.shape
+    step, one = mass.stride()
+    assert mass.dtype == torch.float32 and rows == cache.rows and places >= cache.max_pages * cache.page_size
+    assert one == 1 and (rows == 1 or step >= places)
     if mass.get_device() != cache._device:
         _scattered("mass", mass.get_device(), cache._device)
-    return mass.data_ptr(), max(mass.stride(0), mass.shape[1])
+    return mass.data_ptr(), max(step, places)
 
 
 def csd_cache_evict(cache: PagedCache, mass, keep, buf: EvictBuffers, sinks: int = 0, recent: int = 0, stream=None):
@@ -433,17 +437,19 @@ def csd_attention_mass(q, lse, cache: PagedCache, layer: int, mass, scale: float
     """mass [rows, places] float32 += the attention weights that the new tokens q [rows, T, q_heads, D] give each place, summed over tokens
     and heads; lse [rows, T, q_heads] is what csd_attention (masks None) or csd_attention_tree left in buf.lse for the same q, scale, n_new
     and masks.  fresh: the new tokens' own places begin at 0 (the first layer of a pass).  Returns mass.  Serving form: no gradient."""
+    rows, T, q_heads, dim = q.shape
     qs = q.stride()
-    assert q.dtype == cache.dtype and q.dim() == 4 and qs[3] == 1 and q.shape[0] == cache.rows and q.shape[3] == cache.head_dim
-    assert lse.dtype == torch.float32 and lse.shape == q.shape[:3] and lse.is_contiguous()
+    assert q.dtype == cache.dtype and qs[3] == 1 and rows == cache.rows and dim == cache.head_dim
+    assert lse.dtype == torch.float32 and lse.shape == (rows, T, q_heads) and lse.is_contiguous()
     dev = cache._device
     if not (q.get_device() == lse.get_device() == dev):
         _scattered("csd_attention_mass", q.get_device(), lse.get_device(), dev)
-    T = q.shape[1]
-    _check(_lib().csd_attention_mass(q.data_ptr(), qs[0], qs[1], qs[2], T, q.shape[2], lse.data_ptr(), cache._ref, layer,
-                                     cache.head_dim ** -0.5 if scale is None else scale, None if n_new is None else _rows_arg(n_new, cache, "n_new"),
-                                     None if masks is None else _nodes_arg(masks, cache, T, torch.int64, "masks"), *_mass_arg(mass, cache),
-                                     1 if fresh else 0, _stream_ptr(stream, dev)), "csd_attention_mass")
+    rc = _lib().csd_attention_mass(q.data_ptr(), qs[0], qs[1], qs[2], T, q_heads, lse.data_ptr(), cache._ref, layer,
+                                   dim ** -0.5 if scale is None else scale, None if n_new is None else _rows_arg(n_new, cache, "n_new"),
+                                   None if masks is None else _nodes_arg(masks, cache, T, torch.int64, "masks"), *_mass_arg(mass, cache),
+                                   1 if fresh else 0, _stream_ptr(stream, dev))
+    if rc:
+        _check(rc, "csd_attention_mass")
     return mass
 
 
