@@ -24,7 +24,7 @@ struct PlanParams {
     int *positions;
 };
 
-// A block per row, a thread per node.  Ancestors by doubling: six rounds reach the root of any tree of 64 nodes.  Latency alone.
+// A block per row, a thread per node.  Ancestors by doubling: six rounds reach the root of any tree of 64 nodes.  Latency alone, once per step.
 __global__ void __launch_bounds__(CSD_TREE_MAX_NODES) plan_kernel(const PlanParams p)
 {
     __shared__ unsigned long long seen[CSD_TREE_MAX_NODES];

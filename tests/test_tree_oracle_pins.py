@@ -3,6 +3,8 @@ host refuses before anything is launched.  No GPU."""
 
 import itertools
 import math
+import os
+import re
 from ctypes import byref
 
 import numpy as np
@@ -178,3 +180,33 @@ def test_verification_refuses_what_it_cannot_do():
                 dict(ocm=None), dict(tau=-0.1), dict(tau=math.nan), dict(tau=math.inf), dict(out=None)):
         assert call(**bad) == INVALID_ARG, bad
     assert call(T=65, sb=65 * 50) == UNSUPPORTED
+
+
+# ---- rules of the sources ----
+
+CSRC = os.path.join(os.path.dirname(os.path.abspath(build.__file__)), "csrc")
+
+
+def _code(name):
+    with open(os.path.join(CSRC, name)) as f:
+        return re.sub(r"//[^\n]*", "", f.read())
+
+
+@pytest.mark.parametrize("name", ["csd_tree.cuh", "csd_verify_tree.cuh", "csd_keep.cuh", "csd_mass.cuh"])
+def test_nothing_is_loaded_as_read_only(name):
+    """Kernels that start beside their predecessor must not load what it writes as data that nobody writes; each waits before anything else."""
+    code = _code(name)
+    assert not re.findall(r"__ldg\(|ld_stream16|\.nc\b", code)
+    for kernel in re.split(r"__global__", code)[1:]:
+        assert "wait_for_stream();" in kernel
+
+
+def test_blocks_that_give_up_still_meet_and_stay():
+    """The kernel of the attention mass: a wait that ran out leaves no barrier of the cluster out, and the block lingers before its memory goes."""
+    code = _code("csd_mass.cuh")
+    end = code[code.rindex("if (*give_up)"):]
+    assert "CSD_CACHE_INTERNAL" in end and end.index("ptx::linger();") < end.index("tmem_dealloc")
+    # three roles, each with the same two meetings to a run and none inside a test of `ok`
+    assert len(re.findall(r"if \(blocks > 1\) \{\s*cluster_meet\(\);\s*cluster_meet\(\);\s*\}", code)) == 2
+    assert len(re.findall(r"if \(blocks > 1\) cluster_meet\(\);", code)) == 2
+    assert not re.search(r"ok[^\n;]*\)\s*\{?\s*cluster_meet", code)
