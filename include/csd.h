@@ -29,7 +29,7 @@
  *     only), but for the blocks of a thread-block cluster, which the hardware schedules
  *     together: in the LM-head pair kernel their barrier waits on each other are
  *     bounded in time, and every path of both blocks reaches the two cluster barriers
- *     they meet at; in csd_verify_tree, csd_attention_mass and csd_cache_evict all
+ *     they meet at; in csd_verify_tree, csd_cache_commit_path, csd_attention_mass and csd_cache_evict all
  *     blocks of a cluster take the same branches to the same cluster barriers.  With csd_set_overlap on, the warps that finalise a batch row wait for
  *     the PREVIOUS launch on the stream: a bounded poll (2^14 loads) of a completion
  *     word, then the hardware's wait for that grid to retire, which always ends.
@@ -720,7 +720,7 @@ csd_status_t csd_verify_tree(const void *logits, csd_dtype_t dtype, int B, int T
  * - 1 (the root and the accepted nodes, csd_verify_tree's outputs), which become the row's last tokens in that order: their keys and values move
  * together in every layer, the other new tokens are dropped and pages that nothing uses are free.  path: DEVICE int32 [rows, T], T <=
  * CSD_TREE_MAX_NODES; ascending within a row, as a path through a tree is: an entry that is not above the one before it, or not among
- * the granted tokens, ends what is kept (CSD_CACHE_BAD_PATH).  Two launches; asynchronous.
+ * the granted tokens, ends what is kept (CSD_CACHE_BAD_PATH).  One launch; asynchronous.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *accept_len, const int32_t *path, int T, void *stream);
 

@@ -781,13 +781,8 @@ csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *acce
     p.accept_len = accept_len;
     p.path = path;
     p.T = T;
-    // a block per 128 vectors of a token, as long as that is a few waves of blocks
-    long long blocks = (2ll * cache->layers * cache->heads * p.pool.vecs + keep::kPathThreads - 1) / keep::kPathThreads;
-    const long long cap = (64ll * host::multiprocessors() + cache->rows - 1) / cache->rows;
-    if (blocks > cap) blocks = cap;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const csd_status_t rc = launch(keep::path_move_kernel, dim3(static_cast<unsigned int>(blocks), static_cast<unsigned int>(cache->rows)), keep::kPathThreads, 0, st, p);
-    return rc != CSD_OK ? rc : launch(keep::path_commit_kernel, dim3(static_cast<unsigned int>(cache->rows)), pages::kRowThreads, 0, st, p);
+    return launch_clusters(keep::path_kernel, dim3(static_cast<unsigned int>(cache->rows * keep::kPathBlocks)), keep::kPathThreads, 0,
+                           static_cast<cudaStream_t>(stream), keep::kPathBlocks, p);
 }
 
 size_t csd_cache_evict_workspace_bytes(int rows, int width)

@@ -4,8 +4,8 @@
 // place may be both a source and a target, so the order matters: a thread moves the same 16 bytes of every token (path), or a block the
 // same head of every token with a barrier between a piece's loads and its stores (eviction); no two blocks touch the same bytes.
 //
-// Bound: memory for the moves, latency for the choice (a few dependent passes over 4 bytes per place).  A path of one row in 32 layers takes 6.1 us
-// (two launches), 64 paths in 28 layers 19.6 (35 MB read and written); cutting 16 rows of about 1021 tokens to 1008 in 16 layers 69 us, of
+// Bound: memory for the moves, latency for the choice (a few dependent passes over 4 bytes per place).  A path of one row in 32 layers takes 6.1 us,
+// 64 paths in 28 layers 19.6 (35 MB read and written); cutting 16 rows of about 1021 tokens to 1008 in 16 layers 69 us, of
 // which the moves of 147 MB read and written take 50 and the choice 11; 8 prompts of 6000 to 16384 to 4096 in 4 layers 151 us, 128 and 19.
 #pragma once
 
@@ -29,153 +29,8 @@ struct Pool {
     int layers, heads, vecs;               // vecs: 16-byte vectors of a head
 };
 
-// ---- the accepted path -----------------------------------------------------------------------------------------
+// ---- clusters ----
 
-constexpr int kPathThreads = 128;
-
-struct PathParams {
-    View v;
-    Pool pool;
-    const int *accept_len, *path;
-    int T;
-};
-
-// How many of the row's granted tokens stay: the accepted ones and the root, as far as the path names them in ascending order.  One
-// warp; lane i and i + 32 hold entries i and i + 32 of the path.
-__device__ __forceinline__ int path_kept(const PathParams &p, int r, int granted, int (&entry)[2], bool &bad)
-{
-    const int lane = threadIdx.x & 31;
-    const int keep = min(max(ptx::ld_written(p.accept_len + r), -1), granted - 1) + 1;
-    const int *path = p.path + static_cast<long long>(r) * p.T;
-    int fine = 0;
-    bool all = true;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int i = lane + 32 * k;
-        entry[k] = i < p.T ? ptx::ld_written(path + i) : -1;
-        const int before = i == 0 ? -1 : (i <= p.T ? ptx::ld_written(path + i - 1) : 0x7fffffff);
-        const bool ok = i < keep && i < p.T && entry[k] > before && entry[k] >= 0 && entry[k] < granted;
-        const unsigned int not_ok = __ballot_sync(kFull, !ok);
-        if (all) fine += not_ok ? __ffs(not_ok) - 1 : 32;
-        all = all && not_ok == 0u;
-    }
-    fine = min(fine, keep);
-    bad = fine < keep;
-    return fine;
-}
-
-// grid (blocks over a token's vectors in all layers, rows).  A thread owns one 16-byte vector of every token: it reads token path[i]'s before it
-// writes token i's, in ascending i, and path[i] >= i, so what it still has to read is never overwritten.
-__global__ void __launch_bounds__(kPathThreads) path_move_kernel(const PathParams p)
-{
-    __shared__ long long from_off[CSD_TREE_MAX_NODES], to_off[CSD_TREE_MAX_NODES];     // of the tokens that move
-    __shared__ int n_moves;
-    ptx::wait_for_stream();
-    const int r = blockIdx.y, lane = threadIdx.x & 31;
-    if (threadIdx.x < 32) {
-        const int granted = p.v.granted[r], base = p.v.lens[r] - granted;
-        const int *row = p.v.table + static_cast<long long>(r) * p.v.max_pages;
-        int entry[2], at = 0;
-        bool bad;
-        const int n = granted > 0 ? path_kept(p, r, granted, entry, bad) : 0;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int i = lane + 32 * k;
-            bool moves = i < n && entry[k] != i;
-            long long from = 0, to = 0;
-            if (moves) {
-                const int a = base + entry[k], b = base + i;
-                const int pa = row[a >> p.v.page_shift], pb = row[b >> p.v.page_shift];
-                moves = pa >= 0 && pa < p.v.n_pages && pb >= 0 && pb < p.v.n_pages;
-                if (!moves) atomicOr(p.v.flags, CSD_CACHE_BAD_PAGE);
-                from = pa * p.pool.page + (a & (p.v.page_size - 1)) * p.pool.token;
-                to = pb * p.pool.page + (b & (p.v.page_size - 1)) * p.pool.token;
-            }
-            const unsigned int m = __ballot_sync(kFull, moves);
-            if (moves) {
-                const int j = at + __popc(m & ((1u << lane) - 1u));
-                from_off[j] = from;
-                to_off[j] = to;
-            }
-            at += __popc(m);
-        }
-        if (lane == 0) n_moves = at;
-    }
-    __syncthreads();
-    const int n = n_moves;
-    if (n == 0) return;
-    const int per_plane = p.pool.heads * p.pool.vecs, all = 2 * p.pool.layers * per_plane;
-    for (int c = blockIdx.x * kPathThreads + threadIdx.x; c < all; c += gridDim.x * kPathThreads) {
-        const int plane = c / per_plane, in_plane = c - plane * per_plane, h = in_plane / p.pool.vecs, vec = in_plane - h * p.pool.vecs;
-        char *base = ((plane & 1) ? p.pool.v : p.pool.k) + (plane >> 1) * p.pool.layer + h * p.pool.head + vec * 16;
-        for (int i = 0; i < n; i += 4) {
-            uint4 x[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i + k < n) x[k] = ptx::ld_written(reinterpret_cast<const uint4 *>(base + from_off[i + k]));
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i + k < n) *reinterpret_cast<uint4 *>(base + to_off[i + k]) = x[k];
-        }
-    }
-}
-
-// The bookkeeping after the moves: a block per row.
-__global__ void __launch_bounds__(pages::kRowThreads) path_commit_kernel(const PathParams p)
-{
-    __shared__ int kept;
-    ptx::wait_for_stream();
-    const int r = blockIdx.x;
-    const int len = p.v.lens[r], granted = max(p.v.granted[r], 0);
-    if (threadIdx.x < 32) {
-        int entry[2];
-        bool bad;
-        const int n = path_kept(p, r, granted, entry, bad);
-        if (threadIdx.x == 0) {
-            kept = n;
-            if (bad) atomicOr(p.v.flags, CSD_CACHE_BAD_PATH);
-        }
-    }
-    __syncthreads();
-    pages::shorten(p.v, r, len, len - granted + kept);
-}
-
-// ---- a budget --------------------------------------------------------------------------------------------------
-//
-// A row of len > keep tokens keeps its first S (sinks), its last R (recent), and of the places between the W = keep - S - R with the
-// largest mass (lowest place on ties).  New places: with F = S + W, the recent tokens become the last, F .. keep - 1, in order; a chosen
-// place below F stays; the chosen places from F on (movers), in ascending order, fill the places below F that were not chosen (holes),
-// in ascending order.  So as many tokens move as the row loses at most, and R.
-
-constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32, kBins = 2048, kMostBlocks = 8;
-constexpr int kKeys = 6144;                // keys that a block keeps in shared memory; a larger share is read again
-
-struct RowPlan {
-    int early, front;                      // pairs [0, early): movers from places below `keep`; [early, front): the others; then the recent tokens
-    int from, to, recent;                  // which go from place `from` to place `to`
-    int len, keep;                         // tokens before and after (equal: nothing happens)
-};
-
-struct EvictParams {
-    View v;
-    Pool pool;
-    float *mass;
-    long long mass_stride;
-    const int *keep_rows;                  // null: `keep` for every row
-    int keep, sinks, recent, width;        // width: columns of kept, pairs and offsets
-    int *kept, *evicted;
-    RowPlan *plans;                        // [rows]
-    int2 *pairs;                           // [rows, width] mover, hole: places
-    longlong2 *offsets;                    // [rows, width] where from and where to within a layer's pool, in bytes; -1: no such page
-};
-
-// Masses in descending order are keys in descending order; NaN below everything, one zero.
-__device__ __forceinline__ unsigned int mass_key(float x)
-{
-    if (x != x) return 0u;
-    const unsigned int u = __float_as_uint(x + 0.0f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
 __device__ __forceinline__ unsigned int cluster_rank()
 {
     unsigned int r;
@@ -214,6 +69,141 @@ __device__ __forceinline__ void cluster_meet(unsigned int blocks)
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// ---- the accepted path -----------------------------------------------------------------------------------------
+
+constexpr int kPathThreads = 512, kPathBlocks = 8;      // blocks of a cluster, which has a row
+
+struct PathParams {
+    View v;
+    Pool pool;
+    const int *accept_len, *path;
+    int T;
+};
+
+// How many of the row's granted tokens stay: the accepted ones and the root, as far as the path names them in ascending order.  One
+// warp; lane i and i + 32 hold entries i and i + 32 of the path.
+__device__ __forceinline__ int path_kept(const PathParams &p, int r, int granted, int (&entry)[2], bool &bad)
+{
+    const int lane = threadIdx.x & 31;
+    const int keep = min(max(ptx::ld_written(p.accept_len + r), -1), granted - 1) + 1;
+    const int *path = p.path + static_cast<long long>(r) * p.T;
+    int fine = 0;
+    bool all = true;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = lane + 32 * k;
+        entry[k] = i < p.T ? ptx::ld_written(path + i) : -1;
+        const int before = i == 0 ? -1 : (i <= p.T ? ptx::ld_written(path + i - 1) : 0x7fffffff);
+        const bool ok = i < keep && i < p.T && entry[k] > before && entry[k] >= 0 && entry[k] < granted;
+        const unsigned int not_ok = __ballot_sync(kFull, !ok);
+        if (all) fine += not_ok ? __ffs(not_ok) - 1 : 32;
+        all = all && not_ok == 0u;
+    }
+    fine = min(fine, keep);
+    bad = fine < keep;
+    return fine;
+}
+
+// A cluster has a row.  A thread owns 16-byte vectors of every token: it reads token path[i]'s before it writes token i's, in ascending i, and
+// path[i] >= i, so what it still has to read is never overwritten.  Every block works out for itself what moves where; once all have, the first
+// does the bookkeeping, beside the moves: pages that it frees are only given away by later launches.
+__global__ void __launch_bounds__(kPathThreads) path_kernel(const PathParams p)
+{
+    __shared__ long long from_off[CSD_TREE_MAX_NODES], to_off[CSD_TREE_MAX_NODES];     // of the tokens that move
+    __shared__ int n_moves, n_kept;
+    ptx::wait_for_stream();
+    const unsigned int rank = cluster_rank();
+    const int r = blockIdx.x / kPathBlocks, tid = threadIdx.x, lane = tid & 31;
+    const int len = p.v.lens[r], granted = max(p.v.granted[r], 0);
+    if (tid < 32) {
+        const int base = len - granted;
+        const int *row = p.v.table + static_cast<long long>(r) * p.v.max_pages;
+        int entry[2], at = 0;
+        bool bad;
+        const int n = path_kept(p, r, granted, entry, bad);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = lane + 32 * k;
+            bool moves = i < n && entry[k] != i;
+            long long from = 0, to = 0;
+            if (moves) {
+                const int a = base + entry[k], b = base + i;
+                const int pa = row[a >> p.v.page_shift], pb = row[b >> p.v.page_shift];
+                moves = pa >= 0 && pa < p.v.n_pages && pb >= 0 && pb < p.v.n_pages;
+                if (!moves) atomicOr(p.v.flags, CSD_CACHE_BAD_PAGE);
+                from = pa * p.pool.page + (a & (p.v.page_size - 1)) * p.pool.token;
+                to = pb * p.pool.page + (b & (p.v.page_size - 1)) * p.pool.token;
+            }
+            const unsigned int m = __ballot_sync(kFull, moves);
+            if (moves) {
+                const int j = at + __popc(m & ((1u << lane) - 1u));
+                from_off[j] = from;
+                to_off[j] = to;
+            }
+            at += __popc(m);
+        }
+        if (lane == 0) {
+            n_moves = at;
+            n_kept = n;
+            if (bad && rank == 0) atomicOr(p.v.flags, CSD_CACHE_BAD_PATH);
+        }
+    }
+    cluster_meet(kPathBlocks);                       // no block reads the tables any more
+    if (rank == 0) pages::shorten(p.v, r, len, len - granted + n_kept, kPathThreads);
+    const int n = n_moves;
+    if (n == 0) return;
+    const int per_plane = p.pool.heads * p.pool.vecs, all = 2 * p.pool.layers * per_plane;
+    for (int c = static_cast<int>(rank) * kPathThreads + tid; c < all; c += kPathBlocks * kPathThreads) {
+        const int plane = c / per_plane, in_plane = c - plane * per_plane, h = in_plane / p.pool.vecs, vec = in_plane - h * p.pool.vecs;
+        char *base = ((plane & 1) ? p.pool.v : p.pool.k) + (plane >> 1) * p.pool.layer + h * p.pool.head + vec * 16;
+        for (int i = 0; i < n; i += 4) {
+            uint4 x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k < n) x[k] = ptx::ld_written(reinterpret_cast<const uint4 *>(base + from_off[i + k]));
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k < n) *reinterpret_cast<uint4 *>(base + to_off[i + k]) = x[k];
+        }
+    }
+}
+
+// ---- a budget --------------------------------------------------------------------------------------------------
+//
+// A row of len > keep tokens keeps its first S (sinks), its last R (recent), and of the places between the W = keep - S - R with the
+// largest mass (lowest place on ties).  New places: with F = S + W, the recent tokens become the last, F .. keep - 1, in order; a chosen
+// place below F stays; the chosen places from F on (movers), in ascending order, fill the places below F that were not chosen (holes),
+// in ascending order.  So as many tokens move as the row loses at most, and R.
+
+constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32, kBins = 2048, kMostBlocks = 8;
+constexpr int kKeys = 6144;                // keys that a block keeps in shared memory; a larger share is read again
+
+struct RowPlan {
+    int early, front;                      // pairs [0, early): movers from places below `keep`; [early, front): the others; then the recent tokens
+    int from, to, recent;                  // which go from place `from` to place `to`
+    int len, keep;                         // tokens before and after (equal: nothing happens)
+};
+
+struct EvictParams {
+    View v;
+    Pool pool;
+    float *mass;
+    long long mass_stride;
+    const int *keep_rows;                  // null: `keep` for every row
+    int keep, sinks, recent, width;        // width: columns of kept, pairs and offsets
+    int *kept, *evicted;
+    RowPlan *plans;                        // [rows]
+    int2 *pairs;                           // [rows, width] mover, hole: places
+    longlong2 *offsets;                    // [rows, width] where from and where to within a layer's pool, in bytes; -1: no such page
+};
+
+// Masses in descending order are keys in descending order; NaN below everything, one zero.
+__device__ __forceinline__ unsigned int mass_key(float x)
+{
+    if (x != x) return 0u;
+    const unsigned int u = __float_as_uint(x + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
 struct PickShared {
     unsigned int keys[kKeys];
     unsigned int mine[kBins], all[kBins];              // counts of this block; of the cluster (the first block's)

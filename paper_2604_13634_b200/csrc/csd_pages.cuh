@@ -224,12 +224,12 @@ __device__ __forceinline__ void release(const View &v, int page)
     if (atomicSub(v.refs + page, 1) == 1) atomicOr(v.free_bits + (page >> 5), 1u << (page & 31));
 }
 
-// A row of len tokens keeps `to` of them.  All threads of a block of kRowThreads.
-__device__ __forceinline__ void shorten(const View &v, int r, int len, int to)
+// A row of len tokens keeps `to` of them.  All threads of a block.
+__device__ __forceinline__ void shorten(const View &v, int r, int len, int to, int threads = kRowThreads)
 {
     const int first = pages_of(to, v.page_shift), held = pages_of(len, v.page_shift);
     int *row = v.table + static_cast<long long>(r) * v.max_pages;
-    for (int i = first + threadIdx.x; i < held; i += kRowThreads) {
+    for (int i = first + threadIdx.x; i < held; i += threads) {
         release(v, row[i]);
         row[i] = -1;
     }
