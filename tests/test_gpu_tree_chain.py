@@ -95,3 +95,81 @@ def test_what_a_call_reads_was_written_just_before(q_heads):
     for _ in range(4):
         for a, b in zip(go(False), want):
             assert torch.equal(a, b)
+
+
+class Step:
+    """One step of the tree pass over a cache of its own: everything a call needs, so that two of them share nothing."""
+
+    def __init__(self, seed, rows=6, T=12, heads=24, D=128, V=2000):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.cache, self.layers = PagedCache(rows, 20 * rows, 16, 2, 2, D, torch.bfloat16, 300), 2
+        self.qkv = torch.randn(rows, T, heads + 4, D, generator=gen, device="cuda").to(torch.bfloat16)
+        self.heads, self.rope = heads, RopePlan(D)
+        self.logits = torch.randn(rows, T, V, generator=gen, device="cuda").to(torch.bfloat16)
+        self.parents = torch.tensor([-1, 0, 0, 1, 1, 2, 3, 3, 4, 6, 8, 9][:T], dtype=torch.int32, device="cuda")
+        self.tokens = self.logits.float().argmax(-1)[:, self.parents.clamp(min=0).long()].int().contiguous()      # every child matches
+        self.plan, self.buf, self.out = TreePlan(self.cache, T), AttentionBuffers(self.cache, T, heads, tree=True), TreeBuffers(rows, T)
+        self.ocm, self.evict = Ocm(256, lam=2), EvictBuffers(self.cache, 70)
+        self.mass = torch.zeros(rows, self.cache.max_pages * 16, device="cuda")
+        self.offset = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+
+    def __call__(self):
+        c = self.cache
+        q, k, v = self.qkv.split([self.heads, 2, 2], dim=2)
+        csd_cache_extend(c, self.plan.T)
+        csd_tree_plan(self.parents, c, self.plan, n_new=c.granted, offset=self.offset)
+        for layer in range(self.layers):
+            turned = csd_rope_append(q, k, v, c, layer, self.rope, n_new=c.granted, positions=self.plan.positions)
+            csd_attention_tree(turned, c, layer, self.buf, self.plan.masks, n_new=c.granted)
+            csd_attention_mass(turned, self.buf.lse, c, layer, self.mass, n_new=c.granted, masks=self.plan.masks, fresh=layer == 0)
+        csd_verify_tree(self.logits, self.tokens, self.parents, self.ocm, 0.3, self.out, n_nodes=c.granted)
+        csd_cache_commit_path(c, self.out.accept_len, self.out.path)
+        csd_cache_evict(c, self.mass, 70, self.evict, sinks=2, recent=16)
+        self.offset += self.evict.evicted
+
+    def state(self):
+        torch.cuda.synchronize()
+        assert self.cache.stats()["flags"] == 0
+        return [x.clone() for x in (self.cache.meta, self.cache.k, self.cache.v, self.mass, self.offset, self.buf.out, self.buf.lse, self.out.path)]
+
+
+def test_a_step_captured_and_replayed():
+    eager, played = Step(1), Step(1)
+    for _ in range(2):                                               # what is asked of the device once is asked outside the capture
+        eager()
+        played()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        played()
+    for _ in range(30):
+        eager()
+        graph.replay()
+    for a, b in zip(eager.state(), played.state()):
+        assert torch.equal(a, b)
+    assert int(eager.offset.sum()) > 0 and int(eager.cache.lens.max()) <= 70
+    eager.ocm.close()
+    played.ocm.close()
+
+
+def test_two_passes_at_once():
+    """Two caches, each on a stream of its own, at the same time: what each gives alone.  (36, 48, 144 and 864 query rows to a key head: every kernel.)"""
+    for heads in ((6, 8), (24, 144)):
+        alone = []
+        for i, h in enumerate(heads):
+            s = Step(3 + i, heads=h)
+            for _ in range(25):
+                s()
+            alone.append(s.state())
+            s.ocm.close()
+        both, streams = [Step(3 + i, heads=h) for i, h in enumerate(heads)], [torch.cuda.Stream() for _ in heads]
+        for _ in range(25):
+            for s, stream in zip(both, streams):
+                with torch.cuda.stream(stream):
+                    s()
+        torch.cuda.synchronize()
+        for s, want in zip(both, alone):
+            for a, b in zip(s.state(), want):
+                assert torch.equal(a, b)
+            s.ocm.close()
