@@ -4,7 +4,7 @@
 //
 // The softmax's sums are known (lse), so the keys alone are read once more: half of the bytes of attention, and no value is touched.
 // Bound: memory; with more than about 200 query rows to a key head the exponentials (16 a clock and SM).  96 rows of 500 to 4000 tokens, 8 key
-// heads of 128, 36 query rows each: 82.8 us, 5.4 TB/s; one row of 131071 and one token 54.8 us, 4.9 TB/s; one row of 700 10.1 us.
+// heads of 128, 36 query rows each: 83 to 85 us, 5.4 TB/s; one row of 131071 and one token 54.8 us, 4.9 TB/s; one row of 700 10.7 to 11.7 us.
 //
 //   A tile is 128 places of a row and key head, and the FIRST operand of the product: S = K Q^T (tcgen05.mma, M = 128 places, N = the
 //   head's query rows), so that a thread finds all scores of one place in its own lane of tensor memory and adds their exponentials

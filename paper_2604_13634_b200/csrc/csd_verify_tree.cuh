@@ -10,8 +10,8 @@
 // memory (another stream may be updating it: two answers could differ) and a second barrier spreads what it decided.  All blocks of a
 // cluster take the same branches, so they meet at the same barriers, which the hardware schedules together and which always end.
 //
-// Bound: that chain.  48 rows of up to 40 nodes over 151936 bf16 logits, at most 8 of them visited in a row: 34.8 us (137 rows, 42 MB; all
-// 983 rows would be 299 MB, 46 us at the copy rate), 3.5 us a node with memory look-ups at every second; 11.4 us for one row and three nodes of 128256.
+// Bound: that chain.  48 rows of up to 40 nodes over 151936 bf16 logits, at most 8 of them visited in a row: 36 us (137 rows, 42 MB; all
+// 983 rows would be 299 MB, 46 us at the copy rate), 4 us a node with memory look-ups at every second; 11.9 us for one row and three nodes of 128256.
 // Sending for the rows of two children while a node's are reduced: 41 us.
 #pragma once
 
