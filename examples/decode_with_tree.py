@@ -55,6 +55,7 @@ class TreeDecoder:
         self.plan, self.buffers = csd.TreePlan(cache, nodes), csd.AttentionBuffers(cache, nodes, target.q_heads, tree=True)
         self.out, self.ocm = csd.TreeBuffers(rows, nodes, device=dev), csd.Ocm(4096, lam=6)
         self.offset = torch.zeros(rows, dtype=torch.int32, device=dev)                      # what positions are ahead of places
+        self.mass = None
         if budget is not None:
             self.mass = torch.zeros(rows, cache.max_pages * cache.page_size, device=dev)
             self.evict = csd.EvictBuffers(cache, budget + slack)
@@ -85,7 +86,7 @@ class TreeDecoder:
         hidden = self.hidden(tokens, self.cache.granted)
         csd.csd_verify_tree(hidden @ self.target.head.T, tokens, self.parents, self.ocm, 0.3, self.out)
         self.ocm.update(self.out.rej_draft, self.out.rej_target)
-        csd.csd_cache_commit_path(self.cache, self.out.accept_len, self.out.path)
+        csd.csd_cache_commit_path(self.cache, self.out.accept_len, self.out.path, self.mass)
         if self.budget is not None:
             # rows `slack` over the budget go down to it, the others stay as they are
             keep = torch.where(self.cache.lens >= self.budget + self.slack, self.budget, self.budget + self.slack).to(torch.int32)

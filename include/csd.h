@@ -720,9 +720,11 @@ csd_status_t csd_verify_tree(const void *logits, csd_dtype_t dtype, int B, int T
  * - 1 (the root and the accepted nodes, csd_verify_tree's outputs), which become the row's last tokens in that order: their keys and values move
  * together in every layer, the other new tokens are dropped and pages that nothing uses are free.  path: DEVICE int32 [rows, T], T <=
  * CSD_TREE_MAX_NODES; ascending within a row, as a path through a tree is: an entry that is not above the one before it, or not among
- * the granted tokens, ends what is kept (CSD_CACHE_BAD_PATH).  One launch; asynchronous.
+ * the granted tokens, ends what is kept (CSD_CACHE_BAD_PATH).  mass: NULL, or the accumulated weights of the places (csd_attention_mass), which
+ * move with their tokens; those of the dropped tokens become 0.  One launch; asynchronous.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
-csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *accept_len, const int32_t *path, int T, void *stream);
+csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *accept_len, const int32_t *path, int T, float *mass, int64_t mass_stride,
+                                   void *stream);
 
 /* ---- a cache kept to a budget ---- */
 
@@ -732,6 +734,7 @@ csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *acce
  * csd_attention_tree, whose q, scale, n_new, masks and lse these are.  A token with lse = -inf, or without a place, adds nothing; rows without new tokens stay
  * as they are; what lies in places that a token does not see does not matter.  fresh != 0: the places of the new tokens [lens - n_new,
  * lens) begin at 0 whatever mass held there -- for the first layer of a pass, when mass sums over layers.
+ * csd_cache_commit_path and csd_cache_evict move masses with their tokens; rows that continue others (csd_cache_fork) take theirs by the caller's copy.
  * q: as for csd_attention.  lse: DEVICE float [rows, T, q_heads].  mass: as for csd_cache_evict.
  * Scores, exponentials and sums in float32, added in a fixed order.  One launch; asynchronous.
  * Errors: INVALID_ARG, UNSUPPORTED (as csd_attention), CUDA. */

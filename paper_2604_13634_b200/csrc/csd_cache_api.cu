@@ -767,11 +767,12 @@ csd_status_t csd_cache_truncate(const csd_cache_t *cache, const int32_t *new_len
 
 csd_status_t csd_cache_commit(const csd_cache_t *cache, const int32_t *accept_len, void *stream) { return shorten(cache, nullptr, accept_len, stream); }
 
-csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *accept_len, const int32_t *path, int T, void *stream)
+csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *accept_len, const int32_t *path, int T, float *mass, int64_t mass_stride, void *stream)
 {
     const csd_status_t ok = check_cache(cache);
     if (ok != CSD_OK) return ok;
     if (!accept_len || !path || T <= 0) return CSD_ERR_INVALID_ARG;
+    if (mass && cache->rows > 1 && mass_stride < static_cast<int64_t>(cache->max_pages) * cache->page_size) return CSD_ERR_INVALID_ARG;
     if (T > CSD_TREE_MAX_NODES || 2ll * cache->layers * cache->heads * (cache->dim / 8) > INT_MAX) return CSD_ERR_UNSUPPORTED;
     host::other_work_enqueued();
     keep::PathParams p;
@@ -781,6 +782,8 @@ csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *acce
     p.accept_len = accept_len;
     p.path = path;
     p.T = T;
+    p.mass = mass;
+    p.mass_stride = mass_stride;
     return launch_clusters(keep::path_kernel, dim3(static_cast<unsigned int>(cache->rows * keep::kPathBlocks)), keep::kPathThreads, 0,
                            static_cast<cudaStream_t>(stream), keep::kPathBlocks, p);
 }

@@ -78,6 +78,8 @@ struct PathParams {
     Pool pool;
     const int *accept_len, *path;
     int T;
+    float *mass;                           // null: none
+    long long mass_stride;
 };
 
 // How many of the row's granted tokens stay: the accepted ones and the root, as far as the path names them in ascending order.  One
@@ -141,6 +143,18 @@ __global__ void __launch_bounds__(kPathThreads) path_kernel(const PathParams p)
                 to_off[j] = to;
             }
             at += __popc(m);
+        }
+        if (p.mass && rank == 0) {
+            // the new tokens' masses go with them: all are read before one is written; those of the dropped ones become 0
+            float *const mass = p.mass + r * p.mass_stride + base;
+            float x[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) x[k] = lane + 32 * k < n ? mass[entry[k]] : 0.f;
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (lane + 32 * k < n) mass[lane + 32 * k] = x[k];
+            for (int i = n + lane; i < granted; i += 32) mass[i] = 0.f;
         }
         if (lane == 0) {
             n_moves = at;

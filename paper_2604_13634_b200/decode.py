@@ -48,7 +48,7 @@ SIGNATURES = {
     "csd_cache_extend": (c_int, [POINTER(CacheStruct), c_int, c_void_p, c_void_p]),
     "csd_cache_truncate": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
     "csd_cache_commit": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p]),
-    "csd_cache_commit_path": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p, c_int, c_void_p]),
+    "csd_cache_commit_path": (c_int, [POINTER(CacheStruct), c_void_p, c_void_p, c_int, c_void_p, c_int64, c_void_p]),
     "csd_cache_evict_workspace_bytes": (c_size_t, [c_int, c_int]),
     "csd_cache_evict": (c_int, [POINTER(CacheStruct), c_void_p, c_int64, c_int, c_void_p, c_int, c_int, c_void_p, c_int, c_void_p, c_void_p, c_size_t,
                                 c_void_p]),
@@ -289,12 +289,13 @@ def csd_cache_commit(cache: PagedCache, accept_len, stream=None):
     _check(_lib().csd_cache_commit(cache._ref, _rows_arg(accept_len, cache, "accept_len"), _stream_ptr(stream, cache._device)), "csd_cache_commit")
 
 
-def csd_cache_commit_path(cache: PagedCache, accept_len, path, stream=None):
+def csd_cache_commit_path(cache: PagedCache, accept_len, path, mass=None, stream=None):
     """After the verification of a tree (TreeBuffers' accept_len and path [rows, T]): of the last extension's tokens, path[row, 0 ..
-    accept_len[row]] stay and move together."""
+    accept_len[row]] stay and move together.  mass [rows, places]: what csd_attention_mass has summed moves with its tokens; pass it
+    wherever there is one, or the kept tokens would be found with the weights of the nodes whose places they take."""
     _, T = path.shape
     rc = _lib().csd_cache_commit_path(cache._ref, _rows_arg(accept_len, cache, "accept_len"), _nodes_arg(path, cache, T, torch.int32, "path"), T,
-                                      _stream_ptr(stream, cache._device))
+                                      *((None, 0) if mass is None else _mass_arg(mass, cache)), _stream_ptr(stream, cache._device))
     if rc:
         _check(rc, "csd_cache_commit_path")
 

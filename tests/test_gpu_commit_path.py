@@ -144,3 +144,29 @@ def test_refusals():
     for accept, path in ((i32([0]), i32(np.zeros((2, 3)))), (i32([0, 0]), i32(np.zeros((3, 3)))), (i32([0, 0]), i32(np.zeros((2, 3))).long())):
         with pytest.raises(AssertionError):
             csd_cache_commit_path(cache, accept, path)
+
+
+@pytest.mark.parametrize("T", [1, 9, 64])
+def test_masses_move_with_their_tokens(T):
+    """Kept tokens' masses at their new places, zeros where tokens were dropped, everything else as it was; a stride of its own."""
+    rng, rows = np.random.default_rng(T), 4
+    x = Twin(rows, 60, 16, 1, 1, 64, 200)
+    x.extend(5, [5, 0, 3, 1])
+    csd_cache_commit(x.cache, i32([9] * rows))
+    x.books.commit([9] * rows)
+    news = [T, T, max(0, T - 2), 0]
+    x.extend(T, news)
+    lengths = [int(rng.integers(1, T + 1)) for _ in range(rows)]
+    path, accept = [some_path(rng, T, n) for n in lengths], [n - 1 for n in lengths]
+    lens = x.cache.lens.tolist()
+    mass = torch.rand(rows, x.cache.max_pages * 16 + 3, device="cuda")
+    before = mass.cpu().numpy().copy()
+    csd_cache_commit_path(x.cache, i32(accept), i32(path), mass[:, :x.cache.max_pages * 16])
+    for b, (n, g) in enumerate(zip(lens, news)):
+        kept, _ = O.kept_of_path(g, accept[b], path[b])
+        want = before[b].copy()
+        want[n - g:n] = 0.0
+        want[n - g:n - g + len(kept)] = before[b][[n - g + i for i in kept]]
+        assert np.array_equal(mass[b].cpu().numpy(), want), b
+    with pytest.raises(AssertionError):
+        csd_cache_commit_path(x.cache, i32(accept), i32(path), mass[:, :40])

@@ -78,7 +78,7 @@ def test_what_a_call_reads_was_written_just_before(q_heads):
             wait()
             ocm.update(out.rej_draft, out.rej_target)
             wait()
-            csd_cache_commit_path(cache, out.accept_len, out.path)
+            csd_cache_commit_path(cache, out.accept_len, out.path, mass)
             wait()
             csd_cache_evict(cache, mass, 100 if s % 5 else 80, evict, sinks=4, recent=20)
             wait()
@@ -124,7 +124,7 @@ class Step:
             csd_attention_tree(turned, c, layer, self.buf, self.plan.masks, n_new=c.granted)
             csd_attention_mass(turned, self.buf.lse, c, layer, self.mass, n_new=c.granted, masks=self.plan.masks, fresh=layer == 0)
         csd_verify_tree(self.logits, self.tokens, self.parents, self.ocm, 0.3, self.out, n_nodes=c.granted)
-        csd_cache_commit_path(c, self.out.accept_len, self.out.path)
+        csd_cache_commit_path(c, self.out.accept_len, self.out.path, self.mass)
         csd_cache_evict(c, self.mass, 70, self.evict, sinks=2, recent=16)
         self.offset += self.evict.evicted
 

@@ -156,8 +156,8 @@ def test_tree_calls_refuse_what_they_cannot_do():
         SOMEWHERE, *s3, T, heads, lse, byref(c), layer, 1.0, None, masks, to, stride, 0, None)
     assert mass(lse=None) == mass(to=None) == mass(masks=SOMEWHERE + 4) == mass(stride=63) == mass(layer=1) == INVALID_ARG
     assert mass(T=65) == mass(heads=3) == UNSUPPORTED
-    path = lambda T=3, accept=SOMEWHERE, at=SOMEWHERE: L.csd_cache_commit_path(byref(c), accept, at, T, None)  # noqa: E731
-    assert path(accept=None) == path(at=None) == path(T=0) == INVALID_ARG and path(T=65) == UNSUPPORTED
+    path = lambda T=3, accept=SOMEWHERE, at=SOMEWHERE, mass=None, stride=0: L.csd_cache_commit_path(byref(c), accept, at, T, mass, stride, None)  # noqa: E731
+    assert path(accept=None) == path(at=None) == path(T=0) == path(mass=SOMEWHERE, stride=63) == INVALID_ARG and path(T=65) == UNSUPPORTED
 
 
 def test_eviction_refuses_what_it_cannot_do():
