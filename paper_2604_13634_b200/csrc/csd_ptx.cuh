@@ -57,6 +57,48 @@ __device__ __forceinline__ bool elect_one()
 
 __device__ __forceinline__ unsigned int smem_u32(const void *p) { return static_cast<unsigned int>(__cvta_generic_to_shared(p)); }
 
+// Thread-block clusters.  A block may touch another's shared memory only once that one is known to run, and no longer when it may have
+// left: all threads of all blocks meet before the first such access of a kernel, and after the last.  Arriving as the kernel begins and
+// waiting behind the wait for the stream hides the first meeting.
+__device__ __forceinline__ unsigned int cluster_rank()
+{
+    unsigned int r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ unsigned int cluster_size()
+{
+    unsigned int r;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_meet()
+{
+    cluster_arrive();
+    cluster_wait();
+}
+// What lies at a shared-memory address of this block in block `rank` of the cluster.
+__device__ __forceinline__ unsigned int in_block(unsigned int addr, unsigned int rank)
+{
+    unsigned int r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void st_cluster(unsigned int addr, unsigned int v)
+{
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
 __device__ __forceinline__ void mbar_init(unsigned int bar, unsigned int count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");

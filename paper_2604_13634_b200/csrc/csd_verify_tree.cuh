@@ -27,6 +27,10 @@
 namespace csd {
 namespace verify_tree {
 
+using ptx::cluster_meet;
+using ptx::in_block;
+using ptx::st_cluster;
+
 constexpr int kThreads = 512, kWarps = kThreads / 32, kMaxCluster = 8, kNodes = CSD_TREE_MAX_NODES;
 constexpr int kAtOnce = 8;                 // 16-byte loads in flight per thread: all of a row of 262144 bf16 logits, shared by eight blocks
 
@@ -118,35 +122,6 @@ struct Lane<__nv_bfloat16> {
     }
 };
 
-__device__ __forceinline__ unsigned int cluster_rank()
-{
-    unsigned int r;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ unsigned int cluster_size()
-{
-    unsigned int r;
-    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ unsigned int in_block(unsigned int addr, unsigned int rank)
-{
-    unsigned int r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void st_cluster(unsigned int addr, unsigned int v)
-{
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
-__device__ __forceinline__ void cluster_meet()
-{
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 // This warp's share of a logit row: (max, lowest index) of it.
 template <typename T>
 __device__ __forceinline__ Best row_share(const T *row, int V, unsigned int rank, unsigned int blocks)
@@ -203,23 +178,31 @@ __global__ void __launch_bounds__(kThreads, 2) verify_tree_kernel(const Params p
     __shared__ Best of_warps[2][kMaxCluster * kWarps];                  // of all warps of the cluster, this block's copy
     __shared__ int decision, n_shared;
     __shared__ int path[kNodes], rec_d[kNodes], rec_t[kNodes], rescued[kNodes];        // the first block's
+    ptx::cluster_arrive();                                              // that all blocks run is waited for behind the stream
     ptx::wait_for_stream();
-    const unsigned int rank = cluster_rank(), blocks = cluster_size();
+    const unsigned int rank = ptx::cluster_rank(), blocks = ptx::cluster_size();
     const int b = blockIdx.x / blocks, tid = threadIdx.x, lane = tid & 31;
     // The tree is read by the first block and handed to the others: whatever another stream may do to it meanwhile, all walk the same one
     // and meet at the same barriers.
+    const bool hands_over = rank == 0 && tid < kNodes;
+    int nodes = 0, tok = -1, up = -1;
+    if (hands_over) {
+        nodes = min(p.n_nodes ? ptx::ld_written(p.n_nodes + b) : p.T, p.T);
+        if (tid < p.T) {
+            tok = ptx::ld_written(p.tokens + static_cast<long long>(b) * p.T + tid);
+            up = ptx::ld_written(p.parents + b * p.parent_stride + tid);
+        }
+    }
     if (tid < kNodes) {
         path[tid] = rec_d[tid] = rec_t[tid] = -1;
         rescued[tid] = 0;
-        if (rank == 0) {
-            const int nodes = min(p.n_nodes ? ptx::ld_written(p.n_nodes + b) : p.T, p.T);
-            const int tok = tid < p.T ? ptx::ld_written(p.tokens + static_cast<long long>(b) * p.T + tid) : -1;
-            const int up = tid < p.T ? ptx::ld_written(p.parents + b * p.parent_stride + tid) : -1;
-            for (unsigned int q = 0; q < blocks; ++q) {
-                st_cluster(in_block(ptx::smem_u32(&token[tid]), q), static_cast<unsigned int>(tok));
-                st_cluster(in_block(ptx::smem_u32(&parent[tid]), q), static_cast<unsigned int>(up));
-                if (tid == 0) st_cluster(in_block(ptx::smem_u32(&n_shared), q), static_cast<unsigned int>(nodes));
-            }
+    }
+    ptx::cluster_wait();
+    if (hands_over) {
+        for (unsigned int q = 0; q < blocks; ++q) {
+            st_cluster(in_block(ptx::smem_u32(&token[tid]), q), static_cast<unsigned int>(tok));
+            st_cluster(in_block(ptx::smem_u32(&parent[tid]), q), static_cast<unsigned int>(up));
+            if (tid == 0) st_cluster(in_block(ptx::smem_u32(&n_shared), q), static_cast<unsigned int>(nodes));
         }
     }
     cluster_meet();
