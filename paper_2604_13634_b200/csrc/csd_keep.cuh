@@ -21,6 +21,9 @@ namespace csd {
 namespace keep {
 
 using pages::View;
+using ptx::cluster_rank;
+using ptx::cluster_size;
+using ptx::st_cluster;
 
 // Keys and values of a cache as the moves address them, in elements of two bytes.
 struct Pool {
@@ -31,28 +34,7 @@ struct Pool {
 
 // ---- clusters ----
 
-__device__ __forceinline__ unsigned int cluster_rank()
-{
-    unsigned int r;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ unsigned int cluster_size()
-{
-    unsigned int r;
-    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ unsigned int in_block(const void *mine, unsigned int rank)
-{
-    unsigned int r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(ptx::smem_u32(mine)), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void st_cluster(unsigned int addr, unsigned int v)
-{
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
+__device__ __forceinline__ unsigned int in_block(const void *mine, unsigned int rank) { return ptx::in_block(ptx::smem_u32(mine), rank); }
 __device__ __forceinline__ void add_cluster(unsigned int addr, unsigned int v)
 {
     asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
@@ -60,13 +42,10 @@ __device__ __forceinline__ void add_cluster(unsigned int addr, unsigned int v)
 // All threads of all blocks of the cluster.
 __device__ __forceinline__ void cluster_meet(unsigned int blocks)
 {
-    if (blocks == 1) {
+    if (blocks == 1)
         __syncthreads();
-        return;
-    }
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    else
+        ptx::cluster_meet();
 }
 
 // ---- the accepted path -----------------------------------------------------------------------------------------
@@ -262,12 +241,14 @@ __device__ __forceinline__ void before_me(PickShared &s, int &turn, unsigned int
 __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictParams p)
 {
     __shared__ PickShared s;
-    ptx::wait_for_stream();
     const unsigned int rank = cluster_rank(), blocks = cluster_size();
+    if (blocks > 1) ptx::cluster_arrive();                             // that all blocks run is waited for behind the stream
+    ptx::wait_for_stream();
     const int r = blockIdx.x / blocks, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int len = p.v.lens[r];
     int keep = min(max(p.keep_rows ? ptx::ld_written(p.keep_rows + r) : p.keep, 0), p.width);
     if (blocks > 1) {
+        ptx::cluster_wait();
         // as the first block has read them: whatever another stream may do meanwhile, all blocks meet at the same barriers
         if (rank == 0 && tid < static_cast<int>(blocks)) {
             const unsigned int to = in_block(s.found, tid);

@@ -59,10 +59,9 @@ def test_the_rule_sees_what_it_is_about():
     assert breaks_the_rule("cluster_meet(); st_cluster(a, 1);", names) is True
     assert breaks_the_rule("cluster_arrive(); cluster_wait(); st_cluster(a, 1); cluster_meet();", names) is False
     seen = {n for f in FILES for n, broken in kernels(f) if broken is not None}
-    assert {"verify_tree_kernel", "lmhead_stats_pair_kernel"} <= seen
+    assert seen == {"verify_tree_kernel", "evict_pick_kernel", "mass_kernel", "lmhead_stats_pair_kernel"}
 
 
-@pytest.mark.parametrize("name", ["csd_verify_tree.cuh", "csd_lmhead.cuh"])
+@pytest.mark.parametrize("name", FILES)
 def test_blocks_meet_around_their_accesses(name):
-    got = kernels(name)
-    assert got and not [n for n, broken in got if broken]
+    assert not [n for n, broken in kernels(name) if broken]
