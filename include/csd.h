@@ -721,7 +721,8 @@ csd_status_t csd_verify_tree(const void *logits, csd_dtype_t dtype, int B, int T
  * together in every layer, the other new tokens are dropped and pages that nothing uses are free.  path: DEVICE int32 [rows, T], T <=
  * CSD_TREE_MAX_NODES; ascending within a row, as a path through a tree is: an entry that is not above the one before it, or not among
  * the granted tokens, ends what is kept (CSD_CACHE_BAD_PATH).  mass: NULL, or the accumulated weights of the places (csd_attention_mass), which
- * move with their tokens; those of the dropped tokens become 0.  One launch; asynchronous.
+ * move with their tokens; those of the dropped tokens become 0.  A grant above the row's length counts as the length.  One launch;
+ * asynchronous.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 csd_status_t csd_cache_commit_path(const csd_cache_t *cache, const int32_t *accept_len, const int32_t *path, int T, float *mass, int64_t mass_stride,
                                    void *stream);

@@ -32,6 +32,9 @@ struct Pool {
     int layers, heads, vecs;               // vecs: 16-byte vectors of a head
 };
 
+// Tokens of a row, as far as its table reaches: the arrays are the caller's memory, and what they say is bounded before it becomes an address.
+__device__ __forceinline__ int row_len(const View &v, int r) { return min(max(ptx::ld_written(v.lens + r), 0), v.max_pages << v.page_shift); }
+
 // ---- clusters ----
 
 __device__ __forceinline__ unsigned int in_block(const void *mine, unsigned int rank) { return ptx::in_block(ptx::smem_u32(mine), rank); }
@@ -95,7 +98,7 @@ __global__ void __launch_bounds__(kPathThreads) path_kernel(const PathParams p)
     ptx::wait_for_stream();
     const unsigned int rank = cluster_rank();
     const int r = blockIdx.x / kPathBlocks, tid = threadIdx.x, lane = tid & 31;
-    const int len = p.v.lens[r], granted = max(p.v.granted[r], 0);
+    const int len = row_len(p.v, r), granted = min(max(ptx::ld_written(p.v.granted + r), 0), len);
     if (tid < 32) {
         const int base = len - granted;
         const int *row = p.v.table + static_cast<long long>(r) * p.v.max_pages;
