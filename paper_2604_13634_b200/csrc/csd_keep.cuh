@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
     if (blocks > 1) ptx::cluster_arrive();                             // that all blocks run is waited for behind the stream
     ptx::wait_for_stream();
     const int r = blockIdx.x / blocks, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int len = p.v.lens[r];
+    int len = row_len(p.v, r);
     int keep = min(max(p.keep_rows ? ptx::ld_written(p.keep_rows + r) : p.keep, 0), p.width);
     if (blocks > 1) {
         ptx::cluster_wait();

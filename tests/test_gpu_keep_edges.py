@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import tree_oracle as O
-from paper_2604_13634_b200 import PagedCache, csd_cache_commit_path, csd_cache_extend
+from paper_2604_13634_b200 import EvictBuffers, PagedCache, csd_cache_commit_path, csd_cache_evict, csd_cache_extend
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +70,25 @@ def test_a_length_that_the_table_cannot_hold(length):
         order = list(range(93)) + [95]
         assert torch.equal(contents(cache, 1, 94), before[:, order])
         assert torch.equal(mass[1, :94], weights[1, order]) and not mass[1, 94:].any()
+
+
+@pytest.mark.parametrize("length,keep", [(97, 50), (2 ** 31 - 1, 50), (1000, 96), (1000, 120), (-1, 50)])
+def test_evicting_from_a_length_that_the_table_cannot_hold(length, keep):
+    cache, mass = filled([40, 96, 33], seed=3)
+    before, table, weights = contents(cache, 1, 96), cache.table.clone(), mass.clone()
+    cache.lens[1] = length
+    buf = EvictBuffers(cache, 120)
+    csd_cache_evict(cache, mass, keep, buf, sinks=2, recent=10)
+    torch.cuda.synchronize()
+    n = 96 if length > 0 else 0
+    where = O.evict(weights[1].tolist(), n, keep, 2, 10)
+    assert cache.lens.tolist() == [40, len(where), 33] and buf.evicted.tolist() == [0, n - len(where), 0]
+    assert buf.kept[1].tolist() == where + [-1] * (120 - len(where))
+    want = weights.clone()
+    if n:
+        want[1] = 0.0
+        want[1, :len(where)] = weights[1, where]
+    assert torch.equal(mass, want) and torch.equal(contents(cache, 1, len(where)), before[:, where])
+    held = -(-len(where) // 16) if n else 6
+    assert torch.equal(cache.table[:, :held], table[:, :held]) and torch.equal(cache.table[[0, 2]], table[[0, 2]])
+    assert cache.stats()["flags"] == 0

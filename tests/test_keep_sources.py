@@ -7,7 +7,7 @@ import pytest
 
 from test_cluster_sources import bodies, code_of
 
-RAW = {"path_kernel": r"v\.(?:lens|granted)\[|v\.lens\s*\+"}
+RAW = {name: r"v\.(?:lens|granted)\[|v\.lens\s*\+" for name in ("path_kernel", "evict_pick_kernel", "evict_move_kernel", "evict_finish_kernel")}
 
 
 @pytest.mark.parametrize("kernel", sorted(RAW))
