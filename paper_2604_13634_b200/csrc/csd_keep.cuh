@@ -202,7 +202,8 @@ __device__ __forceinline__ unsigned int mass_key(float x)
 }
 struct PickShared {
     unsigned int keys[kKeys];
-    unsigned int mine[kBins], all[kBins];              // counts of this block; of the cluster (the first block's)
+    __align__(16) unsigned int mine[kBins];            // counts of this block, read four at a time
+    __align__(16) unsigned int all[kBins];             // of the cluster (the first block's)
     unsigned int of_warp[kPickWarps][2], of_block[2][kMostBlocks][2];
     unsigned int found[3], refused[kMostBlocks], scan[kPickWarps];      // found: digit, how many with it are chosen, how many have it
 };
