@@ -561,7 +561,6 @@ csd_status_t run_mass(mass::Params p, const csd_cache_t *cache, int layer, cudaS
     if (!kernel_ready(mass::mass_kernel<T>, ready, limit, 1, 0)) return CSD_ERR_CUDA;
     attention::Params &a = p.a;
     a.halves = (a.D + 63) / 64;
-    a.d16 = (a.D + 15) / 16 * 16;
     a.box_rows = cache->page_size < mass::kTile ? cache->page_size : mass::kTile;
     // Query rows: as many as 32 KiB hold, in two sets where both fit there; the rest of the shared memory is for the ring of keys.
     const int fits = 32768 / (a.halves * 128) / 16 * 16, most = fits < mass::kMostRows ? fits : mass::kMostRows;

@@ -33,6 +33,7 @@ namespace csd {
 namespace mass {
 
 using attention::Cursor;
+using ptx::cluster_meet;
 using ptx::mbar_arrive;
 using ptx::mbar_expect_tx;
 using ptx::mbar_init;
@@ -80,18 +81,10 @@ struct Tiles {
     }
 };
 
-__device__ __forceinline__ void cluster_meet()
-{
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ int ld_cluster(const int *mine, unsigned int rank)
 {
-    unsigned int at;
     int v;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(rank));
-    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(ptx::in_block(smem_u32(mine), rank)) : "memory");
     return v;
 }
 
@@ -108,9 +101,7 @@ mass_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ P
     volatile int *give_up = &give_up_flag;
     const attention::Params &a = p.a;
 
-    unsigned int rank, blocks;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(blocks));
+    const unsigned int rank = ptx::cluster_rank(), blocks = ptx::cluster_size();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const unsigned int rows_bytes = static_cast<unsigned int>(a.halves * p.q_rows * 128);
     const unsigned int q_smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
