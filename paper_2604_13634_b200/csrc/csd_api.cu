@@ -381,8 +381,11 @@ csd_status_t run_step(const void *logits, csd_dtype_t dtype, int B, int K, int V
     return cudaGetLastError() == cudaSuccess ? CSD_OK : CSD_ERR_CUDA;
 }
 
-// Blocks of a cluster that share a logit row of the tree's walk.
-unsigned int verify_tree_blocks(int, int V, int elt)
+// Blocks of a cluster that share a logit row of the tree's walk: eight, fewer where a block would get less than 4 KiB of it.  A rule on the row
+// alone.  8, 4, 2, 1 blocks: one batch row of 128256 bf16 logits and a walk of up to four steps 10.5, 10.8, 14.1, 19.7 us, up to nine 26.1, 26.9,
+// 34.6, 49.9; one row of 500 9.2, 9.2, 9.2, 8.7; 64 of 2000 26.9, 17.2, 16.4, 16.1.  Batches whose clusters of eight do not all fit the GPU
+// would do better with four: 48 rows of 151936 37.4, 36.4, 43.3, 59.4 us, 96 rows 38.7, 30.7, 35.6, 47.4.
+unsigned int verify_tree_blocks(int V, int elt)
 {
     unsigned int blocks = 8;
     while (blocks > 1 && static_cast<long long>(V) * elt < 4096ll * blocks) blocks /= 2;
@@ -808,7 +811,7 @@ csd_status_t csd_verify_tree(const void *logits, csd_dtype_t dtype, int B, int T
     p.accept_len = accept_len; p.next_token = next_token; p.path = path;
     p.rescued = rescued_mask;
     p.rej_d = rej_draft; p.rej_t = rej_target;
-    const unsigned int blocks = verify_tree_blocks(B, V, elt_bytes(dtype));
+    const unsigned int blocks = verify_tree_blocks(V, elt_bytes(dtype));
     cudaLaunchConfig_t cfg;
     std::memset(&cfg, 0, sizeof cfg);
     cfg.gridDim = dim3(static_cast<unsigned int>(B) * blocks);
