@@ -707,8 +707,9 @@ csd_status_t csd_attention_tree(const void *q, int64_t q_stride_b, int64_t q_str
  * rows of the nodes on the path are read, so only those can raise CSD_FLAG_NAN_LOGIT (a NaN, or a maximum that is not finite; that row's
  * results are undefined).
  * tokens: int32 [B, T]; a token outside [0, V) can be neither accepted nor rescued and is not recorded (CSD_FLAG_BAD_DRAFT where its parent
- * was reached).  parents: as for csd_tree_plan; a node without an earlier parent is never reached.  n_nodes: DEVICE [B] (NULL: T); nodes from
- * it on do not exist; a row without any gives accept_len 0, next_token -1 and a path of -1.
+ * was reached and no child of it had the token t*).  parents: as for csd_tree_plan, but never NULL: a chain's are -1, 0, 1, ...  A node without an
+ * earlier parent is never reached.  n_nodes: DEVICE [B] (NULL: T); nodes from it on do not exist; a row without any gives accept_len 0,
+ * next_token -1 and a path of -1.
  * accept_len and path are the arguments of csd_cache_commit_path.
  * One launch; asynchronous; no workspace.  Errors: INVALID_ARG, UNSUPPORTED (T > CSD_TREE_MAX_NODES), CUDA. */
 csd_status_t csd_verify_tree(const void *logits, csd_dtype_t dtype, int B, int T, int V, int64_t stride_b, int64_t stride_t,

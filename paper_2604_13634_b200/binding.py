@@ -346,7 +346,7 @@ class TreeBuffers:
 
 def csd_verify_tree(logits, tokens, parents, ocm: Ocm, tau: float, buf: TreeBuffers, n_nodes=None, stream=None):
     """Verification loop of Algorithm 1 (greedy) on trees: logits [B, T, V], tokens [B, T] int32 (node 0 the root), parents [B, T] or [T]
-    int32, n_nodes [B] int32.  buf.accept_len and buf.path go to csd_cache_commit_path, buf.rej_draft and buf.rej_target to Ocm.update;
+    int32 (never None: a chain's are -1, 0, 1, ...), n_nodes [B] int32.  buf.accept_len and buf.path go to csd_cache_commit_path, buf.rej_draft and buf.rej_target to Ocm.update;
     the memory is only read."""
     B, T, V = logits.shape
     zs, ps, both = logits.stride(), parents.stride(), (B, T)
