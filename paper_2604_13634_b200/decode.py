@@ -327,12 +327,14 @@ def csd_cache_evict(cache: PagedCache, mass, keep, buf: EvictBuffers, sinks: int
     """Rows of more than keep tokens (an int, or int32 [rows] on the device) keep the first `sinks`, the last `recent` and the best by mass
     [rows, places] of the rest; keys, values and masses move together.  buf.kept: the place before of every place after (-1: none);
     buf.evicted: tokens lost, what positions of later tokens run ahead of their places (csd_tree_plan's offset is the sum of these)."""
-    rows = None
+    rows, most = None, 2 ** 31 - 1
     if isinstance(keep, torch.Tensor):
         rows, keep = _rows_arg(keep, cache, "keep"), 0
+    if not 0 <= keep <= buf.keep or sinks < 0 or recent < 0:
+        raise CsdError(f"csd_cache_evict: keep={keep} of buffers for {buf.keep}, sinks={sinks}, recent={recent}")
     if not (buf.kept.shape == (cache.rows, buf.keep) and buf.kept.get_device() == cache._device):
         raise CsdError("csd_cache_evict: buffers of another cache")
-    _check(_lib().csd_cache_evict(cache._ref, *_mass_arg(mass, cache), keep, rows, sinks, recent, buf.kept.data_ptr(), buf.keep, buf.evicted.data_ptr(),
+    _check(_lib().csd_cache_evict(cache._ref, *_mass_arg(mass, cache), keep, rows, min(sinks, most), min(recent, most), buf.kept.data_ptr(), buf.keep, buf.evicted.data_ptr(),
                                   buf.workspace.data_ptr(), buf.ws_bytes, _stream_ptr(stream, cache._device)), "csd_cache_evict")
 
 
