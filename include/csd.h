@@ -30,7 +30,8 @@
  *     together: in the LM-head pair kernel their barrier waits on each other are
  *     bounded in time, and every path of both blocks reaches the two cluster barriers
  *     they meet at; in csd_verify_tree, csd_cache_commit_path, csd_attention_mass and csd_cache_evict all
- *     blocks of a cluster take the same branches to the same cluster barriers.  With csd_set_overlap on, the warps that finalise a batch row wait for
+ *     blocks of a cluster take the same branches to the same cluster barriers, the first of them before one
+ *     touches another's shared memory.  With csd_set_overlap on, the warps that finalise a batch row wait for
  *     the PREVIOUS launch on the stream: a bounded poll (2^14 loads) of a completion
  *     word, then the hardware's wait for that grid to retire, which always ends.
  *   - Determinism: for fixed (B,K,V,dtype) every output, including the sums s,

@@ -36,8 +36,9 @@
 //
 // Trees (kTree): the new tokens are the nodes of a tree, and token t sees every place before the new ones and the new tokens u whose bit is
 // set in masks[b,t].  Only the tiles with new tokens differ: a thread holds its rows' masks and tests a bit where the chain compares places.
-// 26 nodes of 32 heads over 2000 tokens: 19.8 us; 64 nodes of 64 heads over 30001: 79 us, bound by the products (512 query rows to a key head); 32
-// ragged rows up to 8191 with up to 40 nodes of 40 heads: 194 us; 16 rows of up to 3000 with eight nodes of 16 heads of 64: 29.7 us.
+// 26 nodes of 32 heads over 2000 tokens: 19.6 to 19.8 us; 64 nodes of 64 heads over 30001: 79 to 80 us, bound by the products (512 query rows
+// to a key head); 32 ragged rows up to 8191 with up to 40 nodes of 40 heads: 194 us; 16 rows of up to 3000 with eight nodes of 16 heads of 64:
+// 29.3 to 29.7 us.  Pass after pass without a pause the GPU's clock falls: up to 90 us and 216 for the two that the products bind.
 #pragma once
 
 #include <cuda.h>

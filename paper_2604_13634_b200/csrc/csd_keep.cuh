@@ -5,8 +5,8 @@
 // same head of every token with a barrier between a piece's loads and its stores (eviction); no two blocks touch the same bytes.
 //
 // Bound: memory for the moves, latency for the choice (a few dependent passes over 4 bytes per place).  A path of one row in 32 layers takes 6.1 to 7.1 us,
-// 64 paths in 28 layers 19.6 to 20.4 (35 MB read and written); cutting 16 rows of about 1021 tokens to 1008 in 16 layers 69 to 72 us, of
-// which the moves of 147 MB read and written take 50 and the choice 11; 8 prompts of 6000 to 16384 to 4096 in 4 layers 151 to 154 us, 128 and 19.
+// 64 paths in 28 layers 19.3 to 20.4 (35 MB read and written); cutting 16 rows of about 1021 tokens to 1008 in 16 layers 69 to 72 us, of
+// which the moves of 147 MB read and written take 50 and the choice 11; 8 prompts of 6000 to 16384 to 4096 in 4 layers 151 to 155 us, 128 and 19.
 #pragma once
 
 #include <cuda_runtime.h>

@@ -3,12 +3,15 @@
 //   mass[b,j] += sum_{t,h} exp(scale q[b,t,h].k[b,j,h / g] - lse[b,t,h])      over the tokens that see place j
 //
 // The softmax's sums are known (lse), so the keys alone are read once more: half of the bytes of attention, and no value is touched.
-// Bound: memory; with more than about 200 query rows to a key head the exponentials (16 a clock and SM).  96 rows of 500 to 4000 tokens, 8 key
-// heads of 128, 36 query rows each: 83 to 85 us, 5.4 TB/s; one row of 131071 and one token 54.8 us, 4.9 TB/s; one row of 700 10.7 to 11.7 us.
+// Bound: memory for large batches of up to about 64 query rows to a key head.  96 rows of 500 to 4000 tokens, 8 key heads of 128, 36 query rows
+// each: 83 to 86 us, 5.3 TB/s; one row of 131071 and one token 54.8 us, 4.9 TB/s; one row of 700 10.7 to 11.7 us.  Beyond, latency from scores to
+// exponentials and back, with one set of query rows instead of two; and every further pass loads the keys again (from L2), as its loop lies outside
+// the loads.  32 rows of 500 to 4000, 8 key heads of 128 (147 MB of keys, 23 us): with 4, 36, 64, 100 and 128 query rows 43, 44, 47, 58 and 62
+// us, in two passes with 132, 192 and 256 81, 92 and 108; with 128 and 132 neither DRAM nor any unit of the SM is more than 40 % busy.
 //
 //   A tile is 128 places of a row and key head, and the FIRST operand of the product: S = K Q^T (tcgen05.mma, M = 128 places, N = the
 //   head's query rows), so that a thread finds all scores of one place in its own lane of tensor memory and adds their exponentials
-//   without an exchange.  Up to kMostRows query rows at a time; more are further passes over the tile.
+//   without an exchange.  Up to kMostRows query rows at a time (those that 32 KiB hold: 64 of 256 elements); more are further passes.
 //   The places of all rows, in tiles, are split evenly over clusters of blocks; a cluster's blocks share its tiles' key heads among
 //   themselves.  A run of up to kRunTiles tiles keeps its sums in shared memory over all heads of a block; at its end the blocks' sums are
 //   added in the order of the blocks through distributed shared memory.  No atomics: results are bit-reproducible for given lengths.

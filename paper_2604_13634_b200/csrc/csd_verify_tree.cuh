@@ -5,13 +5,14 @@
 //
 // Only the logit rows of the nodes that the walk visits are read: (accepted + 1) V elements of a batch row, where a pass over all nodes
 // would read T V.  The price is a chain of dependent passes, one per accepted token.  A thread-block cluster has a batch row: every block
-// reduces its share of the node's logits to (max, lowest index), hands it to all others through distributed shared memory, and after one
-// cluster barrier each of them knows t* and, where a child has that token, the next node.  Where none has, the first block alone asks the
+// reduces its share of the node's logits to (max, lowest index), hands it to all others through distributed shared memory (once all are
+// known to run: they meet as the kernel begins), and after one cluster barrier each of them knows t* and, where a child has that token, the next node.  Where none has, the first block alone asks the
 // memory (another stream may be updating it: two answers could differ) and a second barrier spreads what it decided.  All blocks of a
 // cluster take the same branches, so they meet at the same barriers, which the hardware schedules together and which always end.
 //
-// Bound: that chain.  48 rows of up to 40 nodes over 151936 bf16 logits, at most 8 of them visited in a row: 36 us (137 rows, 42 MB; all
-// 983 rows would be 299 MB, 46 us at the copy rate), 4 us a node with memory look-ups at every second; 11.9 us for one row and three nodes of 128256.
+// Bound: that chain.  48 rows of up to 40 nodes over 151936 bf16 logits, at most 8 of them visited in a row: 36 to 37 us (137 rows, 42 MB; all
+// 983 rows would be 299 MB, 46 us at the copy rate), 4 us a node with memory look-ups at every second; 11.4 to 12.1 us for one row and three
+// nodes of 128256.  48 rows are 384 blocks of which 296 run at a time, so that some rows begin when others have ended.
 // Sending for the rows of two children while a node's are reduced: 41 us.
 #pragma once
 
